@@ -388,6 +388,72 @@ int sbp_attn_context_bwd(const sbp_view4_t *dO, const sbp_view4_t *P,
                          const sbp_view4_t *V, sbp_view4_t *dP, sbp_view4_t *dV,
                          int32_t p, int32_t r, hipStream_t stream);
 
+/* ------------------------------------------------- softmax attention --- */
+
+/* What a query sees, and the scores' scale. len_q, len_k: device arrays of one
+ * int32 per sequence (its rows of Q, and of K and V, that are in use; read when the
+ * call runs, clamped to [0, rows]), or NULL for all rows. Query i of a sequence sees
+ * key j when
+ *     i < len_q,  j < len_k,
+ *     causal:      j <= i + len_k - len_q   (the last query sees the last key)
+ *     window > 0:  j >  i + len_k - len_q - window. */
+typedef struct {
+    float scale;      /* finite and > 0 (else SBP_ERR_SHAPE); usually 1/sqrt(D) */
+    int32_t causal;   /* 0 or 1 */
+    int32_t window;   /* >= 0; 0: none */
+    const int32_t *len_q;
+    const int32_t *len_k;
+} sbp_attn_opts_t;
+
+/* Attention of rank r's heads without scores or probabilities in memory.
+ *
+ *   sbp_attn_core_fwd   O_i = sum_j P_ij V_j,  P_ij = exp(scale Q_i.K_j - lse_i),
+ *                       lse_i = log sum_j exp(scale Q_i.K_j), over the keys j that
+ *                       query i sees
+ *   sbp_attn_core_bwd   from dO, O and lse: dV = P^T dO, dS = P (dO V^T - rowsum(dO O)),
+ *                       dQ = scale dS K, dK = scale dS^T Q, with P recomputed
+ *
+ * Q, dO, O, dQ: [B][H][Sq][D]; K, V, dK, dV: [B][Hk][Sk][D]; lse: [B][H][Sq][1], fp32.
+ * H is a multiple of Hk: query heads h G .. h G + G - 1 (G = H / Hk) share key head h,
+ * whose gradients sum over them. 1 <= D <= 128. Q, K, V and dO are bf16; O and the
+ * gradients bf16 (rounded to nearest even) or fp32; SBP_ACCUMULATE adds to an fp32
+ * gradient (not to O or lse: SBP_ERR_SHAPE). Scores, row statistics and sums are fp32;
+ * P and dS are rounded to bf16 as operands of the matrix products, so fp32 outputs
+ * carry that rounding too.
+ *
+ * Head split: key heads split over p devices by the balanced rule, query heads with
+ * them (rank r has G per key head of its share). Q, K and V share one scope; dO, O
+ * and lse may be GLOBAL or LOCAL. Outputs hold rank r's heads. Every operand is Split
+ * on heads; nothing is a partial sum.
+ *
+ * Rows that see no key get O = 0, lse = -infinity and zero gradients (accumulated
+ * gradients stay as they are); so do rows past len_q and keys past len_k, whose inputs
+ * are never read. Within the lengths a non-finite K, V, Q or dO row may reach every
+ * row of its head and sequence, also those that do not see it. lse may be NULL
+ * in the forward call.
+ *
+ * ws: the forward call uses a workspace, if it has one, to split the keys of few rows
+ * over workgroups. The backward call needs 8 bytes per query row of the rank
+ * (8 B H_r Sq, rounded up to 32), else SBP_ERR_WORKSPACE, and splits with the rest.
+ * Results are the same up to fp32 summation order and identical for identical
+ * workspace sizes.
+ *
+ * Errors: those of the calls above; SBP_ERR_SHAPE also for D outside [1, 128], H not a
+ * multiple of Hk, more than 2^29 rows of a sequence, or more of them in all than a
+ * launch covers (B H_r Sq > 2^28 - 16, or 2^24 tiles of 32 keys or of 32 rows of a
+ * group). Outputs may interleave in one buffer
+ * (dQ, dK and dV as parts of a fused gradient) when their strides agree and their
+ * columns do not meet. */
+int sbp_attn_core_fwd(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_view4_t *V,
+                      const sbp_attn_opts_t *opts, sbp_view4_t *O, sbp_view4_t *lse,
+                      int32_t p, int32_t r, const sbp_workspace_t *ws,
+                      hipStream_t stream);
+int sbp_attn_core_bwd(const sbp_view4_t *dO, const sbp_view4_t *Q,
+                      const sbp_view4_t *K, const sbp_view4_t *V, const sbp_view4_t *O,
+                      const sbp_view4_t *lse, const sbp_attn_opts_t *opts,
+                      sbp_view4_t *dQ, sbp_view4_t *dK, sbp_view4_t *dV, int32_t p,
+                      int32_t r, const sbp_workspace_t *ws, hipStream_t stream);
+
 /* ------------------------------------- cost model and strategy search --- */
 
 /* Collectives of the alpha-beta model (Sec. 3.1, Table 2). */

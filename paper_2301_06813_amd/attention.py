@@ -1,0 +1,113 @@
+"""Softmax attention of rank r's heads, from torch tensors.
+
+Convenience over the binding (``sbp_attn_core_fwd``, ``sbp_attn_core_bwd``): takes
+4-D tensors [batch][heads][rows][head_dim] (any strides with unit column stride,
+e.g. parts of a fused QKV activation), allocates the outputs and makes the call.
+All computation happens in libsbp.so.
+
+Q, K and V hold every head (``scope`` SBP_GLOBAL: rank r of p takes its share of the
+key heads, and the query heads that share them) or rank r's heads (SBP_LOCAL). The
+backward call's O, lse and dO may be either.
+"""
+from __future__ import annotations
+
+import math
+
+import torch
+
+from . import sbp
+
+_EMPTY = torch.empty
+
+
+def rank_heads(heads: int, kv_heads: int, p: int, r: int):
+    """(first query head, query heads, first key head, key heads) of rank r."""
+    group = heads // kv_heads if kv_heads else 1
+    hk = kv_heads // p + (r < kv_heads % p)
+    k0 = r * (kv_heads // p) + min(r, kv_heads % p)
+    return k0 * group, hk * group, k0, hk
+
+
+def _same_device(*tensors):
+    """The library's calls run on the current device, whose tensors these must be."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError("tensors are on %s, the current device is cuda:%d"
+                             % (t.device, device))
+
+
+def _opts(Q, scale, causal, window, len_q, len_k):
+    for t in (len_q, len_k):
+        if t is not None and t.shape != Q.shape[:1]:
+            raise ValueError("one length per sequence")
+    if scale is None:
+        scale = 1.0 / math.sqrt(Q.shape[-1])
+    return sbp.attn_opts(scale, causal, window, len_q, len_k)
+
+
+def _local(x, full, scope):
+    """View of an operand over query heads: LOCAL when it holds the rank's heads only."""
+    return sbp.view4(x, scope if x.shape[1] == full else sbp.SBP_LOCAL)
+
+
+def _rows(lse):
+    return lse.unsqueeze(-1) if lse.dim() == 3 else lse
+
+
+def core_fwd(Q, K, V, p: int = 1, r: int = 0, *, scale=None, causal: bool = False,
+             window: int = 0, len_q=None, len_k=None, lse: bool = True, out=None,
+             out_dtype=None, scope=sbp.SBP_GLOBAL, stream=None, ws=None):
+    """(O, lse): O [batch][local heads][rows][head_dim] in Q's dtype (or out_dtype, or
+    the given tensor `out`) and the rows' log-sum-exp [batch][local heads][rows] in
+    fp32, which the backward pass reads (None with lse=False)."""
+    B, H, sq, D = Q.shape
+    _same_device(Q, K, V, len_q, len_k, out)
+    hq = rank_heads(H, K.shape[1], p, r)[1] if scope == sbp.SBP_GLOBAL else H
+    if out is None:
+        # [batch][rows][heads][head_dim] in memory: what the output projection reads
+        out = _EMPTY((B, sq, hq, D), dtype=out_dtype or Q.dtype, device=Q.device).transpose(1, 2)
+    z = _EMPTY((B, hq, sq), dtype=torch.float32, device=Q.device) if lse else None
+    sbp.sbp_attn_core_fwd(sbp.view4(Q, scope), sbp.view4(K, scope), sbp.view4(V, scope),
+                          _opts(Q, scale, causal, window, len_q, len_k),
+                          sbp.view4(out, sbp.SBP_LOCAL),
+                          sbp.view4(z.unsqueeze(-1), sbp.SBP_LOCAL) if lse else None, p, r, stream,
+                          ws)
+    return out, z
+
+
+def bwd_workspace_bytes(B: int, hq: int, sq: int) -> int:
+    """Workspace that the backward call cannot do without."""
+    return 8 * ((B * hq * sq + 3) // 4 * 4)
+
+
+def core_bwd(dO, Q, K, V, O, lse, p: int = 1, r: int = 0, *, scale=None, causal: bool = False,
+             window: int = 0, len_q=None, len_k=None, out=None, grad_dtype=None,
+             accumulate: bool = False, scope=sbp.SBP_GLOBAL, stream=None, ws=None):
+    """(dQ, dK, dV) of rank r's heads, in the inputs' dtype (or grad_dtype), or in the
+    three given tensors `out` (accumulate: added to their fp32 contents). lse is
+    [batch][heads][rows] as core_fwd returns it."""
+    B, H, sq, D = Q.shape
+    Hk, sk = K.shape[1:3]
+    _same_device(dO, Q, K, V, O, lse, len_q, len_k, *(out or ()))
+    hq, hk = (H, Hk) if scope != sbp.SBP_GLOBAL else rank_heads(H, Hk, p, r)[1::2]
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the tensors to add to")
+        dt = grad_dtype or Q.dtype
+        out = (_EMPTY((B, sq, hq, D), dtype=dt, device=Q.device).transpose(1, 2),
+               _EMPTY((B, sk, hk, D), dtype=dt, device=Q.device).transpose(1, 2),
+               _EMPTY((B, sk, hk, D), dtype=dt, device=Q.device).transpose(1, 2))
+    need = bwd_workspace_bytes(B, hq, sq)
+    if ws is None and need > sbp.SBP_WORKSPACE_BYTES:
+        # more rows than the kept workspace has room for: one of this call's own
+        ws = _EMPTY(need, dtype=torch.uint8, device=Q.device)
+        if stream is not None:
+            ws.record_stream(torch.cuda.ExternalStream(stream))
+    o = sbp.SBP_ACCUMULATE if accumulate else sbp.SBP_LOCAL
+    sbp.sbp_attn_core_bwd(_local(dO, H, scope), sbp.view4(Q, scope), sbp.view4(K, scope),
+                          sbp.view4(V, scope), _local(O, H, scope),
+                          _local(_rows(lse), H, scope),
+                          _opts(Q, scale, causal, window, len_q, len_k), sbp.view4(out[0], o),
+                          sbp.view4(out[1], o), sbp.view4(out[2], o), p, r, stream, ws)
+    return out

@@ -14,4 +14,7 @@ int run_gemm(const sbpi::Gemm &g, hipStream_t s);
 // Two independent products (a backward pair) in one launch or in turn.
 int run_gemm_pair(const sbpi::Gemm &gd, const sbpi::Gemm &gw, hipStream_t s);
 
+// Records a HIP error for sbp_last_hip_error(); SBP_ERR_HIP.
+int hip_error(hipError_t e);
+
 }  // namespace sbpa

@@ -566,6 +566,7 @@ int run_gemm(const sbpi::Gemm &g, hipStream_t s) { return run(g, Ws{}, s); }
 int run_gemm_pair(const sbpi::Gemm &gd, const sbpi::Gemm &gw, hipStream_t s) {
     return run_pair(gd, gw, Ws{}, s);
 }
+int hip_error(hipError_t e) { return hip_fail(e); }
 }  // namespace sbpa
 
 extern "C" {

@@ -47,7 +47,8 @@ EXPORTS = ("sbp_shard_index", "sbp_signature", "sbp_linear_fwd", "sbp_linear_bwd
            "sbp_nd_linear_fwd", "sbp_nd_linear_bwd_data", "sbp_nd_linear_bwd_weight",
            "sbp_nd_linear_bwd", "sbp_attn_scores", "sbp_attn_context", "sbp_attn_scores_bwd",
            "sbp_attn_context_bwd", "sbp_set_override_orients", "sbp_collective_cost",
-           "sbp_boxing_cost", "sbp_chain_cost", "sbp_search_strategy", "sbp_linear_bwd_noalloc")
+           "sbp_boxing_cost", "sbp_chain_cost", "sbp_search_strategy", "sbp_linear_bwd_noalloc",
+           "sbp_attn_core_fwd", "sbp_attn_core_bwd")
 
 SBP_COLL_ALLREDUCE, SBP_COLL_ALLGATHER, SBP_COLL_REDUCESCATTER, SBP_COLL_ALLTOALL = 0, 1, 2, 3
 SBP_SIG_DP, SBP_SIG_COL, SBP_SIG_KS, SBP_SIG_PB, SBP_SIG_BP, SBP_SIG_BB = 0, 1, 2, 3, 4, 5
@@ -103,6 +104,12 @@ class sbp_view4_t(ctypes.Structure):
                 ("rows", ctypes.c_int64), ("cols", ctypes.c_int64),
                 ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
                 ("ld", ctypes.c_int64), ("dtype", ctypes.c_int32), ("scope", ctypes.c_int32)]
+
+
+class sbp_attn_opts_t(ctypes.Structure):
+    _fields_ = [("scale", ctypes.c_float), ("causal", ctypes.c_int32),
+                ("window", ctypes.c_int32), ("len_q", ctypes.c_void_p),
+                ("len_k", ctypes.c_void_p)]
 
 
 class sbp_chain_t(ctypes.Structure):
@@ -222,6 +229,11 @@ def lib():
         for fn in ("sbp_attn_scores_bwd", "sbp_attn_context_bwd"):
             getattr(L, fn).argtypes = [V4, V4, V4, V4, V4, ctypes.c_int32, ctypes.c_int32,
                                        ctypes.c_void_p]
+        OPT = P(sbp_attn_opts_t)
+        L.sbp_attn_core_fwd.argtypes = [V4, V4, V4, OPT, V4, V4, ctypes.c_int32, ctypes.c_int32, WS,
+                                        ctypes.c_void_p]
+        L.sbp_attn_core_bwd.argtypes = [V4, V4, V4, V4, V4, V4, OPT, V4, V4, V4, ctypes.c_int32,
+                                        ctypes.c_int32, WS, ctypes.c_void_p]
         D = ctypes.c_double
         L.sbp_collective_cost.argtypes = [ctypes.c_int32, ctypes.c_int32, D, D, D, P(D)]
         L.sbp_boxing_cost.argtypes = [P(sbp_layout_t), P(sbp_layout_t), D, D, D, P(D),
@@ -512,6 +524,47 @@ def sbp_attn_context_bwd(dO, P_, V, dP, dV, p: int, r: int, stream=None):
     """dP = dO V^T and dV = P^T dO per (batch, local head)."""
     _check(lib().sbp_attn_context_bwd(ctypes.byref(dO), ctypes.byref(P_), ctypes.byref(V),
                                       ctypes.byref(dP), ctypes.byref(dV), p, r, _stream(stream)))
+
+
+# ---------------------------------------------------- softmax attention
+def attn_opts(scale: float, causal: bool = False, window: int = 0, len_q=None,
+              len_k=None) -> sbp_attn_opts_t:
+    """sbp_attn_opts_t; len_q and len_k are contiguous int32 device tensors, one
+    length per sequence (kept alive by the caller), or None."""
+    return sbp_attn_opts_t(scale, causal, window, _lens(len_q), _lens(len_k))
+
+
+def _lens(t):
+    if t is None:
+        return None
+    import torch
+    if t.dtype != torch.int32 or t.dim() != 1 or not t.is_contiguous():
+        raise ValueError("lengths are a contiguous 1-D int32 tensor")
+    return t.data_ptr()
+
+
+def sbp_attn_core_fwd(Q, K, V, opts: sbp_attn_opts_t, O, lse, p: int, r: int, stream=None, ws=None):
+    """O and lse (a view, or None) of rank r's heads."""
+    s = current_stream() if stream is None else stream
+    ref = ctypes.byref
+    rc = (_lib or lib()).sbp_attn_core_fwd(ref(Q), ref(K), ref(V), ref(opts), ref(O),
+                                           None if lse is None else ref(lse), p, r,
+                                           ref(_ws(ws, s)), ctypes.c_void_p(s))
+    if rc:
+        _check(rc)
+
+
+def sbp_attn_core_bwd(dO, Q, K, V, O, lse, opts: sbp_attn_opts_t, dQ, dK, dV, p: int, r: int,
+                      stream=None, ws=None):
+    """dQ, dK and dV of rank r's heads from dO, O and lse. The workspace has to hold 8
+    bytes per query row of the rank."""
+    s = current_stream() if stream is None else stream
+    ref = ctypes.byref
+    rc = (_lib or lib()).sbp_attn_core_bwd(ref(dO), ref(Q), ref(K), ref(V), ref(O), ref(lse),
+                                           ref(opts), ref(dQ), ref(dK), ref(dV), p, r,
+                                           ref(_ws(ws, s)), ctypes.c_void_p(s))
+    if rc:
+        _check(rc)
 
 
 # ------------------------------------------- cost model and search

@@ -335,6 +335,68 @@ int sbp_nd_linear_bwd(const sbp_view_t *dY, const sbp_nd_layout_t *ldy,
                       sbp_view_t *dW, sbp_nd_layout_t *ldw_out,
                       const sbp_workspace_t *ws, hipStream_t stream);
 
+/* --------------------------------------- gated feed-forward block --- */
+
+/* act(x): SILU x sigmoid(x); GELU, the Gaussian error linear unit in its tanh form,
+ * 0.5 x (1 + tanh(sqrt(2/pi) (x + 0.044715 x^3))); RELU max(x, 0). */
+typedef enum { SBP_ACT_SILU = 0, SBP_ACT_GELU = 1, SBP_ACT_RELU = 2 } sbp_act_t;
+
+/* The first half of a gated feed-forward block on rank r's shares,
+ *     H = act(X Wg) * (X Wu)   (element-wise product),
+ * both projections, the activation and the product in one kernel for bf16. X: M x K,
+ * state *lx; Wg, Wu: K x N, both in state *lw. The product with the down projection is
+ * an ordinary linear (sbp_linear_fwd on H).
+ *
+ * Signatures: those of Y = X W whose Y is no partial sum -- DP, COL and BB (an
+ * activation of a partial sum is no partial sum of activations); else
+ * SBP_ERR_SIGNATURE. H takes Y's state, dH dY's, dX and the weights' gradients
+ * dX's and dW's:
+ *     DP   H S(0)   dH S(0)   dX S(0)   dWg, dWu P
+ *     COL  H S(1)   dH S(1)   dX P      dWg, dWu S(1)
+ *     BB   H B      dH P      dX P      dWg, dWu P
+ *
+ * sbp_gated_fwd: H, and with G and U (both or neither NULL) the projections
+ * G = X Wg, U = X Wu for the backward pass. Inputs bf16 or fp32; H, G and U have the
+ * inputs' dtype (SBP_ERR_DTYPE) and the local shape. H is computed from the fp32 sums,
+ * not from the rounded G and U. fp32 calls need G and U (SBP_ERR_NULL).
+ *
+ * sbp_gated_bwd: from dH, G and U
+ *     dU = dH * act(G),  dG = dH * U * act'(G),
+ *     dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU.
+ * G and U: H's state, as the forward call left them. dG, dU: local m x n buffers of
+ * the inputs' dtype that the call fills (bf16: rounded, as the operands of the
+ * products, whose fp32 results carry that rounding too). dX, dWg, dWu: fp32, or for bf16
+ * inputs bf16 where they are no partial sum of several devices (a sum over one device
+ * is the tensor); SBP_ACCUMULATE adds to fp32 contents. dWg and dWu have one dtype. dX is
+ * rounded once, from the sum of both products.
+ *
+ * No output may overlap an input or another output. ws as for sbp_linear_fwd. Errors:
+ * those of the linear calls; SBP_ERR_SHAPE also for an unknown act and for outputs of 2^22
+ * tiles of 64 x 64 or more. */
+int sbp_gated_fwd(const sbp_view_t *X, const sbp_layout_t *lx, const sbp_view_t *Wg,
+                  const sbp_view_t *Wu, const sbp_layout_t *lw, int32_t act,
+                  sbp_view_t *H, sbp_layout_t *lh_out, sbp_view_t *G, sbp_view_t *U,
+                  const sbp_workspace_t *ws, hipStream_t stream);
+int sbp_gated_bwd(const sbp_view_t *dH, const sbp_layout_t *ldh, const sbp_view_t *X,
+                  const sbp_layout_t *lx, const sbp_view_t *Wg, const sbp_view_t *Wu,
+                  const sbp_layout_t *lw, int32_t act, const sbp_view_t *G,
+                  const sbp_view_t *U, sbp_view_t *dG, sbp_view_t *dU, sbp_view_t *dX,
+                  sbp_layout_t *ldx_out, sbp_view_t *dWg, sbp_view_t *dWu,
+                  sbp_layout_t *ldw_out, const sbp_workspace_t *ws, hipStream_t stream);
+/* nd forms: one of DP, COL and BB on every mesh axis. */
+int sbp_nd_gated_fwd(const sbp_view_t *X, const sbp_nd_layout_t *lx, const sbp_view_t *Wg,
+                     const sbp_view_t *Wu, const sbp_nd_layout_t *lw, int32_t act,
+                     sbp_view_t *H, sbp_nd_layout_t *lh_out, sbp_view_t *G, sbp_view_t *U,
+                     const sbp_workspace_t *ws, hipStream_t stream);
+int sbp_nd_gated_bwd(const sbp_view_t *dH, const sbp_nd_layout_t *ldh,
+                     const sbp_view_t *X, const sbp_nd_layout_t *lx,
+                     const sbp_view_t *Wg, const sbp_view_t *Wu,
+                     const sbp_nd_layout_t *lw, int32_t act, const sbp_view_t *G,
+                     const sbp_view_t *U, sbp_view_t *dG, sbp_view_t *dU,
+                     sbp_view_t *dX, sbp_nd_layout_t *ldx_out, sbp_view_t *dWg,
+                     sbp_view_t *dWu, sbp_nd_layout_t *ldw_out,
+                     const sbp_workspace_t *ws, hipStream_t stream);
+
 /* ------------------------------ attention core under a head split --- */
 
 /* A strided 4-D view [batch][heads][rows][cols]: element (b, h, i, j) is at

@@ -115,6 +115,11 @@ hipError_t launch_split_reduce_pair(const Gemm &gd, int sd, const float *wsd, co
 bool plan_bf16_bwd(const Gemm &gd, const Gemm &gw, Plan *pd, Plan *pw);
 hipError_t launch_bf16_bwd_group(const Gemm &gd, const Plan &pd, const Gemm &gw,
                                  const Plan &pw, float *ws, hipStream_t s);
+// Plans of the gated block's backward products in one grid (gated_bwd.hip): gd its dX
+// over both pairs of operands, gw dWg and dWu as a batch of two; dma: the pipelined
+// kernels can read every operand. Both share an instance, split reductions in even
+// numbers of 64-wide blocks (no 128-wide stage holds two pairs) and fit gd.ws_floats.
+void plan_bf16_gated_bwd(const Gemm &gd, const Gemm &gw, bool dma, Plan *pd, Plan *pw);
 // Whether 16-byte loads can read both operands of an fp32 product (base, leading
 // dimension and contiguous extent multiples of 4 floats).
 bool f32_vec4(const Gemm &g);

@@ -599,9 +599,19 @@ __device__ __forceinline__ void dma_tile_body(const Args &g, const int L, char *
     auto issue = [&](int kb, int stage) {
         char *base = smem + stage * STAGE;
         const int k0 = k_begin + kb * BKD;
-        TA::template issue<SHIFT>(Ab, g.lda, m0, g.m + shift_m(g), k0, k_lim, base, wave, lane);
-        TB::template issue<SHIFT>(Bb, g.ldb, n0, g.n + shift_n(g), k0, k_lim, base + A_BYTES, wave,
-                                  lane);
+        if constexpr (two_pairs<Args>) {
+            const bool second = k0 >= g.kp;
+            const int k = second ? k0 - g.kp : k0;
+            const int lim = second ? k_lim - g.kp : min(k_lim, g.k1);
+            TA::template issue<false>(second ? g.A2 : Ab, second ? g.lda2 : g.lda, m0, g.m, k, lim,
+                                      base, wave, lane);
+            TB::template issue<false>(second ? g.B2 : Bb, second ? g.ldb2 : g.ldb, n0, g.n, k, lim,
+                                      base + A_BYTES, wave, lane);
+        } else {
+            TA::template issue<SHIFT>(Ab, g.lda, m0, g.m + shift_m(g), k0, k_lim, base, wave, lane);
+            TB::template issue<SHIFT>(Bb, g.ldb, n0, g.n + shift_n(g), k0, k_lim, base + A_BYTES,
+                                      wave, lane);
+        }
     };
     f32x16 acc[MI][NI];
 #pragma unroll
@@ -643,47 +653,59 @@ __device__ __forceinline__ void dma_tile_body(const Args &g, const int L, char *
         using RB = RegTile<BN, NW, B_KMAJ>;
         typename RA::Regs va[2];
         typename RB::Regs vb[2];
-        const int whole = min(RA::whole_steps(m0, g.m, g.lda, k_begin, k_lim, g.k),
-                              RB::whole_steps(n0, g.n, g.ldb, k_begin, k_lim, g.k));
-        if (whole > 0) {
-            RA ra;
-            RB rb;
-            ra.init(Ab, g.lda, m0, g.m, k_begin, tid);
-            rb.init(Bb, g.ldb, n0, g.n, k_begin, tid);
-            auto load = [&](int r) {
-                ra.load(va[r], g.lda);
-                rb.load(vb[r], g.ldb);
-            };
-            auto fill = [&](int stage, int r) {
-                RA::store(va[r], smem + stage * STAGE, tid);
-                RB::store(vb[r], smem + stage * STAGE + A_BYTES, tid);
-            };
-            auto step = [&](int it, auto par) {   // par: (it + 1) % 2
-                constexpr int P = decltype(par)::value;
-                if (it + 1 < whole) fill(P, P);
-                if (it + 3 < whole) load(P);
-                compute(smem + (1 - P) * STAGE);
+        // reduction indices [k_begin, k_lim) of one pair of operands with k_all of them
+        auto reduce = [&](const uint16_t *Ab, int64_t lda, const uint16_t *Bb, int64_t ldb,
+                          const int k_begin, const int k_lim, const int k_all) {
+            const int nkb = max(0, (k_lim - k_begin + BKD - 1) / BKD);
+            const int whole = min(RA::whole_steps(m0, g.m, lda, k_begin, k_lim, k_all),
+                                  RB::whole_steps(n0, g.n, ldb, k_begin, k_lim, k_all));
+            if (whole > 0) {
+                RA ra;
+                RB rb;
+                ra.init(Ab, lda, m0, g.m, k_begin, tid);
+                rb.init(Bb, ldb, n0, g.n, k_begin, tid);
+                auto load = [&](int r) {
+                    ra.load(va[r], lda);
+                    rb.load(vb[r], ldb);
+                };
+                auto fill = [&](int stage, int r) {
+                    RA::store(va[r], smem + stage * STAGE, tid);
+                    RB::store(vb[r], smem + stage * STAGE + A_BYTES, tid);
+                };
+                auto step = [&](int it, auto par) {   // par: (it + 1) % 2
+                    constexpr int P = decltype(par)::value;
+                    if (it + 1 < whole) fill(P, P);
+                    if (it + 3 < whole) load(P);
+                    compute(smem + (1 - P) * STAGE);
+                    __syncthreads();
+                };
+                load(0);
+                if (whole > 1) load(1);
+                fill(0, 0);
+                if (whole > 2) load(0);
                 __syncthreads();
-            };
-            load(0);
-            if (whole > 1) load(1);
-            fill(0, 0);
-            if (whole > 2) load(0);
-            __syncthreads();
-            for (int it = 0; it < whole; it += 2) {
-                step(it, std::integral_constant<int, 1>{});
-                if (it + 1 < whole) step(it + 1, std::integral_constant<int, 0>{});
+                for (int it = 0; it < whole; it += 2) {
+                    step(it, std::integral_constant<int, 1>{});
+                    if (it + 1 < whole) step(it + 1, std::integral_constant<int, 0>{});
+                }
             }
-        }
-        for (int it = whole; it < nkb; ++it) {
-            const int k0 = k_begin + it * BKD;
-            RA::load_edge(va[0], Ab, g.lda, m0, g.m, k0, k_lim, tid);
-            RB::load_edge(vb[0], Bb, g.ldb, n0, g.n, k0, k_lim, tid);
-            RA::store(va[0], smem, tid);
-            RB::store(vb[0], smem + A_BYTES, tid);
-            __syncthreads();
-            compute(smem);
-            __syncthreads();
+            for (int it = whole; it < nkb; ++it) {
+                const int k0 = k_begin + it * BKD;
+                RA::load_edge(va[0], Ab, lda, m0, g.m, k0, k_lim, tid);
+                RB::load_edge(vb[0], Bb, ldb, n0, g.n, k0, k_lim, tid);
+                RA::store(va[0], smem, tid);
+                RB::store(vb[0], smem + A_BYTES, tid);
+                __syncthreads();
+                compute(smem);
+                __syncthreads();
+            }
+        };
+        if constexpr (two_pairs<Args>) {
+            reduce(Ab, g.lda, Bb, g.ldb, min(k_begin, g.k1), min(k_lim, g.k1), g.k1);
+            reduce(g.A2, g.lda2, g.B2, g.ldb2, max(0, k_begin - g.kp), max(0, k_lim - g.kp),
+                   g.k - g.kp);
+        } else {
+            reduce(Ab, g.lda, Bb, g.ldb, k_begin, k_lim, g.k);
         }
     }
 
@@ -723,7 +745,8 @@ __device__ __forceinline__ void dma_tile_body(const Args &g, const int L, char *
     const bool partial = ACCUM != ACC_ALL && g.splits > 1;
     const bool add = ACCUM == ACC_ALL || (ACCUM == ACC_SOME && g.accumulate);
     const int ldw = (int)sbpi::partial_ld(g.n);
-    float *const ws_out = g.ws + (size_t)split * (size_t)g.m * (size_t)ldw;
+    const int slice = two_pairs<Args> ? L / per_b * g.splits + split : split;
+    float *const ws_out = g.ws + (size_t)slice * (size_t)g.m * (size_t)ldw;
     const bool ws_vec = shift_n(g) % 4 == 0;
     // the tile's first output row and column (SHIFT: kernel index minus the
     // shift; may be negative, and bounds are then checked as unsigned)

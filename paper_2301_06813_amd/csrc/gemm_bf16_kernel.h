@@ -28,6 +28,8 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
+#include <type_traits>
+
 #include "gemm.h"
 
 namespace sbpk {
@@ -84,6 +86,20 @@ __device__ __forceinline__ int shift_m(const GemmArgsShift &g) { return g.sm; }
 __device__ __forceinline__ int shift_n(const GemmArgsShift &g) { return g.sn; }
 __device__ __forceinline__ int shift_k(const GemmArgsShift &g) { return g.sk; }
 __device__ __forceinline__ int kmask_of(const GemmArgsShift &g) { return g.kmask; }
+
+// Arguments of a product whose reduction runs over two operand pairs in turn,
+// C = A B + A2 B2 (dX = dG Wg^T + dU Wu^T of a gated block): reduction indices
+// [0, kp) are the first pair's, of which [0, k1) exist (kp is k1 rounded up to whole
+// stages, so that no stage holds both), and [kp, k) the second's. Or, with nbatch = 2,
+// of two products that share A and split their reduction alike (dWg and dWu); each has
+// its own slices of the workspace, the second's behind the first's.
+struct GemmArgsTwo : GemmArgs {
+    const uint16_t *A2, *B2;
+    int64_t lda2, ldb2;
+    int32_t k1, kp;
+};
+template <class Args>
+constexpr bool two_pairs = std::is_base_of<GemmArgsTwo, Args>::value;
 
 // Operand and output bases of batch item z (uniform per work item).
 template <bool OUT_F32>

@@ -801,6 +801,101 @@ static Plan plan_model(const Gemm &g, double *time) {
     return best;
 }
 
+// The instances that the gated block's backward products exist for
+// (gated_products.h); the last two also added to their outputs.
+struct GatedCode {
+    int bm, bn, code;
+    bool acc;
+};
+static constexpr GatedCode kGatedCodes[] = {{256, 256, 1, false}, {128, 128, 12, false},
+                                            {64, 64, 12, false},  {128, 128, 4, true},
+                                            {64, 64, 4, true}};
+
+// Blocks of 64 a split, an even number.
+static void split_even(int kb, int s, int *splits, int *per) {
+    split_of(kb, s, splits, per);
+    if (kb <= 0) return;
+    *per = (*per + 1) & ~1;
+    *splits = (kb + *per - 1) / *per;
+}
+
+static void plan_gated_uncached(const Gemm &gd, const Gemm &gw, bool dma, Plan *pd, Plan *pw) {
+    const int kd = kblocks(gd.k), kw = kblocks(gw.k);
+    double best = 1e30;
+    auto consider = [&](int bm, int bn, const Instance *in, auto &&time) {
+        int last_d = 0;
+        for (int a = 1; a <= 16; ++a) {
+            int sd, perd;
+            split_even(kd, a, &sd, &perd);
+            if (sd == last_d) continue;
+            last_d = sd;
+            int last_w = 0;
+            for (int b = 1; b <= 32; ++b) {
+                int sw, perw;
+                split_even(kw, b, &sw, &perw);
+                if (sw == last_w) continue;
+                last_w = sw;
+                const double need = (sd > 1 ? (double)sd * gd.m * partial_ld(gd.n) : 0.0) +
+                                    (sw > 1 ? 2.0 * sw * gw.m * partial_ld(gw.n) : 0.0);
+                if (need > ws_budget(gd)) continue;
+                const double t = time(sd, perd, sw, perw);
+                if (t >= best * 0.999) continue;
+                best = t;
+                *pd = in ? Plan{bm, bn, sd, perd, true, in->ns, in->kg, in->epi, 0, in->bk}
+                         : Plan{bm, bn, sd, perd, false};
+                *pw = *pd;
+                pw->splits = sw;
+                pw->kblk_per_split = perw;
+            }
+        }
+    };
+    if (dma) {
+        for (const GatedCode &g : kGatedCodes)
+            for (const PipeClass &c : kPipe) {
+                if (c.bm != g.bm || c.bn != g.bn || c.code != g.code) continue;
+                consider(c.bm, c.bn, find_instance(c.code, c.bm, c.bn),
+                         [&](int sd, int perd, int sw, int perw) {
+                             if (!g.acc && ((gd.accumulate && sd == 1) || (gw.accumulate && sw == 1)))
+                                 return 1e30;
+                             return model_pair(gd, gw, c, sd, perd, sw, perw, false);
+                         });
+            }
+        return;
+    }
+    for (const GenericTile &t : kGeneric) {
+        if (!(t.bm == 128 && t.bn == 128) && !(t.bm == 64 && t.bn == 64)) continue;
+        consider(t.bm, t.bn, nullptr, [&](int sd, int perd, int sw, int perw) {
+            auto items = [&](const Gemm &g, int s) {
+                return (double)((g.m + t.bm - 1) / t.bm) * (double)((g.n + t.bn - 1) / t.bn) * s *
+                       (double)g.nbatch();
+            };
+            const double nd = items(gd, sd), nw = items(gw, sw), q = (nd + nw) / kCUs;
+            const double steps = std::max((nd * perd + nw * perw) / kCUs + std::min(perd, perw) / 2.0,
+                                          (double)std::max(perd, perw));
+            double tm = steps * t.step + q * 1e-6;
+            if (sd > 1) tm += (sd * 2.0 + 0.5) * 4.0 * gd.m * gd.n / 6e12 + 3e-6;
+            if (sw > 1) tm += 2.0 * (sw * 2.0 + 0.5) * 4.0 * gw.m * gw.n / 6e12 + 3e-6;
+            return tm;
+        });
+    }
+}
+
+void plan_bf16_gated_bwd(const Gemm &gd, const Gemm &gw, bool dma, Plan *pd, Plan *pw) {
+    // kept like the other pairs; no linear's pair has a batch of two
+    const PairKey k{key_of(gd, dma), key_of(gw, dma), -1};
+    auto it = pair_cache.find(k);
+    PairPlan p;
+    if (it != pair_cache.end()) {
+        p = it->second;
+    } else {
+        p.grouped = true;
+        plan_gated_uncached(gd, gw, dma, &p.d, &p.w);
+        keep(pair_cache, k, p);
+    }
+    *pd = p.d;
+    *pw = p.w;
+}
+
 // fp32 products (gemm_f32.hip). Measured on MI355X, a 32-wide reduction step of
 // a 128 x 128 tile takes a compute unit 2.1 us however many workgroups share
 // it (fp32 MFMA bound); one of a 64 x 64 tile 0.55 us when two or more

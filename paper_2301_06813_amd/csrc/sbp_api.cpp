@@ -14,6 +14,7 @@
 
 #include "../../include/sbp.h"
 #include "api_internal.h"
+#include "gated.h"
 #include "gemm.h"
 
 namespace {
@@ -559,6 +560,228 @@ int linear_bwd(const sbp_view_t *dY, const L *ldy, const sbp_view_t *X, const L 
     return SBP_OK;
 }
 
+// ------------------------------------------------ gated feed-forward block
+// Devices over which a state is a partial sum (1: the tensor is whole).
+int64_t partial_devices(const sbp_layout_t &l) { return l.kind == SBP_PARTIAL ? l.p : 1; }
+int64_t partial_devices(const sbp_nd_layout_t &l) {
+    int64_t n = 1;
+    for (int a = 0; a < l.ndim; ++a)
+        if (l.kind[a] == SBP_PARTIAL) n *= l.p[a];
+    return n;
+}
+
+typedef std::pair<uintptr_t, uintptr_t> Span;
+
+Span span_of(const Local &x) { return extent(x.ptr, x.rows, x.cols, x.ld, x.dtype); }
+Span span_of(const sbp_view_t *v) { return extent(v->data, v->rows, v->cols, v->ld, v->dtype); }
+
+sbpi::Mat mat_of(const Local &x) { return {const_cast<char *>(x.ptr), x.ld}; }
+sbpi::Mat mat_of(const sbp_view_t *v) { return {v->data, v->ld}; }
+
+// An element-wise operand or output in H's state: rank r's rows x cols of it.
+template <class L>
+int gate_input(const sbp_view_t *v, const L *l, const Local &x, const Local &w, int64_t rows,
+               int64_t cols, Local *out) {
+    int rc = local_input(v, l, out);
+    if (rc) return rc;
+    if (out->dtype != x.dtype) return SBP_ERR_DTYPE;
+    if (out->rows != rows || out->cols != cols) return SBP_ERR_SHAPE;
+    if (out->global && ((x.global && out->grows != x.grows) || (w.global && out->gcols != w.gcols)))
+        return SBP_ERR_SHAPE;
+    return SBP_OK;
+}
+
+int plain_output(const sbp_view_t *v, int64_t rows, int64_t cols, int32_t dtype) {
+    int rc = check_view_common(v);
+    if (rc) return rc;
+    if (v->dtype != dtype) return SBP_ERR_DTYPE;
+    if (v->rows != rows || v->cols != cols || v->scope == SBP_ACCUMULATE) return SBP_ERR_SHAPE;
+    return SBP_OK;
+}
+
+// A gradient in state st: fp32 where it is a partial sum of several devices.
+template <class L>
+int gradient(const sbp_view_t *v, int64_t rows, int64_t cols, int32_t in_dtype, const L &st) {
+    int rc = check_view_common(v);
+    if (rc) return rc;
+    if (v->rows != rows || v->cols != cols) return SBP_ERR_SHAPE;
+    if (v->dtype != SBP_F32 && (in_dtype == SBP_F32 || partial_devices(st) > 1 ||
+                                v->scope == SBP_ACCUMULATE))
+        return SBP_ERR_DTYPE;
+    return SBP_OK;
+}
+
+// A launch's workgroups (64 x 64 tiles of 512 threads at most) fit its 32-bit thread
+// count.
+bool tiles_fit(int64_t m, int64_t n) {
+    return (double)((m + 63) / 64) * (double)((n + 63) / 64) < 4194304.0;
+}
+
+// X, Wg and Wu of rank r, and the states st of H, dH, dX and the weights' gradients. H must
+// be whole on every device that holds it: act of a partial sum is no partial sum.
+template <class L>
+int gate_operands(const sbp_view_t *X, const L *lx, const sbp_view_t *Wg, const sbp_view_t *Wu,
+                  const L *lw, int32_t act, Local *x, Local *wg, Local *wu, L st[4]) {
+    if (!X || !Wg || !Wu || !lx || !lw) return SBP_ERR_NULL;
+    int rc = resolve(PAIR_XW, lx, lw, st);
+    if (rc) return rc;
+    if (is_partial(st[0])) return SBP_ERR_SIGNATURE;
+    if (act != SBP_ACT_SILU && act != SBP_ACT_GELU && act != SBP_ACT_RELU) return SBP_ERR_SHAPE;
+    if ((rc = local_input(X, lx, x))) return rc;
+    if ((rc = local_input(Wg, lw, wg))) return rc;
+    if ((rc = local_input(Wu, lw, wu))) return rc;
+    if (x->dtype != wg->dtype || x->dtype != wu->dtype) return SBP_ERR_DTYPE;
+    if (x->global && wg->global && x->gcols != wg->grows) return SBP_ERR_SHAPE;
+    if (x->global && wu->global && x->gcols != wu->grows) return SBP_ERR_SHAPE;
+    if (x->cols != wg->rows || wu->rows != wg->rows || wu->cols != wg->cols) return SBP_ERR_SHAPE;
+    if (!tiles_fit(x->rows, wg->cols) || !tiles_fit(x->rows, x->cols) ||
+        !tiles_fit(x->cols, wg->cols))
+        return SBP_ERR_SHAPE;
+    return SBP_OK;
+}
+
+sbpi::Gated gate_of(const Local &x, const Local &wg, const Local &wu, int32_t act, const Ws &w) {
+    sbpi::Gated a;
+    a.dtype = x.dtype;
+    a.act = act;
+    a.m = x.rows;
+    a.k = x.cols;
+    a.n = wg.cols;
+    a.x = mat_of(x);
+    a.wg = mat_of(wg);
+    a.wu = mat_of(wu);
+    a.ws = w.ptr;
+    a.ws_floats = w.floats;
+    return a;
+}
+
+sbpi::Gemm f32_product(int orient, const sbpi::Mat &A, const sbpi::Mat &B, const sbpi::Mat &C,
+                       int64_t m, int64_t n, int64_t k, int acc) {
+    sbpi::Gemm g{orient, SBP_F32, SBP_F32, A.p, A.ld, B.p, B.ld, C.p, C.ld, m, n, k};
+    g.accumulate = acc;
+    return g;
+}
+
+template <class L>
+int gated_fwd(const sbp_view_t *X, const L *lx, const sbp_view_t *Wg, const sbp_view_t *Wu,
+              const L *lw, int32_t act, sbp_view_t *H, L *lh_out, sbp_view_t *G, sbp_view_t *U,
+              const sbp_workspace_t *ws, hipStream_t stream) {
+    if (!H || (!G) != (!U)) return SBP_ERR_NULL;
+    Local x, wg, wu;
+    L st[4];
+    int rc = gate_operands(X, lx, Wg, Wu, lw, act, &x, &wg, &wu, st);
+    if (rc) return rc;
+    sbp_view_t *const outs[3] = {H, G, U};
+    for (const sbp_view_t *o : outs)
+        if (o && (rc = plain_output(o, x.rows, wg.cols, x.dtype))) return rc;
+    if (x.dtype == SBP_F32 && !G) return SBP_ERR_NULL;
+    Ws w;
+    if ((rc = check_ws(ws, &w))) return rc;
+    const Span ins[4] = {span_of(x), span_of(wg), span_of(wu), w.span};
+    for (int i = 0; i < 3 && outs[i]; ++i) {
+        for (const Span &s : ins)
+            if (overlaps(span_of(outs[i]), s)) return SBP_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlaps(span_of(outs[i]), span_of(outs[j]))) return SBP_ERR_ALIAS;
+    }
+    for (int i = 0; i < 3; ++i)
+        if (overlaps(ins[i], w.span)) return SBP_ERR_ALIAS;
+    if (x.rows > 0 && wg.cols > 0) {
+        sbpi::Gated a = gate_of(x, wg, wu, act, w);
+        a.h = mat_of(H);
+        if (G) {
+            a.g = mat_of(G);
+            a.u = mat_of(U);
+        }
+        hipError_t e;
+        if (x.dtype == SBP_F32) {
+            // two products on the fp32 kernels, then the gate
+            if ((rc = run(f32_product(sbpi::OR_FWD, a.x, a.wg, a.g, a.m, a.n, a.k, 0), w, stream)))
+                return rc;
+            if ((rc = run(f32_product(sbpi::OR_FWD, a.x, a.wu, a.u, a.m, a.n, a.k, 0), w, stream)))
+                return rc;
+            e = sbpi::launch_gated_act(a, stream);
+        } else {
+            e = sbpi::launch_gated_fwd(a, stream);
+        }
+        if (e != hipSuccess) return hip_fail(e);
+    }
+    if (lh_out) *lh_out = st[0];
+    return SBP_OK;
+}
+
+template <class L>
+int gated_bwd(const sbp_view_t *dH, const L *ldh, const sbp_view_t *X, const L *lx,
+              const sbp_view_t *Wg, const sbp_view_t *Wu, const L *lw, int32_t act,
+              const sbp_view_t *G, const sbp_view_t *U, sbp_view_t *dG, sbp_view_t *dU,
+              sbp_view_t *dX, L *ldx_out, sbp_view_t *dWg, sbp_view_t *dWu, L *ldw_out,
+              const sbp_workspace_t *ws, hipStream_t stream) {
+    if (!dH || !G || !U || !dG || !dU || !dX || !dWg || !dWu || !ldh) return SBP_ERR_NULL;
+    Local x, wg, wu, dh, g, u;
+    L st[4];
+    int rc = gate_operands(X, lx, Wg, Wu, lw, act, &x, &wg, &wu, st);
+    if (rc) return rc;
+    if ((rc = check_pair(ldh, lw))) return rc;
+    if (!one_signature(lx, lw, ldh)) return SBP_ERR_SIGNATURE;
+    if ((rc = gate_input(dH, ldh, x, wg, x.rows, wg.cols, &dh))) return rc;
+    if ((rc = gate_input(G, &st[0], x, wg, x.rows, wg.cols, &g))) return rc;
+    if ((rc = gate_input(U, &st[0], x, wg, x.rows, wg.cols, &u))) return rc;
+    if ((rc = plain_output(dG, x.rows, wg.cols, x.dtype))) return rc;
+    if ((rc = plain_output(dU, x.rows, wg.cols, x.dtype))) return rc;
+    if ((rc = gradient(dX, x.rows, x.cols, x.dtype, st[2]))) return rc;
+    if ((rc = gradient(dWg, wg.rows, wg.cols, x.dtype, st[3]))) return rc;
+    if ((rc = gradient(dWu, wg.rows, wg.cols, x.dtype, st[3]))) return rc;
+    if (dWg->dtype != dWu->dtype) return SBP_ERR_DTYPE;
+    Ws w;
+    if ((rc = check_ws(ws, &w))) return rc;
+    const Span ins[7] = {span_of(x), span_of(wg), span_of(wu), span_of(dh),
+                         span_of(g), span_of(u),  w.span};
+    const sbp_view_t *const outs[5] = {dG, dU, dX, dWg, dWu};
+    for (int i = 0; i < 5; ++i) {
+        for (const Span &s : ins)
+            if (overlaps(span_of(outs[i]), s)) return SBP_ERR_ALIAS;
+        for (int j = 0; j < i; ++j)
+            if (overlaps(span_of(outs[i]), span_of(outs[j]))) return SBP_ERR_ALIAS;
+    }
+    for (int i = 0; i < 6; ++i)
+        if (overlaps(ins[i], w.span)) return SBP_ERR_ALIAS;
+    sbpi::Gated a = gate_of(x, wg, wu, act, w);
+    a.dh = mat_of(dh);
+    a.g = mat_of(g);
+    a.u = mat_of(u);
+    a.dg = mat_of(dG);
+    a.du = mat_of(dU);
+    a.dx = mat_of(dX);
+    a.dwg = mat_of(dWg);
+    a.dwu = mat_of(dWu);
+    a.dx_dtype = dX->dtype;
+    a.dw_dtype = dWg->dtype;
+    a.dx_acc = dX->scope == SBP_ACCUMULATE;
+    a.dwg_acc = dWg->scope == SBP_ACCUMULATE;
+    a.dwu_acc = dWu->scope == SBP_ACCUMULATE;
+    hipError_t e = sbpi::launch_gated_grad(a, stream);
+    if (e != hipSuccess) return hip_fail(e);
+    if (x.dtype == SBP_F32) {
+        // each projection's pair of products; the second adds its dX to the first's
+        using sbpi::OR_BWD_DATA;
+        using sbpi::OR_BWD_WEIGHT;
+        if ((rc = run_pair(f32_product(OR_BWD_DATA, a.dg, a.wg, a.dx, a.m, a.k, a.n, a.dx_acc),
+                           f32_product(OR_BWD_WEIGHT, a.x, a.dg, a.dwg, a.k, a.n, a.m, a.dwg_acc),
+                           w, stream)))
+            return rc;
+        if ((rc = run_pair(f32_product(OR_BWD_DATA, a.du, a.wu, a.dx, a.m, a.k, a.n, 1),
+                           f32_product(OR_BWD_WEIGHT, a.x, a.du, a.dwu, a.k, a.n, a.m, a.dwu_acc),
+                           w, stream)))
+            return rc;
+    } else {
+        e = sbpi::launch_gated_products(a, stream);
+        if (e != hipSuccess) return hip_fail(e);
+    }
+    if (ldx_out) *ldx_out = st[2];
+    if (ldw_out) *ldw_out = st[3];
+    return SBP_OK;
+}
+
 }  // namespace
 
 namespace sbpa {
@@ -745,6 +968,40 @@ int sbp_nd_linear_bwd(const sbp_view_t *dY, const sbp_nd_layout_t *ldy, const sb
                       sbp_view_t *dX, sbp_nd_layout_t *ldx_out, sbp_view_t *dW,
                       sbp_nd_layout_t *ldw_out, const sbp_workspace_t *ws, hipStream_t stream) {
     return linear_bwd(dY, ldy, X, lx, W, lw, dX, ldx_out, dW, ldw_out, ws, stream);
+}
+
+int sbp_gated_fwd(const sbp_view_t *X, const sbp_layout_t *lx, const sbp_view_t *Wg,
+                  const sbp_view_t *Wu, const sbp_layout_t *lw, int32_t act, sbp_view_t *H,
+                  sbp_layout_t *lh_out, sbp_view_t *G, sbp_view_t *U, const sbp_workspace_t *ws,
+                  hipStream_t stream) {
+    return gated_fwd(X, lx, Wg, Wu, lw, act, H, lh_out, G, U, ws, stream);
+}
+
+int sbp_gated_bwd(const sbp_view_t *dH, const sbp_layout_t *ldh, const sbp_view_t *X,
+                  const sbp_layout_t *lx, const sbp_view_t *Wg, const sbp_view_t *Wu,
+                  const sbp_layout_t *lw, int32_t act, const sbp_view_t *G, const sbp_view_t *U,
+                  sbp_view_t *dG, sbp_view_t *dU, sbp_view_t *dX, sbp_layout_t *ldx_out,
+                  sbp_view_t *dWg, sbp_view_t *dWu, sbp_layout_t *ldw_out,
+                  const sbp_workspace_t *ws, hipStream_t stream) {
+    return gated_bwd(dH, ldh, X, lx, Wg, Wu, lw, act, G, U, dG, dU, dX, ldx_out, dWg, dWu, ldw_out,
+                     ws, stream);
+}
+
+int sbp_nd_gated_fwd(const sbp_view_t *X, const sbp_nd_layout_t *lx, const sbp_view_t *Wg,
+                     const sbp_view_t *Wu, const sbp_nd_layout_t *lw, int32_t act, sbp_view_t *H,
+                     sbp_nd_layout_t *lh_out, sbp_view_t *G, sbp_view_t *U,
+                     const sbp_workspace_t *ws, hipStream_t stream) {
+    return gated_fwd(X, lx, Wg, Wu, lw, act, H, lh_out, G, U, ws, stream);
+}
+
+int sbp_nd_gated_bwd(const sbp_view_t *dH, const sbp_nd_layout_t *ldh, const sbp_view_t *X,
+                     const sbp_nd_layout_t *lx, const sbp_view_t *Wg, const sbp_view_t *Wu,
+                     const sbp_nd_layout_t *lw, int32_t act, const sbp_view_t *G,
+                     const sbp_view_t *U, sbp_view_t *dG, sbp_view_t *dU, sbp_view_t *dX,
+                     sbp_nd_layout_t *ldx_out, sbp_view_t *dWg, sbp_view_t *dWu,
+                     sbp_nd_layout_t *ldw_out, const sbp_workspace_t *ws, hipStream_t stream) {
+    return gated_bwd(dH, ldh, X, lx, Wg, Wu, lw, act, G, U, dG, dU, dX, ldx_out, dWg, dWu, ldw_out,
+                     ws, stream);
 }
 
 const char *sbp_strerror(int code) {

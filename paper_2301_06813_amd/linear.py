@@ -197,3 +197,89 @@ def call_bwd_nd(factors, mesh, coord, X, W, dY, stream=None):
     dW = alloc_out_L("bwd_weight", L, M, K, N, X.dtype, X.device)
     st = run_bwd_L(L, X, W, dY, dX, dW, stream)
     return dX, dW, st
+
+
+# ------------------------------------------------ gated feed-forward block
+def _same_device(*tensors):
+    """The library's calls run on the current device, whose tensors these must be."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if t is not None and t.device.index != device:
+            raise ValueError("tensors are on %s, the current device is cuda:%d"
+                             % (t.device, device))
+
+
+def gated_fwd_L(L: dict, X, Wg, Wu, act: str = "silu", save: bool = True, stream=None, ws=None):
+    """(H, G, U) of the device's shares of global X, Wg and Wu under the states in L
+    (``layouts`` or ``nd_layouts``): H = act(X Wg) * (X Wu), and the projections that the
+    backward pass reads (None with save=False)."""
+    _same_device(X, Wg, Wu)
+    nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
+    M, K = X.shape
+    m, n = shard(L["x"], M, K).rows, shard(L["w"], K, Wg.shape[1]).cols
+    new = lambda: torch.empty((m, n), dtype=X.dtype, device=X.device)
+    H = new()
+    # the fp32 path has no form without the projections in memory
+    G, U = (new(), new()) if save or X.dtype == torch.float32 else (None, None)
+    loc = lambda t: None if t is None else sbp.view(t, sbp.SBP_LOCAL)
+    fn = sbp.sbp_nd_gated_fwd if nd else sbp.sbp_gated_fwd
+    fn(sbp.view(X), L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act], loc(H), loc(G),
+       loc(U), stream, ws)
+    return (H, G, U) if save else (H, None, None)
+
+
+def gated_bwd_L(L: dict, dH, X, Wg, Wu, G, U, act: str = "silu", out=None, grad_dtype=None,
+                accumulate: bool = False, stream=None, ws=None):
+    """(dX, dWg, dWu) of the device's shares, from the upstream gradient dH (global, or the
+    device's share) and the G and U of gated_fwd. They are in the inputs' dtype where no
+    partial sum of several devices forbids it (or in grad_dtype), or go to the three given
+    tensors `out` (accumulate: added to their fp32 contents)."""
+    _same_device(dH, X, Wg, Wu, G, U, *(out or ()))
+    nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
+    M, K = X.shape
+    N = Wg.shape[1]
+    x, w = shard(L["x"], M, K), shard(L["w"], K, N)
+    m, n = x.rows, w.cols
+
+    def alloc(rows, cols, state):
+        dt = grad_dtype or (torch.float32 if partial_devices(state) > 1 else X.dtype)
+        return torch.empty((rows, cols), dtype=dt, device=X.device)
+
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs the tensors to add to")
+        out = alloc(m, x.cols, L["dx"]), alloc(w.rows, n, L["dw"]), alloc(w.rows, n, L["dw"])
+    pre = torch.empty((2, m, n), dtype=X.dtype, device=X.device)   # dG, dU
+    if stream is not None:
+        pre.record_stream(torch.cuda.ExternalStream(stream))
+    loc = lambda t: sbp.view(t, sbp.SBP_LOCAL)
+    grad = lambda t: sbp.view(t, sbp.SBP_ACCUMULATE if accumulate else sbp.SBP_LOCAL)
+    mine = lambda t: sbp.view(t, sbp.SBP_GLOBAL if tuple(t.shape) == (M, N) else sbp.SBP_LOCAL)
+    fn = sbp.sbp_nd_gated_bwd if nd else sbp.sbp_gated_bwd
+    fn(mine(dH), L["dy"], sbp.view(X), L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act],
+       mine(G), mine(U), loc(pre[0]), loc(pre[1]), grad(out[0]), grad(out[1]), grad(out[2]), stream,
+       ws)
+    return out
+
+
+def partial_devices(l) -> int:
+    """Devices over which a 1-D or nd state is a partial sum (1: the tensor is whole)."""
+    if isinstance(l, sbp.sbp_nd_layout_t):
+        n = 1
+        for a in range(l.ndim):
+            n *= l.p[a] if l.kind[a] == sbp.SBP_PARTIAL else 1
+        return n
+    return l.p if l.kind == sbp.SBP_PARTIAL else 1
+
+
+def gated_fwd(sig: str, p: int, r: int, X, Wg, Wu, act: str = "silu", save: bool = True,
+              stream=None, ws=None):
+    """gated_fwd_L under signature sig ("DP", "COL" or "BB") on rank r of p."""
+    return gated_fwd_L(layouts(sig, p, r), X, Wg, Wu, act, save, stream, ws)
+
+
+def gated_bwd(sig: str, p: int, r: int, dH, X, Wg, Wu, G, U, act: str = "silu", out=None,
+              grad_dtype=None, accumulate: bool = False, stream=None, ws=None):
+    """gated_bwd_L under signature sig on rank r of p."""
+    return gated_bwd_L(layouts(sig, p, r), dH, X, Wg, Wu, G, U, act, out, grad_dtype, accumulate,
+                       stream, ws)

@@ -48,10 +48,13 @@ EXPORTS = ("sbp_shard_index", "sbp_signature", "sbp_linear_fwd", "sbp_linear_bwd
            "sbp_nd_linear_bwd", "sbp_attn_scores", "sbp_attn_context", "sbp_attn_scores_bwd",
            "sbp_attn_context_bwd", "sbp_set_override_orients", "sbp_collective_cost",
            "sbp_boxing_cost", "sbp_chain_cost", "sbp_search_strategy", "sbp_linear_bwd_noalloc",
-           "sbp_attn_core_fwd", "sbp_attn_core_bwd")
+           "sbp_attn_core_fwd", "sbp_attn_core_bwd", "sbp_gated_fwd", "sbp_gated_bwd",
+           "sbp_nd_gated_fwd", "sbp_nd_gated_bwd")
 
 SBP_COLL_ALLREDUCE, SBP_COLL_ALLGATHER, SBP_COLL_REDUCESCATTER, SBP_COLL_ALLTOALL = 0, 1, 2, 3
 SBP_SIG_DP, SBP_SIG_COL, SBP_SIG_KS, SBP_SIG_PB, SBP_SIG_BP, SBP_SIG_BB = 0, 1, 2, 3, 4, 5
+SBP_ACT_SILU, SBP_ACT_GELU, SBP_ACT_RELU = 0, 1, 2
+ACTS = {"silu": SBP_ACT_SILU, "gelu": SBP_ACT_GELU, "relu": SBP_ACT_RELU}
 SIG_IDS = {"DP": 0, "COL": 1, "KS": 2, "PB": 3, "BP": 4, "BB": 5}
 
 SBP_MAX_MESH_DIMS = 4
@@ -223,6 +226,13 @@ def lib():
         L.sbp_nd_linear_bwd.argtypes = [P(sbp_view_t), ND, P(sbp_view_t), ND, P(sbp_view_t), ND,
                                         P(sbp_view_t), ND, P(sbp_view_t), ND, WS,
                                         ctypes.c_void_p]
+        V = P(sbp_view_t)
+        for fn, LAY in (("sbp_gated_fwd", P(sbp_layout_t)), ("sbp_nd_gated_fwd", ND)):
+            getattr(L, fn).argtypes = [V, LAY, V, V, LAY, ctypes.c_int32, V, LAY, V, V, WS,
+                                       ctypes.c_void_p]
+        for fn, LAY in (("sbp_gated_bwd", P(sbp_layout_t)), ("sbp_nd_gated_bwd", ND)):
+            getattr(L, fn).argtypes = [V, LAY, V, LAY, V, V, LAY, ctypes.c_int32, V, V, V, V, V, LAY,
+                                       V, V, LAY, WS, ctypes.c_void_p]
         V4 = P(sbp_view4_t)
         for fn in ("sbp_attn_scores", "sbp_attn_context"):
             getattr(L, fn).argtypes = [V4, V4, V4, ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p]
@@ -495,6 +505,60 @@ def sbp_nd_linear_bwd(dY, ldy, X, lx, W, lw, dX, dW, stream=None, ws=None):
     if rc:
         _check(rc)
     return sx, sw
+
+
+# -------------------------------------------- gated feed-forward block
+def _gated_fwd(fn, X, lx, Wg, Wu, lw, act, H, G, U, stream, ws):
+    lh = type(lx)()
+    s = current_stream() if stream is None else stream
+    ref = ctypes.byref
+    rc = getattr(_lib or lib(), fn)(ref(X), ref(lx), ref(Wg), ref(Wu), ref(lw), act, ref(H),
+                                    ref(lh), None if G is None else ref(G),
+                                    None if U is None else ref(U), ref(_ws(ws, s)),
+                                    ctypes.c_void_p(s))
+    if rc:
+        _check(rc)
+    return lh
+
+
+def _gated_bwd(fn, dH, ldh, X, lx, Wg, Wu, lw, act, G, U, dG, dU, dX, dWg, dWu, stream, ws):
+    sx, sw = type(lx)(), type(lx)()
+    s = current_stream() if stream is None else stream
+    ref = ctypes.byref
+    rc = getattr(_lib or lib(), fn)(ref(dH), ref(ldh), ref(X), ref(lx), ref(Wg), ref(Wu), ref(lw),
+                                    act, ref(G), ref(U), ref(dG), ref(dU), ref(dX), ref(sx),
+                                    ref(dWg), ref(dWu), ref(sw), ref(_ws(ws, s)),
+                                    ctypes.c_void_p(s))
+    if rc:
+        _check(rc)
+    return sx, sw
+
+
+def sbp_gated_fwd(X, lx: sbp_layout_t, Wg, Wu, lw: sbp_layout_t, act: int, H, G=None, U=None,
+                  stream=None, ws=None) -> sbp_layout_t:
+    """H_r = act(X_r Wg_r) * (X_r Wu_r), and the projections into G and U; returns H's
+    state."""
+    return _gated_fwd("sbp_gated_fwd", X, lx, Wg, Wu, lw, act, H, G, U, stream, ws)
+
+
+def sbp_gated_bwd(dH, ldh: sbp_layout_t, X, lx: sbp_layout_t, Wg, Wu, lw: sbp_layout_t, act: int,
+                  G, U, dG, dU, dX, dWg, dWu, stream=None, ws=None):
+    """dG, dU, dX, dWg and dWu of the gated block; returns (dX state, dWg and dWu state)."""
+    return _gated_bwd("sbp_gated_bwd", dH, ldh, X, lx, Wg, Wu, lw, act, G, U, dG, dU, dX, dWg, dWu,
+                      stream, ws)
+
+
+def sbp_nd_gated_fwd(X, lx: sbp_nd_layout_t, Wg, Wu, lw: sbp_nd_layout_t, act: int, H, G=None,
+                     U=None, stream=None, ws=None) -> sbp_nd_layout_t:
+    """sbp_gated_fwd on nd shares; returns H's nd state."""
+    return _gated_fwd("sbp_nd_gated_fwd", X, lx, Wg, Wu, lw, act, H, G, U, stream, ws)
+
+
+def sbp_nd_gated_bwd(dH, ldh: sbp_nd_layout_t, X, lx: sbp_nd_layout_t, Wg, Wu, lw: sbp_nd_layout_t,
+                     act: int, G, U, dG, dU, dX, dWg, dWu, stream=None, ws=None):
+    """sbp_gated_bwd on nd shares; returns (dX state, dWg and dWu state)."""
+    return _gated_bwd("sbp_nd_gated_bwd", dH, ldh, X, lx, Wg, Wu, lw, act, G, U, dG, dU, dX, dWg,
+                      dWu, stream, ws)
 
 
 # ------------------------------------------------------- attention core

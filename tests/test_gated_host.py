@@ -1,0 +1,151 @@
+"""Host-side checks of the gated feed-forward calls: every case has exactly one defect,
+so no call reaches a kernel; fake device addresses, skipped wherever a GPU is visible."""
+import pytest
+
+from paper_2301_06813_amd import linear, sbp
+
+BF, F32 = sbp.SBP_BF16, sbp.SBP_F32
+GL, LO, ACC = sbp.SBP_GLOBAL, sbp.SBP_LOCAL, sbp.SBP_ACCUMULATE
+MB = 1 << 20
+
+
+def _gpu_visible():
+    try:
+        import torch
+        return torch.cuda.is_available()
+    except Exception:
+        return False
+
+
+pytestmark = pytest.mark.skipif(_gpu_visible(), reason="uses fake device addresses")
+
+
+def v(at, rows, cols, dtype=BF, scope=LO, ld=None):
+    """A view `at` MiB into the fake device memory."""
+    return sbp.raw_view(None if at is None else at * MB, rows, cols, ld or cols, dtype, scope)
+
+
+# M 40, K 48, N 64 under COL on rank 1 of 2: 32 columns of both weights
+L = linear.layouts("COL", 2, 1) if not _gpu_visible() else None
+
+
+def fwd_args():
+    return dict(x=v(16, 40, 48, scope=GL), lx=L["x"], wg=v(32, 48, 64, scope=GL),
+                wu=v(48, 48, 64, scope=GL), lw=L["w"], act=sbp.SBP_ACT_SILU, h=v(64, 40, 32),
+                g=v(80, 40, 32), u=v(96, 40, 32), ws=sbp.NO_WORKSPACE)
+
+
+def bwd_args():
+    return dict(fwd_args(), dh=v(112, 40, 32), ldh=L["dy"], dg=v(128, 40, 32), du=v(144, 40, 32),
+                dx=v(160, 40, 48, F32), dwg=v(176, 48, 32), dwu=v(192, 48, 32))
+
+
+def fwd(c):
+    sbp.sbp_gated_fwd(c["x"], c["lx"], c["wg"], c["wu"], c["lw"], c["act"], c["h"], c["g"], c["u"],
+                      stream=0, ws=c["ws"])
+
+
+def bwd(c):
+    sbp.sbp_gated_bwd(c["dh"], c["ldh"], c["x"], c["lx"], c["wg"], c["wu"], c["lw"], c["act"],
+                      c["g"], c["u"], c["dg"], c["du"], c["dx"], c["dwg"], c["dwu"], stream=0,
+                      ws=c["ws"])
+
+
+def sig(name, p=2, r=1):
+    x, w = linear.input_layouts(name, p, r)
+    return dict(lx=x, lw=w)
+
+
+SHARED = [
+    ("K split: a partial sum", lambda: sig("KS"), sbp.SBP_ERR_SIGNATURE),
+    ("X a partial sum", lambda: sig("PB"), sbp.SBP_ERR_SIGNATURE),
+    ("weights a partial sum", lambda: sig("BP"), sbp.SBP_ERR_SIGNATURE),
+    ("no signature", lambda: dict(lx=sbp.split(0, 2, 1), lw=sbp.split(0, 2, 1)),
+     sbp.SBP_ERR_SIGNATURE),
+    ("ranks differ", lambda: dict(lw=sbp.split(1, 2, 0)), sbp.SBP_ERR_LAYOUT),
+    ("unknown act", lambda: dict(act=3), sbp.SBP_ERR_SHAPE),
+    ("negative act", lambda: dict(act=-1), sbp.SBP_ERR_SHAPE),
+    ("mixed dtypes", lambda: dict(wu=v(48, 48, 64, F32, GL)), sbp.SBP_ERR_DTYPE),
+    ("unknown dtype", lambda: dict(x=v(16, 40, 48, 5, GL)), sbp.SBP_ERR_DTYPE),
+    ("inner dimensions differ", lambda: dict(x=v(16, 40, 56, scope=GL)), sbp.SBP_ERR_SHAPE),
+    ("weights' shapes differ", lambda: dict(wu=v(48, 48, 62, scope=GL)), sbp.SBP_ERR_SHAPE),
+    ("accumulating input", lambda: dict(x=v(16, 40, 48, scope=ACC)), sbp.SBP_ERR_SHAPE),
+    ("ld < cols", lambda: dict(wg=v(32, 48, 64, scope=GL, ld=32)), sbp.SBP_ERR_SHAPE),
+    ("null weights", lambda: dict(wg=v(None, 48, 64, scope=GL)), sbp.SBP_ERR_NULL),
+    ("misaligned", lambda: dict(x=sbp.raw_view(16 * MB + 1, 40, 48, 48, BF, GL)), sbp.SBP_ERR_ALIGN),
+    ("G's shape", lambda: dict(g=v(80, 40, 31)), sbp.SBP_ERR_SHAPE),
+    ("U's dtype", lambda: dict(u=v(96, 40, 32, F32)), sbp.SBP_ERR_DTYPE),
+    ("workspace size < 0", lambda: dict(ws=sbp.sbp_workspace_t(300 * MB, -4)), sbp.SBP_ERR_SHAPE),
+    ("null workspace", lambda: dict(ws=sbp.sbp_workspace_t(None, 64)), sbp.SBP_ERR_NULL),
+    ("misaligned workspace", lambda: dict(ws=sbp.sbp_workspace_t(300 * MB + 4, MB)),
+     sbp.SBP_ERR_ALIGN),
+    ("workspace on Wu", lambda: dict(ws=sbp.sbp_workspace_t(48 * MB, MB)), sbp.SBP_ERR_ALIAS),
+    ("workspace on G", lambda: dict(ws=sbp.sbp_workspace_t(80 * MB, MB)), sbp.SBP_ERR_ALIAS),
+    ("more tiles than a launch covers",
+     lambda: dict(x=v(16, 1 << 22, 48, scope=GL), wg=v(1024, 48, 1 << 13, scope=GL),
+                  wu=v(2048, 48, 1 << 13, scope=GL)), sbp.SBP_ERR_SHAPE),
+]
+FWD = SHARED + [
+    ("H's shape", lambda: dict(h=v(64, 40, 64)), sbp.SBP_ERR_SHAPE),
+    ("H's dtype", lambda: dict(h=v(64, 40, 32, F32)), sbp.SBP_ERR_DTYPE),
+    ("accumulating H", lambda: dict(h=v(64, 40, 32, scope=ACC)), sbp.SBP_ERR_SHAPE),
+    ("G without U", lambda: dict(u=None), sbp.SBP_ERR_NULL),
+    ("U without G", lambda: dict(g=None), sbp.SBP_ERR_NULL),
+    ("H on X", lambda: dict(h=v(16, 40, 32)), sbp.SBP_ERR_ALIAS),
+    ("G on H", lambda: dict(g=v(64, 40, 32)), sbp.SBP_ERR_ALIAS),
+    ("U on G", lambda: dict(u=v(80, 40, 32)), sbp.SBP_ERR_ALIAS),
+    ("fp32 without G and U",
+     lambda: dict(x=v(16, 40, 48, F32, GL), wg=v(32, 48, 64, F32, GL), wu=v(48, 48, 64, F32, GL),
+                  h=v(64, 40, 32, F32), g=None, u=None), sbp.SBP_ERR_NULL),
+]
+BWD = SHARED + [
+    ("dH's state", lambda: dict(ldh=sbp.broadcast(2, 1)), sbp.SBP_ERR_SIGNATURE),
+    ("dH's rank", lambda: dict(ldh=sbp.split(1, 2, 0)), sbp.SBP_ERR_LAYOUT),
+    ("dH's shape", lambda: dict(dh=v(112, 41, 32)), sbp.SBP_ERR_SHAPE),
+    ("global dH's columns", lambda: dict(dh=v(112, 40, 65, scope=GL)), sbp.SBP_ERR_SHAPE),
+    ("dH's dtype", lambda: dict(dh=v(112, 40, 32, F32)), sbp.SBP_ERR_DTYPE),
+    ("dG's dtype", lambda: dict(dg=v(128, 40, 32, F32)), sbp.SBP_ERR_DTYPE),
+    ("accumulating dU", lambda: dict(du=v(144, 40, 32, scope=ACC)), sbp.SBP_ERR_SHAPE),
+    ("bf16 partial sum", lambda: dict(dx=v(160, 40, 48)), sbp.SBP_ERR_DTYPE),
+    ("accumulating bf16", lambda: dict(dwg=v(176, 48, 32, BF, ACC)), sbp.SBP_ERR_DTYPE),
+    ("dWg and dWu of two dtypes", lambda: dict(dwg=v(176, 48, 32, F32)), sbp.SBP_ERR_DTYPE),
+    ("dWu's shape", lambda: dict(dwu=v(192, 48, 64)), sbp.SBP_ERR_SHAPE),
+    ("dX on dH", lambda: dict(dx=v(112, 40, 48, F32)), sbp.SBP_ERR_ALIAS),
+    ("dG on G", lambda: dict(dg=v(80, 40, 32)), sbp.SBP_ERR_ALIAS),
+    ("dU on dG", lambda: dict(du=v(128, 40, 32)), sbp.SBP_ERR_ALIAS),
+    ("dWu on dWg", lambda: dict(dwu=v(176, 48, 32)), sbp.SBP_ERR_ALIAS),
+    ("workspace on dWu", lambda: dict(ws=sbp.sbp_workspace_t(192 * MB, MB)), sbp.SBP_ERR_ALIAS),
+    ("workspace on dH", lambda: dict(ws=sbp.sbp_workspace_t(112 * MB, MB)), sbp.SBP_ERR_ALIAS),
+]
+
+
+@pytest.mark.parametrize("name,change,code", FWD, ids=[c[0] for c in FWD])
+def test_forward_refusals(name, change, code):
+    with pytest.raises(sbp.SbpError) as ei:
+        fwd({**fwd_args(), **change()})
+    assert ei.value.code == code
+
+
+@pytest.mark.parametrize("name,change,code", BWD, ids=[c[0] for c in BWD])
+def test_backward_refusals(name, change, code):
+    with pytest.raises(sbp.SbpError) as ei:
+        bwd({**bwd_args(), **change()})
+    assert ei.value.code == code
+
+
+def test_mesh_with_a_partial_sum():
+    # a K split on one mesh axis leaves H a partial sum there
+    n = linear.nd_layouts(("DP", "KS"), (2, 2), (0, 1))
+    with pytest.raises(sbp.SbpError) as ei:
+        sbp.sbp_nd_gated_fwd(v(16, 40, 48, scope=GL), n["x"], v(32, 48, 64, scope=GL),
+                             v(48, 48, 64, scope=GL), n["w"], 0, v(64, 20, 64), v(80, 20, 64),
+                             v(96, 20, 64), stream=0, ws=sbp.NO_WORKSPACE)
+    assert ei.value.code == sbp.SBP_ERR_SIGNATURE
+
+
+def test_partial_devices():
+    assert linear.partial_devices(sbp.partial(4, 1)) == 4
+    assert linear.partial_devices(sbp.broadcast(4, 1)) == 1
+    n = linear.nd_layouts(("DP", "COL"), (2, 3), (0, 0))
+    assert linear.partial_devices(n["dx"]) == 3 and linear.partial_devices(n["dw"]) == 2
+    assert linear.partial_devices(n["y"]) == 1

@@ -124,7 +124,9 @@ void attn_core_dq_kernel(BwdArgs f) {
     constexpr int NW = S::NW, ROWS = S::ROWS, KB = KT / 32, KS = DP / 16, DB = DP / 32;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
     const CoreArgs &a = f.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform, so that what
+                                                                 // depends on it is scalar
     const int kg = wave % KG, wr = wave / KG;
 
     const int per = f.tiles_q * f.splits_q;
@@ -146,26 +148,32 @@ void attn_core_dq_kernel(BwdArgs f) {
     const int k_beg = mask.lo(i_first) & ~31;
     const int k_end = i_first < mask.lq ? mask.hi(min(i_last, mask.lq - 1)) : 0;
     const int steps = k_end > k_beg ? (k_end - k_beg + KG * KT - 1) / (KG * KT) : 0;
+    // steps whose keys every row of the tile sees (rows past the sequence's end aside)
+    Walk walk{steps, 0, steps};
+    if (steps > 0) {
+        const int all = min(mask.hi(i_first), mask.lk);
+        walk.nb = all > k_beg ? min(steps, (all - k_beg) / (KG * KT)) : 0;
+        walk.na = min(walk.nb, (mask.lo(i_last) - k_beg + KG * KT - 1) / (KG * KT));
+        walk.na = max(walk.na, 0);
+    }
     const int per_split = (steps + f.splits_q - 1) / f.splits_q;
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
-
-    const int wrow = row0 + wr * 32;
-    const int w_hi = mask.hi(wrow / a.group);
-    const int w_lo = mask.lo(min(wrow + 31, f.rows - 1) / a.group);
     const int hi = mask.hi(i), lo = mask.lo(i);
 
     const uint16_t *K = static_cast<const uint16_t *>(a.k.p) + (int64_t)b * a.k.sb +
                         (int64_t)hk * a.k.sh;
     const uint16_t *V = static_cast<const uint16_t *>(a.v.p) + (int64_t)b * a.v.sb +
                         (int64_t)hk * a.v.sh;
+    const int place_k = Tile::place(a.k.ld, a.d, wave, lane);
+    const int place_v = Tile::place(a.v.ld, a.d, wave, lane);
     typename Tile::Regs rk, rv;
-    auto issue = [&](int st, int stage) {
-        const int k0 = k_beg + st * (KG * KT);
+    auto issue = [&](int x, int stage) {
+        const int k0 = k_beg + walk.step(x) * (KG * KT);
         const int n = min(KG * KT, mask.lk - k0);
         char *lds = smem + stage * S::STAGE;
         if constexpr (DMA) {
-            Tile::issue(K + (int64_t)k0 * a.k.ld, a.k.ld, n, a.d, lds, wave, lane);
-            Tile::issue(V + (int64_t)k0 * a.v.ld, a.v.ld, n, a.d, lds + Tile::BYTES, wave, lane);
+            Tile::issue(K + (int64_t)k0 * a.k.ld, a.k.ld, n, place_k, lds, wave);
+            Tile::issue(V + (int64_t)k0 * a.v.ld, a.v.ld, n, place_v, lds + Tile::BYTES, wave);
         } else {
             Tile::load(rk, K + (int64_t)k0 * a.k.ld, a.k.ld, n, a.d, tid);
             Tile::load(rv, V + (int64_t)k0 * a.v.ld, a.v.ld, n, a.d, tid);
@@ -195,38 +203,33 @@ void attn_core_dq_kernel(BwdArgs f) {
         gf[ks] = row_frag(G, ks * 16 + 8 * half, live ? a.d : 0, DMA);
     }
     const int64_t stat = ((int64_t)b * a.kv_heads * a.group + head) * a.sq + i;
-    const f32x16 s_init = splat16(live ? f.nl[stat] : -INFINITY);
-    const f32x16 d_init = splat16(live ? f.nd[stat] : 0.f);
     const float c = a.scale * LOG2E;
+    const float l2 = live ? f.nl[stat] * c : -INFINITY;
+    const f32x16 d_init = splat16(live ? f.nd[stat] : 0.f);
 
     f32x16 o[DB];
 #pragma unroll
     for (int x = 0; x < DB; ++x) o[x] = splat16(0.f);
 
-    for (int st = s0; st < s1; ++st) {
-        const int stage = (st - s0) & 1;
-        wait_vm<0>();
-        __syncthreads();
-        if (st + 1 < s1) issue(st + 1, stage ^ 1);
-        const char *kt = smem + stage * S::STAGE, *vt = kt + Tile::BYTES;
-        const int kw = k_beg + st * (KG * KT) + kg * KT;
-        const bool edge = kw + KT > w_hi || kw < w_lo;
+    // a step's keys; EDGE: some row of the wave does not see all of them
+    typename Tile::Reader rd(lds_at(smem) + kg * KT / Tile::RPS * Tile::SEG, lane);
+    auto step = [&](int kw, auto edge) {
+        constexpr bool EDGE = decltype(edge)::value;
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
-            f32x16 s = s_init, dp = d_init;
+            f32x16 s = splat16(0.f), dp = d_init;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
                 s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    Tile::frag(kt, kg * KT + kb * 32, ks, lane), qf[ks], s, 0, 0, 0);
+                    rd.frag(kb * 32, ks, 0), qf[ks], s, 0, 0, 0);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
                 dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    Tile::frag(vt, kg * KT + kb * 32, ks, lane), gf[ks], dp, 0, 0, 0);
+                    rd.frag(kb * 32, ks, Tile::BYTES), gf[ks], dp, 0, 0, 0);
 #pragma unroll
-            for (int r = 0; r < 16; ++r) s[r] = exp2_(s[r] * c) * dp[r];
-            if (edge) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
+            for (int r = 0; r < 16; ++r) {
+                s[r] = exp2_(__builtin_fmaf(s[r], c, l2)) * dp[r];
+                if constexpr (EDGE) {
                     const int key = kw + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
                     s[r] = key >= lo && key < hi ? s[r] : 0.f;
                 }
@@ -237,12 +240,22 @@ void attn_core_dq_kernel(BwdArgs f) {
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
                     o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        Tile::frag_t(kt, db * 32, kg * KT + kb * 32 + 16 * x, lane), p, o[db], 0, 0,
-                        0);
+                        rd.frag_t(db, kb * 32 + 16 * x, 0), p, o[db], 0, 0, 0);
             }
         }
-        if (st + 1 < s1) arrive(stage ^ 1);
-    }
+    };
+    auto take = [&](int x, auto edge) {
+        const int stage = (x - s0) & 1;
+        wait_vm<0>();
+        __syncthreads();
+        if (x + 1 < s1) issue(x + 1, stage ^ 1);
+        step(k_beg + walk.step(x) * (KG * KT) + kg * KT, edge);
+        rd.move(stage ? -S::STAGE : S::STAGE);
+        if (x + 1 < s1) arrive(stage ^ 1);
+    };
+    int x = s0;
+    for (; x < min(s1, walk.masked()); ++x) take(x, std::true_type{});
+    for (; x < s1; ++x) take(x, std::false_type{});
 
     if constexpr (KG > 1) {
         __syncthreads();
@@ -319,7 +332,9 @@ void attn_core_dkv_kernel(BwdArgs f) {
     constexpr int KS = DP / 16, DB = DP / 32;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
     const CoreArgs &a = f.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform, so that what
+                                                                 // depends on it is scalar
     const int kg = wave % KG, wk = wave / KG;
 
     // keys with more rows (earlier causal tiles) first within a (sequence, head)
@@ -343,24 +358,53 @@ void attn_core_dkv_kernel(BwdArgs f) {
         if (mask.window)
             i_max = min(i_max, min(j0 + KEYS, mask.lk) - 1 - mask.off + mask.window);
     }
+    // of a head: first the steps with rows that do not see every key of the tile
     const int nq = i_max > i_min ? (i_max - i_min + QROWS - 1) / QROWS : 0;
-    const int steps = nq * a.group;
+    Walk walk{nq, 0, nq};
+    if (nq > 0) {
+        if (mask.causal)
+            walk.na = min(nq, max(0, j0 + KEYS - 1 - mask.off - i_min + QROWS - 1) / QROWS);
+        if (mask.window)
+            walk.nb = max(walk.na, min(nq, max(0, j0 - mask.off + mask.window - i_min) / QROWS));
+    }
+    const int ne = walk.masked(), ni = nq - ne;   // masked steps of a head, and others
+    const int steps = nq * a.group, edges = ne * a.group;
     const int per_split = (steps + f.splits_k - 1) / f.splits_k;
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
 
-    // this lane's key is seen by rows [lo, hi); rows [w_lo, w_hi) see every key of the wave
+    // this lane's key is seen by rows [lo, hi)
     const int lo = mask.causal ? key - mask.off : 0;
     const int hi = mask.window ? key - mask.off + mask.window : INT32_MAX;
-    const int w_lo = mask.causal ? jw + 31 - mask.off : 0;
-    const int w_hi = mask.window ? jw - mask.off + mask.window : INT32_MAX;
 
     const uint16_t *Q = static_cast<const uint16_t *>(a.q.p) + (int64_t)b * a.q.sb;
     const uint16_t *G = static_cast<const uint16_t *>(a.dout.p) + (int64_t)b * a.dout.sb;
+    const int place_q = Tile::place(a.q.ld, a.d, wave, lane);
+    const int place_g = Tile::place(a.dout.ld, a.d, wave, lane);
     typename Tile::Regs rq, rg;
     float rs = 0.f;
-    auto issue = [&](int st, int stage) {
-        const int64_t h = (int64_t)hk * a.group + st / nq;
-        const int i0 = i_min + st % nq * QROWS;
+    // the next step to load: the iy-th of head ih among the masked ones, or the others
+    int ih = 0, iy = 0;
+    if (s0 < edges) {
+        ih = s0 / ne;
+        iy = s0 % ne;
+    } else if (s0 < s1) {
+        ih = (s0 - edges) / ni;
+        iy = ne + (s0 - edges) % ni;
+    }
+    int ii = i_min + walk.step(iy) * QROWS;
+    auto issue = [&](int x, int stage) {   // step x, the next one
+        const int64_t h = (int64_t)hk * a.group + ih;
+        const int i0 = ii;
+        ++iy;
+        if (iy == (x < edges ? ne : nq)) {
+            ++ih;
+            iy = x < edges ? 0 : ne;
+            if (x + 1 == edges) {
+                ih = 0;
+                iy = ne;
+            }
+        }
+        ii = i_min + walk.step(iy) * QROWS;
         const int n = min(QROWS, mask.lq - i0);
         const uint16_t *q = Q + h * a.q.sh + (int64_t)i0 * a.q.ld;
         const uint16_t *g = G + h * a.dout.sh + (int64_t)i0 * a.dout.ld;
@@ -369,8 +413,8 @@ void attn_core_dkv_kernel(BwdArgs f) {
         // rows past n: zeros, also as statistics (their Q and dO are zero, so P = 1 and
         // dS = 0 meet rows of zeros)
         if constexpr (DMA) {
-            Tile::issue(q, a.q.ld, n, a.d, lds, wave, lane);
-            Tile::issue(g, a.dout.ld, n, a.d, lds + Tile::BYTES, wave, lane);
+            Tile::issue(q, a.q.ld, n, place_q, lds, wave);
+            Tile::issue(g, a.dout.ld, n, place_g, lds + Tile::BYTES, wave);
             constexpr int W = NST / 64;   // waves per statistic
             if (wave < 2 * W) {
                 const int x = (wave % W) * 64 + lane;
@@ -395,6 +439,7 @@ void attn_core_dkv_kernel(BwdArgs f) {
             if (tid < 2 * NST) reinterpret_cast<float *>(lds + 2 * Tile::BYTES)[tid] = rs;
         }
     };
+    int iw = ii + kg * QT;   // this wave's rows of the step to compute
     if (s0 < s1) {
         issue(s0, 0);
         arrive(0);
@@ -420,22 +465,19 @@ void attn_core_dkv_kernel(BwdArgs f) {
         dv[x] = splat16(0.f);
     }
 
-    for (int st = s0; st < s1; ++st) {
-        const int stage = (st - s0) & 1;
-        wait_vm<0>();
-        __syncthreads();
-        if (st + 1 < s1) issue(st + 1, stage ^ 1);
-        const char *qt = smem + stage * S::STAGE, *gt = qt + Tile::BYTES;
-        const float *nl = reinterpret_cast<const float *>(gt + Tile::BYTES), *nd = nl + NST;
-        const int iw = i_min + st % nq * QROWS + kg * QT;
+    // a step's rows from i_wave on; EDGE: some key of the wave is not seen by all of them
+    typename Tile::Reader rd(lds_at(smem) + kg * QT / Tile::RPS * Tile::SEG, lane);
+    uint32_t stat = lds_at(smem) + 2 * Tile::BYTES + (kg * QT + 4 * half) * 4;
+    auto step = [&](int i_wave, auto edge) {
+        constexpr bool EDGE = decltype(edge)::value;
 #pragma unroll
         for (int qb = 0; qb < QT / 32; ++qb) {
-            const int r0 = kg * QT + qb * 32, i0 = iw + qb * 32;
+            const int r0 = qb * 32, i0 = i_wave + qb * 32;
             f32x16 s, dp;
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const f32x4 x = *reinterpret_cast<const f32x4 *>(nl + r0 + 8 * q + 4 * half);
-                const f32x4 y = *reinterpret_cast<const f32x4 *>(nd + r0 + 8 * q + 4 * half);
+                const f32x4 x = *(SBP_LDS const f32x4 *)(stat + (r0 + 8 * q) * 4);
+                const f32x4 y = *(SBP_LDS const f32x4 *)(stat + (NST + r0 + 8 * q) * 4);
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     s[4 * q + e] = x[e];
@@ -444,20 +486,16 @@ void attn_core_dkv_kernel(BwdArgs f) {
             }
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::frag(qt, r0, ks, lane), kf[ks], s,
-                                                            0, 0, 0);
+                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.frag(r0, ks, 0), kf[ks], s, 0, 0, 0);
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(Tile::frag(gt, r0, ks, lane), vf[ks],
-                                                             dp, 0, 0, 0);
+                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.frag(r0, ks, Tile::BYTES), vf[ks], dp,
+                                                             0, 0, 0);
 #pragma unroll
             for (int r = 0; r < 16; ++r) {
                 s[r] = exp2_(s[r] * c);
                 dp[r] *= s[r];
-            }
-            if (i0 < w_lo || i0 + 32 > w_hi) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
+                if constexpr (EDGE) {
                     const int i = i0 + 8 * (r >> 2) + 4 * half + (r & 3);
                     const bool seen = i >= lo && i < hi;
                     s[r] = seen ? s[r] : 0.f;
@@ -470,14 +508,29 @@ void attn_core_dkv_kernel(BwdArgs f) {
 #pragma unroll
                 for (int db = 0; db < DB; ++db) {
                     dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        Tile::frag_t(gt, db * 32, r0 + 16 * x, lane), p, dv[db], 0, 0, 0);
+                        rd.frag_t(db, r0 + 16 * x, Tile::BYTES), p, dv[db], 0, 0, 0);
                     dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        Tile::frag_t(qt, db * 32, r0 + 16 * x, lane), ds, dk[db], 0, 0, 0);
+                        rd.frag_t(db, r0 + 16 * x, 0), ds, dk[db], 0, 0, 0);
                 }
             }
         }
-        if (st + 1 < s1) arrive(stage ^ 1);
-    }
+    };
+    auto take = [&](int x, auto edge) {
+        const int stage = (x - s0) & 1;
+        wait_vm<0>();
+        __syncthreads();
+        const int next = ii + kg * QT;
+        if (x + 1 < s1) issue(x + 1, stage ^ 1);
+        step(iw, edge);
+        iw = next;
+        const int by = stage ? -S::STAGE : S::STAGE;
+        rd.move(by);
+        stat += by;
+        if (x + 1 < s1) arrive(stage ^ 1);
+    };
+    int x = s0;
+    for (; x < min(s1, edges); ++x) take(x, std::true_type{});
+    for (; x < s1; ++x) take(x, std::false_type{});
 
     if constexpr (KG > 1) {
         __syncthreads();

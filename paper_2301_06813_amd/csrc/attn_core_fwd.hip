@@ -81,7 +81,9 @@ void attn_core_fwd_kernel(FwdArgs f) {
     constexpr int NW = S::NW, ROWS = S::ROWS, KB = KT / 32, KS = DP / 16, DB = DP / 32;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
     const CoreArgs &a = f.a;
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, half = lane >> 5;
+    const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
+    const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform, so that what
+                                                                 // depends on it is scalar
     const int kg = wave % KG, wr = wave / KG;
 
     // heavier (later) causal tiles first within a (sequence, head)
@@ -105,13 +107,16 @@ void attn_core_fwd_kernel(FwdArgs f) {
     const int k_beg = mask.lo(i_first) & ~31;
     const int k_end = i_first < mask.lq ? mask.hi(min(i_last, mask.lq - 1)) : 0;
     const int steps = k_end > k_beg ? (k_end - k_beg + KG * KT - 1) / (KG * KT) : 0;
+    // steps whose keys every row of the tile sees (rows past the sequence's end aside)
+    Walk walk{steps, 0, steps};
+    if (steps > 0) {
+        const int all = min(mask.hi(i_first), mask.lk);
+        walk.nb = all > k_beg ? min(steps, (all - k_beg) / (KG * KT)) : 0;
+        walk.na = min(walk.nb, (mask.lo(i_last) - k_beg + KG * KT - 1) / (KG * KT));
+        walk.na = max(walk.na, 0);
+    }
     const int per_split = (steps + f.splits - 1) / f.splits;
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
-
-    // this wave's rows that need no mask see [w_lo, w_hi)
-    const int wrow = row0 + wr * 32;
-    const int w_hi = mask.hi(wrow / a.group);
-    const int w_lo = mask.lo(min(wrow + 31, f.rows - 1) / a.group);
     const int hi = mask.hi(i), lo = mask.lo(i);
 
     const uint16_t *Q = static_cast<const uint16_t *>(a.q.p) + (int64_t)b * a.q.sb +
@@ -121,14 +126,16 @@ void attn_core_fwd_kernel(FwdArgs f) {
     const uint16_t *V = static_cast<const uint16_t *>(a.v.p) + (int64_t)b * a.v.sb +
                         (int64_t)hk * a.v.sh;
 
+    const int place_k = Tile::place(a.k.ld, a.d, wave, lane);
+    const int place_v = Tile::place(a.v.ld, a.d, wave, lane);
     typename Tile::Regs rk, rv;
-    auto issue = [&](int st, int stage) {
-        const int k0 = k_beg + st * (KG * KT);
+    auto issue = [&](int x, int stage) {
+        const int k0 = k_beg + walk.step(x) * (KG * KT);
         const int n = min(KG * KT, mask.lk - k0);
         char *lds = smem + stage * S::STAGE;
         if constexpr (DMA) {
-            Tile::issue(K + (int64_t)k0 * a.k.ld, a.k.ld, n, a.d, lds, wave, lane);
-            Tile::issue(V + (int64_t)k0 * a.v.ld, a.v.ld, n, a.d, lds + Tile::BYTES, wave, lane);
+            Tile::issue(K + (int64_t)k0 * a.k.ld, a.k.ld, n, place_k, lds, wave);
+            Tile::issue(V + (int64_t)k0 * a.v.ld, a.v.ld, n, place_v, lds + Tile::BYTES, wave);
         } else {
             Tile::load(rk, K + (int64_t)k0 * a.k.ld, a.k.ld, n, a.d, tid);
             Tile::load(rv, V + (int64_t)k0 * a.v.ld, a.v.ld, n, a.d, tid);
@@ -160,13 +167,8 @@ void attn_core_fwd_kernel(FwdArgs f) {
 #pragma unroll
     for (int x = 0; x < DB; ++x) o[x] = splat16(0.f);
 
-    for (int st = s0; st < s1; ++st) {
-        const int stage = (st - s0) & 1;
-        wait_vm<0>();
-        __syncthreads();
-        if (st + 1 < s1) issue(st + 1, stage ^ 1);
-        const char *kt = smem + stage * S::STAGE, *vt = kt + Tile::BYTES;
-
+    typename Tile::Reader rd(lds_at(smem) + kg * KT / Tile::RPS * Tile::SEG, lane);
+    auto step = [&](int kw, auto edge) {
         f32x16 s[KB];
 #pragma unroll
         for (int kb = 0; kb < KB; ++kb) {
@@ -174,10 +176,9 @@ void attn_core_fwd_kernel(FwdArgs f) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
                 s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    Tile::frag(kt, kg * KT + kb * 32, ks, lane), qf[ks], s[kb], 0, 0, 0);
+                    rd.frag(kb * 32, ks, 0), qf[ks], s[kb], 0, 0, 0);
         }
-        const int kw = k_beg + st * (KG * KT) + kg * KT;
-        if (kw + KT > w_hi || kw < w_lo) {
+        if constexpr (decltype(edge)::value) {
 #pragma unroll
             for (int kb = 0; kb < KB; ++kb)
 #pragma unroll
@@ -218,12 +219,23 @@ void attn_core_fwd_kernel(FwdArgs f) {
 #pragma unroll
                 for (int db = 0; db < DB; ++db)
                     o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        Tile::frag_t(vt, db * 32, kg * KT + kb * 32 + 16 * x, lane), p, o[db], 0, 0,
-                        0);
+                        rd.frag_t(db, kb * 32 + 16 * x, Tile::BYTES), p, o[db], 0, 0, 0);
             }
         }
-        if (st + 1 < s1) arrive(stage ^ 1);
-    }
+    };
+    auto take = [&](int x, auto edge) {
+        const int stage = (x - s0) & 1;
+        wait_vm<0>();
+        __syncthreads();
+        if (x + 1 < s1) issue(x + 1, stage ^ 1);
+        step(k_beg + walk.step(x) * (KG * KT) + kg * KT, edge);
+        rd.move(stage ? -S::STAGE : S::STAGE);
+        if (x + 1 < s1) arrive(stage ^ 1);
+    };
+    int x = s0;
+    for (; x < min(s1, walk.masked()); ++x) take(x, std::true_type{});
+    for (; x < s1; ++x) take(x, std::false_type{});
+
     float l0, l1;
     halves(l, &l0, &l1);
     l = l0 + l1;

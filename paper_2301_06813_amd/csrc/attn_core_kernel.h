@@ -22,40 +22,50 @@ using sbpi::CoreView;
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
 
-// A tile of ROWS rows of DP bf16 values in LDS, rows in 16-byte chunks. Chunk c of
-// row r sits at r*RB + 16*(c ^ f(r)). Two kinds of reads share the tile: 16-byte
-// fragments of 16 consecutive rows (the same chunk of each: f takes every value
-// on rows that start on the same bank), and transpose reads of 4 consecutive rows
-// and 4 aligned chunks (f moves those rows' 64 bytes to distinct quarters of the
-// 64 banks, or halves where a row is half the banks long).
+// A tile of ROWS rows of DP bf16 values in LDS. A direct-to-LDS load of a wave fills 1 KB,
+// RPS whole rows in 16-byte chunks; these segments lie 1040 bytes apart, and within one
+// chunk c of row b is stored as chunk c ^ swz(b). Two kinds of reads share the tile:
+// 16-byte fragments (the same chunk of 16 consecutive rows) and transpose reads (4
+// aligned chunks of 4 consecutive rows). Both meet every bank once: rows of a segment
+// that start on the same bank differ in swz, by 4 where they are neighbours in a transpose
+// read, and consecutive segments are one chunk apart. swz only changes the bits of c that
+// step through the head dimension, so a lane needs 4 addresses for the fragments and one
+// per 32 columns for the transposed ones; rows, stages' halves and the other reads are
+// constant offsets.
 template <int DP, int ROWS, int NW>
 struct RowTile {
     static_assert(DP == 64 || DP == 128, "head dimension padded to 64 or 128");
-    static constexpr int RB = DP * 2;
-    static constexpr int CPR = DP / 8;
-    static constexpr int BYTES = ROWS * RB;
-    static constexpr int SEGS = BYTES / 1024;
-    static constexpr int NV = SEGS / NW;      // 16-byte chunks per thread
+    static constexpr int RB = DP * 2;          // bytes of a row
+    static constexpr int CPR = DP / 8;         // its chunks
+    static constexpr int RPS = 1024 / RB;      // rows of a segment
+    static constexpr int SEG = 1040;
+    static constexpr int SEGS = ROWS / RPS;
+    static constexpr int BYTES = SEGS * SEG;
+    static constexpr int NV = SEGS / NW;       // 16-byte chunks per thread
     static_assert(SEGS % NW == 0, "tile too small for the wave count");
 
-    __device__ __forceinline__ static int swz(int r) {
-        return DP == 128 ? ((r & 3) << 2) | ((r >> 2) & 3) : (((r >> 1) & 1) << 2) | ((r >> 2) & 3);
+    __host__ __device__ static constexpr int swz(int b) {   // b: row of a segment
+        return DP == 128 ? (b & 3) << 2 : (((b >> 1) & 1) << 2) | (((b >> 2) & 1) << 1);
+    }
+    __host__ __device__ static constexpr int at(int row, int c) {
+        return row / RPS * SEG + row % RPS * RB + ((c ^ swz(row % RPS)) << 4);
     }
 
-    // Rows [0, n) of the tile at `base` (uniform) go to LDS, rows past n and
-    // columns past d as zeros. Direct-to-LDS loads: base and ld 16-byte aligned,
-    // d a multiple of 8, ROWS * ld * 2 < 2^31.
-    __device__ __forceinline__ static void issue(const uint16_t *base, int64_t ld, int n, int d,
-                                                 char *lds, int wave, int lane) {
-        const i32x4 r = make_rsrc(base);
+    // Direct-to-LDS loads: base and ld 16-byte aligned, d a multiple of 8,
+    // ROWS * ld * 2 < 2^31. A lane's place in the tile's first NW segments:
+    __device__ __forceinline__ static int place(int64_t ld, int d, int wave, int lane) {
+        const int b = lane / CPR, c = (lane % CPR) ^ swz(b);
+        return c * 8 < d ? ((wave * RPS + b) * (int)ld + c * 8) * 2 : OOB;
+    }
+    // Rows [0, n) at `base` (uniform), n > 0, go to LDS; rows past n and columns past d lie
+    // outside the buffer and arrive as zeros.
+    __device__ __forceinline__ static void issue(const uint16_t *base, int64_t ld, int n, int place,
+                                                 char *lds, int wave) {
+        i32x4 r = make_rsrc(base);
+        r[2] = __builtin_amdgcn_readfirstlane(n * (int)ld * 2);
 #pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int s = i * NW + wave;
-            const int row = s * (1024 / RB) + lane / CPR;
-            const int c = (lane % CPR) ^ swz(row);
-            const bool ok = row < n && c * 8 < d;
-            dma16(r, lds + s * 1024, ok ? (row * (int)ld + c * 8) * 2 : OOB);
-        }
+        for (int i = 0; i < NV; ++i)
+            dma16(r, lds + (i * NW + wave) * SEG, place + i * (NW * RPS * (int)ld * 2));
     }
 
     // The same through registers, for rows at any element alignment and stride.
@@ -77,34 +87,55 @@ struct RowTile {
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int q = i * 64 * NW + tid;
-            const int row = q / CPR, c = q % CPR;
-            *reinterpret_cast<u32x4 *>(lds + row * RB + ((c ^ swz(row)) << 4)) = v[i];
+            *reinterpret_cast<u32x4 *>(lds + at(q / CPR, q % CPR)) = v[i];
         }
     }
 
-    // Rows [r0, r0 + 32), columns [16 ks, 16 ks + 16) with the columns as reduction
-    // (8 h + 0..7 of them for half h).
-    __device__ __forceinline__ static bf16x8 frag(const char *lds, int r0, int ks, int lane) {
-        const int row = r0 + (lane & 31);
-        const int c = ks * 2 + (lane >> 5);
-        return *reinterpret_cast<const bf16x8 *>(lds + row * RB + ((c ^ swz(row)) << 4));
-    }
-    // Columns [c0, c0 + 32), rows [r0, r0 + 16) with the rows as reduction (rows
-    // 4 h + 0..3 and 8 + 4 h + 0..3 for half h).
-    __device__ __forceinline__ static bf16x8 frag_t(const char *lds, int c0, int r0, int lane) {
-        const int g = lane >> 4, t = lane & 15;
-        const int mn = c0 + 16 * (g & 1) + 4 * (t & 3);
-        s16x4 x[2];
+    // A lane's read addresses in the tile at byte `base` of LDS.
+    struct Reader {
+        uint32_t f[4], t[DP / 32];
+
+        __device__ __forceinline__ Reader(uint32_t base, int lane) {
+            const int row = lane & 31, half = lane >> 5;
+            constexpr int STEP = DP == 128 ? 4 : 2;   // chunks between addresses
 #pragma unroll
-        for (int hh = 0; hh < 2; ++hh) {
-            const int row = r0 + hh * 8 + (g >> 1) * 4 + (t >> 2);
-            const int off = row * RB + (((mn >> 3) ^ swz(row)) << 4) + ((mn & 7) << 1);
-            x[hh] = __builtin_amdgcn_ds_read_tr16_b64_v4i16((SBP_LDS s16x4 *)(lds + off));
+            for (int j = 0; j < 4; ++j) f[j] = base + at(row, STEP * j + half);
+            const int g = lane >> 4, u = lane & 15;
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db)
+                t[db] = base + at((g >> 1) * 4 + (u >> 2), db * 4 + 2 * (g & 1) + ((u & 3) >> 1)) +
+                        8 * (u & 1);
         }
-        s16x8 v8 = {x[0][0], x[0][1], x[0][2], x[0][3], x[1][0], x[1][1], x[1][2], x[1][3]};
-        return __builtin_bit_cast(bf16x8, v8);
-    }
+        __device__ __forceinline__ void move(int by) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) f[j] += by;
+#pragma unroll
+            for (int db = 0; db < DP / 32; ++db) t[db] += by;
+        }
+        // Rows [r0, r0 + 32), columns [16 ks, 16 ks + 16) with the columns as reduction
+        // (8 h + 0..7 of them for half h). r0 and the byte offset `off` are constants.
+        __device__ __forceinline__ bf16x8 frag(int r0, int ks, int off) const {
+            const uint32_t p = DP == 128 ? f[ks >> 1] : f[ks];
+            const int at = r0 / RPS * SEG + (DP == 128 ? (ks & 1) * 32 : 0) + off;
+            return *(SBP_LDS const bf16x8 *)(p + at);
+        }
+        // Columns [32 db, 32 db + 32), rows [r0, r0 + 16) with the rows as reduction (rows
+        // 4 h + 0..3 and 8 + 4 h + 0..3 for half h).
+        __device__ __forceinline__ bf16x8 frag_t(int db, int r0, int off) const {
+            const uint32_t p = t[db];
+            const s16x4 x = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (SBP_LDS s16x4 *)(p + r0 / RPS * SEG + off));
+            const s16x4 y = __builtin_amdgcn_ds_read_tr16_b64_v4i16(
+                (SBP_LDS s16x4 *)(p + (r0 + 8) / RPS * SEG + off));
+            const s16x8 v8 = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+            return __builtin_bit_cast(bf16x8, v8);
+        }
+    };
 };
+
+__device__ __forceinline__ uint32_t lds_at(const void *p) {
+    return (uint32_t)(uintptr_t)(SBP_LDS const void *)p;
+}
 
 // 8 columns of a row in memory (columns past d as zeros), at any alignment.
 __device__ __forceinline__ bf16x8 row_frag(const uint16_t *row, int at, int d, bool aligned) {
@@ -156,6 +187,19 @@ struct SeqMask {
     }
     __device__ __forceinline__ int lo(int i) const {
         return window ? max(0, i + 1 + off - window) : 0;
+    }
+};
+
+// The order in which a workgroup takes the n steps of its walk: first those that need
+// the mask, [0, na) and [nb, n), then the others. Two loops, so that the second holds no
+// code of the first (as a branch inside one loop, the two forms' accumulators cost
+// copies in every step).
+struct Walk {
+    int n, na, nb;
+    __device__ __forceinline__ int masked() const { return na + n - nb; }
+    __device__ __forceinline__ int step(int x) const {
+        const int e = masked();
+        return x < na ? x : x < e ? nb + (x - na) : na + (x - e);
     }
 };
 

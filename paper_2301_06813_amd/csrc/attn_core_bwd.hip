@@ -20,16 +20,31 @@
 // every sum is fp32.
 #include <math.h>
 
+#include <algorithm>
+
 #include "attn_core_kernel.h"
 #include "gemm.h"
 #include "profile.h"
 
 namespace sbpk {
 
+// Under a causal mask the first keys are seen by every row and the last by few, so the
+// first tiles' walks are split over more workgroups. Level j: key tiles [tile[j],
+// tile[j+1]), split v[j] ways (falling); its work items start at item[j], and its
+// partials, where v[j] > 1, at slot[j], of one (sequence, key head).
+constexpr int MAX_LEVELS = 8;
+struct Levels {
+    int32_t n;
+    int32_t tile[MAX_LEVELS + 1], v[MAX_LEVELS], item[MAX_LEVELS], slot[MAX_LEVELS];
+    int32_t items;                     // of one (sequence, key head)
+    int32_t split_keys;                // keys of the tiles with v > 1
+};
+
 struct BwdArgs {
     CoreArgs a;
     int32_t tiles_q, splits_q, rows;   // dQ: row tiles, key splits; rows = sq * group
-    int32_t tiles_k, splits_k;         // dK, dV: key tiles, row splits
+    int32_t keys;                      // dK, dV: keys of a tile, and its splits
+    Levels lev;
     int32_t vec_q, vec_k, vec_v;       // outputs allow 4-value stores
     const float *nl, *nd;              // row statistics: -lse / scale, -D, per (b, head, i)
     float *part;                       // split partials
@@ -82,9 +97,9 @@ __global__ __launch_bounds__(256) void attn_core_stat_kernel(CoreArgs a, float *
     const bool live = lse != -INFINITY;
     float x = 0.f;
     if (live && at < a.d) {
-        const bf16x8 g = row_frag(static_cast<const uint16_t *>(a.dout.p) + b * a.dout.sb +
-                                      h * a.dout.sh + i * a.dout.ld,
-                                  at, a.d, false);
+        const bf16x8 g = row_frag<false>(static_cast<const uint16_t *>(a.dout.p) + b * a.dout.sb +
+                                             h * a.dout.sh + i * a.dout.ld,
+                                         at, a.d);
         const int64_t o = b * a.o.sb + h * a.o.sh + i * a.o.ld;
         if (a.o_f32) {
             const float *p = static_cast<const float *>(a.o.p) + o;
@@ -92,7 +107,7 @@ __global__ __launch_bounds__(256) void attn_core_stat_kernel(CoreArgs a, float *
             for (int e = 0; e < 8; ++e)
                 if (at + e < a.d) x += (float)g[e] * p[at + e];
         } else {
-            const bf16x8 y = row_frag(static_cast<const uint16_t *>(a.o.p) + o, at, a.d, false);
+            const bf16x8 y = row_frag<false>(static_cast<const uint16_t *>(a.o.p) + o, at, a.d);
 #pragma unroll
             for (int e = 0; e < 8; ++e) x += (float)g[e] * (float)y[e];
         }
@@ -106,22 +121,75 @@ __global__ __launch_bounds__(256) void attn_core_stat_kernel(CoreArgs a, float *
 }
 
 // ------------------------------------------------------------------- dQ
-template <int DP, int KG, int KT>
+// Both kernels walk with 32 x 32 blocks of scores a wave, in two phases: S and dP of the
+// next block, whose products alternate, beside this block's exponentials and roundings;
+// then this block's products with them. What is written between two products stays
+// there (sched_barrier): left to itself the compiler read operands right before
+// their use and put the vector work behind the products. The loads of a step are spread over
+// its products too. With 128 columns the sums leave room for one wave per SIMD, which
+// hides nothing behind another.
+
+// S and dP of one block: S from the operand rows at `r` and `qf`, dP from the rows OFF bytes
+// behind and `gf`. beside(i), i = 0 .. KS: what is written between the products.
+template <int KS, int OFF, class Reader, class Beside>
+__device__ __forceinline__ void block_scores(f32x16 &s, f32x16 &dp, const Reader &r, int r0,
+                                             const bf16x8 *qf, const bf16x8 *gf, Beside beside) {
+    // operands are read AHEAD products early: a read of LDS takes longer than two products
+    constexpr int AHEAD = KS < 4 ? KS : 4;
+    bf16x8 q[KS], g[KS];
+#pragma unroll
+    for (int ks = 0; ks < AHEAD; ++ks) {
+        q[ks] = r.frag(r0, ks, 0);
+        g[ks] = r.frag(r0, ks, OFF);
+    }
+    beside(0);
+    __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+    for (int ks = 0; ks < KS; ++ks) {
+        if (ks + AHEAD < KS) {
+            q[ks + AHEAD] = r.frag(r0, ks + AHEAD, 0);
+            g[ks + AHEAD] = r.frag(r0, ks + AHEAD, OFF);
+        }
+        s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[ks], qf[ks], s, 0, 0, 0);
+        dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g[ks], gf[ks], dp, 0, 0, 0);
+        beside(ks + 1);
+        __builtin_amdgcn_sched_barrier(0);
+    }
+}
+
+// Part i of 0 .. PARTS - 1 of a block's 16 values holds value r.
+__device__ __forceinline__ constexpr bool in_part(int r, int i, int parts) {
+    return r >= 16 * i / parts && r < 16 * (i + 1) / parts;
+}
+
+// A direct-to-LDS load to come: two tiles.
+struct Fetch {
+    i32x4 x, y;
+    char *lds;
+};
+
+template <int DP, int KG, int KT, bool DMA>
 struct DqShape {
     static constexpr int NW = 4;
     static constexpr int ROWS = 32 * NW / KG;
     using Tile = RowTile<DP, KG * KT, NW>;
     static constexpr int STAGE = 2 * Tile::BYTES;
-    static constexpr int LDS = 2 * STAGE;
-    static constexpr int OCC = LDS > 81920 ? 1 : 2;
+    static constexpr int LOADS = 2 * Tile::NV;
+    static constexpr int OCC = DP > 64 ? 1 : 2;
+    static constexpr int FIT = 163840 / OCC / STAGE;
+    static constexpr int NS = !DMA ? 3 : FIT > 4 ? 4 : FIT;
+    static constexpr int PUT = NW * 32 * 68 * 4;     // put_rows
+    static constexpr int LDS = NS * STAGE > PUT ? NS * STAGE : PUT;
+    static_assert(FIT >= NS && NS >= 3, "three stages");
 };
 
 template <int DP, int KG, int KT, bool DMA>
-__global__ __launch_bounds__(256, (DqShape<DP, KG, KT>::OCC))
+__global__ __launch_bounds__(256, (DqShape<DP, KG, KT, DMA>::OCC))
 void attn_core_dq_kernel(BwdArgs f) {
-    using S = DqShape<DP, KG, KT>;
+    using S = DqShape<DP, KG, KT, DMA>;
     using Tile = typename S::Tile;
-    constexpr int NW = S::NW, ROWS = S::ROWS, KB = KT / 32, KS = DP / 16, DB = DP / 32;
+    constexpr int NW = S::NW, ROWS = S::ROWS, NS = S::NS;
+    constexpr int NB = KT / 32, KS = DP / 16, DB = DP / 32, KEYS = KG * KT;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
     const CoreArgs &a = f.a;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
@@ -129,9 +197,10 @@ void attn_core_dq_kernel(BwdArgs f) {
                                                                  // depends on it is scalar
     const int kg = wave % KG, wr = wave / KG;
 
+    // heavier (later) causal tiles first within a (sequence, head)
     const int per = f.tiles_q * f.splits_q;
-    const int L = remap_xcd(blockIdx.x, gridDim.x);
-    const int bh = L / per, t = L % per;
+    int bh, t;
+    deal(blockIdx.x, a.batch * a.kv_heads, per, &bh, &t);
     const int tile = f.tiles_q - 1 - t / f.splits_q, split = t % f.splits_q;
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const SeqMask mask(a, b);
@@ -147,14 +216,13 @@ void attn_core_dq_kernel(BwdArgs f) {
     const int i_last = (min(row0 + ROWS, f.rows) - 1) / a.group;
     const int k_beg = mask.lo(i_first) & ~31;
     const int k_end = i_first < mask.lq ? mask.hi(min(i_last, mask.lq - 1)) : 0;
-    const int steps = k_end > k_beg ? (k_end - k_beg + KG * KT - 1) / (KG * KT) : 0;
+    const int steps = k_end > k_beg ? (k_end - k_beg + KEYS - 1) / KEYS : 0;
     // steps whose keys every row of the tile sees (rows past the sequence's end aside)
     Walk walk{steps, 0, steps};
     if (steps > 0) {
         const int all = min(mask.hi(i_first), mask.lk);
-        walk.nb = all > k_beg ? min(steps, (all - k_beg) / (KG * KT)) : 0;
-        walk.na = min(walk.nb, (mask.lo(i_last) - k_beg + KG * KT - 1) / (KG * KT));
-        walk.na = max(walk.na, 0);
+        walk.nb = all > k_beg ? min(steps, (all - k_beg) / KEYS) : 0;
+        walk.na = max(0, min(walk.nb, (mask.lo(i_last) - k_beg + KEYS - 1) / KEYS));
     }
     const int per_split = (steps + f.splits_q - 1) / f.splits_q;
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
@@ -167,16 +235,26 @@ void attn_core_dq_kernel(BwdArgs f) {
     const int place_k = Tile::place(a.k.ld, a.d, wave, lane);
     const int place_v = Tile::place(a.v.ld, a.d, wave, lane);
     typename Tile::Regs rk, rv;
-    auto issue = [&](int x, int stage) {
-        const int k0 = k_beg + walk.step(x) * (KG * KT);
-        const int n = min(KG * KT, mask.lk - k0);
-        char *lds = smem + stage * S::STAGE;
+    Fetch to{};
+    // steps past the walk's bring nothing (zeros, to a stage that is not read)
+    auto fetch = [&](int x, int stage) {
+        const int k0 = k_beg + walk.step(x) * KEYS;
+        const int n = x < s1 ? min(KEYS, mask.lk - k0) : 0;
         if constexpr (DMA) {
-            Tile::issue(K + (int64_t)k0 * a.k.ld, a.k.ld, n, place_k, lds, wave);
-            Tile::issue(V + (int64_t)k0 * a.v.ld, a.v.ld, n, place_v, lds + Tile::BYTES, wave);
+            to.x = make_rsrc(K + (int64_t)k0 * a.k.ld);
+            to.y = make_rsrc(V + (int64_t)k0 * a.v.ld);
+            to.x[2] = __builtin_amdgcn_readfirstlane(n * (int)a.k.ld * 2);
+            to.y[2] = __builtin_amdgcn_readfirstlane(n * (int)a.v.ld * 2);
+            to.lds = smem + stage * S::STAGE;
         } else {
             Tile::load(rk, K + (int64_t)k0 * a.k.ld, a.k.ld, n, a.d, tid);
             Tile::load(rv, V + (int64_t)k0 * a.v.ld, a.v.ld, n, a.d, tid);
+        }
+    };
+    auto fetch_part = [&](int p) {
+        if constexpr (DMA) {
+            if (p < Tile::NV) Tile::issue_part(to.x, a.k.ld, place_k, to.lds, wave, p);
+            else Tile::issue_part(to.y, a.v.ld, place_v, to.lds + Tile::BYTES, wave, p - Tile::NV);
         }
     };
     auto arrive = [&](int stage) {
@@ -186,9 +264,18 @@ void attn_core_dq_kernel(BwdArgs f) {
             Tile::store(rv, lds + Tile::BYTES, tid);
         }
     };
-    if (s0 < s1) {
-        issue(s0, 0);
+    if constexpr (DMA) {
+#pragma unroll
+        for (int x = 0; x < NS - 1; ++x) {
+            fetch(s0 + x, x);
+#pragma unroll
+            for (int p = 0; p < S::LOADS; ++p) fetch_part(p);
+        }
+        fetch(s1, NS - 1);   // nothing, for the parts before the first advance
+    } else if (s0 < s1) {
+        fetch(s0, 0);
         arrive(0);
+        if (s0 + 1 < s1) fetch(s0 + 1, 1);
     }
 
     const bool live = valid && i < mask.lq;
@@ -199,106 +286,124 @@ void attn_core_dq_kernel(BwdArgs f) {
     bf16x8 qf[KS], gf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-        qf[ks] = row_frag(Q, ks * 16 + 8 * half, live ? a.d : 0, DMA);
-        gf[ks] = row_frag(G, ks * 16 + 8 * half, live ? a.d : 0, DMA);
+        qf[ks] = row_frag<DMA>(Q, ks * 16 + 8 * half, live ? a.d : 0);
+        gf[ks] = row_frag<DMA>(G, ks * 16 + 8 * half, live ? a.d : 0);
     }
     const int64_t stat = ((int64_t)b * a.kv_heads * a.group + head) * a.sq + i;
     const float c = a.scale * LOG2E;
-    const float l2 = live ? f.nl[stat] * c : -INFINITY;
-    const f32x16 d_init = splat16(live ? f.nd[stat] : 0.f);
+    float l2 = live ? f.nl[stat] * c : -INFINITY, d0 = live ? f.nd[stat] : 0.f;
+    asm volatile("" : "+v"(l2), "+v"(d0));
+    settle(qf);
+    settle(gf);
+    const f32x16 d_init = splat16(d0);
 
     f32x16 o[DB];
 #pragma unroll
     for (int x = 0; x < DB; ++x) o[x] = splat16(0.f);
 
-    // a step's keys; EDGE: some row of the wave does not see all of them
     typename Tile::Reader rd(lds_at(smem) + kg * KT / Tile::RPS * Tile::SEG, lane);
-    auto step = [&](int kw, auto edge) {
-        constexpr bool EDGE = decltype(edge)::value;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            f32x16 s = splat16(0.f), dp = d_init;
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    rd.frag(kb * 32, ks, 0), qf[ks], s, 0, 0, 0);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    rd.frag(kb * 32, ks, Tile::BYTES), gf[ks], dp, 0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = exp2_(__builtin_fmaf(s[r], c, l2)) * dp[r];
-                if constexpr (EDGE) {
-                    const int key = kw + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    s[r] = key >= lo && key < hi ? s[r] : 0.f;
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const bf16x8 p = pack8(s, 8 * x);
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        rd.frag_t(db, kb * 32 + 16 * x, 0), p, o[db], 0, 0, 0);
-            }
+    f32x16 sp[2], dpp[2];           // S and dP of this block and the next, in turn
+    int stage = 0;                  // of the step at work
+    // Waits for the step after x, and prepares the load of a later one.
+    auto advance = [&](int x) {
+        if constexpr (DMA) {
+            wait_vm<(NS - 3) * S::LOADS>();
+            __syncthreads();
+            fetch(x + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+        } else {
+            if (x + 1 < s1) arrive(stage == NS - 1 ? 0 : stage + 1);
+            __syncthreads();
+            if (x + 2 < s1) fetch(x + 2, 0);
         }
     };
+    // EDGE: some row of the tile does not see every key of the step
     auto take = [&](int x, auto edge) {
-        const int stage = (x - s0) & 1;
-        wait_vm<0>();
-        __syncthreads();
-        if (x + 1 < s1) issue(x + 1, stage ^ 1);
-        step(k_beg + walk.step(x) * (KG * KT) + kg * KT, edge);
-        rd.move(stage ? -S::STAGE : S::STAGE);
-        if (x + 1 < s1) arrive(stage ^ 1);
+        constexpr bool EDGE = decltype(edge)::value;
+        const int kw = k_beg + walk.step(x) * KEYS + kg * KT;
+        const bool wrap = stage == NS - 1;
+        const int by = wrap ? -(NS - 1) * S::STAGE : S::STAGE;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const bool last = kb == NB - 1;
+            if (last) advance(x);
+            typename Tile::Reader nx = rd;       // where the next block lies
+            if (last) nx.move(by);
+            // with an even number of blocks a step the two take turns in place
+            constexpr bool TURN = NB % 2 == 0;
+            constexpr int ONE = 1;
+            const int now = TURN ? kb & 1 : 0;
+            f32x16 &s = sp[now], &dp = dpp[now], &s_n = sp[ONE - now], &dp_n = dpp[ONE - now];
+            bf16x8 tk[2][DB], ds[2];
+            s_n = splat16(0.f);
+            dp_n = d_init;
+            __builtin_amdgcn_sched_barrier(0);
+            block_scores<KS, Tile::BYTES>(s_n, dp_n, nx, last ? 0 : (kb + 1) * 32, qf, gf, [&](int part) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (!in_part(r, part, KS + 1)) continue;
+                    s[r] = exp2_(__builtin_fmaf(s[r], c, l2)) * dp[r];
+                    if constexpr (EDGE) {
+                        const int key = kw + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
+                        s[r] = key >= lo && key < hi ? s[r] : 0.f;
+                    }
+                    if (r % 8 == 7) ds[r / 8] = pack8(s, r - 7);
+                }
+                // the first 16 keys' columns
+                if (part > KS - DB) tk[0][part - 1 - (KS - DB)] = rd.frag_t(part - 1 - (KS - DB), kb * 32, 0);
+            });
+            // the loads of a step, spread over its blocks: the last one's first
+            constexpr int PER = (S::LOADS + NB - 1) / NB;
+            const int first = last ? 0 : (kb + 1) * PER;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tk[h][db], ds[h], o[db], 0, 0, 0);
+                    if (h == 0) tk[1][db] = rd.frag_t(db, kb * 32 + 16, 0);
+                    const int k = h * DB + db;
+#pragma unroll
+                    for (int p = PER * k / (2 * DB); p < PER * (k + 1) / (2 * DB); ++p)
+                        if (first + p < S::LOADS) fetch_part(first + p);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            if constexpr (!TURN) {
+                sp[0] = sp[1];
+                dpp[0] = dpp[1];
+            }
+        }
+        rd.move(by);
+        stage = wrap ? 0 : stage + 1;
     };
+    if (s0 < s1) {
+        if constexpr (DMA) wait_vm<(NS - 2) * S::LOADS>();
+        __syncthreads();
+        sp[0] = splat16(0.f);
+        dpp[0] = d_init;
+        block_scores<KS, Tile::BYTES>(sp[0], dpp[0], rd, 0, qf, gf, [](int) {});
+    }
     int x = s0;
     for (; x < min(s1, walk.masked()); ++x) take(x, std::true_type{});
     for (; x < s1; ++x) take(x, std::false_type{});
-
+    wait_vm<0>();      // no load is on its way to LDS any more
     if constexpr (KG > 1) {
+        static_assert((KG - 1) * (NW / KG) * DB * 4096 <= S::LDS, "group results do not fit");
+        if (!join_groups<KG, DB>(o, smem, kg, wr, NW / KG, lane)) return;
+    } else {
         __syncthreads();
-        constexpr int SLOT = DB * 16 * 64;
-        static_assert((KG - 1) * (NW / KG) * SLOT * 4 <= S::LDS, "group results do not fit");
-        float *const base = reinterpret_cast<float *>(smem) + lane;
-        if (kg > 0) {
-            float *p = base + ((kg - 1) * (NW / KG) + wr) * SLOT;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) p[(db * 16 + r) * 64] = o[db][r];
-        }
-        __syncthreads();
-        if (kg > 0) return;
-#pragma unroll
-        for (int k = 1; k < KG; ++k) {
-            const float *p = base + ((k - 1) * (NW / KG) + wr) * SLOT;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[db][r] += p[(db * 16 + r) * 64];
-        }
     }
-    if (!valid) return;
+    const bool whole = f.splits_q == 1;
     const int64_t d4 = (a.d + 3) & ~3;
-    const int64_t at = (int64_t)b * a.dq.sb + head * a.dq.sh + (int64_t)i * a.dq.ld;
-    float *const part =
-        f.part + (((int64_t)split * a.batch * a.kv_heads + bh) * f.rows + row) * d4;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int col = db * 32 + 8 * q + 4 * half;
-            if (col >= a.d) continue;
-            if (f.splits_q > 1) {
-                f32x4 v = {o[db][4 * q], o[db][4 * q + 1], o[db][4 * q + 2], o[db][4 * q + 3]};
-                *reinterpret_cast<f32x4 *>(part + col) = v;
-            } else {
-                grad4(a.dq.p, at, col, a.d, a.dq_f32, a.dq_acc, f.vec_q,
-                      [&](int e) { return o[db][4 * q + e] * a.scale; });
-            }
-        }
+    const RowsOut out{whole ? a.dq.p : f.part, !whole || a.dq_f32, whole && a.dq_acc,
+                      !whole || f.vec_q};
+    float *const put = reinterpret_cast<float *>(smem) + wr * (32 * 68);
+    put_rows<DP>(put, o, whole ? a.scale : 1.f, out, a.d, lane, [&](int r) -> int64_t {
+        const int q = row0 + wr * 32 + r;
+        if (q >= f.rows) return -1;
+        if (!whole) return (((int64_t)split * a.batch * a.kv_heads + bh) * f.rows + q) * d4;
+        const int qi = q / a.group;
+        return (int64_t)b * a.dq.sb + ((int64_t)hk * a.group + (q - qi * a.group)) * a.dq.sh +
+               (int64_t)qi * a.dq.ld;
+    });
 }
 
 // ------------------------------------------------------------ dK and dV
@@ -311,24 +416,32 @@ __device__ __forceinline__ void dma4(i32x4 r, char *lds, int voff) {
                  : "memory", "m0");
 }
 
-template <int DP, int KG, int QT>
+template <int DP, int KG, int QT, bool DMA>
 struct DkvShape {
     static constexpr int NW = 4;
     static constexpr int KEYS = 32 * NW / KG;
     static constexpr int QROWS = KG * QT;
     using Tile = RowTile<DP, QROWS, NW>;
-    static constexpr int NST = QROWS < 64 ? 64 : QROWS;      // floats of one statistic a stage
-    static constexpr int STAGE = 2 * Tile::BYTES + 2 * NST * 4;
-    static constexpr int LDS = 2 * STAGE;
-    static constexpr int OCC = LDS > 81920 || DP > 64 ? 1 : 2;
+    static constexpr int NST = QROWS;                        // floats of one statistic a stage
+    // Q, dO, -lse / scale, -D, and room for a wave's load that brings nothing
+    static constexpr int STAGE = 2 * Tile::BYTES + 256 * 4;
+    static constexpr int LOADS = 2 * Tile::NV + 1;           // a thread's loads of a stage
+    // workgroups of a unit: one where the sums of 32 keys take 128 registers a lane
+    static constexpr int OCC = DP > 64 ? 1 : 2;
+    // stages: a step reads its own and the next one while later ones arrive
+    static constexpr int FIT = 163840 / OCC / STAGE;
+    static constexpr int NS = !DMA ? 3 : FIT > 4 ? 4 : FIT;
+    static constexpr int PUT = NW * 32 * 68 * 4;     // put_rows
+    static constexpr int LDS = NS * STAGE > PUT ? NS * STAGE : PUT;
+    static_assert(FIT >= NS && NS >= 3 && NST % 64 == 0 && 2 * NST <= 256, "three stages, one statistic per thread");
 };
 
 template <int DP, int KG, int QT, bool DMA>
-__global__ __launch_bounds__(256, (DkvShape<DP, KG, QT>::OCC))
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DkvShape<DP, KG, QT, DMA>::OCC, DkvShape<DP, KG, QT, DMA>::OCC)))
 void attn_core_dkv_kernel(BwdArgs f) {
-    using S = DkvShape<DP, KG, QT>;
+    using S = DkvShape<DP, KG, QT, DMA>;
     using Tile = typename S::Tile;
-    constexpr int NW = S::NW, KEYS = S::KEYS, QROWS = S::QROWS, NST = S::NST;
+    constexpr int NW = S::NW, KEYS = S::KEYS, QROWS = S::QROWS, NST = S::NST, NS = S::NS;
     constexpr int KS = DP / 16, DB = DP / 32;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
     const CoreArgs &a = f.a;
@@ -338,10 +451,12 @@ void attn_core_dkv_kernel(BwdArgs f) {
     const int kg = wave % KG, wk = wave / KG;
 
     // keys with more rows (earlier causal tiles) first within a (sequence, head)
-    const int per = f.tiles_k * f.splits_k;
-    const int L = remap_xcd(blockIdx.x, gridDim.x);
-    const int bh = L / per, t = L % per;
-    const int tile = t / f.splits_k, split = t % f.splits_k;
+    int bh, t;
+    deal(blockIdx.x, a.batch * a.kv_heads, f.lev.items, &bh, &t);
+    int lev = 0;
+    while (lev + 1 < f.lev.n && t >= f.lev.item[lev + 1]) ++lev;
+    const int splits = f.lev.v[lev], in_level = t - f.lev.item[lev];
+    const int tile = f.lev.tile[lev] + in_level / splits, split = in_level % splits;
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const SeqMask mask(a, b);
 
@@ -369,7 +484,7 @@ void attn_core_dkv_kernel(BwdArgs f) {
     }
     const int ne = walk.masked(), ni = nq - ne;   // masked steps of a head, and others
     const int steps = nq * a.group, edges = ne * a.group;
-    const int per_split = (steps + f.splits_k - 1) / f.splits_k;
+    const int per_split = (steps + splits - 1) / splits;
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
 
     // this lane's key is seen by rows [lo, hi)
@@ -382,55 +497,83 @@ void attn_core_dkv_kernel(BwdArgs f) {
     const int place_g = Tile::place(a.dout.ld, a.d, wave, lane);
     typename Tile::Regs rq, rg;
     float rs = 0.f;
-    // the next step to load: the iy-th of head ih among the masked ones, or the others
-    int ih = 0, iy = 0;
-    if (s0 < edges) {
-        ih = s0 / ne;
-        iy = s0 % ne;
-    } else if (s0 < s1) {
-        ih = (s0 - edges) / ni;
-        iy = ne + (s0 - edges) % ni;
-    }
-    int ii = i_min + walk.step(iy) * QROWS;
-    auto issue = [&](int x, int stage) {   // step x, the next one
-        const int64_t h = (int64_t)hk * a.group + ih;
-        const int i0 = ii;
-        ++iy;
-        if (iy == (x < edges ? ne : nq)) {
-            ++ih;
-            iy = x < edges ? 0 : ne;
-            if (x + 1 == edges) {
-                ih = 0;
-                iy = ne;
-            }
-        }
-        ii = i_min + walk.step(iy) * QROWS;
-        const int n = min(QROWS, mask.lq - i0);
-        const uint16_t *q = Q + h * a.q.sh + (int64_t)i0 * a.q.ld;
-        const uint16_t *g = G + h * a.dout.sh + (int64_t)i0 * a.dout.ld;
-        const int64_t row = ((int64_t)b * a.kv_heads * a.group + h) * a.sq + i0;
-        char *lds = smem + stage * S::STAGE;
-        // rows past n: zeros, also as statistics (their Q and dO are zero, so P = 1 and
-        // dS = 0 meet rows of zeros)
-        if constexpr (DMA) {
-            Tile::issue(q, a.q.ld, n, place_q, lds, wave);
-            Tile::issue(g, a.dout.ld, n, place_g, lds + Tile::BYTES, wave);
-            constexpr int W = NST / 64;   // waves per statistic
-            if (wave < 2 * W) {
-                const int x = (wave % W) * 64 + lane;
-                dma4(make_rsrc((wave < W ? f.nl : f.nd) + row),
-                     lds + 2 * Tile::BYTES + wave * 256, x < n ? x * 4 : OOB);
-            }
-        } else {
-            Tile::load(rq, q, a.q.ld, n, a.d, tid);
-            Tile::load(rg, g, a.dout.ld, n, a.d, tid);
-            if (tid < 2 * NST) {
-                const int x = tid % NST;
-                rs = x < n ? (tid < NST ? f.nl : f.nd)[row + x] : 0.f;
-            }
+    // a place in the walk: the y-th step of head h among the masked ones, or the others
+    struct Place {
+        int h, y;
+    };
+    auto next = [&](Place &c, int x) {   // from step x to x + 1
+        const bool edge = x < edges;
+        ++c.y;
+        if (c.y == (edge ? ne : nq)) {
+            c.h = x + 1 == edges ? 0 : c.h + 1;
+            c.y = edge && x + 1 != edges ? 0 : ne;
         }
     };
-    static_assert(2 * NST <= 256, "one statistic per thread");
+    Place load{0, 0};
+    if (s0 < edges) load = Place{s0 / ne, s0 % ne};
+    else if (s0 < s1) load = Place{(s0 - edges) / ni, ne + (s0 - edges) % ni};
+    Place work = load;
+    // The loads of a step, S::LOADS of a thread: fetch(x, stage) takes the next step of the
+    // walk, fetch_part(i) issues load i of it. Rows past the sequence's end and steps past the
+    // walk's lie outside their buffers and arrive as zeros, also as statistics: P = 1 and
+    // dS = 0 then meet rows of zeros. From step to step the sources only move on; they are
+    // found anew where the head changes or the walk jumps.
+    Fetch to{};
+    i32x4 to_s{};
+    const uint16_t *at_q = Q, *at_g = G;
+    const float *at_s = f.nl;
+    int i0 = 0;
+    constexpr int W = NST / 64;   // waves that load a statistic, 64 floats each
+    auto seek = [&]() {
+        const int64_t h = (int64_t)hk * a.group + min(load.h, a.group - 1);
+        i0 = i_min + walk.step(load.y) * QROWS;
+        at_q = Q + h * a.q.sh + (int64_t)i0 * a.q.ld;
+        at_g = G + h * a.dout.sh + (int64_t)i0 * a.dout.ld;
+        at_s = (wave < W ? f.nl : f.nd) + ((int64_t)b * a.kv_heads * a.group + h) * a.sq + i0;
+    };
+    seek();
+    auto fetch = [&](int x, int stage) {
+        const int n = x < s1 ? min(QROWS, mask.lq - i0) : 0;
+        if constexpr (DMA) {
+            to.x = make_rsrc(at_q);
+            to.y = make_rsrc(at_g);
+            to_s = make_rsrc(at_s);
+            to.x[2] = __builtin_amdgcn_readfirstlane(n * (int)a.q.ld * 2);
+            to.y[2] = __builtin_amdgcn_readfirstlane(n * (int)a.dout.ld * 2);
+            to_s[2] = __builtin_amdgcn_readfirstlane(wave < 2 * W ? n * 4 : 0);
+            to.lds = smem + stage * S::STAGE;
+        } else {
+            Tile::load(rq, at_q, a.q.ld, n, a.d, tid);
+            Tile::load(rg, at_g, a.dout.ld, n, a.d, tid);
+            if (tid < 2 * NST) {
+                const int y = tid % NST;
+                const float *p = at_s + (tid < NST ? f.nl - (wave < W ? f.nl : f.nd)
+                                                   : f.nd - (wave < W ? f.nl : f.nd));
+                rs = y < n ? p[y] : 0.f;
+            }
+        }
+        if (x + 1 >= s1) return;
+        const Place was = load;
+        next(load, x);
+        if (load.h == was.h && walk.step(load.y) == walk.step(was.y) + 1) {
+            i0 += QROWS;
+            at_q += (int64_t)QROWS * a.q.ld;
+            at_g += (int64_t)QROWS * a.dout.ld;
+            at_s += QROWS;
+        } else {
+            seek();
+        }
+    };
+    auto fetch_part = [&](int i) {
+        if constexpr (DMA) {
+            constexpr int NV = Tile::NV;
+            if (i < NV) Tile::issue_part(to.x, a.q.ld, place_q, to.lds, wave, i);
+            else if (i < 2 * NV)
+                Tile::issue_part(to.y, a.dout.ld, place_g, to.lds + Tile::BYTES, wave, i - NV);
+            else
+                dma4(to_s, to.lds + 2 * Tile::BYTES + wave * 256, (wave % W) * 256 + lane * 4);
+        }
+    };
     auto arrive = [&](int stage) {
         if constexpr (!DMA) {
             char *lds = smem + stage * S::STAGE;
@@ -439,10 +582,18 @@ void attn_core_dkv_kernel(BwdArgs f) {
             if (tid < 2 * NST) reinterpret_cast<float *>(lds + 2 * Tile::BYTES)[tid] = rs;
         }
     };
-    int iw = ii + kg * QT;   // this wave's rows of the step to compute
-    if (s0 < s1) {
-        issue(s0, 0);
+    if constexpr (DMA) {
+#pragma unroll
+        for (int x = 0; x < NS - 1; ++x) {
+            fetch(s0 + x, x);
+#pragma unroll
+            for (int i = 0; i < S::LOADS; ++i) fetch_part(i);
+        }
+        fetch(s1, NS - 1);   // nothing, for the parts before the first advance
+    } else if (s0 < s1) {
+        fetch(s0, 0);
         arrive(0);
+        if (s0 + 1 < s1) fetch(s0 + 1, 1);
     }
 
     const int64_t krow = min(key, a.sk - 1);
@@ -453,9 +604,11 @@ void attn_core_dkv_kernel(BwdArgs f) {
     bf16x8 kf[KS], vf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
-        kf[ks] = row_frag(K, ks * 16 + 8 * half, live ? a.d : 0, DMA);
-        vf[ks] = row_frag(V, ks * 16 + 8 * half, live ? a.d : 0, DMA);
+        kf[ks] = row_frag<DMA>(K, ks * 16 + 8 * half, live ? a.d : 0);
+        vf[ks] = row_frag<DMA>(V, ks * 16 + 8 * half, live ? a.d : 0);
     }
+    settle(kf);
+    settle(vf);
     const float c = a.scale * LOG2E;
 
     f32x16 dk[DB], dv[DB];
@@ -465,141 +618,157 @@ void attn_core_dkv_kernel(BwdArgs f) {
         dv[x] = splat16(0.f);
     }
 
-    // a step's rows from i_wave on; EDGE: some key of the wave is not seen by all of them
+    constexpr int NB = QT / 32;
     typename Tile::Reader rd(lds_at(smem) + kg * QT / Tile::RPS * Tile::SEG, lane);
-    uint32_t stat = lds_at(smem) + 2 * Tile::BYTES + (kg * QT + 4 * half) * 4;
-    auto step = [&](int i_wave, auto edge) {
-        constexpr bool EDGE = decltype(edge)::value;
+    const uint32_t stat0 = lds_at(smem) + 2 * Tile::BYTES + (kg * QT + 4 * half) * 4;
+    f32x16 sp[2], dpp[2];           // S and dP of this block and the next, in turn
+    int stage = 0;                  // of the step at work
+    // The statistics of the block at st: where S and dP start.
+    auto start = [&](f32x16 &s, f32x16 &dp, uint32_t st, int r0) {
 #pragma unroll
-        for (int qb = 0; qb < QT / 32; ++qb) {
-            const int r0 = qb * 32, i0 = i_wave + qb * 32;
-            f32x16 s, dp;
+        for (int q = 0; q < 4; ++q) {
+            const f32x4 x = *(SBP_LDS const f32x4 *)(st + (r0 + 8 * q) * 4);
+            const f32x4 y = *(SBP_LDS const f32x4 *)(st + (NST + r0 + 8 * q) * 4);
 #pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const f32x4 x = *(SBP_LDS const f32x4 *)(stat + (r0 + 8 * q) * 4);
-                const f32x4 y = *(SBP_LDS const f32x4 *)(stat + (NST + r0 + 8 * q) * 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    s[4 * q + e] = x[e];
-                    dp[4 * q + e] = y[e];
-                }
+            for (int e = 0; e < 4; ++e) {
+                s[4 * q + e] = x[e];
+                dp[4 * q + e] = y[e];
             }
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.frag(r0, ks, 0), kf[ks], s, 0, 0, 0);
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(rd.frag(r0, ks, Tile::BYTES), vf[ks], dp,
-                                                             0, 0, 0);
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[r] = exp2_(s[r] * c);
-                dp[r] *= s[r];
-                if constexpr (EDGE) {
-                    const int i = i0 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    const bool seen = i >= lo && i < hi;
-                    s[r] = seen ? s[r] : 0.f;
-                    dp[r] = seen ? dp[r] : 0.f;
-                }
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const bf16x8 p = pack8(s, 8 * x), ds = pack8(dp, 8 * x);
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        rd.frag_t(db, r0 + 16 * x, Tile::BYTES), p, dv[db], 0, 0, 0);
-                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        rd.frag_t(db, r0 + 16 * x, 0), ds, dk[db], 0, 0, 0);
-                }
-            }
+        }
+    };
+    // Waits for the step after x, and prepares the load of a later one.
+    auto advance = [&](int x) {
+        if constexpr (DMA) {
+            wait_vm<(NS - 3) * S::LOADS>();
+            __syncthreads();
+            fetch(x + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+        } else {
+            if (x + 1 < s1) arrive(stage == NS - 1 ? 0 : stage + 1);
+            __syncthreads();
+            if (x + 2 < s1) fetch(x + 2, 0);
         }
     };
     auto take = [&](int x, auto edge) {
-        const int stage = (x - s0) & 1;
-        wait_vm<0>();
-        __syncthreads();
-        const int next = ii + kg * QT;
-        if (x + 1 < s1) issue(x + 1, stage ^ 1);
-        step(iw, edge);
-        iw = next;
-        const int by = stage ? -S::STAGE : S::STAGE;
+        constexpr bool EDGE = decltype(edge)::value;
+        const int iw = i_min + walk.step(work.y) * QROWS + kg * QT;
+        next(work, x);
+        const bool wrap = stage == NS - 1;
+        const int by = wrap ? -(NS - 1) * S::STAGE : S::STAGE;
+        const uint32_t stat = stat0 + stage * S::STAGE;
+#pragma unroll
+        for (int qb = 0; qb < NB; ++qb) {
+            const bool last = qb == NB - 1;
+            const int r0 = qb * 32, i0 = iw + qb * 32, n0 = last ? 0 : r0 + 32;
+            if (last) advance(x);
+            typename Tile::Reader nx = rd;       // where the next block lies
+            if (last) nx.move(by);
+            // with an even number of blocks a step the two take turns in place
+            constexpr bool TURN = NB % 2 == 0;
+            constexpr int ONE = 1;
+            const int now = TURN ? qb & 1 : 0;
+            f32x16 &s = sp[now], &dp = dpp[now], &s_n = sp[ONE - now], &dp_n = dpp[ONE - now];
+            bf16x8 tg[2][DB], tq[2][DB], p[2], ds[2];
+            __builtin_amdgcn_sched_barrier(0);
+            start(s_n, dp_n, last ? stat + by : stat, n0);
+            block_scores<KS, Tile::BYTES>(s_n, dp_n, nx, n0, kf, vf, [&](int part) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (!in_part(r, part, KS + 1)) continue;
+                    s[r] = exp2_(s[r] * c);
+                    dp[r] *= s[r];
+                    if constexpr (EDGE) {
+                        const int i = i0 + 8 * (r >> 2) + 4 * half + (r & 3);
+                        const bool seen = i >= lo && i < hi;
+                        s[r] = seen ? s[r] : 0.f;
+                        dp[r] = seen ? dp[r] : 0.f;
+                    }
+                    if (r % 8 == 7) {
+                        p[r / 8] = pack8(s, r - 7);
+                        ds[r / 8] = pack8(dp, r - 7);
+                    }
+                }
+                // the first 16 rows' columns
+                if (part > KS - DB) {
+                    const int db = part - 1 - (KS - DB);
+                    tg[0][db] = rd.frag_t(db, r0, Tile::BYTES);
+                    tq[0][db] = rd.frag_t(db, r0, 0);
+                }
+            });
+            // the loads of a step, spread over its blocks: the last one's first
+            constexpr int PER = (S::LOADS + NB - 1) / NB;
+            const int first = last ? 0 : (qb + 1) * PER;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    dv[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tg[h][db], p[h], dv[db], 0, 0, 0);
+                    dk[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tq[h][db], ds[h], dk[db], 0, 0, 0);
+                    if (h == 0) {
+                        tg[1][db] = rd.frag_t(db, r0 + 16, Tile::BYTES);
+                        tq[1][db] = rd.frag_t(db, r0 + 16, 0);
+                    }
+                    const int k = h * DB + db;
+#pragma unroll
+                    for (int i = PER * k / (2 * DB); i < PER * (k + 1) / (2 * DB); ++i)
+                        if (first + i < S::LOADS) fetch_part(first + i);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            if constexpr (!TURN) {
+                sp[0] = sp[1];
+                dpp[0] = dpp[1];
+            }
+        }
         rd.move(by);
-        stat += by;
-        if (x + 1 < s1) arrive(stage ^ 1);
+        stage = wrap ? 0 : stage + 1;
     };
+    if (s0 < s1) {
+        if constexpr (DMA) wait_vm<(NS - 2) * S::LOADS>();
+        __syncthreads();
+        start(sp[0], dpp[0], stat0, 0);
+        block_scores<KS, Tile::BYTES>(sp[0], dpp[0], rd, 0, kf, vf, [](int) {});
+    }
     int x = s0;
     for (; x < min(s1, edges); ++x) take(x, std::true_type{});
     for (; x < s1; ++x) take(x, std::false_type{});
-
+    wait_vm<0>();      // no load is on its way to LDS any more
     if constexpr (KG > 1) {
+        // dK, then dV: together they would not fit beside the stages
+        static_assert((KG - 1) * (NW / KG) * DB * 4096 <= S::LDS, "group results do not fit");
+        join_groups<KG, DB>(dk, smem, kg, wk, NW / KG, lane);
+        if (!join_groups<KG, DB>(dv, smem, kg, wk, NW / KG, lane)) return;
+    } else {
         __syncthreads();
-        constexpr int SLOT = 2 * DB * 16 * 64;
-        static_assert((KG - 1) * (NW / KG) * SLOT * 4 <= S::LDS, "group results do not fit");
-        float *const base = reinterpret_cast<float *>(smem) + lane;
-        if (kg > 0) {
-            float *p = base + ((kg - 1) * (NW / KG) + wk) * SLOT;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    p[(db * 32 + r) * 64] = dk[db][r];
-                    p[(db * 32 + 16 + r) * 64] = dv[db][r];
-                }
-        }
-        __syncthreads();
-        if (kg > 0) return;
-#pragma unroll
-        for (int k = 1; k < KG; ++k) {
-            const float *p = base + ((k - 1) * (NW / KG) + wk) * SLOT;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    dk[db][r] += p[(db * 32 + r) * 64];
-                    dv[db][r] += p[(db * 32 + 16 + r) * 64];
-                }
-        }
     }
-    if (key >= a.sk) return;
-    // keys past the sequence's length get zeros (their lanes hold no sums of use)
+    // keys past the sequence's length get zeros (their lanes hold no sums of use). Partials:
+    // the tile's KEYS rows of dK and dV of this (sequence, key head)
+    const bool whole = splits == 1;
     const int64_t d4 = (a.d + 3) & ~3;
-    const int64_t n = (int64_t)a.batch * a.kv_heads * a.sk;
-    float *const part = f.part + (((int64_t)split * n) + (int64_t)bh * a.sk + key) * 2 * d4;
-    const int64_t atk = (int64_t)b * a.dk.sb + (int64_t)hk * a.dk.sh + (int64_t)key * a.dk.ld;
-    const int64_t atv = (int64_t)b * a.dv.sb + (int64_t)hk * a.dv.sh + (int64_t)key * a.dv.ld;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int col = db * 32 + 8 * q + 4 * half;
-            if (col >= a.d) continue;
-            if (f.splits_k > 1) {
-                f32x4 x, y;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = live ? dk[db][4 * q + e] : 0.f;
-                    y[e] = live ? dv[db][4 * q + e] : 0.f;
-                }
-                *reinterpret_cast<f32x4 *>(part + col) = x;
-                *reinterpret_cast<f32x4 *>(part + d4 + col) = y;
-            } else {
-                grad4(a.dk.p, atk, col, a.d, a.dk_f32, a.dk_acc, f.vec_k,
-                      [&](int e) { return live ? dk[db][4 * q + e] * a.scale : 0.f; });
-                grad4(a.dv.p, atv, col, a.d, a.dv_f32, a.dv_acc, f.vec_v,
-                      [&](int e) { return live ? dv[db][4 * q + e] : 0.f; });
-            }
-        }
+    const int64_t slot = (int64_t)(f.lev.slot[lev] + in_level) * a.batch * a.kv_heads + bh;
+    float *const put = reinterpret_cast<float *>(smem) + wk * (32 * 68);
+    const RowsOut out_k{whole ? a.dk.p : f.part, !whole || a.dk_f32, whole && a.dk_acc,
+                        !whole || f.vec_k};
+    const RowsOut out_v{whole ? a.dv.p : f.part + d4, !whole || a.dv_f32, whole && a.dv_acc,
+                        !whole || f.vec_v};
+    put_rows<DP>(put, dk, !live ? 0.f : whole ? a.scale : 1.f, out_k, a.d, lane, [&](int r) -> int64_t {
+        if (jw + r >= a.sk) return -1;
+        if (!whole) return (slot * KEYS + wk * 32 + r) * 2 * d4;
+        return (int64_t)b * a.dk.sb + (int64_t)hk * a.dk.sh + (int64_t)(jw + r) * a.dk.ld;
+    });
+    put_rows<DP>(put, dv, live ? 1.f : 0.f, out_v, a.d, lane, [&](int r) -> int64_t {
+        if (jw + r >= a.sk) return -1;
+        if (!whole) return (slot * KEYS + wk * 32 + r) * 2 * d4;
+        return (int64_t)b * a.dv.sb + (int64_t)hk * a.dv.sh + (int64_t)(jw + r) * a.dv.ld;
+    });
 }
 
 // Adds the splits' partials in split order. A thread owns 4 columns of a row of dQ
-// (KV false) or of dK and dV.
+// (KV false) or of dK and dV (of the tiles that are split).
 template <bool KV>
 __global__ __launch_bounds__(256) void attn_core_sum_kernel(BwdArgs f) {
     const CoreArgs &a = f.a;
     const int quads = (a.d + 3) >> 2;
-    const int64_t d4 = quads * 4, per = KV ? a.sk : f.rows;
-    const int64_t n = (int64_t)a.batch * a.kv_heads * per;
+    const int64_t d4 = quads * 4, per = KV ? f.lev.split_keys : f.rows;
+    const int64_t bhs = (int64_t)a.batch * a.kv_heads, n = bhs * per;
     const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
     if (id >= n * quads) return;
     const int64_t at = id / quads;
@@ -607,9 +776,15 @@ __global__ __launch_bounds__(256) void attn_core_sum_kernel(BwdArgs f) {
     const int bh = (int)(at / per), row = (int)(at % per);
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
     if constexpr (KV) {
+        const int tile = row / f.keys;
+        int lev = 0;
+        while (lev + 1 < f.lev.n && tile >= f.lev.tile[lev + 1]) ++lev;
+        const int v = f.lev.v[lev];
+        const int64_t slot = f.lev.slot[lev] + (int64_t)(tile - f.lev.tile[lev]) * v;
+        const float *p = f.part + ((slot * bhs + bh) * f.keys + row % f.keys) * 2 * d4 + col;
+        const int64_t step = bhs * f.keys * 2 * d4;
         f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
-        for (int s = 0; s < f.splits_k; ++s) {
-            const float *p = f.part + ((int64_t)s * n + at) * 2 * d4 + col;
+        for (int s = 0; s < v; ++s, p += step) {
             x += *reinterpret_cast<const f32x4 *>(p);
             y += *reinterpret_cast<const f32x4 *>(p + d4);
         }
@@ -667,6 +842,78 @@ bool vec4(const CoreView &v, bool f32) {
            v.sb % 4 == 0 && v.sh % 4 == 0;
 }
 
+// Steps of key tile t's walk, every row and key in use.
+int64_t tile_steps(const CoreArgs &a, int64_t t, int keys, int rows) {
+    const int64_t off = (int64_t)a.sk - a.sq, j0 = t * keys;
+    int64_t n = a.sq;
+    if (a.causal && a.window) n = std::min<int64_t>(n, keys + a.window);
+    else if (a.causal) n -= std::min<int64_t>(n, std::max<int64_t>(0, j0 - off));
+    return (n + rows - 1) / rows * a.group;
+}
+
+// Wave groups (returned) and splits of the dK and dV launch: the pair that the following
+// time expects least of. A step of a workgroup takes `step` us, an item `fixed` besides;
+// the busiest unit has an even share of all items and half of the longest; partials are
+// written and read once, by a launch of their own.
+int plan_dkv(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs *f) {
+    const size_t d4 = (a.d + 3) & ~3;
+    const bool wide = a.d > 64;
+    const double slots = cus * (wide ? 1.0 : 2.0), fixed = 4.0;
+    double best = 1e300;
+    int best_kg = 1;
+    for (int kg = 1; kg <= 2; ++kg) {
+        const int keys = 128 / kg, rows = 64;
+        const int64_t tiles = ((int64_t)a.sk + keys - 1) / keys;
+        const double step = (kg == 1 ? 2 : 1) * (wide ? 0.95 : 0.55);
+        const int64_t longest = tile_steps(a, 0, keys, rows);
+        for (int v = 1; v <= sbpk::MAX_LEVELS && v <= std::max<int64_t>(1, longest / 2); ++v) {
+            // walks of more than `target` steps are split; they get no longer from tile to
+            // tile
+            const int64_t target = std::max<int64_t>(1, (longest + v - 1) / v);
+            sbpk::Levels lev{};
+            int64_t partials = 0, items = 0, at = 0;
+            double total = 0;
+            for (int64_t w = v; w >= 1 && at < tiles; --w) {
+                int64_t lo = at, hi = tiles;   // the end of the tiles of w parts or more
+                while (lo < hi) {
+                    const int64_t mid = (lo + hi) / 2;
+                    if (w == 1 || tile_steps(a, mid, keys, rows) > (w - 1) * target) lo = mid + 1;
+                    else hi = mid;
+                }
+                if (lo == at) continue;
+                const int j = lev.n++;
+                lev.tile[j] = (int32_t)at;
+                lev.v[j] = (int32_t)w;
+                lev.item[j] = (int32_t)items;
+                lev.slot[j] = (int32_t)partials;
+                items += (lo - at) * w;
+                if (w > 1) {
+                    partials += (lo - at) * w;
+                    lev.split_keys = (int32_t)std::min<int64_t>(a.sk, lo * keys);
+                }
+                total += (lo - at) * 0.5 *
+                         (double)(tile_steps(a, at, keys, rows) + tile_steps(a, lo - 1, keys, rows));
+                at = lo;
+            }
+            lev.tile[lev.n] = (int32_t)tiles;
+            lev.items = (int32_t)items;
+            const double part = (double)partials * bhs * keys * 2 * d4;   // floats
+            if (part > (double)room || (double)items * bhs > 16777215.0) break;
+            const double item = target * step + fixed;
+            const double all = (total * step + items * fixed) * bhs / slots;
+            const double t = std::max(item, all + 0.5 * item) +
+                             (partials ? 4.0 + part * 8 / 4e6 : 0.0);
+            if (t < best * 0.98) {
+                best = t;
+                best_kg = kg;
+                f->lev = lev;
+                f->keys = keys;
+            }
+        }
+    }
+    return best_kg;
+}
+
 }  // namespace
 
 hipError_t launch_core_bwd(const CoreArgs &a, hipStream_t s) {
@@ -694,8 +941,8 @@ hipError_t launch_core_bwd(const CoreArgs &a, hipStream_t s) {
         if (e != hipSuccess) return e;
 
         int kg = 1;
-        while (kg < 4 && ((f.rows + 128 / kg - 1) / (128 / kg)) * bhs < cus) kg *= 2;
-        const int rows = 128 / kg, keys = kg == 4 ? 128 : 64 * kg;
+        while (kg < 2 && ((f.rows + 128 / kg - 1) / (128 / kg)) * bhs < cus) kg *= 2;
+        const int rows = 128 / kg, keys = 64;
         f.tiles_q = (f.rows + rows - 1) / rows;
         const int64_t steps = ((int64_t)a.sk + keys - 1) / keys;
         int64_t splits = 1;
@@ -706,10 +953,8 @@ hipError_t launch_core_bwd(const CoreArgs &a, hipStream_t s) {
         const int64_t blocks = f.tiles_q * bhs * splits;
         if (kg == 1)
             e = wide ? launch_dq<128, 1, 64>(f, blocks, s) : launch_dq<64, 1, 64>(f, blocks, s);
-        else if (kg == 2)
-            e = wide ? launch_dq<128, 2, 64>(f, blocks, s) : launch_dq<64, 2, 64>(f, blocks, s);
         else
-            e = wide ? launch_dq<128, 4, 32>(f, blocks, s) : launch_dq<64, 4, 32>(f, blocks, s);
+            e = wide ? launch_dq<128, 2, 32>(f, blocks, s) : launch_dq<64, 2, 32>(f, blocks, s);
         if (e != hipSuccess) return e;
         if (splits > 1) {
             const int64_t items = qrows * (int64_t)(d4 / 4);
@@ -718,27 +963,15 @@ hipError_t launch_core_bwd(const CoreArgs &a, hipStream_t s) {
             if (e != hipSuccess) return e;
         }
     }
-    const int64_t krows = bhs * a.sk;
-    if (krows == 0) return hipSuccess;
-    int kg = 1;
-    while (kg < 4 && ((a.sk + 128 / kg - 1) / (128 / kg)) * bhs < cus) kg *= 2;
-    const int keys = 128 / kg, qr = kg == 4 ? 128 : 64;
-    f.tiles_k = (a.sk + keys - 1) / keys;
-    const int64_t steps = (((int64_t)a.sq + qr - 1) / qr) * a.group;
-    int64_t splits = 1;
-    while (f.tiles_k * bhs * splits * 2 <= 2 * cus && steps / (splits * 2) >= 2 &&
-           (size_t)krows * 2 * d4 * splits * 2 <= room)
-        splits *= 2;
-    f.splits_k = (int)splits;
-    const int64_t blocks = f.tiles_k * bhs * splits;
+    if (bhs * a.sk == 0) return hipSuccess;
+    const int kg = plan_dkv(a, bhs, cus, room, &f);
+    const int64_t blocks = bhs * f.lev.items;
     if (kg == 1)
         e = wide ? launch_dkv<128, 1, 64>(f, blocks, s) : launch_dkv<64, 1, 64>(f, blocks, s);
-    else if (kg == 2)
-        e = wide ? launch_dkv<128, 2, 32>(f, blocks, s) : launch_dkv<64, 2, 32>(f, blocks, s);
     else
-        e = wide ? launch_dkv<128, 4, 32>(f, blocks, s) : launch_dkv<64, 4, 32>(f, blocks, s);
-    if (e != hipSuccess || splits == 1) return e;
-    const int64_t items = krows * (int64_t)(d4 / 4);
+        e = wide ? launch_dkv<128, 2, 32>(f, blocks, s) : launch_dkv<64, 2, 32>(f, blocks, s);
+    if (e != hipSuccess || f.lev.split_keys == 0) return e;
+    const int64_t items = bhs * f.lev.split_keys * (int64_t)(d4 / 4);
     return launch_kernel(sbpk::attn_core_sum_kernel<true>, "attn_core_sum_kernel<1>",
                          dim3((unsigned)((items + 255) / 256)), dim3(256), s, f);
 }

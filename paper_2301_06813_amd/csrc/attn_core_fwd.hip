@@ -88,8 +88,8 @@ void attn_core_fwd_kernel(FwdArgs f) {
 
     // heavier (later) causal tiles first within a (sequence, head)
     const int per = f.tiles * f.splits;
-    const int L = remap_xcd(blockIdx.x, gridDim.x);
-    const int bh = L / per, t = L % per;
+    int bh, t;
+    deal(blockIdx.x, a.batch * a.kv_heads, per, &bh, &t);
     const int tile = f.tiles - 1 - t / f.splits, split = t % f.splits;
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const SeqMask mask(a, b);
@@ -158,7 +158,8 @@ void attn_core_fwd_kernel(FwdArgs f) {
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-        qf[ks] = row_frag(Q, ks * 16 + 8 * half, live ? a.d : 0, DMA);
+        qf[ks] = row_frag<DMA>(Q, ks * 16 + 8 * half, live ? a.d : 0);
+    settle(qf);
 
     const float c = a.scale * LOG2E;
     const float grow = 8.f / c;

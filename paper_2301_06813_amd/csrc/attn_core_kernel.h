@@ -68,6 +68,12 @@ struct RowTile {
             dma16(r, lds + (i * NW + wave) * SEG, place + i * (NW * RPS * (int)ld * 2));
     }
 
+    // One of the NV loads of issue(), of buffer `r`.
+    __device__ __forceinline__ static void issue_part(i32x4 r, int64_t ld, int place, char *lds,
+                                                      int wave, int i) {
+        dma16(r, lds + (i * NW + wave) * SEG, place + i * (NW * RPS * (int)ld * 2));
+    }
+
     // The same through registers, for rows at any element alignment and stride.
     typedef u32x4 Regs[NV];
     __device__ __forceinline__ static void load(Regs &v, const uint16_t *base, int64_t ld, int n,
@@ -137,14 +143,28 @@ __device__ __forceinline__ uint32_t lds_at(const void *p) {
     return (uint32_t)(uintptr_t)(SBP_LDS const void *)p;
 }
 
-// 8 columns of a row in memory (columns past d as zeros), at any alignment.
-__device__ __forceinline__ bf16x8 row_frag(const uint16_t *row, int at, int d, bool aligned) {
+// 8 columns of a row in memory (columns past d as zeros): ALIGNED rows have 16-byte
+// blocks that lie wholly before or past d; others are read at any alignment.
+template <bool ALIGNED>
+__device__ __forceinline__ bf16x8 row_frag(const uint16_t *row, int at, int d) {
     u32x4 v = {0u, 0u, 0u, 0u};
-    if (at + 8 <= d)
-        v = aligned ? *reinterpret_cast<const u32x4 *>(row + at) : ld16_any(row + at);
-    else if (at < d)
-        v = ld16_tail(row, at, d);
+    if constexpr (ALIGNED) {
+        if (at < d) v = *reinterpret_cast<const u32x4 *>(row + at);
+    } else {
+        if (at + 8 <= d) v = ld16_any(row + at);
+        else if (at < d) v = ld16_tail(row, at, d);
+    }
     return __builtin_bit_cast(bf16x8, v);
+}
+
+// Waits here for the loads of x. The compiler does not see the direct-to-LDS loads; left to
+// the first use inside a loop, its wait would be for every load in flight, in every pass
+// (the loads of later stages among them: dK and dV of 16 heads over 4, 8192 x 128 causal,
+// 625 us with those waits and 609 without).
+template <int N>
+__device__ __forceinline__ void settle(bf16x8 (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; ++i) asm volatile("" : "+v"(x[i]));
 }
 
 __device__ __forceinline__ bf16x8 pack8(const f32x16 &x, int q0) {
@@ -189,6 +209,121 @@ struct SeqMask {
         return window ? max(0, i + 1 + off - window) : 0;
     }
 };
+
+// Hands the sums of wave groups 1 .. KG - 1 to group 0 through LDS, lane by lane, in group
+// order; called by the whole workgroup, whose LDS is free before and after. Returns whether
+// this wave is of group 0. `unit` counts the waves of a group. LDS: (KG - 1) * units * N * 4 KB.
+template <int KG, int N>
+__device__ __forceinline__ bool join_groups(f32x16 *acc, char *smem, int kg, int unit, int units,
+                                            int lane) {
+    f32x4 *const base = reinterpret_cast<f32x4 *>(smem) + lane;
+    __syncthreads();
+    if (kg > 0) {
+        f32x4 *p = base + ((kg - 1) * units + unit) * (N * 4 * 64);
+#pragma unroll
+        for (int i = 0; i < N * 4; ++i)
+            p[i * 64] = f32x4{acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1],
+                              acc[i / 4][i % 4 * 4 + 2], acc[i / 4][i % 4 * 4 + 3]};
+    }
+    __syncthreads();
+    for (int k = 1; kg == 0 && k < KG; ++k) {
+        const f32x4 *p = base + ((k - 1) * units + unit) * (N * 4 * 64);
+#pragma unroll
+        for (int i = 0; i < N * 4; ++i) {
+            const f32x4 v = p[i * 64];
+#pragma unroll
+            for (int e = 0; e < 4; ++e) acc[i / 4][i % 4 * 4 + e] += v[e];
+        }
+    }
+    __syncthreads();
+    return kg == 0;
+}
+
+// Where 32 result rows of a wave go: bf16 or fp32, overwritten or added to; `vec`: rows
+// allow stores of 4 values.
+struct RowsOut {
+    void *p;
+    bool f32, add, vec;
+};
+
+// Stores a wave's result (lane l holds column l % 32, here a row of the output, and in
+// acc[db] register q value 32 db + 8 (q / 4) + 4 (l / 32) + q % 4 of it), times `mul` (0 where
+// it is 0), through `tile`, 32 x 68 floats of LDS of its own, 64 columns at a time: 16 lanes
+// then store a row's 64 values side by side. The loop is not unrolled: straight-line
+// stores of every type made the kernels' code several times longer than their loops, and
+// short launches waited for it. at(r): element offset of row r, or < 0 for none.
+template <int DP, class At>
+__device__ __forceinline__ void put_rows(float *tile, const f32x16 *acc, float mul, const RowsOut &o,
+                                         int d, int lane, At at) {
+    const int half = lane >> 5;
+#pragma unroll
+    for (int c0 = 0; c0 < DP; c0 += 64) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const f32x16 &a = acc[c0 / 32 + i / 4];
+            const int q = i % 4 * 4;
+            f32x4 v;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) v[e] = mul != 0.f ? a[q + e] * mul : 0.f;
+            *reinterpret_cast<f32x4 *>(tile + (lane & 31) * 68 + i / 4 * 32 + 2 * q + 4 * half) = v;
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        const int left = d - c0 - (lane & 15) * 4;   // values of the row from this lane's first
+#pragma unroll 1
+        for (int it = 0; it < 8; ++it) {
+            const int r = it * 4 + (lane >> 4);
+            const f32x4 v = *reinterpret_cast<const f32x4 *>(tile + r * 68 + (lane & 15) * 4);
+            const int64_t off = at(r);
+            if (off < 0 || left <= 0) continue;
+            const int64_t e0 = off + c0 + (lane & 15) * 4;
+            if (o.f32) {
+                float *p = static_cast<float *>(o.p) + e0;
+                if (o.vec && left >= 4) {
+                    f32x4 w = v;
+                    if (o.add) w += *reinterpret_cast<const f32x4 *>(p);
+                    *reinterpret_cast<f32x4 *>(p) = w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < left) p[e] = o.add ? p[e] + v[e] : v[e];
+                }
+            } else {
+                uint16_t *p = static_cast<uint16_t *>(o.p) + e0;
+                if (o.vec && left >= 4) {
+                    u32x2 w;
+                    w[0] = (uint32_t)f32_to_bf16_bits(v[0]) | (uint32_t)f32_to_bf16_bits(v[1]) << 16;
+                    w[1] = (uint32_t)f32_to_bf16_bits(v[2]) | (uint32_t)f32_to_bf16_bits(v[3]) << 16;
+                    *reinterpret_cast<u32x2 *>(p) = w;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        if (e < left) p[e] = f32_to_bf16_bits(v[e]);
+                }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+    }
+}
+
+// Which (sequence, key head) and which of its `per` items, heaviest first, a workgroup takes.
+// Workgroups go to the XCDs in turn. Where the heads are a multiple of 8, each XCD takes
+// whole heads, one after the other, whose keys then stay in its L2; else the heads'
+// items are dealt out in turn, all heaviest ones first, so that a head that is spread over
+// several XCDs leaves none with its heavier half (16 query heads over 4 key heads, 8192 x 128
+// causal: dQ 563 us in one
+// head after the other and 412 dealt out, dK and dV 878 and 625).
+__device__ __forceinline__ void deal(int wg, int heads, int per, int *bh, int *item) {
+    if (heads % 8 == 0) {
+        const int l = remap_xcd(wg, heads * per);
+        *bh = l / per;
+        *item = l % per;
+    } else {
+        *bh = wg % heads;
+        *item = wg / heads;
+    }
+}
 
 // The order in which a workgroup takes the n steps of its walk: first those that need
 // the mask, [0, na) and [nb, n), then the others. Two loops, so that the second holds no

@@ -3,13 +3,16 @@
 //   P = exp(scale Q K^T - lse),  dV = P^T dO,  dS = P (dO V^T - D),
 //   dQ = scale dS K,  dK = scale dS^T Q,  D_i = sum_c dO_ic O_ic.
 //
-// Three launches, none with atomics, so the results do not depend on the order
-// in which workgroups run:
+// Two launches, or three where walks are split, none with atomics, so the results do not
+// depend on the order in which workgroups run:
 //   * row statistics: -lse / scale and D of every query row go to the workspace;
-//   * dQ: a workgroup owns query rows (packed over the query heads that share a
-//     key head, as in the forward kernel) and walks over their keys;
-//   * dK and dV: a workgroup owns keys and walks over the rows that see them, of
-//     every query head that shares the key head.
+//   * the gradients. A workgroup of dK and dV owns keys and walks over the rows that see
+//     them, of every query head that shares the key head; one of dQ owns query rows (packed
+//     over the query heads that share a key head, as in the forward kernel) and walks
+//     over their keys. One launch holds both kinds, dK's and dV's first: they are longer,
+//     and the others fill the units that they leave (16 heads of 1024 x 64, causal: 18 + 23 us
+//     in two launches, 27 in one);
+//   * sums of the parts of split walks.
 // Scores and dO V^T are thus computed twice, seven products where five are needed;
 // the alternative, one pass that adds dQ in memory, needs fp32 atomics (in
 // an order that changes the result) or a partial dQ for every key tile.
@@ -43,11 +46,11 @@ struct Levels {
 struct BwdArgs {
     CoreArgs a;
     int32_t tiles_q, splits_q, rows;   // dQ: row tiles, key splits; rows = sq * group
-    int32_t keys;                      // dK, dV: keys of a tile, and its splits
+    int32_t items_kv;                  // workgroups of dK and dV; those of dQ follow
     Levels lev;
     int32_t vec_q, vec_k, vec_v;       // outputs allow 4-value stores
     const float *nl, *nd;              // row statistics: -lse / scale, -D, per (b, head, i)
-    float *part;                       // split partials
+    float *part_q, *part_kv;           // split partials
 };
 
 // Adds to or overwrites 4 consecutive values of an output row.
@@ -165,7 +168,7 @@ __device__ __forceinline__ constexpr bool in_part(int r, int i, int parts) {
 // A direct-to-LDS load to come: two tiles.
 struct Fetch {
     i32x4 x, y;
-    char *lds;
+    uint32_t lds;
 };
 
 template <int DP, int KG, int KT, bool DMA>
@@ -178,29 +181,38 @@ struct DqShape {
     static constexpr int OCC = DP > 64 ? 1 : 2;
     static constexpr int FIT = 163840 / OCC / STAGE;
     static constexpr int NS = !DMA ? 3 : FIT > 4 ? 4 : FIT;
-    static constexpr int PUT = NW * 32 * 68 * 4;     // put_rows
+    static constexpr int PUT = NW * PUT_FLOATS<DP> * 4;
     static constexpr int LDS = NS * STAGE > PUT ? NS * STAGE : PUT;
-    static_assert(FIT >= NS && NS >= 3, "three stages");
+    static_assert(FIT >= NS && NS >= 3 && LDS <= 163840 / OCC, "three stages");
 };
 
 template <int DP, int KG, int KT, bool DMA>
-__global__ __launch_bounds__(256, (DqShape<DP, KG, KT, DMA>::OCC))
-void attn_core_dq_kernel(BwdArgs f) {
+__device__ __forceinline__ void attn_core_dq(const BwdArgs &f, int wg, char *smem) {
     using S = DqShape<DP, KG, KT, DMA>;
     using Tile = typename S::Tile;
     constexpr int NW = S::NW, ROWS = S::ROWS, NS = S::NS;
     constexpr int NB = KT / 32, KS = DP / 16, DB = DP / 32, KEYS = KG * KT;
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    const uint32_t lds0 = lds_at(smem);
     const CoreArgs &a = f.a;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform, so that what
                                                                  // depends on it is scalar
     const int kg = wave % KG, wr = wave / KG;
 
+    // the arguments, read at once: the compiler loads each where it is first used, and each
+    // first load is a trip to memory (read one by one, a workgroup's first loads of tiles were
+    // issued 0.35 us later)
+    asm volatile("" ::"s"(a.q.p), "s"(a.q.sb), "s"(a.q.sh), "s"(a.q.ld), "s"(a.dout.p),
+                 "s"(a.dout.sb), "s"(a.dout.sh), "s"(a.dout.ld), "s"(a.k.p), "s"(a.k.sb),
+                 "s"(a.k.sh), "s"(a.k.ld), "s"(a.v.p), "s"(a.v.sb), "s"(a.v.sh), "s"(a.v.ld),
+                 "s"(a.len_q), "s"(a.len_k), "s"(a.batch), "s"(a.kv_heads), "s"(a.group),
+                 "s"(a.sq), "s"(a.sk), "s"(a.d), "s"(a.causal), "s"(a.window), "s"(a.scale),
+                 "s"(f.tiles_q), "s"(f.splits_q), "s"(f.rows));
+    asm volatile("" ::"s"(f.nl), "s"(f.nd), "s"(a.dq.p), "s"(f.part_q));
     // heavier (later) causal tiles first within a (sequence, head)
     const int per = f.tiles_q * f.splits_q;
     int bh, t;
-    deal(blockIdx.x, a.batch * a.kv_heads, per, &bh, &t);
+    deal(wg, a.batch * a.kv_heads, per, &bh, &t);
     const int tile = f.tiles_q - 1 - t / f.splits_q, split = t % f.splits_q;
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
     const SeqMask mask(a, b);
@@ -245,7 +257,7 @@ void attn_core_dq_kernel(BwdArgs f) {
             to.y = make_rsrc(V + (int64_t)k0 * a.v.ld);
             to.x[2] = __builtin_amdgcn_readfirstlane(n * (int)a.k.ld * 2);
             to.y[2] = __builtin_amdgcn_readfirstlane(n * (int)a.v.ld * 2);
-            to.lds = smem + stage * S::STAGE;
+            to.lds = lds0 + stage * S::STAGE;
         } else {
             Tile::load(rk, K + (int64_t)k0 * a.k.ld, a.k.ld, n, a.d, tid);
             Tile::load(rv, V + (int64_t)k0 * a.v.ld, a.v.ld, n, a.d, tid);
@@ -253,8 +265,8 @@ void attn_core_dq_kernel(BwdArgs f) {
     };
     auto fetch_part = [&](int p) {
         if constexpr (DMA) {
-            if (p < Tile::NV) Tile::issue_part(to.x, a.k.ld, place_k, to.lds, wave, p);
-            else Tile::issue_part(to.y, a.v.ld, place_v, to.lds + Tile::BYTES, wave, p - Tile::NV);
+            if (p < Tile::NV) Tile::issue(to.x, a.k.ld, place_k, to.lds, wave, p);
+            else Tile::issue(to.y, a.v.ld, place_v, to.lds + Tile::BYTES, wave, p - Tile::NV);
         }
     };
     auto arrive = [&](int stage) {
@@ -301,7 +313,7 @@ void attn_core_dq_kernel(BwdArgs f) {
 #pragma unroll
     for (int x = 0; x < DB; ++x) o[x] = splat16(0.f);
 
-    typename Tile::Reader rd(lds_at(smem) + kg * KT / Tile::RPS * Tile::SEG, lane);
+    typename Tile::Reader rd(lds0 + kg * KT / Tile::RPS * Tile::SEG, lane);
     f32x16 sp[2], dpp[2];           // S and dP of this block and the next, in turn
     int stage = 0;                  // of the step at work
     // Waits for the step after x, and prepares the load of a later one.
@@ -317,7 +329,7 @@ void attn_core_dq_kernel(BwdArgs f) {
         }
     };
     // EDGE: some row of the tile does not see every key of the step
-    auto take = [&](int x, auto edge) {
+    auto take = [&](int x, auto edge) __attribute__((always_inline)) {
         constexpr bool EDGE = decltype(edge)::value;
         const int kw = k_beg + walk.step(x) * KEYS + kg * KT;
         const bool wrap = stage == NS - 1;
@@ -385,31 +397,24 @@ void attn_core_dq_kernel(BwdArgs f) {
     for (; x < min(s1, walk.masked()); ++x) take(x, std::true_type{});
     for (; x < s1; ++x) take(x, std::false_type{});
     wait_vm<0>();      // no load is on its way to LDS any more
-    if constexpr (KG > 1) {
-        static_assert((KG - 1) * (NW / KG) * DB * 4096 <= S::LDS, "group results do not fit");
-        if (!join_groups<KG, DB>(o, smem, kg, wr, NW / KG, lane)) return;
-    } else {
-        __syncthreads();
-    }
+    __syncthreads();
     const bool whole = f.splits_q == 1;
     const int64_t d4 = (a.d + 3) & ~3;
-    const RowsOut out{whole ? a.dq.p : f.part, !whole || a.dq_f32, whole && a.dq_acc,
-                      !whole || f.vec_q};
-    float *const put = reinterpret_cast<float *>(smem) + wr * (32 * 68);
-    put_rows<DP>(put, o, whole ? a.scale : 1.f, out, a.d, lane, [&](int r) -> int64_t {
-        const int q = row0 + wr * 32 + r;
-        if (q >= f.rows) return -1;
-        if (!whole) return (((int64_t)split * a.batch * a.kv_heads + bh) * f.rows + q) * d4;
-        const int qi = q / a.group;
-        return (int64_t)b * a.dq.sb + ((int64_t)hk * a.group + (q - qi * a.group)) * a.dq.sh +
-               (int64_t)qi * a.dq.ld;
-    });
+    const RowsOut out{whole ? a.dq.p : f.part_q, whole ? a.d : (int)d4, !whole || a.dq_f32,
+                      whole && a.dq_acc, !whole || f.vec_q};
+    const int64_t off = !valid ? -1
+                        : whole ? (int64_t)b * a.dq.sb + head * a.dq.sh + (int64_t)i * a.dq.ld
+                                : (((int64_t)split * a.batch * a.kv_heads + bh) * f.rows + row) * d4;
+    float *const put = reinterpret_cast<float *>(smem);
+    stage_rows<DP>(put + wave * PUT_FLOATS<DP>, o, whole ? a.scale : 1.f, lane);
+    __syncthreads();
+    store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
 }
 
 // ------------------------------------------------------------ dK and dV
-// One dword per lane into LDS (lane l at lds + 4 l).
-__device__ __forceinline__ void dma4(i32x4 r, char *lds, int voff) {
-    const uint32_t m0 = __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(SBP_LDS void *)lds);
+// One dword per lane to byte `lds` of LDS (uniform) and on (lane l at + 4 l).
+__device__ __forceinline__ void dma4_at(i32x4 r, uint32_t lds, int voff) {
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds);
     asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dword %1, %2, 0 offen lds"
                  :
                  : "s"(m0), "v"(voff), "s"(r)
@@ -431,28 +436,39 @@ struct DkvShape {
     // stages: a step reads its own and the next one while later ones arrive
     static constexpr int FIT = 163840 / OCC / STAGE;
     static constexpr int NS = !DMA ? 3 : FIT > 4 ? 4 : FIT;
-    static constexpr int PUT = NW * 32 * 68 * 4;     // put_rows
+    static constexpr int PUT = NW * 2 * PUT_FLOATS<DP> * 4;
     static constexpr int LDS = NS * STAGE > PUT ? NS * STAGE : PUT;
-    static_assert(FIT >= NS && NS >= 3 && NST % 64 == 0 && 2 * NST <= 256, "three stages, one statistic per thread");
+    static_assert(FIT >= NS && NS >= 3 && LDS <= 163840 / OCC, "three stages");
+    static_assert(NST % 64 == 0 && 2 * NST <= 256, "one statistic per thread");
 };
 
 template <int DP, int KG, int QT, bool DMA>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(DkvShape<DP, KG, QT, DMA>::OCC, DkvShape<DP, KG, QT, DMA>::OCC)))
-void attn_core_dkv_kernel(BwdArgs f) {
+__device__ __forceinline__ void attn_core_dkv(const BwdArgs &f, int wg, char *smem) {
     using S = DkvShape<DP, KG, QT, DMA>;
     using Tile = typename S::Tile;
     constexpr int NW = S::NW, KEYS = S::KEYS, QROWS = S::QROWS, NST = S::NST, NS = S::NS;
     constexpr int KS = DP / 16, DB = DP / 32;
-    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    const uint32_t lds0 = lds_at(smem);
     const CoreArgs &a = f.a;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform, so that what
                                                                  // depends on it is scalar
     const int kg = wave % KG, wk = wave / KG;
 
+    // the arguments, read at once: the compiler loads each where it is first used, and each
+    // first load is a trip to memory (read one by one, a workgroup's first loads of tiles were
+    // issued 0.35 us later)
+    asm volatile("" ::"s"(a.q.p), "s"(a.q.sb), "s"(a.q.sh), "s"(a.q.ld), "s"(a.dout.p),
+                 "s"(a.dout.sb), "s"(a.dout.sh), "s"(a.dout.ld), "s"(a.k.p), "s"(a.k.sb),
+                 "s"(a.k.sh), "s"(a.k.ld), "s"(a.v.p), "s"(a.v.sb), "s"(a.v.sh), "s"(a.v.ld),
+                 "s"(a.len_q), "s"(a.len_k), "s"(a.batch), "s"(a.kv_heads), "s"(a.group),
+                 "s"(a.sq), "s"(a.sk), "s"(a.d), "s"(a.causal), "s"(a.window), "s"(a.scale),
+                 "s"(f.lev.items), "s"(f.lev.n));
+    asm volatile("" ::"s"(f.nl), "s"(f.nd), "s"(a.dk.p), "s"(a.dv.p), "s"(f.part_kv),
+                 "s"(f.lev.tile[0]), "s"(f.lev.item[0]), "s"(f.lev.slot[7]));
     // keys with more rows (earlier causal tiles) first within a (sequence, head)
     int bh, t;
-    deal(blockIdx.x, a.batch * a.kv_heads, f.lev.items, &bh, &t);
+    deal(wg, a.batch * a.kv_heads, f.lev.items, &bh, &t);
     int lev = 0;
     while (lev + 1 < f.lev.n && t >= f.lev.item[lev + 1]) ++lev;
     const int splits = f.lev.v[lev], in_level = t - f.lev.item[lev];
@@ -541,7 +557,7 @@ void attn_core_dkv_kernel(BwdArgs f) {
             to.x[2] = __builtin_amdgcn_readfirstlane(n * (int)a.q.ld * 2);
             to.y[2] = __builtin_amdgcn_readfirstlane(n * (int)a.dout.ld * 2);
             to_s[2] = __builtin_amdgcn_readfirstlane(wave < 2 * W ? n * 4 : 0);
-            to.lds = smem + stage * S::STAGE;
+            to.lds = lds0 + stage * S::STAGE;
         } else {
             Tile::load(rq, at_q, a.q.ld, n, a.d, tid);
             Tile::load(rg, at_g, a.dout.ld, n, a.d, tid);
@@ -567,11 +583,11 @@ void attn_core_dkv_kernel(BwdArgs f) {
     auto fetch_part = [&](int i) {
         if constexpr (DMA) {
             constexpr int NV = Tile::NV;
-            if (i < NV) Tile::issue_part(to.x, a.q.ld, place_q, to.lds, wave, i);
+            if (i < NV) Tile::issue(to.x, a.q.ld, place_q, to.lds, wave, i);
             else if (i < 2 * NV)
-                Tile::issue_part(to.y, a.dout.ld, place_g, to.lds + Tile::BYTES, wave, i - NV);
+                Tile::issue(to.y, a.dout.ld, place_g, to.lds + Tile::BYTES, wave, i - NV);
             else
-                dma4(to_s, to.lds + 2 * Tile::BYTES + wave * 256, (wave % W) * 256 + lane * 4);
+                dma4_at(to_s, to.lds + 2 * Tile::BYTES + wave * 256, (wave % W) * 256 + lane * 4);
         }
     };
     auto arrive = [&](int stage) {
@@ -619,8 +635,8 @@ void attn_core_dkv_kernel(BwdArgs f) {
     }
 
     constexpr int NB = QT / 32;
-    typename Tile::Reader rd(lds_at(smem) + kg * QT / Tile::RPS * Tile::SEG, lane);
-    const uint32_t stat0 = lds_at(smem) + 2 * Tile::BYTES + (kg * QT + 4 * half) * 4;
+    typename Tile::Reader rd(lds0 + kg * QT / Tile::RPS * Tile::SEG, lane);
+    const uint32_t stat0 = lds0 + 2 * Tile::BYTES + (kg * QT + 4 * half) * 4;
     f32x16 sp[2], dpp[2];           // S and dP of this block and the next, in turn
     int stage = 0;                  // of the step at work
     // The statistics of the block at st: where S and dP start.
@@ -648,7 +664,7 @@ void attn_core_dkv_kernel(BwdArgs f) {
             if (x + 2 < s1) fetch(x + 2, 0);
         }
     };
-    auto take = [&](int x, auto edge) {
+    auto take = [&](int x, auto edge) __attribute__((always_inline)) {
         constexpr bool EDGE = decltype(edge)::value;
         const int iw = i_min + walk.step(work.y) * QROWS + kg * QT;
         next(work, x);
@@ -731,58 +747,78 @@ void attn_core_dkv_kernel(BwdArgs f) {
     for (; x < min(s1, edges); ++x) take(x, std::true_type{});
     for (; x < s1; ++x) take(x, std::false_type{});
     wait_vm<0>();      // no load is on its way to LDS any more
-    if constexpr (KG > 1) {
-        // dK, then dV: together they would not fit beside the stages
-        static_assert((KG - 1) * (NW / KG) * DB * 4096 <= S::LDS, "group results do not fit");
-        join_groups<KG, DB>(dk, smem, kg, wk, NW / KG, lane);
-        if (!join_groups<KG, DB>(dv, smem, kg, wk, NW / KG, lane)) return;
-    } else {
-        __syncthreads();
-    }
+    __syncthreads();
     // keys past the sequence's length get zeros (their lanes hold no sums of use). Partials:
     // the tile's KEYS rows of dK and dV of this (sequence, key head)
     const bool whole = splits == 1;
     const int64_t d4 = (a.d + 3) & ~3;
     const int64_t slot = (int64_t)(f.lev.slot[lev] + in_level) * a.batch * a.kv_heads + bh;
-    float *const put = reinterpret_cast<float *>(smem) + wk * (32 * 68);
-    const RowsOut out_k{whole ? a.dk.p : f.part, !whole || a.dk_f32, whole && a.dk_acc,
-                        !whole || f.vec_k};
-    const RowsOut out_v{whole ? a.dv.p : f.part + d4, !whole || a.dv_f32, whole && a.dv_acc,
-                        !whole || f.vec_v};
-    put_rows<DP>(put, dk, !live ? 0.f : whole ? a.scale : 1.f, out_k, a.d, lane, [&](int r) -> int64_t {
-        if (jw + r >= a.sk) return -1;
-        if (!whole) return (slot * KEYS + wk * 32 + r) * 2 * d4;
-        return (int64_t)b * a.dk.sb + (int64_t)hk * a.dk.sh + (int64_t)(jw + r) * a.dk.ld;
-    });
-    put_rows<DP>(put, dv, live ? 1.f : 0.f, out_v, a.d, lane, [&](int r) -> int64_t {
-        if (jw + r >= a.sk) return -1;
-        if (!whole) return (slot * KEYS + wk * 32 + r) * 2 * d4;
-        return (int64_t)b * a.dv.sb + (int64_t)hk * a.dv.sh + (int64_t)(jw + r) * a.dv.ld;
-    });
+    const RowsOut out_k{whole ? a.dk.p : f.part_kv, whole ? a.d : (int)d4, !whole || a.dk_f32,
+                        whole && a.dk_acc, !whole || f.vec_k};
+    const RowsOut out_v{whole ? a.dv.p : f.part_kv + d4, whole ? a.d : (int)d4,
+                        !whole || a.dv_f32, whole && a.dv_acc, !whole || f.vec_v};
+    int64_t off_k = -1, off_v = -1;
+    if (key < a.sk) {
+        off_k = off_v = (slot * KEYS + wk * 32 + (lane & 31)) * 2 * d4;
+        if (whole) {
+            off_k = (int64_t)b * a.dk.sb + (int64_t)hk * a.dk.sh + (int64_t)key * a.dk.ld;
+            off_v = (int64_t)b * a.dv.sb + (int64_t)hk * a.dv.sh + (int64_t)key * a.dv.ld;
+        }
+    }
+    constexpr int PUT = PUT_FLOATS<DP>;
+    float *const put = reinterpret_cast<float *>(smem);
+    stage_rows<DP>(put + wave * 2 * PUT, dk, !live ? 0.f : whole ? a.scale : 1.f, lane);
+    stage_rows<DP>(put + wave * 2 * PUT + PUT, dv, live ? 1.f : 0.f, lane);
+    __syncthreads();
+    store_rows<DP, KG>(put + wk * KG * 2 * PUT, 2 * PUT, kg, out_k, off_k, lane);
+    store_rows<DP, KG>(put + wk * KG * 2 * PUT + PUT, 2 * PUT, kg, out_v, off_v, lane);
 }
 
-// Adds the splits' partials in split order. A thread owns 4 columns of a row of dQ
-// (KV false) or of dK and dV (of the tiles that are split).
-template <bool KV>
-__global__ __launch_bounds__(256) void attn_core_sum_kernel(BwdArgs f) {
+// Keys of a tile of dK and dV and rows of a step of its walk, which two wave groups share;
+// KG groups share a step of dQ's.
+constexpr int DKV_KG = 2, DKV_KEYS = 128 / DKV_KG, DKV_ROWS = 64;
+template <int DP, int KG, bool DMA>
+struct BwdShape {
+    static constexpr int KT = 64 / KG;
+    using Dq = DqShape<DP, KG, KT, DMA>;
+    using Dkv = DkvShape<DP, DKV_KG, DKV_ROWS / DKV_KG, DMA>;
+    static constexpr int LDS = Dq::LDS > Dkv::LDS ? Dq::LDS : Dkv::LDS;
+    static constexpr int OCC = Dq::OCC;
+    static_assert(Dq::OCC == Dkv::OCC && Dkv::KEYS == DKV_KEYS && Dkv::QROWS == DKV_ROWS, "");
+};
+
+template <int DP, int KG, bool DMA>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(BwdShape<DP, KG, DMA>::OCC, BwdShape<DP, KG, DMA>::OCC)))
+void attn_core_bwd_kernel(BwdArgs f) {
+    using S = BwdShape<DP, KG, DMA>;
+    __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    const int wg = blockIdx.x;
+    if (wg < f.items_kv) attn_core_dkv<DP, DKV_KG, DKV_ROWS / DKV_KG, DMA>(f, wg, smem);
+    else attn_core_dq<DP, KG, S::KT, DMA>(f, wg - f.items_kv, smem);
+}
+
+// Adds the splits' partials in split order. A thread owns 4 columns of a row of dQ, or of
+// dK and dV (of the tiles that are split); the workgroups of dQ come first.
+__global__ __launch_bounds__(256) void attn_core_sum_kernel(BwdArgs f, int blocks_q) {
     const CoreArgs &a = f.a;
+    const bool kv = (int)blockIdx.x >= blocks_q;
     const int quads = (a.d + 3) >> 2;
-    const int64_t d4 = quads * 4, per = KV ? f.lev.split_keys : f.rows;
+    const int64_t d4 = quads * 4, per = kv ? f.lev.split_keys : f.rows;
     const int64_t bhs = (int64_t)a.batch * a.kv_heads, n = bhs * per;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+    const int64_t id = (int64_t)(blockIdx.x - (kv ? blocks_q : 0)) * 256 + threadIdx.x;
     if (id >= n * quads) return;
     const int64_t at = id / quads;
     const int col = (int)(id % quads) * 4;
     const int bh = (int)(at / per), row = (int)(at % per);
     const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
-    if constexpr (KV) {
-        const int tile = row / f.keys;
+    if (kv) {
+        const int tile = row / DKV_KEYS;
         int lev = 0;
         while (lev + 1 < f.lev.n && tile >= f.lev.tile[lev + 1]) ++lev;
         const int v = f.lev.v[lev];
         const int64_t slot = f.lev.slot[lev] + (int64_t)(tile - f.lev.tile[lev]) * v;
-        const float *p = f.part + ((slot * bhs + bh) * f.keys + row % f.keys) * 2 * d4 + col;
-        const int64_t step = bhs * f.keys * 2 * d4;
+        const float *p = f.part_kv + ((slot * bhs + bh) * DKV_KEYS + row % DKV_KEYS) * 2 * d4 + col;
+        const int64_t step = bhs * DKV_KEYS * 2 * d4;
         f32x4 x = {0.f, 0.f, 0.f, 0.f}, y = x;
         for (int s = 0; s < v; ++s, p += step) {
             x += *reinterpret_cast<const f32x4 *>(p);
@@ -795,7 +831,7 @@ __global__ __launch_bounds__(256) void attn_core_sum_kernel(BwdArgs f) {
     } else {
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         for (int s = 0; s < f.splits_q; ++s)
-            x += *reinterpret_cast<const f32x4 *>(f.part + ((int64_t)s * n + at) * d4 + col);
+            x += *reinterpret_cast<const f32x4 *>(f.part_q + ((int64_t)s * n + at) * d4 + col);
         const int i = row / a.group;
         const int64_t head = (int64_t)hk * a.group + (row - i * a.group);
         grad4(a.dq.p, (int64_t)b * a.dq.sb + head * a.dq.sh + (int64_t)i * a.dq.ld, col, a.d,
@@ -809,108 +845,132 @@ namespace sbpi {
 
 namespace {
 
-template <int DP, int KG, int KT>
-hipError_t launch_dq(const sbpk::BwdArgs &f, int64_t blocks, hipStream_t s) {
+template <int DP, int KG>
+hipError_t launch_bwd(const sbpk::BwdArgs &f, int64_t blocks, hipStream_t s) {
     char name[160];
     name[0] = 0;
     if (profiling())
-        snprintf(name, sizeof(name), "attn_core_dq_kernel<%d,%d,%d,%d>", DP, KG, KT,
-                 (int)f.a.aligned);
+        snprintf(name, sizeof(name), "attn_core_bwd_kernel<%d,%d,%d>", DP, KG, (int)f.a.aligned);
     if (f.a.aligned)
-        return launch_kernel(sbpk::attn_core_dq_kernel<DP, KG, KT, true>, name,
+        return launch_kernel(sbpk::attn_core_bwd_kernel<DP, KG, true>, name,
                              dim3((unsigned)blocks), dim3(256), s, f);
-    return launch_kernel(sbpk::attn_core_dq_kernel<DP, KG, KT, false>, name,
-                         dim3((unsigned)blocks), dim3(256), s, f);
+    return launch_kernel(sbpk::attn_core_bwd_kernel<DP, KG, false>, name, dim3((unsigned)blocks),
+                         dim3(256), s, f);
 }
 
-template <int DP, int KG, int QT>
-hipError_t launch_dkv(const sbpk::BwdArgs &f, int64_t blocks, hipStream_t s) {
-    char name[160];
-    name[0] = 0;
-    if (profiling())
-        snprintf(name, sizeof(name), "attn_core_dkv_kernel<%d,%d,%d,%d>", DP, KG, QT,
-                 (int)f.a.aligned);
-    if (f.a.aligned)
-        return launch_kernel(sbpk::attn_core_dkv_kernel<DP, KG, QT, true>, name,
-                             dim3((unsigned)blocks), dim3(256), s, f);
-    return launch_kernel(sbpk::attn_core_dkv_kernel<DP, KG, QT, false>, name,
-                         dim3((unsigned)blocks), dim3(256), s, f);
-}
-
-bool vec4(const CoreView &v, bool f32) {
-    return reinterpret_cast<uintptr_t>(v.p) % (f32 ? 16 : 8) == 0 && v.ld % 4 == 0 &&
-           v.sb % 4 == 0 && v.sh % 4 == 0;
+bool vec4(const CoreView &v, int d, bool f32) {
+    return d % 4 == 0 && reinterpret_cast<uintptr_t>(v.p) % (f32 ? 16 : 8) == 0 &&
+           v.ld % 4 == 0 && v.sb % 4 == 0 && v.sh % 4 == 0;
 }
 
 // Steps of key tile t's walk, every row and key in use.
-int64_t tile_steps(const CoreArgs &a, int64_t t, int keys, int rows) {
-    const int64_t off = (int64_t)a.sk - a.sq, j0 = t * keys;
+int64_t kv_steps(const CoreArgs &a, int64_t t) {
+    const int64_t off = (int64_t)a.sk - a.sq, j0 = t * sbpk::DKV_KEYS;
     int64_t n = a.sq;
-    if (a.causal && a.window) n = std::min<int64_t>(n, keys + a.window);
+    if (a.causal && a.window) n = std::min<int64_t>(n, sbpk::DKV_KEYS + a.window);
     else if (a.causal) n -= std::min<int64_t>(n, std::max<int64_t>(0, j0 - off));
-    return (n + rows - 1) / rows * a.group;
+    return (n + sbpk::DKV_ROWS - 1) / sbpk::DKV_ROWS * a.group;
 }
 
-// Wave groups (returned) and splits of the dK and dV launch: the pair that the following
-// time expects least of. A step of a workgroup takes `step` us, an item `fixed` besides;
-// the busiest unit has an even share of all items and half of the longest; partials are
-// written and read once, by a launch of their own.
-int plan_dkv(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs *f) {
-    const size_t d4 = (a.d + 3) & ~3;
+// One way to split a walk: its longest item and all items, in steps, and the partials.
+struct Way {
+    int64_t longest, items;
+    double steps, part;       // of one (sequence, key head): steps, floats of partials
+};
+
+// dK and dV with the longest walk in v parts: walks of more steps than those parts are split
+// too; they get no longer from tile to tile.
+Way split_kv(const CoreArgs &a, int64_t v, sbpk::Levels *lev) {
+    const int64_t tiles = ((int64_t)a.sk + sbpk::DKV_KEYS - 1) / sbpk::DKV_KEYS;
+    const int64_t target = std::max<int64_t>(1, (kv_steps(a, 0) + v - 1) / v);
+    *lev = sbpk::Levels{};
+    int64_t partials = 0, items = 0, at = 0;
+    double total = 0;
+    for (int64_t w = v; w >= 1 && at < tiles; --w) {
+        int64_t lo = at, hi = tiles;   // the end of the tiles of w parts or more
+        while (w > 1 && lo < hi) {
+            const int64_t mid = (lo + hi) / 2;
+            if (kv_steps(a, mid) > (w - 1) * target) lo = mid + 1;
+            else hi = mid;
+        }
+        if (w == 1) lo = tiles;
+        if (lo == at) continue;
+        const int j = lev->n++;
+        lev->tile[j] = (int32_t)at;
+        lev->v[j] = (int32_t)w;
+        lev->item[j] = (int32_t)items;
+        lev->slot[j] = (int32_t)partials;
+        items += (lo - at) * w;
+        if (w > 1) {
+            partials += (lo - at) * w;
+            lev->split_keys = (int32_t)std::min<int64_t>(a.sk, lo * sbpk::DKV_KEYS);
+        }
+        total += (lo - at) * 0.5 * (double)(kv_steps(a, at) + kv_steps(a, lo - 1));
+        at = lo;
+    }
+    lev->tile[lev->n] = (int32_t)tiles;
+    lev->items = (int32_t)items;
+    return Way{target, items, total, (double)partials * sbpk::DKV_KEYS * 2 * ((a.d + 3) & ~3)};
+}
+
+// dQ with tiles of `rows` rows, every walk in v parts.
+Way split_q(const CoreArgs &a, int64_t rows, int64_t v) {
+    const int64_t packed = (int64_t)a.sq * a.group, tiles = (packed + rows - 1) / rows;
+    const int64_t keys = a.causal && a.window ? std::min<int64_t>(a.sk, a.window + rows / a.group)
+                                              : a.sk;
+    const int64_t steps = (keys + 63) / 64;
+    // a causal walk is half as long on average where it starts at nothing
+    const double mean = a.causal && !a.window
+                            ? steps * (1.0 - 0.5 * std::min<double>(1.0, (double)a.sq / a.sk))
+                            : (double)steps;
+    return Way{(steps + v - 1) / v, tiles * v, mean * tiles,
+               v > 1 ? (double)packed * v * ((a.d + 3) & ~3) : 0.0};
+}
+
+// Wave groups of dQ (returned) and the splits: those that the following time expects least
+// of. An item takes so much a step, and `fixed` besides; the busiest unit has an even share
+// of all items and half of the longest; partials are written and read once, by one more
+// launch.
+int plan_bwd(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs *f) {
     const bool wide = a.d > 64;
     const double slots = cus * (wide ? 1.0 : 2.0), fixed = 4.0;
+    const double step_kv = wide ? 0.95 : 0.75, step_q = wide ? 0.75 : 0.6;
+    constexpr int MOST = sbpk::MAX_LEVELS;
+    sbpk::Levels lev[MOST];
+    Way kv[MOST];
+    int n = 0;
+    for (; n < MOST && (n == 0 || n < kv_steps(a, 0) / 2); ++n) kv[n] = split_kv(a, n + 1, &lev[n]);
     double best = 1e300;
-    int best_kg = 1;
+    int best_kg = 1, best_n = 0;     // whole walks need no room
+    f->splits_q = 1;
     for (int kg = 1; kg <= 2; ++kg) {
-        const int keys = 128 / kg, rows = 64;
-        const int64_t tiles = ((int64_t)a.sk + keys - 1) / keys;
-        const double step = (kg == 1 ? 2 : 1) * (wide ? 0.95 : 0.55);
-        const int64_t longest = tile_steps(a, 0, keys, rows);
-        for (int v = 1; v <= sbpk::MAX_LEVELS && v <= std::max<int64_t>(1, longest / 2); ++v) {
-            // walks of more than `target` steps are split; they get no longer from tile to
-            // tile
-            const int64_t target = std::max<int64_t>(1, (longest + v - 1) / v);
-            sbpk::Levels lev{};
-            int64_t partials = 0, items = 0, at = 0;
-            double total = 0;
-            for (int64_t w = v; w >= 1 && at < tiles; --w) {
-                int64_t lo = at, hi = tiles;   // the end of the tiles of w parts or more
-                while (lo < hi) {
-                    const int64_t mid = (lo + hi) / 2;
-                    if (w == 1 || tile_steps(a, mid, keys, rows) > (w - 1) * target) lo = mid + 1;
-                    else hi = mid;
+        for (int v = 1; v <= MOST; v *= 2) {
+            const Way q = split_q(a, 128 / kg, v);
+            if (v > 1 && q.longest < 2) break;
+            // 128 rows in one group take longer a step, by less than twice
+            const double sq = step_q * (kg == 1 ? 1.7 : 1.0);
+            for (int i = 0; i < n; ++i) {
+                const double part = (kv[i].part + q.part) * bhs;
+                if (part > 0 && (part > (double)room ||
+                                 (double)(kv[i].items + q.items) * bhs > 16777215.0))
+                    continue;
+                const double item = fixed + std::max(kv[i].longest * step_kv, q.longest * sq);
+                const double all = (kv[i].steps * step_kv + q.steps * sq +
+                                    (kv[i].items + q.items) * fixed) * bhs / slots;
+                const double t = std::max(item, all + 0.5 * item) +
+                                 (part > 0 ? 4.0 + part * 8 / 4e6 : 0.0);
+                if (t < best * 0.98) {
+                    best = t;
+                    best_kg = kg;
+                    best_n = i;
+                    f->splits_q = v;
                 }
-                if (lo == at) continue;
-                const int j = lev.n++;
-                lev.tile[j] = (int32_t)at;
-                lev.v[j] = (int32_t)w;
-                lev.item[j] = (int32_t)items;
-                lev.slot[j] = (int32_t)partials;
-                items += (lo - at) * w;
-                if (w > 1) {
-                    partials += (lo - at) * w;
-                    lev.split_keys = (int32_t)std::min<int64_t>(a.sk, lo * keys);
-                }
-                total += (lo - at) * 0.5 *
-                         (double)(tile_steps(a, at, keys, rows) + tile_steps(a, lo - 1, keys, rows));
-                at = lo;
-            }
-            lev.tile[lev.n] = (int32_t)tiles;
-            lev.items = (int32_t)items;
-            const double part = (double)partials * bhs * keys * 2 * d4;   // floats
-            if (part > (double)room || (double)items * bhs > 16777215.0) break;
-            const double item = target * step + fixed;
-            const double all = (total * step + items * fixed) * bhs / slots;
-            const double t = std::max(item, all + 0.5 * item) +
-                             (partials ? 4.0 + part * 8 / 4e6 : 0.0);
-            if (t < best * 0.98) {
-                best = t;
-                best_kg = kg;
-                f->lev = lev;
-                f->keys = keys;
             }
         }
     }
+    f->lev = lev[best_n];
+    f->items_kv = (int32_t)(bhs * f->lev.items);
+    f->tiles_q = (f->rows * best_kg + 127) / 128;
     return best_kg;
 }
 
@@ -920,60 +980,35 @@ hipError_t launch_core_bwd(const CoreArgs &a, hipStream_t s) {
     sbpk::BwdArgs f;
     f.a = a;
     f.rows = a.sq * a.group;
-    f.vec_q = vec4(a.dq, a.dq_f32);
-    f.vec_k = vec4(a.dk, a.dk_f32);
-    f.vec_v = vec4(a.dv, a.dv_f32);
+    f.vec_q = vec4(a.dq, a.d, a.dq_f32);
+    f.vec_k = vec4(a.dk, a.d, a.dk_f32);
+    f.vec_v = vec4(a.dv, a.d, a.dv_f32);
     const int64_t bhs = (int64_t)a.batch * a.kv_heads;
     const int64_t qrows = bhs * f.rows;
     const size_t stat = core_bwd_stat_floats(a);
     float *const nl = a.ws, *const nd = a.ws + stat / 2;
     f.nl = nl;
     f.nd = nd;
-    f.part = a.ws + stat;
-    const size_t room = a.ws_floats - stat;
-    const size_t d4 = (a.d + 3) & ~3;
-    const int cus = device_cus();
-    const bool wide = a.d > 64;
+    const int64_t d4 = (a.d + 3) & ~3;
     hipError_t e;
     if (qrows > 0) {
         e = launch_kernel(sbpk::attn_core_stat_kernel, "attn_core_stat_kernel",
                           dim3((unsigned)((qrows + 15) / 16)), dim3(256), s, a, nl, nd);
         if (e != hipSuccess) return e;
-
-        int kg = 1;
-        while (kg < 2 && ((f.rows + 128 / kg - 1) / (128 / kg)) * bhs < cus) kg *= 2;
-        const int rows = 128 / kg, keys = 64;
-        f.tiles_q = (f.rows + rows - 1) / rows;
-        const int64_t steps = ((int64_t)a.sk + keys - 1) / keys;
-        int64_t splits = 1;
-        while (f.tiles_q * bhs * splits * 2 <= 2 * cus && steps / (splits * 2) >= 2 &&
-               (size_t)qrows * d4 * splits * 2 <= room)
-            splits *= 2;
-        f.splits_q = (int)splits;
-        const int64_t blocks = f.tiles_q * bhs * splits;
-        if (kg == 1)
-            e = wide ? launch_dq<128, 1, 64>(f, blocks, s) : launch_dq<64, 1, 64>(f, blocks, s);
-        else
-            e = wide ? launch_dq<128, 2, 32>(f, blocks, s) : launch_dq<64, 2, 32>(f, blocks, s);
-        if (e != hipSuccess) return e;
-        if (splits > 1) {
-            const int64_t items = qrows * (int64_t)(d4 / 4);
-            e = launch_kernel(sbpk::attn_core_sum_kernel<false>, "attn_core_sum_kernel<0>",
-                              dim3((unsigned)((items + 255) / 256)), dim3(256), s, f);
-            if (e != hipSuccess) return e;
-        }
     }
-    if (bhs * a.sk == 0) return hipSuccess;
-    const int kg = plan_dkv(a, bhs, cus, room, &f);
-    const int64_t blocks = bhs * f.lev.items;
-    if (kg == 1)
-        e = wide ? launch_dkv<128, 1, 64>(f, blocks, s) : launch_dkv<64, 1, 64>(f, blocks, s);
-    else
-        e = wide ? launch_dkv<128, 2, 32>(f, blocks, s) : launch_dkv<64, 2, 32>(f, blocks, s);
-    if (e != hipSuccess || f.lev.split_keys == 0) return e;
-    const int64_t items = bhs * f.lev.split_keys * (int64_t)(d4 / 4);
-    return launch_kernel(sbpk::attn_core_sum_kernel<true>, "attn_core_sum_kernel<1>",
-                         dim3((unsigned)((items + 255) / 256)), dim3(256), s, f);
+    const int kg = plan_bwd(a, bhs, device_cus(), a.ws_floats - stat, &f);
+    f.part_q = a.ws + stat;
+    f.part_kv = f.part_q + (f.splits_q > 1 ? qrows * f.splits_q * d4 : 0);
+    const int64_t blocks = f.items_kv + bhs * f.tiles_q * f.splits_q;
+    if (blocks == 0) return hipSuccess;
+    if (kg == 1) e = a.d > 64 ? launch_bwd<128, 1>(f, blocks, s) : launch_bwd<64, 1>(f, blocks, s);
+    else e = a.d > 64 ? launch_bwd<128, 2>(f, blocks, s) : launch_bwd<64, 2>(f, blocks, s);
+    if (e != hipSuccess) return e;
+    const int64_t sum_q = f.splits_q > 1 ? (qrows * (d4 / 4) + 255) / 256 : 0;
+    const int64_t sum_kv = (bhs * f.lev.split_keys * (d4 / 4) + 255) / 256;
+    if (sum_q + sum_kv == 0) return hipSuccess;
+    return launch_kernel(sbpk::attn_core_sum_kernel, "attn_core_sum_kernel",
+                         dim3((unsigned)(sum_q + sum_kv)), dim3(256), s, f, (int)sum_q);
 }
 
 }  // namespace sbpi

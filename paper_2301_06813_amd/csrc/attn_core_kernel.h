@@ -16,11 +16,26 @@
 
 namespace sbpk {
 
+typedef __bf16 bf16x4 __attribute__((ext_vector_type(4)));
+
 using sbpi::CoreArgs;
 using sbpi::CoreView;
 
 constexpr float LOG2E = 1.4426950408889634f;
 constexpr float LN2 = 0.6931471805599453f;
+
+__device__ __forceinline__ uint32_t lds_at(const void *p) {
+    return (uint32_t)(uintptr_t)(SBP_LDS const void *)p;
+}
+
+// dma16 to byte `lds` of LDS (uniform).
+__device__ __forceinline__ void dma16_at(i32x4 r, uint32_t lds, int voff) {
+    const uint32_t m0 = __builtin_amdgcn_readfirstlane(lds);
+    asm volatile("s_mov_b32 m0, %0\n\tbuffer_load_dwordx4 %1, %2, 0 offen lds"
+                 :
+                 : "s"(m0), "v"(voff), "s"(r)
+                 : "memory", "m0");
+}
 
 // A tile of ROWS rows of DP bf16 values in LDS. A direct-to-LDS load of a wave fills 1 KB,
 // RPS whole rows in 16-byte chunks; these segments lie 1040 bytes apart, and within one
@@ -57,21 +72,11 @@ struct RowTile {
         const int b = lane / CPR, c = (lane % CPR) ^ swz(b);
         return c * 8 < d ? ((wave * RPS + b) * (int)ld + c * 8) * 2 : OOB;
     }
-    // Rows [0, n) at `base` (uniform), n > 0, go to LDS; rows past n and columns past d lie
-    // outside the buffer and arrive as zeros.
-    __device__ __forceinline__ static void issue(const uint16_t *base, int64_t ld, int n, int place,
-                                                 char *lds, int wave) {
-        i32x4 r = make_rsrc(base);
-        r[2] = __builtin_amdgcn_readfirstlane(n * (int)ld * 2);
-#pragma unroll
-        for (int i = 0; i < NV; ++i)
-            dma16(r, lds + (i * NW + wave) * SEG, place + i * (NW * RPS * (int)ld * 2));
-    }
-
-    // One of the NV loads of issue(), of buffer `r`.
-    __device__ __forceinline__ static void issue_part(i32x4 r, int64_t ld, int place, char *lds,
-                                                      int wave, int i) {
-        dma16(r, lds + (i * NW + wave) * SEG, place + i * (NW * RPS * (int)ld * 2));
+    // Load i of the NV that bring the rows of buffer `r` to byte `lds` of LDS. Rows past the
+    // buffer's end and columns past d lie outside it and arrive as zeros.
+    __device__ __forceinline__ static void issue(i32x4 r, int64_t ld, int place, uint32_t lds,
+                                                 int wave, int i) {
+        dma16_at(r, lds + (i * NW + wave) * SEG, place + i * (NW * RPS * (int)ld * 2));
     }
 
     // The same through registers, for rows at any element alignment and stride.
@@ -138,10 +143,6 @@ struct RowTile {
         }
     };
 };
-
-__device__ __forceinline__ uint32_t lds_at(const void *p) {
-    return (uint32_t)(uintptr_t)(SBP_LDS const void *)p;
-}
 
 // 8 columns of a row in memory (columns past d as zeros): ALIGNED rows have 16-byte
 // blocks that lie wholly before or past d; others are read at any alignment.
@@ -210,100 +211,101 @@ struct SeqMask {
     }
 };
 
-// Hands the sums of wave groups 1 .. KG - 1 to group 0 through LDS, lane by lane, in group
-// order; called by the whole workgroup, whose LDS is free before and after. Returns whether
-// this wave is of group 0. `unit` counts the waves of a group. LDS: (KG - 1) * units * N * 4 KB.
-template <int KG, int N>
-__device__ __forceinline__ bool join_groups(f32x16 *acc, char *smem, int kg, int unit, int units,
-                                            int lane) {
-    f32x4 *const base = reinterpret_cast<f32x4 *>(smem) + lane;
-    __syncthreads();
-    if (kg > 0) {
-        f32x4 *p = base + ((kg - 1) * units + unit) * (N * 4 * 64);
-#pragma unroll
-        for (int i = 0; i < N * 4; ++i)
-            p[i * 64] = f32x4{acc[i / 4][i % 4 * 4], acc[i / 4][i % 4 * 4 + 1],
-                              acc[i / 4][i % 4 * 4 + 2], acc[i / 4][i % 4 * 4 + 3]};
-    }
-    __syncthreads();
-    for (int k = 1; kg == 0 && k < KG; ++k) {
-        const f32x4 *p = base + ((k - 1) * units + unit) * (N * 4 * 64);
-#pragma unroll
-        for (int i = 0; i < N * 4; ++i) {
-            const f32x4 v = p[i * 64];
-#pragma unroll
-            for (int e = 0; e < 4; ++e) acc[i / 4][i % 4 * 4 + e] += v[e];
-        }
-    }
-    __syncthreads();
-    return kg == 0;
-}
-
-// Where 32 result rows of a wave go: bf16 or fp32, overwritten or added to; `vec`: rows
-// allow stores of 4 values.
+// Where result rows go: bf16 or fp32, overwritten or added to; `vec`: d is a multiple of 4
+// and the rows allow loads and stores of 4 values.
 struct RowsOut {
     void *p;
+    int32_t d;
     bool f32, add, vec;
 };
 
-// Stores a wave's result (lane l holds column l % 32, here a row of the output, and in
-// acc[db] register q value 32 db + 8 (q / 4) + 4 (l / 32) + q % 4 of it), times `mul` (0 where
-// it is 0), through `tile`, 32 x 68 floats of LDS of its own, 64 columns at a time: 16 lanes
-// then store a row's 64 values side by side. The loop is not unrolled: straight-line
-// stores of every type made the kernels' code several times longer than their loops, and
-// short launches waited for it. at(r): element offset of row r, or < 0 for none.
-template <int DP, class At>
-__device__ __forceinline__ void put_rows(float *tile, const f32x16 *acc, float mul, const RowsOut &o,
-                                         int d, int lane, At at) {
-    const int half = lane >> 5;
+// Results leave through LDS, so that 16 lanes store a row's 64 values side by side and the
+// wave groups of a row are summed on the way (in group order), each group storing a part
+// of the rows. A wave's tile is 32 x DP floats in parts of 32 x 68.
+template <int DP>
+constexpr int PUT_FLOATS = DP / 64 * 32 * 68;
+
+// A wave's result (lane l holds column l % 32, here a row of the output, and in acc[db]
+// register q value 32 db + 8 (q / 4) + 4 (l / 32) + q % 4 of it), times `mul` (0 where that is
+// 0), to its tile.
+template <int DP>
+__device__ __forceinline__ void stage_rows(float *tile, const f32x16 *acc, float mul, int lane) {
+    float *const row = tile + (lane & 31) * 68 + 4 * (lane >> 5);
 #pragma unroll
-    for (int c0 = 0; c0 < DP; c0 += 64) {
+    for (int db = 0; db < DP / 32; ++db)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            const f32x16 &a = acc[c0 / 32 + i / 4];
-            const int q = i % 4 * 4;
+        for (int q = 0; q < 16; q += 4) {
             f32x4 v;
 #pragma unroll
-            for (int e = 0; e < 4; ++e) v[e] = mul != 0.f ? a[q + e] * mul : 0.f;
-            *reinterpret_cast<f32x4 *>(tile + (lane & 31) * 68 + i / 4 * 32 + 2 * q + 4 * half) = v;
+            for (int e = 0; e < 4; ++e) v[e] = mul != 0.f ? acc[db][q + e] * mul : 0.f;
+            *reinterpret_cast<f32x4 *>(row + db / 2 * (32 * 68) + db % 2 * 32 + 2 * q) = v;
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
-        const int left = d - c0 - (lane & 15) * 4;   // values of the row from this lane's first
-#pragma unroll 1
-        for (int it = 0; it < 8; ++it) {
-            const int r = it * 4 + (lane >> 4);
-            const f32x4 v = *reinterpret_cast<const f32x4 *>(tile + r * 68 + (lane & 15) * 4);
-            const int64_t off = at(r);
-            if (off < 0 || left <= 0) continue;
-            const int64_t e0 = off + c0 + (lane & 15) * 4;
-            if (o.f32) {
-                float *p = static_cast<float *>(o.p) + e0;
-                if (o.vec && left >= 4) {
-                    f32x4 w = v;
-                    if (o.add) w += *reinterpret_cast<const f32x4 *>(p);
-                    *reinterpret_cast<f32x4 *>(p) = w;
-                } else {
+}
+
+// Stores the rows of KG groups' tiles, `step` floats apart: group kg the kg-th part of the
+// rows. off: element offset of row (lane % 32), or < 0 for none.
+template <int DP, int KG>
+__device__ __forceinline__ void store_rows(const float *tiles, int step, int kg, const RowsOut &o,
+                                           int64_t off, int lane) {
+    constexpr int N = 8 / KG;
+    const int r0 = kg * (32 / KG) + (lane >> 4);
+    const int lo = (int)off, hi = (int)(off >> 32);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < left) p[e] = o.add ? p[e] + v[e] : v[e];
+    for (int c0 = 0; c0 < DP; c0 += 64) {
+        const float *const t = tiles + c0 / 64 * (32 * 68) + r0 * 68 + (lane & 15) * 4;
+        const int col = c0 + (lane & 15) * 4;
+        auto value = [&](int it) {
+            f32x4 v = *reinterpret_cast<const f32x4 *>(t + it * (4 * 68));
+#pragma unroll
+            for (int k = 1; k < KG; ++k)
+                v += *reinterpret_cast<const f32x4 *>(t + k * step + it * (4 * 68));
+            return v;
+        };
+        auto place = [&](int it) {
+            const int from = 4 * (r0 + 4 * it);
+            const int h = __builtin_amdgcn_ds_bpermute(from, hi);
+            return (int64_t)(((uint64_t)(uint32_t)h << 32) |
+                             (uint32_t)__builtin_amdgcn_ds_bpermute(from, lo));
+        };
+        if (o.vec && !o.f32) {
+#pragma unroll
+            for (int it = 0; it < N; ++it) {
+                const f32x4 v = value(it);
+                const int64_t at = place(it);
+                bf16x4 w;
+#pragma unroll
+                for (int e = 0; e < 4; ++e) w[e] = (__bf16)v[e];
+                if (at >= 0 && col < o.d)
+                    *reinterpret_cast<bf16x4 *>(static_cast<uint16_t *>(o.p) + at + col) = w;
+            }
+        } else if (o.vec) {
+#pragma unroll
+            for (int it = 0; it < N; ++it) {
+                f32x4 v = value(it);
+                const int64_t at = place(it);
+                if (at >= 0 && col < o.d) {
+                    f32x4 *const p = reinterpret_cast<f32x4 *>(static_cast<float *>(o.p) + at + col);
+                    if (o.add) v += *p;
+                    *p = v;
                 }
-            } else {
-                uint16_t *p = static_cast<uint16_t *>(o.p) + e0;
-                if (o.vec && left >= 4) {
-                    u32x2 w;
-                    w[0] = (uint32_t)f32_to_bf16_bits(v[0]) | (uint32_t)f32_to_bf16_bits(v[1]) << 16;
-                    w[1] = (uint32_t)f32_to_bf16_bits(v[2]) | (uint32_t)f32_to_bf16_bits(v[3]) << 16;
-                    *reinterpret_cast<u32x2 *>(p) = w;
-                } else {
+            }
+        } else {
+#pragma unroll 1
+            for (int it = 0; it < N; ++it) {
+                const f32x4 v = value(it);
+                const int64_t at = place(it);
 #pragma unroll
-                    for (int e = 0; e < 4; ++e)
-                        if (e < left) p[e] = f32_to_bf16_bits(v[e]);
+                for (int e = 0; e < 4; ++e) {
+                    if (at < 0 || col + e >= o.d) continue;
+                    if (o.f32) {
+                        float *const p = static_cast<float *>(o.p) + at + col + e;
+                        *p = o.add ? *p + v[e] : v[e];
+                    } else {
+                        static_cast<uint16_t *>(o.p)[at + col + e] = f32_to_bf16_bits(v[e]);
+                    }
                 }
             }
         }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-        __builtin_amdgcn_wave_barrier();
     }
 }
 

@@ -160,17 +160,6 @@ __device__ __forceinline__ void block_scores(f32x16 &s, f32x16 &dp, const Reader
     }
 }
 
-// Part i of 0 .. PARTS - 1 of a block's 16 values holds value r.
-__device__ __forceinline__ constexpr bool in_part(int r, int i, int parts) {
-    return r >= 16 * i / parts && r < 16 * (i + 1) / parts;
-}
-
-// A direct-to-LDS load to come: two tiles.
-struct Fetch {
-    i32x4 x, y;
-    uint32_t lds;
-};
-
 template <int DP, int KG, int KT, bool DMA>
 struct DqShape {
     static constexpr int NW = 4;
@@ -249,7 +238,7 @@ __device__ __forceinline__ void attn_core_dq(const BwdArgs &f, int wg, char *sme
     typename Tile::Regs rk, rv;
     Fetch to{};
     // steps past the walk's bring nothing (zeros, to a stage that is not read)
-    auto fetch = [&](int x, int stage) {
+    auto fetch = [&](int x, int stage) __attribute__((always_inline)) {
         const int k0 = k_beg + walk.step(x) * KEYS;
         const int n = x < s1 ? min(KEYS, mask.lk - k0) : 0;
         if constexpr (DMA) {
@@ -317,7 +306,7 @@ __device__ __forceinline__ void attn_core_dq(const BwdArgs &f, int wg, char *sme
     f32x16 sp[2], dpp[2];           // S and dP of this block and the next, in turn
     int stage = 0;                  // of the step at work
     // Waits for the step after x, and prepares the load of a later one.
-    auto advance = [&](int x) {
+    auto advance = [&](int x) __attribute__((always_inline)) {
         if constexpr (DMA) {
             wait_vm<(NS - 3) * S::LOADS>();
             __syncthreads();
@@ -548,7 +537,7 @@ __device__ __forceinline__ void attn_core_dkv(const BwdArgs &f, int wg, char *sm
         at_s = (wave < W ? f.nl : f.nd) + ((int64_t)b * a.kv_heads * a.group + h) * a.sq + i0;
     };
     seek();
-    auto fetch = [&](int x, int stage) {
+    auto fetch = [&](int x, int stage) __attribute__((always_inline)) {
         const int n = x < s1 ? min(QROWS, mask.lq - i0) : 0;
         if constexpr (DMA) {
             to.x = make_rsrc(at_q);
@@ -653,7 +642,7 @@ __device__ __forceinline__ void attn_core_dkv(const BwdArgs &f, int wg, char *sm
         }
     };
     // Waits for the step after x, and prepares the load of a later one.
-    auto advance = [&](int x) {
+    auto advance = [&](int x) __attribute__((always_inline)) {
         if constexpr (DMA) {
             wait_vm<(NS - 3) * S::LOADS>();
             __syncthreads();

@@ -3,7 +3,7 @@
 // Per sequence and key head, the rows of a group of query heads that share it
 // are packed as row = i * group + g (query i, head g), so K and V are read once
 // for the group and a few query rows fill a tile. A workgroup owns a tile of rows
-// and walks over the keys that any of them sees, 32 KG .. 64 KG at a time: scores
+// and walks over the keys that any of them sees, 64 or 128 at a time: scores
 // as S^T = K Q^T, running maximum m and sum l of each row, O^T += V^T P^T. In these
 // orientations a lane holds one query's scores (half of them, the other half-wave
 // the rest), so m and l are one register each, the rows' scaling needs no
@@ -16,11 +16,17 @@
 //     is skipped by the whole wave.
 //   * P is rounded to bf16 for the second product (the matrix cores' type, rounded
 //     like the framework's other bf16 operands); the row sum adds the fp32 values.
+//   * The next block's scores are computed beside this block's exponentials, and its
+//     maximum beside this block's product with V (written one after the other,
+//     16 heads over 4 of 8192 x 128, causal, took 314 us; so 275, 1.0 PFLOP/s, the
+//     matrix cores busy half of the time at two waves per SIMD).
 //   * With KG wave groups, group k takes the k-th part of every step's keys; their
 //     (m, l, O) are joined through LDS at the end. Few rows and many keys are also
 //     split over workgroups, whose normalised partial outputs and row statistics
 //     go through the workspace.
 #include <math.h>
+
+#include <algorithm>
 
 #include "attn_core_kernel.h"
 #include "gemm.h"
@@ -63,28 +69,44 @@ struct FwdArgs {
     int32_t vec;                     // O allows 4-value stores
 };
 
-template <int DP, int KG, int KT>
+// WPS: waves of a SIMD, of one workgroup or two.
+template <int DP, int KG, int KT, int NW_, int WPS_, bool DMA>
 struct FwdShape {
-    static constexpr int NW = 4;
-    static constexpr int ROWS = 32 * NW / KG;
-    using Tile = RowTile<DP, KG * KT, NW>;
+    static constexpr int NW = NW_, WPS = WPS_;
+    static constexpr int ROWS = 32 * NW / KG, KEYS = KG * KT;
+    using Tile = RowTile<DP, KEYS, NW>;
     static constexpr int STAGE = 2 * Tile::BYTES;    // K, then V
-    static constexpr int LDS = 2 * STAGE;
-    static constexpr int OCC = LDS > 81920 ? 1 : 2;
+    static constexpr int LOADS = 2 * Tile::NV;
+    static constexpr int ROOM = 163840 / (4 * WPS / NW);
+    static constexpr int FIT = ROOM / STAGE;
+    static constexpr int NS = !DMA ? 3 : FIT > 4 ? 4 : FIT;
+    static constexpr int PUT = NW * PUT_FLOATS<DP> * 4;
+    static constexpr int STATS = NW * 64 * 2 * 4;
+    static constexpr int LDS = NS * STAGE > PUT + STATS ? NS * STAGE : PUT + STATS;
+    static_assert(FIT >= NS && NS >= 3 && LDS <= ROOM, "three stages");
 };
 
-template <int DP, int KG, int KT, bool DMA>
-__global__ __launch_bounds__(256, (FwdShape<DP, KG, KT>::OCC))
+template <int DP, int KG, int KT, int NW, int WPS, bool DMA>
+__global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(WPS, WPS)))
 void attn_core_fwd_kernel(FwdArgs f) {
-    using S = FwdShape<DP, KG, KT>;
+    using S = FwdShape<DP, KG, KT, NW, WPS, DMA>;
     using Tile = typename S::Tile;
-    constexpr int NW = S::NW, ROWS = S::ROWS, KB = KT / 32, KS = DP / 16, DB = DP / 32;
+    constexpr int ROWS = S::ROWS, NS = S::NS, KEYS = S::KEYS;
+    constexpr int NB = KT / 32, KS = DP / 16, DB = DP / 32;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
+    const uint32_t lds0 = lds_at(smem);
     const CoreArgs &a = f.a;
     const int tid = threadIdx.x, lane = tid & 63, half = lane >> 5;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);   // uniform, so that what
                                                                  // depends on it is scalar
     const int kg = wave % KG, wr = wave / KG;
+    // the arguments, read at once: the compiler loads each where it is first used, and each
+    // first load is a trip to memory
+    asm volatile("" ::"s"(a.q.p), "s"(a.q.sb), "s"(a.q.sh), "s"(a.q.ld), "s"(a.k.p), "s"(a.k.sb),
+                 "s"(a.k.sh), "s"(a.k.ld), "s"(a.v.p), "s"(a.v.sb), "s"(a.v.sh), "s"(a.v.ld),
+                 "s"(a.o.p), "s"(a.lse.p), "s"(a.len_q), "s"(a.len_k), "s"(a.batch),
+                 "s"(a.kv_heads), "s"(a.group), "s"(a.sq), "s"(a.sk), "s"(a.d), "s"(a.causal),
+                 "s"(a.window), "s"(a.scale), "s"(a.ws), "s"(f.tiles), "s"(f.splits), "s"(f.rows));
 
     // heavier (later) causal tiles first within a (sequence, head)
     const int per = f.tiles * f.splits;
@@ -103,42 +125,48 @@ void attn_core_fwd_kernel(FwdArgs f) {
 
     // the keys that the tile's rows see, and this split's steps of them
     const int i_first = row0 / a.group;
-    const int i_last = min(min(row0 + ROWS, f.rows) - 1, f.rows - 1) / a.group;
+    const int i_last = (min(row0 + ROWS, f.rows) - 1) / a.group;
     const int k_beg = mask.lo(i_first) & ~31;
     const int k_end = i_first < mask.lq ? mask.hi(min(i_last, mask.lq - 1)) : 0;
-    const int steps = k_end > k_beg ? (k_end - k_beg + KG * KT - 1) / (KG * KT) : 0;
+    const int steps = k_end > k_beg ? (k_end - k_beg + KEYS - 1) / KEYS : 0;
     // steps whose keys every row of the tile sees (rows past the sequence's end aside)
     Walk walk{steps, 0, steps};
     if (steps > 0) {
         const int all = min(mask.hi(i_first), mask.lk);
-        walk.nb = all > k_beg ? min(steps, (all - k_beg) / (KG * KT)) : 0;
-        walk.na = min(walk.nb, (mask.lo(i_last) - k_beg + KG * KT - 1) / (KG * KT));
-        walk.na = max(walk.na, 0);
+        walk.nb = all > k_beg ? min(steps, (all - k_beg) / KEYS) : 0;
+        walk.na = max(0, min(walk.nb, (mask.lo(i_last) - k_beg + KEYS - 1) / KEYS));
     }
     const int per_split = (steps + f.splits - 1) / f.splits;
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
     const int hi = mask.hi(i), lo = mask.lo(i);
 
-    const uint16_t *Q = static_cast<const uint16_t *>(a.q.p) + (int64_t)b * a.q.sb +
-                        head * a.q.sh + (int64_t)i * a.q.ld;
     const uint16_t *K = static_cast<const uint16_t *>(a.k.p) + (int64_t)b * a.k.sb +
                         (int64_t)hk * a.k.sh;
     const uint16_t *V = static_cast<const uint16_t *>(a.v.p) + (int64_t)b * a.v.sb +
                         (int64_t)hk * a.v.sh;
-
     const int place_k = Tile::place(a.k.ld, a.d, wave, lane);
     const int place_v = Tile::place(a.v.ld, a.d, wave, lane);
     typename Tile::Regs rk, rv;
-    auto issue = [&](int x, int stage) {
-        const int k0 = k_beg + walk.step(x) * (KG * KT);
-        const int n = min(KG * KT, mask.lk - k0);
-        char *lds = smem + stage * S::STAGE;
+    Fetch to{};
+    // steps past the walk's bring nothing (zeros, to a stage that is not read)
+    auto fetch = [&](int x, int stage) __attribute__((always_inline)) {
+        const int k0 = k_beg + walk.step(x) * KEYS;
+        const int n = x < s1 ? min(KEYS, mask.lk - k0) : 0;
         if constexpr (DMA) {
-            Tile::issue(K + (int64_t)k0 * a.k.ld, a.k.ld, n, place_k, lds, wave);
-            Tile::issue(V + (int64_t)k0 * a.v.ld, a.v.ld, n, place_v, lds + Tile::BYTES, wave);
+            to.x = make_rsrc(K + (int64_t)k0 * a.k.ld);
+            to.y = make_rsrc(V + (int64_t)k0 * a.v.ld);
+            to.x[2] = __builtin_amdgcn_readfirstlane(n * (int)a.k.ld * 2);
+            to.y[2] = __builtin_amdgcn_readfirstlane(n * (int)a.v.ld * 2);
+            to.lds = lds0 + stage * S::STAGE;
         } else {
             Tile::load(rk, K + (int64_t)k0 * a.k.ld, a.k.ld, n, a.d, tid);
             Tile::load(rv, V + (int64_t)k0 * a.v.ld, a.v.ld, n, a.d, tid);
+        }
+    };
+    auto fetch_part = [&](int p) {
+        if constexpr (DMA) {
+            if (p < Tile::NV) Tile::issue(to.x, a.k.ld, place_k, to.lds, wave, p);
+            else Tile::issue(to.y, a.v.ld, place_v, to.lds + Tile::BYTES, wave, p - Tile::NV);
         }
     };
     auto arrive = [&](int stage) {   // register-staged: the loaded step goes to LDS
@@ -148,13 +176,24 @@ void attn_core_fwd_kernel(FwdArgs f) {
             Tile::store(rv, lds + Tile::BYTES, tid);
         }
     };
-
-    if (s0 < s1) {
-        issue(s0, 0);
+    if constexpr (DMA) {
+#pragma unroll
+        for (int x = 0; x < NS - 1; ++x) {
+            fetch(s0 + x, x);
+#pragma unroll
+            for (int p = 0; p < S::LOADS; ++p) fetch_part(p);
+        }
+        fetch(s1, NS - 1);   // nothing, for the parts before the first advance
+    } else if (s0 < s1) {
+        fetch(s0, 0);
         arrive(0);
+        if (s0 + 1 < s1) fetch(s0 + 1, 1);
     }
+
     // rows past a sequence's queries read nothing
     const bool live = valid && i < mask.lq;
+    const uint16_t *Q = static_cast<const uint16_t *>(a.q.p) + (int64_t)b * a.q.sb +
+                        head * a.q.sh + (int64_t)i * a.q.ld;
     bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
@@ -168,31 +207,35 @@ void attn_core_fwd_kernel(FwdArgs f) {
 #pragma unroll
     for (int x = 0; x < DB; ++x) o[x] = splat16(0.f);
 
-    typename Tile::Reader rd(lds_at(smem) + kg * KT / Tile::RPS * Tile::SEG, lane);
-    auto step = [&](int kw, auto edge) {
-        f32x16 s[KB];
+    // Two phases a block of 32 keys: the next block's scores beside this one's exponentials;
+    // then this block's product with V beside the next one's maximum.
+    typename Tile::Reader rd(lds0 + kg * KT / Tile::RPS * Tile::SEG, lane);
+    f32x16 sp[2];                   // scores of this block and the next, in turn
+    int stage = 0;                  // of the step at work
+    auto scores = [&](f32x16 &s, const typename Tile::Reader &r, int r0, auto beside)
+                      __attribute__((always_inline)) {
+        // operands are read AHEAD products early
+        constexpr int AHEAD = KS < 4 ? KS : 4;
+        bf16x8 k[KS];
+        s = splat16(0.f);
 #pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-            s[kb] = splat16(0.f);
+        for (int ks = 0; ks < AHEAD; ++ks) k[ks] = r.frag(r0, ks, 0);
+        beside(0);
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-                s[kb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                    rd.frag(kb * 32, ks, 0), qf[ks], s[kb], 0, 0, 0);
+        for (int ks = 0; ks < KS; ++ks) {
+            if (ks + AHEAD < KS) k[ks + AHEAD] = r.frag(r0, ks + AHEAD, 0);
+            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[ks], qf[ks], s, 0, 0, 0);
+            beside(ks + 1);
+            __builtin_amdgcn_sched_barrier(0);
         }
-        if constexpr (decltype(edge)::value) {
-#pragma unroll
-            for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    const int key = kw + kb * 32 + 8 * (r >> 2) + 4 * half + (r & 3);
-                    s[kb][r] = key >= lo && key < hi ? s[kb][r] : -INFINITY;
-                }
-        }
-        float top = s[0][0];
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb)
-#pragma unroll
-            for (int r = 0; r < 16; ++r) top = fmaxf(top, s[kb][r]);
+    };
+    auto hide = [&](f32x16 &s, int k0, int r) {   // what this row does not see
+        const int key = k0 + 8 * (r >> 2) + 4 * half + (r & 3);
+        s[r] = key >= lo && key < hi ? s[r] : -INFINITY;
+    };
+    // Moves the maximum to `top`, a lane's own scores' maximum, where it grew by enough.
+    auto rise = [&](float top) __attribute__((always_inline)) {
         float t0, t1;
         halves(top, &t0, &t1);
         top = fmaxf(t0, t1);
@@ -206,111 +249,142 @@ void attn_core_fwd_kernel(FwdArgs f) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[db][r] *= x;
         }
-        const float mc = m == -INFINITY ? 0.f : m * c;
-#pragma unroll
-        for (int kb = 0; kb < KB; ++kb) {
-#pragma unroll
-            for (int r = 0; r < 16; ++r) {
-                s[kb][r] = exp2_(__builtin_fmaf(s[kb][r], c, -mc));
-                l += s[kb][r];
-            }
-#pragma unroll
-            for (int x = 0; x < 2; ++x) {
-                const bf16x8 p = pack8(s[kb], 8 * x);
-#pragma unroll
-                for (int db = 0; db < DB; ++db)
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                        rd.frag_t(db, kb * 32 + 16 * x, Tile::BYTES), p, o[db], 0, 0, 0);
-            }
+    };
+    // Waits for the step after x, and prepares the load of a later one.
+    auto advance = [&](int x) __attribute__((always_inline)) {
+        if constexpr (DMA) {
+            wait_vm<(NS - 3) * S::LOADS>();
+            __syncthreads();
+            fetch(x + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+        } else {
+            if (x + 1 < s1) arrive(stage == NS - 1 ? 0 : stage + 1);
+            __syncthreads();
+            if (x + 2 < s1) fetch(x + 2, 0);
         }
     };
-    auto take = [&](int x, auto edge) {
-        const int stage = (x - s0) & 1;
-        wait_vm<0>();
-        __syncthreads();
-        if (x + 1 < s1) issue(x + 1, stage ^ 1);
-        step(k_beg + walk.step(x) * (KG * KT) + kg * KT, edge);
-        rd.move(stage ? -S::STAGE : S::STAGE);
-        if (x + 1 < s1) arrive(stage ^ 1);
+    // EDGE: some row of the tile does not see every key of the step
+    auto take = [&](int x, auto edge) __attribute__((always_inline)) {
+        constexpr bool EDGE = decltype(edge)::value;
+        const int kw = k_beg + walk.step(x) * KEYS + kg * KT;
+        const int kn = k_beg + walk.step(x + 1) * KEYS + kg * KT;
+        const bool wrap = stage == NS - 1;
+        const int by = wrap ? -(NS - 1) * S::STAGE : S::STAGE;
+#pragma unroll
+        for (int kb = 0; kb < NB; ++kb) {
+            const bool last = kb == NB - 1;
+            if (last) advance(x);
+            typename Tile::Reader nx = rd;       // where the next block lies
+            if (last) nx.move(by);
+            // with an even number of blocks a step the two take turns in place
+            constexpr bool TURN = NB % 2 == 0;
+            constexpr int ONE = 1;
+            const int now = TURN ? kb & 1 : 0;
+            f32x16 &s = sp[now], &s_n = sp[ONE - now];
+            bf16x8 tv[2][DB], p[2];
+            const float mc = m == -INFINITY ? 0.f : -m * c;
+            __builtin_amdgcn_sched_barrier(0);
+            scores(s_n, nx, last ? 0 : (kb + 1) * 32, [&](int part) __attribute__((always_inline)) {
+#pragma unroll
+                for (int r = 0; r < 16; ++r) {
+                    if (!in_part(r, part, KS + 1)) continue;
+                    s[r] = exp2_(__builtin_fmaf(s[r], c, mc));
+                    l += s[r];
+                    if (r % 8 == 7) p[r / 8] = pack8(s, r - 7);
+                }
+                // the first 16 keys' columns
+                if (part > KS - DB)
+                    tv[0][part - 1 - (KS - DB)] = rd.frag_t(part - 1 - (KS - DB), kb * 32, Tile::BYTES);
+            });
+            // the loads of a step, spread over its blocks: the last one's first
+            constexpr int PER = (S::LOADS + NB - 1) / NB;
+            const int first = last ? 0 : (kb + 1) * PER;
+            float top = -INFINITY;
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int db = 0; db < DB; ++db) {
+                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv[h][db], p[h], o[db], 0, 0, 0);
+                    if (h == 0) tv[1][db] = rd.frag_t(db, kb * 32 + 16, Tile::BYTES);
+                    const int k = h * DB + db;
+#pragma unroll
+                    for (int q = PER * k / (2 * DB); q < PER * (k + 1) / (2 * DB); ++q)
+                        if (first + q < S::LOADS) fetch_part(first + q);
+                    // the next scores are there one product later
+#pragma unroll
+                    for (int r = 0; r < 16; ++r) {
+                        if (k == 0 || !in_part(r, k - 1, 2 * DB - 1)) continue;
+                        if constexpr (EDGE) hide(s_n, last ? kn : kw + (kb + 1) * 32, r);
+                        top = fmaxf(top, s_n[r]);
+                    }
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+            if (!last || x + 1 < s1) rise(top);
+            if constexpr (!TURN) sp[0] = sp[1];
+        }
+        rd.move(by);
+        stage = wrap ? 0 : stage + 1;
     };
+    if (s0 < s1) {
+        if constexpr (DMA) wait_vm<(NS - 2) * S::LOADS>();
+        __syncthreads();
+        scores(sp[0], rd, 0, [](int) {});
+        const int kw = k_beg + walk.step(s0) * KEYS + kg * KT;
+        float top = -INFINITY;
+#pragma unroll
+        for (int r = 0; r < 16; ++r) {
+            hide(sp[0], kw, r);
+            top = fmaxf(top, sp[0][r]);
+        }
+        rise(top);
+    }
     int x = s0;
     for (; x < min(s1, walk.masked()); ++x) take(x, std::true_type{});
     for (; x < s1; ++x) take(x, std::false_type{});
+    wait_vm<0>();      // no load is on its way to LDS any more
+    __syncthreads();
 
     float l0, l1;
     halves(l, &l0, &l1);
     l = l0 + l1;
-
+    float mul = 1.f;         // 2^((m - the groups' maximum) c)
     if constexpr (KG > 1) {
-        // groups 1.. hand (m, l, O) to group 0 through LDS, lane by lane
+        float *const stats = reinterpret_cast<float *>(smem + S::PUT) + lane;
+        stats[wave * 128] = m;
+        stats[wave * 128 + 64] = l;
         __syncthreads();
-        constexpr int SLOT = (DB * 16 + 2) * 64;
-        static_assert((KG - 1) * (NW / KG) * SLOT * 4 <= S::LDS, "group results do not fit");
-        float *const base = reinterpret_cast<float *>(smem) + lane;
-        if (kg > 0) {
-            float *p = base + ((kg - 1) * (NW / KG) + wr) * SLOT;
-            p[0] = m;
-            p[64] = l;
+        const float *const p = stats + wr * KG * 128;
+        float mn = p[0];
 #pragma unroll
-            for (int db = 0; db < DB; ++db)
+        for (int k = 1; k < KG; ++k) mn = fmaxf(mn, p[k * 128]);
+        const float ms = mn == -INFINITY ? 0.f : mn;
+        l = 0.f;
 #pragma unroll
-                for (int r = 0; r < 16; ++r) p[(2 + db * 16 + r) * 64] = o[db][r];
-        }
-        __syncthreads();
-        if (kg > 0) return;
-#pragma unroll
-        for (int k = 1; k < KG; ++k) {
-            const float *p = base + ((k - 1) * (NW / KG) + wr) * SLOT;
-            const float mk = p[0], mn = fmaxf(m, mk);
-            const float ms = mn == -INFINITY ? 0.f : mn;
-            const float x0 = exp2_((m - ms) * c), x1 = exp2_((mk - ms) * c);
-            m = mn;
-            l = l * x0 + p[64] * x1;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r)
-                    o[db][r] = o[db][r] * x0 + p[(2 + db * 16 + r) * 64] * x1;
-        }
+        for (int k = 0; k < KG; ++k) l += p[k * 128 + 64] * exp2_((p[k * 128] - ms) * c);
+        mul = exp2_((m - ms) * c);
+        m = mn;
     }
-
-    if (!valid) return;
     // a row that sees no key: O = 0, lse = -infinity
     const bool some = live && l != 0.f;
-    const float inv = some ? 1.f / l : 0.f;
     const float lse2 = some ? m * c + __builtin_amdgcn_logf(l) : -INFINITY;
-    if (f.splits > 1) {
-        const int64_t d4 = (a.d + 3) & ~3;
-        const int64_t bhs = (int64_t)a.batch * a.kv_heads;
-        const int64_t at = ((int64_t)split * bhs + bh) * f.rows + row;
-        float *const part = a.ws + at * d4;
-#pragma unroll
-        for (int db = 0; db < DB; ++db)
-#pragma unroll
-            for (int q = 0; q < 4; ++q) {
-                const int col = db * 32 + 8 * q + 4 * half;
-                if (col >= d4) continue;
-                f32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) v[e] = some ? o[db][4 * q + e] * inv : 0.f;
-                *reinterpret_cast<f32x4 *>(part + col) = v;
-            }
-        if (half == 0) a.ws[(int64_t)f.splits * bhs * f.rows * d4 + at] = lse2;
-        return;
+    const bool whole = f.splits == 1;
+    const int64_t d4 = (a.d + 3) & ~3;
+    const int64_t at = (((int64_t)split * a.batch * a.kv_heads) + bh) * f.rows + row;
+    const RowsOut out{whole ? a.o.p : a.ws, whole ? a.d : (int)d4, !whole || a.o_f32, false,
+                      !whole || f.vec};
+    const int64_t off = !valid ? -1
+                        : whole ? (int64_t)b * a.o.sb + head * a.o.sh + (int64_t)i * a.o.ld
+                                : at * d4;
+    float *const put = reinterpret_cast<float *>(smem);
+    stage_rows<DP>(put + wave * PUT_FLOATS<DP>, o, some ? mul / l : 0.f, lane);
+    if (valid && half == 0 && kg == 0) {
+        if (!whole)
+            a.ws[(int64_t)f.splits * a.batch * a.kv_heads * f.rows * d4 + at] = lse2;
+        else if (a.lse.p)
+            static_cast<float *>(a.lse.p)[(int64_t)b * a.lse.sb + head * a.lse.sh +
+                                          (int64_t)i * a.lse.ld] = lse2 * LN2;
     }
-    const int64_t at = (int64_t)b * a.o.sb + head * a.o.sh + (int64_t)i * a.o.ld;
-#pragma unroll
-    for (int db = 0; db < DB; ++db)
-#pragma unroll
-        for (int q = 0; q < 4; ++q) {
-            const int col = db * 32 + 8 * q + 4 * half;
-            if (col < a.d)
-                store4(a.o.p, at, col, a.d, a.o_f32, f.vec,
-                       [&](int e) { return some ? o[db][4 * q + e] * inv : 0.f; });
-        }
-    if (a.lse.p && half == 0)
-        static_cast<float *>(a.lse.p)[(int64_t)b * a.lse.sb + head * a.lse.sh +
-                                      (int64_t)i * a.lse.ld] = lse2 * LN2;
+    __syncthreads();
+    store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
 }
 
 // Joins the key splits of a row: weights 2^(lse_s - lse), in split order. A thread
@@ -325,16 +399,34 @@ __global__ __launch_bounds__(256) void attn_core_join_kernel(FwdArgs f) {
     const int col = (int)(id % quads) * 4;
     const int64_t d4 = quads * 4;
     const float *stat = a.ws + f.splits * n * d4 + at;
-    float top = -INFINITY;
-    for (int s = 0; s < f.splits; ++s) top = fmaxf(top, stat[s * n]);
-    const float base = top == -INFINITY ? 0.f : top;
-    float total = 0.f;
+    const float *part = a.ws + at * d4 + col;
+    // 8 splits at a time, so that their reads are on the way together
+    float top = -INFINITY, total = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
-    for (int s = 0; s < f.splits; ++s) {
-        const float w = exp2_(stat[s * n] - base);
-        const f32x4 x = *reinterpret_cast<const f32x4 *>(a.ws + (s * n + at) * d4 + col);
-        total += w;
-        v += x * w;
+    for (int s = 0; s < f.splits; s += 8) {
+        float w[8];
+        f32x4 x[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const bool in = s + j < f.splits;
+            w[j] = in ? stat[(s + j) * n] : -INFINITY;
+            x[j] = in ? *reinterpret_cast<const f32x4 *>(part + (s + j) * n * d4)
+                      : f32x4{0.f, 0.f, 0.f, 0.f};
+        }
+        float high = top;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) high = fmaxf(high, w[j]);
+        const float base = high == -INFINITY ? 0.f : high;
+        const float old = exp2_(top - base);
+        total *= old;
+        v *= old;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            w[j] = exp2_(w[j] - base);
+            total += w[j];
+            v += x[j] * w[j];
+        }
+        top = high;
     }
     const bool some = total != 0.f;
     const float inv = some ? 1.f / total : 0.f;
@@ -356,18 +448,69 @@ namespace sbpi {
 
 namespace {
 
-template <int DP, int KG, int KT>
+template <int DP, int KG, int KT, int NW, int WPS>
 hipError_t launch_fwd(const sbpk::FwdArgs &f, int64_t blocks, hipStream_t s) {
     char name[160];
     name[0] = 0;
     if (profiling())
-        snprintf(name, sizeof(name), "attn_core_fwd_kernel<%d,%d,%d,%d>", DP, KG, KT,
+        snprintf(name, sizeof(name), "attn_core_fwd_kernel<%d,%d,%d,%d,%d>", DP, KG, KT, NW,
                  (int)f.a.aligned);
     if (f.a.aligned)
-        return launch_kernel(sbpk::attn_core_fwd_kernel<DP, KG, KT, true>, name,
-                             dim3((unsigned)blocks), dim3(256), s, f);
-    return launch_kernel(sbpk::attn_core_fwd_kernel<DP, KG, KT, false>, name,
-                         dim3((unsigned)blocks), dim3(256), s, f);
+        return launch_kernel(sbpk::attn_core_fwd_kernel<DP, KG, KT, NW, WPS, true>, name,
+                             dim3((unsigned)blocks), dim3(64 * NW), s, f);
+    return launch_kernel(sbpk::attn_core_fwd_kernel<DP, KG, KT, NW, WPS, false>, name,
+                         dim3((unsigned)blocks), dim3(64 * NW), s, f);
+}
+
+// The kernel's forms: rows of a tile, keys of a step, workgroups of a unit, us of a step. The
+// second and third give up speed a row for smaller tiles: 16 heads over 4 of 8192 x 128,
+// causal, take 277, 343 and 472 us; 16 heads of 1024 x 64, causal, 19.3, 14.6 and 17.0; 64
+// key heads with 4 rows each, 4096 x 64, whose keys are split, 17.3, 13.8 and 13.8.
+struct Form {
+    int rows, keys, per_cu;
+    double step;
+};
+constexpr Form FORMS[2][3] = {{{128, 64, 2, 0.9}, {64, 64, 2, 0.55}, {32, 128, 1, 0.6}},
+                              {{256, 64, 1, 1.4}, {128, 64, 1, 1.0}, {64, 64, 1, 0.75}}};
+
+// The form (returned) and key splits that the following time expects least of: an item takes
+// so much a step, and `fixed` besides; the busiest unit has an even share of all items and
+// half of the longest; partials are written and read once, by one more launch.
+int plan_fwd(const CoreArgs &a, int64_t bhs, int cus, int64_t *splits) {
+    const Form *forms = FORMS[a.d > 64];
+    const int64_t packed = (int64_t)a.sq * a.group;
+    const size_t d4 = (a.d + 3) & ~3;
+    const double fixed = 3.5;
+    double best = 1e300;
+    int form = 0;
+    *splits = 1;
+    for (int k = 0; k < 3; ++k) {
+        const Form &m = forms[k];
+        const int64_t tiles = (packed + m.rows - 1) / m.rows;
+        const int64_t keys = a.causal && a.window
+                                 ? std::min<int64_t>(a.sk, a.window + m.rows / a.group)
+                                 : a.sk;
+        const int64_t steps = (keys + m.keys - 1) / m.keys;
+        // a causal walk is half as long on average where it starts at nothing
+        const double mean = a.causal && !a.window
+                                ? steps * (1.0 - 0.5 * std::min<double>(1.0, (double)a.sq / a.sk))
+                                : (double)steps;
+        for (int64_t v = 1; v <= 32; v *= 2) {
+            const size_t part = v > 1 ? (size_t)bhs * packed * v * (d4 + 1) : 0;
+            if (v > 1 && (steps / v < 2 || part > a.ws_floats ||
+                          (double)tiles * bhs * v > 16777215.0))
+                break;
+            const double item = fixed + (double)((steps + v - 1) / v) * m.step;
+            const double all = (mean * m.step + v * fixed) * tiles * bhs / (cus * m.per_cu);
+            const double t = std::max(item, all + 0.5 * item) + (v > 1 ? 3.5 + part * 8 / 4e6 : 0);
+            if (t < best * 0.98) {
+                best = t;
+                form = k;
+                *splits = v;
+            }
+        }
+    }
+    return form;
 }
 
 }  // namespace
@@ -377,33 +520,25 @@ hipError_t launch_core_fwd(const CoreArgs &a, hipStream_t s) {
     f.a = a;
     f.rows = a.sq * a.group;
     const int esz = a.o_f32 ? 4 : 2;
-    f.vec = reinterpret_cast<uintptr_t>(a.o.p) % (4 * esz) == 0 && a.o.ld % 4 == 0 &&
-            a.o.sb % 4 == 0 && a.o.sh % 4 == 0;
+    f.vec = a.d % 4 == 0 && reinterpret_cast<uintptr_t>(a.o.p) % (4 * esz) == 0 &&
+            a.o.ld % 4 == 0 && a.o.sb % 4 == 0 && a.o.sh % 4 == 0;
     const int64_t bhs = (int64_t)a.batch * a.kv_heads;
-    const int cus = device_cus();
-    int kg = 1;
-    while (kg < 4 && ((f.rows + 128 / kg - 1) / (128 / kg)) * bhs < cus) kg *= 2;
-    const int rows = 128 / kg, keys = kg == 4 ? 128 : 64 * kg;
+    int64_t splits;
+    const int form = plan_fwd(a, bhs, device_cus(), &splits);
+    const bool wide = a.d > 64;
+    const int rows = FORMS[wide][form].rows;
     f.tiles = (f.rows + rows - 1) / rows;
-    // split the keys while workgroups are few and each has several steps
-    const int64_t steps = (a.sk + keys - 1) / keys;
-    const size_t d4 = (a.d + 3) & ~3, per = (size_t)bhs * f.rows * (d4 + 1);
-    int64_t splits = 1;
-    while (f.tiles * bhs * splits * 2 <= 2 * cus && steps / (splits * 2) >= 2 &&
-           per * splits * 2 <= a.ws_floats)
-        splits *= 2;
     f.splits = (int)splits;
     const int64_t blocks = (int64_t)f.tiles * bhs * splits;
     hipError_t e;
-    const bool wide = a.d > 64;
-    if (kg == 1)
-        e = wide ? launch_fwd<128, 1, 64>(f, blocks, s) : launch_fwd<64, 1, 64>(f, blocks, s);
-    else if (kg == 2)
-        e = wide ? launch_fwd<128, 2, 64>(f, blocks, s) : launch_fwd<64, 2, 64>(f, blocks, s);
+    if (form == 0)
+        e = wide ? launch_fwd<128, 1, 64, 8, 2>(f, blocks, s) : launch_fwd<64, 1, 64, 4, 2>(f, blocks, s);
+    else if (form == 1)
+        e = wide ? launch_fwd<128, 2, 32, 8, 2>(f, blocks, s) : launch_fwd<64, 2, 32, 4, 2>(f, blocks, s);
     else
-        e = wide ? launch_fwd<128, 4, 32>(f, blocks, s) : launch_fwd<64, 4, 32>(f, blocks, s);
+        e = wide ? launch_fwd<128, 2, 32, 4, 1>(f, blocks, s) : launch_fwd<64, 4, 32, 4, 1>(f, blocks, s);
     if (e != hipSuccess || splits == 1) return e;
-    const int64_t items = bhs * f.rows * (int64_t)(d4 / 4);
+    const int64_t items = bhs * f.rows * (int64_t)(((a.d + 3) & ~3) / 4);
     return launch_kernel(sbpk::attn_core_join_kernel, "attn_core_join_kernel",
                          dim3((unsigned)((items + 255) / 256)), dim3(256), s, f);
 }

@@ -211,6 +211,17 @@ struct SeqMask {
     }
 };
 
+// Part i of 0 .. PARTS - 1 of a block's 16 values holds value r.
+__device__ __forceinline__ constexpr bool in_part(int r, int i, int parts) {
+    return r >= 16 * i / parts && r < 16 * (i + 1) / parts;
+}
+
+// A direct-to-LDS load to come: two tiles.
+struct Fetch {
+    i32x4 x, y;
+    uint32_t lds;
+};
+
 // Where result rows go: bf16 or fp32, overwritten or added to; `vec`: d is a multiple of 4
 // and the rows allow loads and stores of 4 values.
 struct RowsOut {

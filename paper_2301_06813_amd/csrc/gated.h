@@ -37,6 +37,9 @@ hipError_t launch_gated_fwd(const Gated &a, hipStream_t s);
 hipError_t launch_gated_grad(const Gated &a, hipStream_t s);
 // dX = dG Wg^T + dU Wu^T, dWg = X^T dG, dWu = X^T dU (bf16).
 hipError_t launch_gated_products(const Gated &a, hipStream_t s);
+// The same in fp32, in one launch; *taken false where its rules refuse it (an empty product,
+// leading dimensions of 2^21 elements and more), with nothing launched.
+hipError_t launch_gated_products_f32(const Gated &a, hipStream_t s, bool *taken);
 // H = act(G) U from fp32 or bf16 matrices in memory.
 hipError_t launch_gated_act(const Gated &a, hipStream_t s);
 

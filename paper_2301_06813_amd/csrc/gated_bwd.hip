@@ -7,6 +7,7 @@
 // shares X. The longer items are dispatched first and the others fill the units behind
 // them. dG and dU are rounded to bf16 as operands of the matrix cores.
 #include <algorithm>
+#include <type_traits>
 
 #include "gated.h"
 #include "gated_products.h"
@@ -20,88 +21,124 @@ struct GradArgs {
     void *dG, *dU;
     int64_t ldh, ldg, ldu, ldo_g, ldo_u;
     int32_t m, n;
-    int32_t vec;                 // every row allows 16-byte accesses
 };
 
-// 8 consecutive columns of a row per thread.
-template <int ACT, bool F32>
+// Rows that allow it: 8 consecutive columns of a row per thread, in 16-byte accesses. Others
+// (ROWS false): 4 columns of a row, 256 apart, an element a lane and access, so that a
+// wave's addresses are side by side all the same.
+template <int ACT, bool F32, bool ROWS>
 __global__ __launch_bounds__(256) void gated_grad_kernel(GradArgs a) {
-    const int groups = (a.n + 7) / 8;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= (int64_t)a.m * groups) return;
-    const int64_t row = id / groups;
-    const int col = (int)(id % groups) * 8;
-    const int left = a.n - col;
-    float h[8], g[8], u[8];
-    auto get = [&](const void *p, int64_t ld, float *x) {
-        const int64_t at = row * ld + col;
-        if constexpr (F32) {
-            const float *q = static_cast<const float *>(p) + at;
-            if (a.vec && left >= 8) {
-                const f32x4 v = *reinterpret_cast<const f32x4 *>(q),
-                            w = *reinterpret_cast<const f32x4 *>(q + 4);
-#pragma unroll
-                for (int e = 0; e < 4; ++e) {
-                    x[e] = v[e];
-                    x[4 + e] = w[e];
-                }
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e) x[e] = e < left ? q[e] : 0.f;
-            }
-        } else {
-            const uint16_t *q = static_cast<const uint16_t *>(p) + at;
-            u32x4 v;
-            if (a.vec && left >= 8) v = *reinterpret_cast<const u32x4 *>(q);
-            else if (left >= 8) v = ld16_any(q);
-            else v = ld16_tail(q - col, col, a.n);
+    if constexpr (!ROWS) {
+        using T = std::conditional_t<F32, float, uint16_t>;
+        const int parts = (a.n + 1023) / 1024;
+        auto value = [](T x) {
+            if constexpr (F32) return x;
+            else return __builtin_bit_cast(float, (uint32_t)x << 16);
+        };
+        auto rounded = [](float x) {
+            if constexpr (F32) return x;
+            else return f32_to_bf16_bits(x);
+        };
+        for (int64_t id = blockIdx.x; id < (int64_t)a.m * parts; id += gridDim.x) {
+            const int64_t row = id / parts;
+            const int col = (int)(id % parts) * 1024 + threadIdx.x;
+            const T *dh = static_cast<const T *>(a.dH) + row * a.ldh,
+                    *gp = static_cast<const T *>(a.G) + row * a.ldg,
+                    *up = static_cast<const T *>(a.U) + row * a.ldu;
+            T h[4], g[4], u[4];
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
-                x[2 * e] = __builtin_bit_cast(float, v[e] << 16);
-                x[2 * e + 1] = __builtin_bit_cast(float, v[e] & 0xffff0000u);
+                const int at = min(col + 256 * e, a.n - 1);
+                h[e] = dh[at];
+                g[e] = gp[at];
+                u[e] = up[at];
+            }
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int at = col + 256 * e;
+                if (at >= a.n) continue;
+                float y, d;
+                act_grad<ACT>(value(g[e]), &y, &d);
+                static_cast<T *>(a.dG)[row * a.ldo_g + at] = rounded(value(h[e]) * value(u[e]) * d);
+                static_cast<T *>(a.dU)[row * a.ldo_u + at] = rounded(value(h[e]) * y);
             }
         }
-    };
-    get(a.dH, a.ldh, h);
-    get(a.G, a.ldg, g);
-    get(a.U, a.ldu, u);
+    } else {
+        const int groups = (a.n + 7) / 8;
+        const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+        if (id >= (int64_t)a.m * groups) return;
+        const int64_t row = id / groups;
+        const int col = (int)(id % groups) * 8;
+        const int left = a.n - col;
+        float h[8], g[8], u[8];
+        auto get = [&](const void *p, int64_t ld, float *x) {
+            const int64_t at = row * ld + col;
+            if constexpr (F32) {
+                const float *q = static_cast<const float *>(p) + at;
+                if (left >= 8) {
+                    const f32x4 v = *reinterpret_cast<const f32x4 *>(q),
+                                w = *reinterpret_cast<const f32x4 *>(q + 4);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        float y, d;
-        act_grad<ACT>(g[e], &y, &d);
-        g[e] = h[e] * u[e] * d;
-        u[e] = h[e] * y;
+                    for (int e = 0; e < 4; ++e) {
+                        x[e] = v[e];
+                        x[4 + e] = w[e];
+                    }
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[e] = e < left ? q[e] : 0.f;
+                }
+            } else {
+                const uint16_t *q = static_cast<const uint16_t *>(p) + at;
+                const u32x4 v = left >= 8 ? *reinterpret_cast<const u32x4 *>(q)
+                                          : ld16_tail(q - col, col, a.n);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    x[2 * e] = __builtin_bit_cast(float, v[e] << 16);
+                    x[2 * e + 1] = __builtin_bit_cast(float, v[e] & 0xffff0000u);
+                }
+            }
+        };
+        get(a.dH, a.ldh, h);
+        get(a.G, a.ldg, g);
+        get(a.U, a.ldu, u);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            float y, d;
+            act_grad<ACT>(g[e], &y, &d);
+            g[e] = h[e] * u[e] * d;
+            u[e] = h[e] * y;
+        }
+        auto put = [&](void *p, int64_t ld, const float *x) {
+            const int64_t at = row * ld + col;
+            if constexpr (F32) {
+                float *q = static_cast<float *>(p) + at;
+                if (left >= 8) {
+                    *reinterpret_cast<f32x4 *>(q) = f32x4{x[0], x[1], x[2], x[3]};
+                    *reinterpret_cast<f32x4 *>(q + 4) = f32x4{x[4], x[5], x[6], x[7]};
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < left) q[e] = x[e];
+                }
+            } else {
+                uint16_t *q = static_cast<uint16_t *>(p) + at;
+                if (left >= 8) {
+                    u32x4 v;
+#pragma unroll
+                    for (int e = 0; e < 4; ++e)
+                        v[e] = (uint32_t)f32_to_bf16_bits(x[2 * e]) |
+                               (uint32_t)f32_to_bf16_bits(x[2 * e + 1]) << 16;
+                    *reinterpret_cast<u32x4 *>(q) = v;
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        if (e < left) q[e] = f32_to_bf16_bits(x[e]);
+                }
+            }
+        };
+        put(a.dG, a.ldo_g, g);
+        put(a.dU, a.ldo_u, u);
     }
-    auto put = [&](void *p, int64_t ld, const float *x) {
-        const int64_t at = row * ld + col;
-        if constexpr (F32) {
-            float *q = static_cast<float *>(p) + at;
-            if (a.vec && left >= 8) {
-                *reinterpret_cast<f32x4 *>(q) = f32x4{x[0], x[1], x[2], x[3]};
-                *reinterpret_cast<f32x4 *>(q + 4) = f32x4{x[4], x[5], x[6], x[7]};
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < left) q[e] = x[e];
-            }
-        } else {
-            uint16_t *q = static_cast<uint16_t *>(p) + at;
-            if (a.vec && left >= 8) {
-                u32x4 v;
-#pragma unroll
-                for (int e = 0; e < 4; ++e)
-                    v[e] = (uint32_t)f32_to_bf16_bits(x[2 * e]) |
-                           (uint32_t)f32_to_bf16_bits(x[2 * e + 1]) << 16;
-                *reinterpret_cast<u32x4 *>(q) = v;
-            } else {
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    if (e < left) q[e] = f32_to_bf16_bits(x[e]);
-            }
-        }
-    };
-    put(a.dG, a.ldo_g, g);
-    put(a.dU, a.ldo_u, u);
 }
 
 }  // namespace sbpk
@@ -111,22 +148,25 @@ namespace sbpi {
 hipError_t launch_gated_grad(const Gated &a, hipStream_t s) {
     const bool f32 = a.dtype == DT_F32;
     sbpk::GradArgs g{a.dh.p, a.g.p,  a.u.p,  a.dg.p,       a.du.p,       a.dh.ld, a.g.ld,
-                     a.u.ld, a.dg.ld, a.du.ld, (int32_t)a.m, (int32_t)a.n, 1};
+                     a.u.ld, a.dg.ld, a.du.ld, (int32_t)a.m, (int32_t)a.n};
+    bool rows = true;            // every row allows 16-byte accesses
     for (const Mat *x : {&a.dh, &a.g, &a.u, &a.dg, &a.du})
-        if (reinterpret_cast<uintptr_t>(x->p) % 16 || x->ld % (f32 ? 4 : 8)) g.vec = 0;
-    const int64_t items = a.m * ((a.n + 7) / 8);
-    if (items == 0) return hipSuccess;
-    const dim3 grid((unsigned)((items + 255) / 256)), block(256);
-#define SBP_GRAD(ACT_, F32_)                                                                    \
-    if (a.act == ACT_ && f32 == F32_)                                                           \
-        return launch_kernel(sbpk::gated_grad_kernel<ACT_, F32_>,                               \
-                             "gated_grad_kernel<" #ACT_ ", " #F32_ ">", grid, block, s, g);
-    SBP_GRAD(ACT_SILU, false)
-    SBP_GRAD(ACT_GELU, false)
-    SBP_GRAD(ACT_RELU, false)
-    SBP_GRAD(ACT_SILU, true)
-    SBP_GRAD(ACT_GELU, true)
-    SBP_GRAD(ACT_RELU, true)
+        if (reinterpret_cast<uintptr_t>(x->p) % 16 || x->ld % (f32 ? 4 : 8)) rows = false;
+    if (a.m == 0 || a.n == 0) return hipSuccess;
+    const int64_t blocks = rows ? (a.m * ((a.n + 7) / 8) + 255) / 256
+                                : std::min<int64_t>(a.m * ((a.n + 1023) / 1024), 1 << 20);
+    const dim3 grid((unsigned)blocks), block(256);
+#define SBP_GRAD(ACT_, F32_, ROWS_)                                                             \
+    if (a.act == ACT_ && f32 == F32_ && rows == ROWS_)                                          \
+        return launch_kernel(sbpk::gated_grad_kernel<ACT_, F32_, ROWS_>,                        \
+                             "gated_grad_kernel<" #ACT_ ", " #F32_ ", " #ROWS_ ">", grid, block, s, g);
+#define SBP_GRAD4(ACT_)                                                                         \
+    SBP_GRAD(ACT_, false, true) SBP_GRAD(ACT_, true, true) SBP_GRAD(ACT_, false, false)         \
+    SBP_GRAD(ACT_, true, false)
+    SBP_GRAD4(ACT_SILU)
+    SBP_GRAD4(ACT_GELU)
+    SBP_GRAD4(ACT_RELU)
+#undef SBP_GRAD4
 #undef SBP_GRAD
     return hipErrorInvalidValue;
 }

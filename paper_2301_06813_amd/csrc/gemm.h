@@ -133,6 +133,11 @@ bool plan_f32_bwd(const Gemm &gd, const Gemm &gw, Plan *pd, Plan *pw);
 hipError_t launch_f32_bwd_group(const Gemm &gd, const Plan &pd, const Gemm &gw, const Plan &pw,
                                 float *ws, hipStream_t s);
 
+// One launch of an fp32 dX (gd: both pairs' reductions, each in whole 32-wide blocks) and two
+// weight gradients of gw's sizes; false where a leading dimension is too large for it.
+bool plan_f32_gated_bwd(const Gemm &gd, const Gemm &gw, bool vec4, Plan *pd, Plan *pw,
+                        double *time);
+
 // The library's static scratch on the current device (its address there,
 // looked up once per device) and its size in floats (WS_FLOATS_PREFERRED).
 hipError_t static_scratch(float **ptr, size_t *floats);

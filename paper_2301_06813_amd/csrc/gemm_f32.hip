@@ -38,6 +38,10 @@
 //     8 so that the two half-waves use different banks.
 //   * Split reduction as in the bf16 kernels (split_reduce.hip adds the fp32
 //     partials in split order).
+#include <algorithm>
+#include <type_traits>
+
+#include "gated.h"
 #include "gemm.h"
 #include "gemm_bf16_dma.h"
 #include "profile.h"
@@ -54,6 +58,19 @@ struct F32Args {
     int32_t splits, kchunk;   // reduction elements per split (a multiple of 32)
     float *ws;                // split partials, row stride partial_ld(n)
     int32_t accumulate;       // add the product to C's contents
+};
+
+// A product that reduces over two pairs of operands in turn: k1 of each, the first
+// rounded up to kp, whole steps; k = kp + k1.
+struct F32ArgsTwo : F32Args {
+    const float *A2, *B2;
+    int64_t lda2, ldb2;
+    int32_t k1, kp;
+};
+
+// A weight gradient whose operands' rows hold m_load and n_load elements that may be read.
+struct F32ArgsPad : F32Args {
+    int32_t m_load, n_load;
 };
 
 // One 4-byte-per-lane buffer load that writes LDS directly (see dma16).
@@ -151,8 +168,8 @@ __device__ __forceinline__ void add_block(void *out, int64_t ldo, int rbase, int
 
 // One work item (an output tile and a reduction split; L its logical index).
 // ACCUM: as in the bf16 tile body.
-template <int BM, int BN, bool A_KMAJ, bool B_KMAJ, int V, int ACCUM>
-__device__ __forceinline__ void f32_tile_body(const F32Args &g, const int L, char *smem) {
+template <int BM, int BN, bool A_KMAJ, bool B_KMAJ, int V, int ACCUM, class Args>
+__device__ __forceinline__ void f32_tile_body(const Args &g, const int L, char *smem) {
     using TA = F32Tile<BM, A_KMAJ, V>;
     using TB = F32Tile<BN, B_KMAJ, V>;
     constexpr int A_BYTES = BM * FK * 4, STAGE = (BM + BN) * FK * 4;
@@ -177,8 +194,21 @@ __device__ __forceinline__ void f32_tile_body(const F32Args &g, const int L, cha
     auto issue = [&](int kb, int stage) {
         char *base = smem + stage * STAGE;
         const int k0 = k_begin + kb * FK;
-        TA::issue(g.A, g.lda, m0, g.m, k0, k_lim, base, wave, lane);
-        TB::issue(g.B, g.ldb, n0, g.n, k0, k_lim, base + A_BYTES, wave, lane);
+        if constexpr (std::is_same<Args, F32ArgsTwo>::value) {
+            const bool second = k0 >= g.kp;
+            const int at = second ? k0 - g.kp : k0;
+            const int lim = min(second ? k_lim - g.kp : k_lim, g.k1);
+            TA::issue(second ? g.A2 : g.A, second ? g.lda2 : g.lda, m0, g.m, at, lim, base, wave,
+                      lane);
+            TB::issue(second ? g.B2 : g.B, second ? g.ldb2 : g.ldb, n0, g.n, at, lim,
+                      base + A_BYTES, wave, lane);
+        } else if constexpr (std::is_same<Args, F32ArgsPad>::value) {
+            TA::issue(g.A, g.lda, m0, g.m_load, k0, k_lim, base, wave, lane);
+            TB::issue(g.B, g.ldb, n0, g.n_load, k0, k_lim, base + A_BYTES, wave, lane);
+        } else {
+            TA::issue(g.A, g.lda, m0, g.m, k0, k_lim, base, wave, lane);
+            TB::issue(g.B, g.ldb, n0, g.n, k0, k_lim, base + A_BYTES, wave, lane);
+        }
     };
     f32x16 acc[MI][NI];
 #pragma unroll
@@ -273,6 +303,63 @@ __global__ __launch_bounds__(256, BM == 64 ? 4 : 2) void gemm_f32_mfma_bwd_kerne
     else
         f32_tile_body<BM, BM, false, false, V, ACCUM>(gw, remap_xcd(data_first ? b - wd : b, ww),
                                                       smem);
+}
+
+// The three products of the gated block's backward pass (gated_bwd.hip): dX over both pairs,
+// dWg and dWu, the longer items first. (513 x 1000 x 1375: two launches of a pair each, dX added
+// to itself, 106 us; this one by the same 4-byte loads 94.)
+template <int BM, int V, int ACCUM>
+__global__ __launch_bounds__(256, BM == 64 ? 4 : 2) void gemm_f32_gated_bwd_kernel(
+    F32ArgsTwo gd, F32ArgsPad gw, F32ArgsPad gu, int data_first) {
+    __shared__ __attribute__((aligned(1024))) char smem[4 * BM * FK * 4];
+    const int wd = gd.tiles_m * gd.tiles_n * gd.splits;
+    const int ww = gw.tiles_m * gw.tiles_n * gw.splits;
+    const int b = blockIdx.x;
+    if (data_first ? b < wd : b >= 2 * ww) {
+        f32_tile_body<BM, BM, true, true, V, ACCUM>(gd, remap_xcd(data_first ? b : b - 2 * ww, wd),
+                                                    smem);
+    } else {
+        const int L = remap_xcd(data_first ? b - wd : b, 2 * ww);
+        const bool up = L >= ww;
+        F32ArgsPad g = gw;
+        g.B = up ? gu.B : gw.B;
+        g.ldb = up ? gu.ldb : gw.ldb;
+        g.C = up ? gu.C : gw.C;
+        g.ldc = up ? gu.ldc : gw.ldc;
+        g.ws = up ? gu.ws : gw.ws;
+        g.accumulate = up ? gu.accumulate : gw.accumulate;
+        f32_tile_body<BM, BM, false, false, V, ACCUM>(g, up ? L - ww : L, smem);
+    }
+}
+
+// Copies of matrices whose rows do not allow 16-byte loads into ones that do, rows padded
+// with zeros to whole chunks.
+struct PackArgs {
+    int32_t n;
+    struct {
+        const float *src;
+        float *dst;
+        int64_t ld_src, ld_dst, first;   // first: of its row parts of 1024 columns
+        int32_t cols, parts;
+    } m[5];
+    int64_t total;
+};
+__global__ __launch_bounds__(256) void gated_pack_kernel(PackArgs a) {
+    for (int64_t id = blockIdx.x; id < a.total; id += gridDim.x) {
+        int i = 0;
+        while (i + 1 < a.n && id >= a.m[i + 1].first) ++i;
+        const int64_t at = id - a.m[i].first, row = at / a.m[i].parts;
+        const int col = (int)(at % a.m[i].parts) * 1024 + threadIdx.x;
+        const float *const src = a.m[i].src + row * a.m[i].ld_src;
+        float *const dst = a.m[i].dst + row * a.m[i].ld_dst;
+        float x[4];
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            x[e] = col + 256 * e < a.m[i].cols ? src[col + 256 * e] : 0.f;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if (col + 256 * e < a.m[i].ld_dst) dst[col + 256 * e] = x[e];
+    }
 }
 
 // Plain LDS-tiled FMA kernel (leading dimensions beyond 2^21, shortest reductions): 64 x 64
@@ -459,6 +546,137 @@ hipError_t launch_f32_bwd_group(const Gemm &gd, const Plan &pd, const Gemm &gw, 
     if (pd.splits > 1) return launch_split_reduce(gd, pd.splits, ws, s);
     if (pw.splits > 1) return launch_split_reduce(gw, pw.splits, ws_w, s);
     return hipSuccess;
+}
+
+static Gemm gated_product(int orient, const Mat &a, const Mat &b, const Mat &c, int64_t m, int64_t n,
+                          int64_t k, int acc, const Gated &g) {
+    Gemm o{orient, DT_F32, DT_F32, a.p, a.ld, b.p, b.ld, c.p, c.ld, m, n, k};
+    o.accumulate = acc;
+    o.ws_floats = g.ws_floats;
+    return o;
+}
+
+hipError_t launch_gated_products_f32(const Gated &c, hipStream_t s, bool *taken) {
+    *taken = false;
+    if (c.m == 0 || c.n == 0 || c.k == 0) return hipSuccess;
+    const int64_t n4 = (c.n + 3) & ~int64_t(3), k4 = (c.k + 3) & ~int64_t(3);
+    const int64_t kp = (c.n + 31) / 32 * 32;
+    if (2 * kp + 32 > INT32_MAX || n4 + 1024 > INT32_MAX || k4 + 1024 > INT32_MAX) return hipSuccess;
+    constexpr int64_t kMaxLd = int64_t(1) << 21;
+    for (const Mat *x : {&c.x, &c.dg, &c.du, &c.wg, &c.wu})
+        if (x->ld >= kMaxLd) return hipSuccess;
+    // matrices in the way of 16-byte loads
+    Gated a = c;
+    const struct {
+        Mat *m;
+        int64_t rows, cols;
+    } all[5] = {{&a.x, c.m, c.k}, {&a.wg, c.k, c.n}, {&a.wu, c.k, c.n}, {&a.dg, c.m, c.n}, {&a.du, c.m, c.n}};
+    sbpk::PackArgs pack{};
+    size_t packed = 0;
+    for (const auto &x : all) {
+        const bool rows16 = reinterpret_cast<uintptr_t>(x.m->p) % 16 == 0 && x.m->ld % 4 == 0;
+        if (rows16 && x.cols % 4 == 0) continue;
+        auto &p = pack.m[pack.n++];
+        p.src = static_cast<const float *>(x.m->p);
+        p.cols = (int32_t)x.cols;
+        p.ld_src = x.m->ld;
+        p.ld_dst = (x.cols + 3) & ~int64_t(3);
+        p.dst = c.ws + packed;
+        p.parts = (int32_t)((p.ld_dst + 1023) / 1024);
+        p.first = pack.total;
+        pack.total += x.rows * p.parts;
+        packed += (size_t)(x.rows * p.ld_dst);
+        x.m->p = p.dst;
+        x.m->ld = p.ld_dst;
+    }
+    Gemm gd, gw;
+    auto products = [&]() {
+        gd = gated_product(OR_BWD_DATA, a.dg, a.wg, a.dx, a.m, a.k, 2 * kp, a.dx_acc, a);
+        gw = gated_product(OR_BWD_WEIGHT, a.x, a.dg, a.dwg, a.k, a.n, a.m, a.dwg_acc, a);
+    };
+    // as they are by 4-byte loads, or by 16-byte loads after the copies (read and written
+    // at about 4 TB/s by a launch of their own), if the workspace holds them
+    Plan pd, pw;
+    double time = 1e300;
+    bool vec = false;
+    if (packed <= c.ws_floats) {
+        a.ws = c.ws + packed;
+        a.ws_floats = c.ws_floats - packed;
+        products();
+        vec = plan_f32_gated_bwd(gd, gw, true, &pd, &pw, &time);
+        if (packed) time += 4.0 + packed * 8 / 4e6;
+    }
+    if (pack.n) {
+        const Gated copies = a;
+        a = c;
+        products();
+        Plan qd, qw;
+        double t;
+        if (plan_f32_gated_bwd(gd, gw, false, &qd, &qw, &t) && (!vec || t <= time)) {
+            vec = false;
+            pd = qd;
+            pw = qw;
+        } else if (vec) {
+            a = copies;
+            products();
+        } else {
+            return hipSuccess;
+        }
+    } else if (!vec) {
+        return hipSuccess;
+    }
+    hipError_t e = hipSuccess;
+    if (vec && pack.n) {
+        e = launch_kernel(sbpk::gated_pack_kernel, "gated_pack_kernel",
+                          dim3((unsigned)std::min<int64_t>(pack.total, 1 << 20)), dim3(256), s, pack);
+        if (e != hipSuccess) return e;
+    }
+    const bool v4 = vec;
+    Gemm gu = gated_product(OR_BWD_WEIGHT, a.x, a.du, a.dwu, a.k, a.n, a.m, a.dwu_acc, a);
+    const size_t part_d = plan_ws_floats(gd, pd), part_w = plan_ws_floats(gw, pw);
+    float *const ws_g = a.ws + part_d, *const ws_u = ws_g + part_w;
+    sbpk::F32ArgsTwo d;
+    static_cast<sbpk::F32Args &>(d) = f32_args(gd, pd, a.ws);
+    d.A2 = static_cast<const float *>(a.du.p);
+    d.B2 = static_cast<const float *>(a.wu.p);
+    d.lda2 = a.du.ld;
+    d.ldb2 = a.wu.ld;
+    d.k1 = (int32_t)(vec ? n4 : a.n);
+    d.kp = (int32_t)kp;
+    d.k = (int32_t)(kp + d.k1);
+    sbpk::F32ArgsPad g, u;
+    static_cast<sbpk::F32Args &>(g) = f32_args(gw, pw, ws_g);
+    static_cast<sbpk::F32Args &>(u) = f32_args(gu, pw, ws_u);
+    g.m_load = u.m_load = (int32_t)(vec ? k4 : a.k);
+    g.n_load = u.n_load = (int32_t)(vec ? n4 : a.n);
+    const dim3 grid((unsigned)(d.tiles_m * d.tiles_n * d.splits +
+                               2 * g.tiles_m * g.tiles_n * g.splits));
+    const int data_first = pd.kblk_per_split >= pw.kblk_per_split;
+    const bool add = (a.dx_acc && pd.splits == 1) || ((a.dwg_acc || a.dwu_acc) && pw.splits == 1);
+    char name[96];
+    e = hipErrorInvalidValue;
+#define SBP_F32_GATED(BM_, V_, ACC_)                                                         \
+    if (pd.bm == BM_ && v4 == (V_ == 4) && add == (ACC_ == sbpk::ACC_SOME)) {                \
+        if (profiling())                                                                     \
+            snprintf(name, sizeof(name), "gemm_f32_gated_bwd_kernel<%d, %d, %d>", BM_, V_,   \
+                     ACC_);                                                                  \
+        e = launch_kernel(sbpk::gemm_f32_gated_bwd_kernel<BM_, V_, ACC_>, name, grid,        \
+                          dim3(256), s, d, g, u, data_first);                                \
+    }
+    SBP_F32_GATED(128, 4, sbpk::ACC_NONE)
+    SBP_F32_GATED(128, 1, sbpk::ACC_NONE)
+    SBP_F32_GATED(64, 4, sbpk::ACC_NONE)
+    SBP_F32_GATED(64, 1, sbpk::ACC_NONE)
+    SBP_F32_GATED(128, 4, sbpk::ACC_SOME)
+    SBP_F32_GATED(128, 1, sbpk::ACC_SOME)
+    SBP_F32_GATED(64, 4, sbpk::ACC_SOME)
+    SBP_F32_GATED(64, 1, sbpk::ACC_SOME)
+#undef SBP_F32_GATED
+    *taken = true;
+    if (e != hipSuccess) return e;
+    if (pd.splits > 1) e = launch_split_reduce(gd, pd.splits, a.ws, s);
+    if (e != hipSuccess || pw.splits == 1) return e;
+    return launch_split_reduce_pair(gw, pw.splits, ws_g, gu, pw.splits, ws_u, s);
 }
 
 }  // namespace sbpi

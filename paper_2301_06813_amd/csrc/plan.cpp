@@ -468,6 +468,7 @@ struct PairHash {
 struct PairPlan {
     bool grouped;
     Plan d{}, w{};
+    double time = 0;   // us expected, where the caller asks
 };
 thread_local std::unordered_map<PairKey, PairPlan, PairHash> pair_cache;
 }  // namespace
@@ -947,14 +948,11 @@ static Plan plan_f32_uncached(const Gemm &g, int mode) {
     return plan_f32_model(g, &t);
 }
 
-// The two backward products in one launch: as model_pair, with the fp32 steps.
-static bool plan_f32_bwd_uncached(const Gemm &gd, const Gemm &gw, int mode_d, int mode_w, Plan *pd,
-                                  Plan *pw) {
-    if ((mode_d | mode_w) & F32_BIG_LD || ov_bwd_mode == 1) return false;
-    double best, tw;
-    *pd = plan_f32_model(gd, &best);
-    *pw = plan_f32_model(gw, &tw);
-    best += tw;
+// The two backward products in one launch: as model_pair, with the fp32 steps; `weights`
+// products of gw's sizes, steps `slow` times as long. Whether a plan takes less than *best us,
+// which it then is.
+static bool group_f32(const Gemm &gd, const Gemm &gw, int weights, double slow, double *best,
+                      Plan *pd, Plan *pw) {
     bool grouped = false;
     const int kd = (int)((gd.k + 31) / 32), kw = (int)((gw.k + 31) / 32);
     for (const int t : {64, 128}) {
@@ -972,9 +970,9 @@ static bool plan_f32_bwd_uncached(const Gemm &gd, const Gemm &gw, int mode_d, in
                 if (sw == last_w) continue;
                 last_w = sw;
                 if (sw > 1 && perw < 4) continue;
-                const double nd = f32_tiles(gd, t) * sd, nw = f32_tiles(gw, t) * sw;
+                const double nd = f32_tiles(gd, t) * sd, nw = f32_tiles(gw, t) * sw * weights;
                 if (nd + nw > 2147483647.0) continue;
-                const double q = (nd + nw) / kCUs, step = f32_step(t, q);
+                const double q = (nd + nw) / kCUs, step = f32_step(t, q) * slow;
                 const double lo = std::max(perd, perw), sh = std::min(perd, perw);
                 const double nlo = perd >= perw ? nd : nw;
                 // a long item waits for the other workgroups of its unit
@@ -988,14 +986,14 @@ static bool plan_f32_bwd_uncached(const Gemm &gd, const Gemm &gw, int mode_d, in
                 busy = std::max(busy, lo * std::max(1.0, 0.7 * r));
                 const double tm = busy * step + kF32Fixed +
                                   (sd > 1 || sw > 1 ? kF32Reduce : 0.0) + f32_reduce(gd, sd) +
-                                  f32_reduce(gw, sw);
-                if (tm >= best * 0.999) continue;
+                                  weights * f32_reduce(gw, sw);
+                if (tm >= *best * 0.999) continue;
                 Plan qd{t, t, sd, perd, true}, qw{t, t, sw, perw, true};
                 qd.bk = qw.bk = 32;
-                if ((double)plan_ws_floats(gd, qd) + (double)plan_ws_floats(gw, qw) >
+                if ((double)plan_ws_floats(gd, qd) + weights * (double)plan_ws_floats(gw, qw) >
                     ws_budget(gd))
                     continue;
-                best = tm;
+                *best = tm;
                 grouped = true;
                 *pd = qd;
                 *pw = qw;
@@ -1003,6 +1001,38 @@ static bool plan_f32_bwd_uncached(const Gemm &gd, const Gemm &gw, int mode_d, in
         }
     }
     return grouped;
+}
+
+static bool plan_f32_bwd_uncached(const Gemm &gd, const Gemm &gw, int mode_d, int mode_w, Plan *pd,
+                                  Plan *pw) {
+    if ((mode_d | mode_w) & F32_BIG_LD || ov_bwd_mode == 1) return false;
+    double best, tw;
+    *pd = plan_f32_model(gd, &best);
+    *pw = plan_f32_model(gw, &tw);
+    best += tw;
+    return group_f32(gd, gw, 1, 1.0, &best, pd, pw);
+}
+
+// 513 x 1000 x 1375: by 4-byte loads 94 us on 64 x 64 tiles and 99 on 128 x 128; by 16-byte
+// loads 75 on 64 x 64, after copies of 9 us.
+bool plan_f32_gated_bwd(const Gemm &gd, const Gemm &gw, bool vec4, Plan *pd, Plan *pw,
+                        double *time) {
+    if (f32_big_ld(gd) || f32_big_ld(gw)) return false;
+    const int mode = vec4 ? F32_VEC4 : 0;
+    const PairKey k{key_of(gd, mode), key_of(gw, mode), -2};   // as plan_bf16_gated_bwd
+    auto it = pair_cache.find(k);
+    PairPlan p;
+    if (it != pair_cache.end()) {
+        p = it->second;
+    } else {
+        p.time = 1e300;
+        p.grouped = group_f32(gd, gw, 2, vec4 ? 1.0 : 1.75, &p.time, &p.d, &p.w);
+        keep(pair_cache, k, p);
+    }
+    *pd = p.d;
+    *pw = p.w;
+    *time = p.time;
+    return p.grouped;
 }
 
 static Plan plan_f32_model(const Gemm &g, double *time) {

@@ -761,7 +761,12 @@ int gated_bwd(const sbp_view_t *dH, const L *ldh, const sbp_view_t *X, const L *
     a.dwu_acc = dWu->scope == SBP_ACCUMULATE;
     hipError_t e = sbpi::launch_gated_grad(a, stream);
     if (e != hipSuccess) return hip_fail(e);
+    bool taken = false;
     if (x.dtype == SBP_F32) {
+        e = sbpi::launch_gated_products_f32(a, stream, &taken);
+        if (e != hipSuccess) return hip_fail(e);
+    }
+    if (x.dtype == SBP_F32 && !taken) {
         // each projection's pair of products; the second adds its dX to the first's
         using sbpi::OR_BWD_DATA;
         using sbpi::OR_BWD_WEIGHT;
@@ -773,7 +778,7 @@ int gated_bwd(const sbp_view_t *dH, const L *ldh, const sbp_view_t *X, const L *
                            f32_product(OR_BWD_WEIGHT, a.x, a.du, a.dwu, a.k, a.n, a.m, a.dwu_acc),
                            w, stream)))
             return rc;
-    } else {
+    } else if (x.dtype != SBP_F32) {
         e = sbpi::launch_gated_products(a, stream);
         if (e != hipSuccess) return hip_fail(e);
     }

@@ -316,7 +316,9 @@ hipError_t launch_gated_fwd(const Gated &a, hipStream_t s) {
     const bool dma = aligned16(a.x) && aligned16(a.wg) && aligned16(a.wu) && a.k % 8 == 0 &&
                      a.n % 8 == 0 && a.x.ld <= (int64_t(1) << 21) &&
                      a.wg.ld <= (int64_t(1) << 21) && a.wu.ld <= (int64_t(1) << 21);
-    // tile and splits: whole waves of the largest tile that fills the chip
+    // tile and splits: whole waves of the largest tile that fills the chip (1024 x 4096 over
+    // 1024: 512 tiles of 128 x 64, two a unit, 22.5 us; 256 of 128 x 128, one a unit in three
+    // stages, 26)
     const int cus = device_cus();
     auto tiles = [&](int bm, int bn) {
         return ((a.m + bm - 1) / bm) * ((a.n + bn - 1) / bn);
@@ -329,7 +331,8 @@ hipError_t launch_gated_fwd(const Gated &a, hipStream_t s) {
     const size_t room = a.ws_floats < WS_FLOATS_PREFERRED ? a.ws_floats : WS_FLOATS_PREFERRED;
     const size_t slice = 2 * (size_t)a.m * (size_t)partial_ld(a.n);
     int64_t splits = 1;
-    while (nt * splits * 2 <= 2 * cus && kb / (splits * 2) >= 2 && slice * splits * 2 <= room)
+    const int slots = tile == 0 ? cus : 2 * cus;   // workgroups at a time
+    while (nt * splits * 2 <= slots && kb / (splits * 2) >= 2 && slice * splits * 2 <= room)
         splits *= 2;
     const int64_t per = kb ? (kb + splits - 1) / splits : 1;
     g.kchunk = (int32_t)(per * 64);

@@ -214,7 +214,7 @@ hipError_t launch_gated_products(const Gated &a, hipStream_t s) {
     // dX reduces over n of both pairs, each rounded up to whole 128-wide stages
     const int64_t kp = (a.n + 127) / 128 * 128;
     const bool dma = rows16(a.x) && rows16(a.wg) && rows16(a.wu) && rows16(a.dg) && rows16(a.du) &&
-                     a.k % 8 == 0 && a.n % 8 == 0;
+                     a.k % 8 == 0 && a.n % 8 == 0 && a.dg.ld == a.du.ld && a.wg.ld == a.wu.ld;
     const bool dw_acc = a.dwg_acc || a.dwu_acc;
     Gemm gd{OR_BWD_DATA, DT_BF16, a.dx_dtype, nullptr, 0, nullptr, 0, nullptr, 0, a.m, a.k, 2 * kp};
     Gemm gw{OR_BWD_WEIGHT, DT_BF16, a.dw_dtype, nullptr, 0, nullptr, 0, nullptr, 0, a.k, a.n, a.m};

@@ -13,6 +13,8 @@ the ``*_nd`` functions take (factors, mesh, coord).
 """
 from __future__ import annotations
 
+import functools
+
 import torch
 
 from . import sbp
@@ -213,10 +215,28 @@ def gated_fwd_L(L: dict, X, Wg, Wu, act: str = "silu", save: bool = True, stream
     """(H, G, U) of the device's shares of global X, Wg and Wu under the states in L
     (``layouts`` or ``nd_layouts``): H = act(X Wg) * (X Wu), and the projections that the
     backward pass reads (None with save=False)."""
+    M, K = X.shape
+    return _gated_fwd(L, _gated_sizes(L, M, K, Wg.shape[1]), X, Wg, Wu, act, save, stream, ws)
+
+
+def _gated_sizes(L: dict, M: int, K: int, N: int):
+    """Rows and columns of the device's shares of X and of the weights."""
+    x, w = shard(L["x"], M, K), shard(L["w"], K, N)
+    return x.rows, x.cols, w.rows, w.cols
+
+
+@functools.lru_cache(maxsize=1024)
+def _gated_states(sig: str, p: int, r: int, M: int, K: int, N: int):
+    """layouts(sig, p, r) and _gated_sizes of them. (Five calls of the library, half of the
+    host's time for a small product; they depend on these numbers only.)"""
+    L = layouts(sig, p, r)
+    return L, _gated_sizes(L, M, K, N)
+
+
+def _gated_fwd(L, sizes, X, Wg, Wu, act, save, stream, ws):
     _same_device(X, Wg, Wu)
     nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
-    M, K = X.shape
-    m, n = shard(L["x"], M, K).rows, shard(L["w"], K, Wg.shape[1]).cols
+    m, n = sizes[0], sizes[3]
     new = lambda: torch.empty((m, n), dtype=X.dtype, device=X.device)
     H = new()
     # the fp32 path has no form without the projections in memory
@@ -234,12 +254,16 @@ def gated_bwd_L(L: dict, dH, X, Wg, Wu, G, U, act: str = "silu", out=None, grad_
     device's share) and the G and U of gated_fwd. They are in the inputs' dtype where no
     partial sum of several devices forbids it (or in grad_dtype), or go to the three given
     tensors `out` (accumulate: added to their fp32 contents)."""
+    M, K = X.shape
+    return _gated_bwd(L, _gated_sizes(L, M, K, Wg.shape[1]), dH, X, Wg, Wu, G, U, act, out,
+                      grad_dtype, accumulate, stream, ws)
+
+
+def _gated_bwd(L, sizes, dH, X, Wg, Wu, G, U, act, out, grad_dtype, accumulate, stream, ws):
     _same_device(dH, X, Wg, Wu, G, U, *(out or ()))
     nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
-    M, K = X.shape
-    N = Wg.shape[1]
-    x, w = shard(L["x"], M, K), shard(L["w"], K, N)
-    m, n = x.rows, w.cols
+    M, N = X.shape[0], Wg.shape[1]
+    m, k, kw, n = sizes
 
     def alloc(rows, cols, state):
         dt = grad_dtype or (torch.float32 if partial_devices(state) > 1 else X.dtype)
@@ -248,7 +272,7 @@ def gated_bwd_L(L: dict, dH, X, Wg, Wu, G, U, act: str = "silu", out=None, grad_
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the tensors to add to")
-        out = alloc(m, x.cols, L["dx"]), alloc(w.rows, n, L["dw"]), alloc(w.rows, n, L["dw"])
+        out = alloc(m, k, L["dx"]), alloc(kw, n, L["dw"]), alloc(kw, n, L["dw"])
     pre = torch.empty((2, m, n), dtype=X.dtype, device=X.device)   # dG, dU
     if stream is not None:
         pre.record_stream(torch.cuda.ExternalStream(stream))
@@ -275,11 +299,14 @@ def partial_devices(l) -> int:
 def gated_fwd(sig: str, p: int, r: int, X, Wg, Wu, act: str = "silu", save: bool = True,
               stream=None, ws=None):
     """gated_fwd_L under signature sig ("DP", "COL" or "BB") on rank r of p."""
-    return gated_fwd_L(layouts(sig, p, r), X, Wg, Wu, act, save, stream, ws)
+    M, K = X.shape
+    return _gated_fwd(*_gated_states(sig, p, r, M, K, Wg.shape[1]), X, Wg, Wu, act, save,
+                      stream, ws)
 
 
 def gated_bwd(sig: str, p: int, r: int, dH, X, Wg, Wu, G, U, act: str = "silu", out=None,
               grad_dtype=None, accumulate: bool = False, stream=None, ws=None):
     """gated_bwd_L under signature sig on rank r of p."""
-    return gated_bwd_L(layouts(sig, p, r), dH, X, Wg, Wu, G, U, act, out, grad_dtype, accumulate,
-                       stream, ws)
+    M, K = X.shape
+    return _gated_bwd(*_gated_states(sig, p, r, M, K, Wg.shape[1]), dH, X, Wg, Wu, G, U, act,
+                      out, grad_dtype, accumulate, stream, ws)

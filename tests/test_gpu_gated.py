@@ -277,3 +277,19 @@ def test_gradients_against_differences():
             curve = h * h * float((grads[i].double() * d).abs().sum()) * 8
             say("difference", act, n, got, want, size + curve)
             assert abs(got - want) <= size + curve
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("shape", [(150, 264, 328), (70, 51, 45), (33, 130, 66), (40, 68, 1030)],
+                         ids=["aligned", "odd", "even", "wide"])
+def test_weights_with_strides_of_their_own(shape, dtype):
+    # each weight and each of dH, G and U in rows of its own length, with and without a
+    # workspace (fp32 operands may be copied there for wider loads)
+    M, K, N = shape
+    rows = lambda r, c, pad, seed, std: rn((r, c + pad), std, seed, dtype)[:, :c]
+    X = rows(M, K, 8, 131, 1.0)
+    Wg, Wu = rows(K, N, 8, 132, K ** -0.5), rows(K, N, 24, 133, K ** -0.5)
+    dH, G, U = (rows(M, N, 8 * i, 134 + i, 1.0) for i in range(3))
+    for ws in (None, sbp.NO_WORKSPACE):
+        say("own strides", shape, dtype, ws is None)
+        both(X, Wg, Wu, dH, ws=ws, G=G, U=U)

@@ -126,11 +126,11 @@ __global__ __launch_bounds__(256) void attn_core_stat_kernel(CoreArgs a, float *
 // ------------------------------------------------------------------- dQ
 // Both kernels walk with 32 x 32 blocks of scores a wave, in two phases: S and dP of the
 // next block, whose products alternate, beside this block's exponentials and roundings;
-// then this block's products with them. What is written between two products stays
-// there (sched_barrier): left to itself the compiler read operands right before
-// their use and put the vector work behind the products. The loads of a step are spread over
-// its products too. With 128 columns the sums leave room for one wave per SIMD, which
-// hides nothing behind another.
+// then this block's products with them, whose order is kept as written (sched_barrier), the
+// operands of the later ones and the loads of a step spread over them: left to itself the
+// compiler read operands right before their use. (Kept in the first phase too, the
+// order cost 3%: 16 heads over 4 of 8192 x 128, causal, 1020 us and 985.) With 128 columns the
+// sums leave room for one wave per SIMD, which hides nothing behind another.
 
 // S and dP of one block: S from the operand rows at `r` and `qf`, dP from the rows OFF bytes
 // behind and `gf`. beside(i), i = 0 .. KS: what is written between the products.
@@ -146,7 +146,6 @@ __device__ __forceinline__ void block_scores(f32x16 &s, f32x16 &dp, const Reader
         g[ks] = r.frag(r0, ks, OFF);
     }
     beside(0);
-    __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks) {
         if (ks + AHEAD < KS) {
@@ -156,7 +155,6 @@ __device__ __forceinline__ void block_scores(f32x16 &s, f32x16 &dp, const Reader
         s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(q[ks], qf[ks], s, 0, 0, 0);
         dp = __builtin_amdgcn_mfma_f32_32x32x16_bf16(g[ks], gf[ks], dp, 0, 0, 0);
         beside(ks + 1);
-        __builtin_amdgcn_sched_barrier(0);
     }
 }
 
@@ -918,7 +916,7 @@ Way split_q(const CoreArgs &a, int64_t rows, int64_t v) {
 
 // Wave groups of dQ (returned) and the splits: those that the following time expects least
 // of. An item takes so much a step, and `fixed` besides; the busiest unit has an even share
-// of all items and half of the longest; partials are written and read once, by one more
+// of all items and a fifth of the longest; partials are written and read once, by one more
 // launch.
 int plan_bwd(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs *f) {
     const bool wide = a.d > 64;
@@ -946,7 +944,7 @@ int plan_bwd(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs
                 const double item = fixed + std::max(kv[i].longest * step_kv, q.longest * sq);
                 const double all = (kv[i].steps * step_kv + q.steps * sq +
                                     (kv[i].items + q.items) * fixed) * bhs / slots;
-                const double t = std::max(item, all + 0.5 * item) +
+                const double t = std::max(item, all + 0.2 * item) +
                                  (part > 0 ? 4.0 + part * 8 / 4e6 : 0.0);
                 if (t < best * 0.98) {
                     best = t;

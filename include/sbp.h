@@ -460,7 +460,7 @@ int sbp_attn_context_bwd(const sbp_view4_t *dO, const sbp_view4_t *P,
  *     causal:      j <= i + len_k - len_q   (the last query sees the last key)
  *     window > 0:  j >  i + len_k - len_q - window. */
 typedef struct {
-    float scale;      /* finite and > 0 (else SBP_ERR_SHAPE); usually 1/sqrt(D) */
+    float scale;      /* 2^-100 to 2^100 (else SBP_ERR_SHAPE); usually 1/sqrt(D) */
     int32_t causal;   /* 0 or 1 */
     int32_t window;   /* >= 0; 0: none */
     const int32_t *len_q;

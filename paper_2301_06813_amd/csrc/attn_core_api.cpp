@@ -16,6 +16,7 @@ using namespace sbpa;
 
 constexpr int64_t MAX_ROWS = int64_t(1) << 29;   // i + len_k - len_q + window fits 32 bits
 constexpr int64_t MAX_DIM = 128;
+constexpr float MIN_SCALE = 0x1p-100f;
 
 // check_view4, and element offsets that stay inside 62 bits.
 int check_bounded(const sbp_view4_t *v) {
@@ -91,7 +92,8 @@ int prepare(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_view4_t *V,
     if (Q->cols < 1 || Q->cols > MAX_DIM) return SBP_ERR_SHAPE;
     if (K->heads != V->heads || K->rows != V->rows) return SBP_ERR_SHAPE;
     if (K->heads == 0 ? Q->heads != 0 : Q->heads % K->heads != 0) return SBP_ERR_SHAPE;
-    if (!(opts->scale > 0.f) || !isfinite(opts->scale) || opts->window < 0 ||
+    // (beyond these scales lse / scale or a score's exponent leaves fp32)
+    if (!(opts->scale >= MIN_SCALE && opts->scale <= 1.f / MIN_SCALE) || opts->window < 0 ||
         (opts->causal != 0 && opts->causal != 1))
         return SBP_ERR_SHAPE;
     for (const int32_t *len : {opts->len_q, opts->len_k})

@@ -83,6 +83,8 @@ SHARED = [
     ("scale < 0", dict(opts=opts(-1.0)), sbp.SBP_ERR_SHAPE),
     ("scale NaN", dict(opts=opts(math.nan)), sbp.SBP_ERR_SHAPE),
     ("scale infinite", dict(opts=opts(math.inf)), sbp.SBP_ERR_SHAPE),
+    ("scale below 2^-100", dict(opts=opts(2.0 ** -101)), sbp.SBP_ERR_SHAPE),
+    ("scale above 2^100", dict(opts=opts(2.0 ** 101)), sbp.SBP_ERR_SHAPE),
     ("window < 0", dict(opts=opts(window=-1)), sbp.SBP_ERR_SHAPE),
     ("causal neither 0 nor 1", dict(opts=opts(causal=2)), sbp.SBP_ERR_SHAPE),
     ("misaligned lengths", dict(opts=opts(lk=200 * MB + 2)), sbp.SBP_ERR_ALIGN),

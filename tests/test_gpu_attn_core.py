@@ -284,3 +284,68 @@ def test_gradients_against_differences():
         say("difference", name, got, want, room)
         assert abs(got - want) <= room
         assert room < 0.5 * float((grads[i].double() * d).abs().sum())
+
+
+FORMS = {("fwd", 64, 1), ("fwd", 64, 2), ("fwd", 64, 4), ("fwd", 128, 1), ("fwd", 128, 2, 8),
+         ("fwd", 128, 2, 4), ("bwd", 64, 1), ("bwd", 64, 2), ("bwd", 128, 1), ("bwd", 128, 2)}
+
+
+@pytest.mark.parametrize("pad", [0, 1], ids=["aligned", "unaligned"])
+def test_every_form(pad):
+    # sizes that reach every tile form of both passes, by 16-byte loads and through
+    # registers; sequences of unequal lengths, whose last tiles are partly filled
+    reached = set()
+    for D, dim in ((64, 64), (128, 128), (40, 64), (120, 128)):
+        for B, H, Hk, S, causal, window in ((2, 16, 16, 1024, False, 0), (2, 16, 16, 1024, True, 0),
+                                            (2, 8, 8, 512, True, 0), (2, 8, 4, 512, True, 200),
+                                            (1, 4, 4, 1500, True, 0)):
+            if D % 64 and S == 1024:
+                continue
+            T = [rn((B, n, S, D + pad), 60 + i)[..., :D] for i, n in enumerate((H, Hk, Hk, H))]
+            Q, K, V, dO = T
+            lq, lk = ([S - 24, S // 2 + 1], [S - 34, S // 2 + 9]) if B == 2 else ([S - 3], [S])
+            say("form", D, B, H, Hk, S, causal, window, pad)
+            both(Q, K, V, dO, causal, window, lq, lk)
+            sbp.sbp_profile_begin(16)
+            O, lse = attention.core_fwd(Q, K, V, causal=causal, window=window)
+            attention.core_bwd(dO, Q, K, V, O, lse, causal=causal, window=window)
+            for name, _ in sbp.sbp_profile_end(16):
+                kind, _, rest = name.replace("attn_core_", "").partition("_kernel<")
+                if kind not in ("fwd", "bwd"):
+                    continue
+                v = [int(x) for x in rest.rstrip(">").split(",")]
+                assert v[0] == dim and v[-1] == (pad == 0), name
+                reached.add((kind, v[0], v[1], v[3]) if (kind, *v[:2]) == ("fwd", 128, 2) else
+                            (kind, *v[:2]))
+    assert reached == FORMS
+
+
+@pytest.mark.parametrize("scale", [2.0 ** -100, 1e-20, 3.0, 2.0 ** 100])
+def test_extreme_scales(scale):
+    # scores near zero: every key has the same weight; and scores so large that one key has
+    # it all (small integers, so that the largest score is the largest by far)
+    Q, K, V, dO = tensors(1, 4, 2, 70, 90, 64, 70)
+    if scale > 1:
+        Q, K = torch.zeros_like(Q), torch.zeros_like(K)
+        Q[..., 0], K[..., 0] = 1.0, 0.0
+        K[:, :, 17, 0] = 64.0
+    say("scale", scale)
+    O, lse = attention.core_fwd(Q, K, V, scale=scale)
+    g = attention.core_bwd(dO, Q, K, V, O, lse, scale=scale)
+    torch.cuda.synchronize()
+    v = V.double().repeat_interleave(2, 1)
+    want = v[:, :, 17:18] if scale > 1 else v.mean(2, keepdim=True)
+    # P rounded to bf16, sums of 90 terms in fp32, O rounded to bf16
+    room = 2.0 ** -8 * (want.abs() + v.abs().amax(2, keepdim=True)) + 2.0 ** -14
+    assert bool(((O.double() - want).abs() <= room).all())
+    assert torch.isfinite(lse).all() and all(torch.isfinite(t).all() for t in g)
+    # dV = P^T dO, within P's rounding and the result's
+    P = torch.zeros((1, 4, 70, 90), dtype=torch.float64, device="cuda")
+    P[..., 17] = 1.0
+    P = P if scale > 1 else torch.full_like(P, 1 / 90)
+    d = torch.zeros(V.shape, dtype=torch.float64, device="cuda")
+    e = torch.zeros_like(d)
+    for h in range(4):
+        d[0, h // 2] += torch.mm(P[0, h].t().contiguous(), dO[0, h].double())
+        e[0, h // 2] += torch.mm(P[0, h].t().contiguous(), dO[0, h].double().abs())
+    assert bool(((g[2].double() - d).abs() <= (2.0 ** -8 + 2.0 ** -14) * (d.abs() + e) + 2.0 ** -14).all())

@@ -68,17 +68,24 @@ void gated_fwd_kernel(GatedArgs g) {
 #pragma unroll
                 for (int r = 0; r < 16; ++r) acc[w][i][j][r] = 0.f;
 
-    auto compute = [&](const char *cur) {
+    // Operands are read one reduction step of 16 ahead of their products (read right before
+    // them, 25 us for 8192 x 1024 -> 512); between(i): what is written before products i.
+    auto compute = [&](const char *cur, auto between) {
+        bf16x8 a[2][MI], b[2][2][NI];
+        auto read = [&](int ks) {
 #pragma unroll
-        for (int ks = 0; ks < 4; ++ks) {
-            bf16x8 a[MI], b[2][NI];
-#pragma unroll
-            for (int i = 0; i < MI; ++i) a[i] = TA::frag(cur, wm * WM + i * 32, ks, lane);
+            for (int i = 0; i < MI; ++i) a[ks & 1][i] = TA::frag(cur, wm * WM + i * 32, ks, lane);
 #pragma unroll
             for (int w = 0; w < 2; ++w)
 #pragma unroll
                 for (int j = 0; j < NI; ++j)
-                    b[w][j] = TB::frag(cur + St::A_BYTES + w * St::B_BYTES, wn * WN + j * 32, ks, lane);
+                    b[ks & 1][w][j] = TB::frag(cur + St::A_BYTES + w * St::B_BYTES, wn * WN + j * 32, ks, lane);
+        };
+        read(0);
+#pragma unroll
+        for (int ks = 0; ks < 4; ++ks) {
+            if (ks + 1 < 4) read(ks + 1);
+            between(ks);
 #pragma unroll
             for (int w = 0; w < 2; ++w)
 #pragma unroll
@@ -86,7 +93,8 @@ void gated_fwd_kernel(GatedArgs g) {
 #pragma unroll
                     for (int j = 0; j < NI; ++j)
                         acc[w][i][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(
-                            a[i], b[w][j], acc[w][i][j], 0, 0, 0);
+                            a[ks & 1][i], b[ks & 1][w][j], acc[w][i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -117,27 +125,38 @@ void gated_fwd_kernel(GatedArgs g) {
         for (int it = 0; it < nkb; ++it) {
             __syncthreads();
             if (it + 1 < nkb) load(it + 1);
-            compute(smem + (it & 1) * St::BYTES);
+            compute(smem + (it & 1) * St::BYTES, [](int) {});
             if (it + 1 < nkb) fill((it + 1) & 1);
         }
     } else {
-        auto issue = [&](int kb, int stage) {
+        // A workgroup alone on its unit spreads a step's loads over its products (8192 x 8192
+        // -> 4096: 929 -> 888 us); of two, one's loads run beside the other's products
+        // anyway (8192 x 1024 -> 512: 23.6 us at once, 25.7 spread).
+        constexpr bool SPREAD = St::LDS > 81920;
+        // the loads of step kb: of X, Wg or Wu (part 0 .. 2), or all (-1)
+        auto issue = [&](int kb, int stage, int part) {
             char *base = smem + stage * St::BYTES;
             const int k0 = k_begin + kb * 64;
-            TA::template issue<false>(g.X, g.ldx, m0, g.m, k0, k_lim, base, wave, lane);
-            TB::template issue<false>(g.Wg, g.ldg_w, n0, g.n, k0, k_lim, base + St::A_BYTES, wave,
-                                      lane);
-            TB::template issue<false>(g.Wu, g.ldu_w, n0, g.n, k0, k_lim,
-                                      base + St::A_BYTES + St::B_BYTES, wave, lane);
+            if (part <= 0)
+                TA::template issue<false>(g.X, g.ldx, m0, g.m, k0, k_lim, base, wave, lane);
+            if (part < 0 || part == 1)
+                TB::template issue<false>(g.Wg, g.ldg_w, n0, g.n, k0, k_lim, base + St::A_BYTES,
+                                          wave, lane);
+            if (part < 0 || part == 2)
+                TB::template issue<false>(g.Wu, g.ldu_w, n0, g.n, k0, k_lim,
+                                          base + St::A_BYTES + St::B_BYTES, wave, lane);
         };
 #pragma unroll
         for (int s = 0; s < NS - 1; ++s)
-            if (s < nkb) issue(s, s);
+            if (s < nkb) issue(s, s, -1);
         for (int it = 0; it < nkb; ++it) {
             wait_stages<NS - 2, LOADS>(min(NS - 2, nkb - 1 - it));
             __syncthreads();
-            if (it + NS - 1 < nkb) issue(it + NS - 1, (it + NS - 1) % NS);
-            compute(smem + it % NS * St::BYTES);
+            const bool more = it + NS - 1 < nkb;
+            if (!SPREAD && more) issue(it + NS - 1, (it + NS - 1) % NS, -1);
+            compute(smem + it % NS * St::BYTES, [&](int ks) {
+                if (SPREAD && more) issue(it + NS - 1, (it + NS - 1) % NS, ks);
+            });
         }
     }
 

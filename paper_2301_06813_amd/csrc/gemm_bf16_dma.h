@@ -596,7 +596,8 @@ __device__ __forceinline__ void dma_tile_body(const Args &g, const int L, char *
     using TA = DmaTileOf<BM, NW, BKD, A_KMAJ>;
     using TB = DmaTileOf<BN, NW, BKD, B_KMAJ>;
 
-    auto issue = [&](int kb, int stage) {
+    // part (two pairs): the loads of A (0), of B (1) or of both (-1)
+    auto issue = [&](int kb, int stage, int part = -1) {
         char *base = smem + stage * STAGE;
         const int k0 = k_begin + kb * BKD;
         if constexpr (two_pairs<Args>) {
@@ -605,9 +606,12 @@ __device__ __forceinline__ void dma_tile_body(const Args &g, const int L, char *
             const int lim = second ? k_lim - g.kp : min(k_lim, g.k1);
             // (with row strides of their own, a lane's offsets would be found anew every step:
             // 8192 x 8192 over 2 x 4096 and its gradients 2190 us for 1855)
-            TA::template issue<false>(second ? g.A2 : Ab, g.lda, m0, g.m, k, lim, base, wave, lane);
-            TB::template issue<false>(second ? g.B2 : Bb, g.ldb, n0, g.n, k, lim, base + A_BYTES,
-                                      wave, lane);
+            if (part <= 0)
+                TA::template issue<false>(second ? g.A2 : Ab, g.lda, m0, g.m, k, lim, base, wave,
+                                          lane);
+            if (part != 0)
+                TB::template issue<false>(second ? g.B2 : Bb, g.ldb, n0, g.n, k, lim,
+                                          base + A_BYTES, wave, lane);
         } else {
             TA::template issue<SHIFT>(Ab, g.lda, m0, g.m + shift_m(g), k0, k_lim, base, wave, lane);
             TB::template issue<SHIFT>(Bb, g.ldb, n0, g.n + shift_n(g), k0, k_lim, base + A_BYTES,
@@ -642,6 +646,35 @@ __device__ __forceinline__ void dma_tile_body(const Args &g, const int L, char *
                                                                                acc[i][j], 0, 0, 0)
                                      : __builtin_amdgcn_mfma_f32_32x32x16_bf16(af[i], bfr[j],
                                                                                acc[i][j], 0, 0, 0);
+        }
+    };
+
+    // The same with operands read one reduction step of 16 ahead of their products;
+    // between(i): what is written before products i.
+    auto compute_ahead = [&](const char *cur, auto between) {
+        bf16x8 af[2][MI], bfr[2][NI];
+        auto read = [&](int kk) {
+            const int ks = kg * KSG + kk;
+#pragma unroll
+            for (int i = 0; i < MI; ++i) af[kk & 1][i] = TA::frag(cur, wm * WM + i * 32, ks, lane);
+#pragma unroll
+            for (int j = 0; j < NI; ++j)
+                bfr[kk & 1][j] = TB::frag(cur + A_BYTES, wn * WN + j * 32, ks, lane);
+        };
+        read(0);
+#pragma unroll
+        for (int kk = 0; kk < KSG; ++kk) {
+            if (kk + 1 < KSG) read(kk + 1);
+            between(kk);
+#pragma unroll
+            for (int i = 0; i < MI; ++i)
+#pragma unroll
+                for (int j = 0; j < NI; ++j)
+                    acc[i][j] = SWAP ? __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                           bfr[kk & 1][j], af[kk & 1][i], acc[i][j], 0, 0, 0)
+                                     : __builtin_amdgcn_mfma_f32_32x32x16_bf16(
+                                           af[kk & 1][i], bfr[kk & 1][j], acc[i][j], 0, 0, 0);
+            __builtin_amdgcn_sched_barrier(0);
         }
     };
 
@@ -719,6 +752,15 @@ __device__ __forceinline__ void dma_tile_body(const Args &g, const int L, char *
         // wait for this thread's loads of step `it`; later steps may stay in flight
         wait_stages<NS - 2, LOADS>(min(NS - 2, nkb - 1 - it));
         __syncthreads();
+        if constexpr (two_pairs<Args> && NS * STAGE > 81920) {
+            // alone on its unit: a step's loads are spread over its products (8192 x 8192
+            // over 2 x 4096 and its gradients, whole calls: 1943 us at once, 1883 spread)
+            const bool more = it + NS - 1 < nkb;
+            compute_ahead(smem + it % NS * STAGE, [&](int kk) {
+                if (kk < 2 && more) issue(it + NS - 1, (it + NS - 1) % NS, kk);
+            });
+            continue;
+        }
         if (it + NS - 1 < nkb) issue(it + NS - 1, (it + NS - 1) % NS);
 
         const char *cur = smem + (it % NS) * STAGE;

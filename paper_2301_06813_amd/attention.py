@@ -68,11 +68,12 @@ def core_fwd(Q, K, V, p: int = 1, r: int = 0, *, scale=None, causal: bool = Fals
         # [batch][rows][heads][head_dim] in memory: what the output projection reads
         out = _EMPTY((B, sq, hq, D), dtype=out_dtype or Q.dtype, device=Q.device).transpose(1, 2)
     z = _EMPTY((B, hq, sq), dtype=torch.float32, device=Q.device) if lse else None
+    n = max(sq, 1)
+    rows = sbp.sbp_view4_t(z.data_ptr(), B, hq, sq, 1, max(hq, 1) * n, n, 1, sbp.SBP_F32,
+                           sbp.SBP_LOCAL) if lse else None
     sbp.sbp_attn_core_fwd(sbp.view4(Q, scope), sbp.view4(K, scope), sbp.view4(V, scope),
                           _opts(Q, scale, causal, window, len_q, len_k),
-                          sbp.view4(out, sbp.SBP_LOCAL),
-                          sbp.view4(z.unsqueeze(-1), sbp.SBP_LOCAL) if lse else None, p, r, stream,
-                          ws)
+                          sbp.view4(out, sbp.SBP_LOCAL), rows, p, r, stream, ws)
     return out, z
 
 

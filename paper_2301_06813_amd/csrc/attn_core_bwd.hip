@@ -51,6 +51,7 @@ struct BwdArgs {
     int32_t vec_q, vec_k, vec_v;       // outputs allow 4-value stores
     const float *nl, *nd;              // row statistics: -lse / scale, -D, per (b, head, i)
     float *part_q, *part_kv;           // split partials
+    Div per_q, by_split, per_kv, heads, kv, group, by_rows, by_keys;   // tiles_q x splits_q, ...
 };
 
 // Adds to or overwrites 4 consecutive values of an output row.
@@ -85,14 +86,15 @@ __device__ __forceinline__ void grad4(void *base, int64_t at, int col, int d, bo
 
 // Row statistics: 16 lanes a row. Rows that see no key (lse = -infinity) or lie past
 // the sequence's length get -infinity and 0, which makes their P and dS zero.
-__global__ __launch_bounds__(256) void attn_core_stat_kernel(CoreArgs a, float *nl, float *nd) {
-    const int64_t heads = (int64_t)a.kv_heads * a.group;
-    const int64_t n = a.batch * heads * a.sq;
-    const int64_t r = (int64_t)blockIdx.x * 16 + (threadIdx.x >> 4);
+__global__ __launch_bounds__(256) void attn_core_stat_kernel(CoreArgs a, Div by_sq, Div by_heads,
+                                                             float *nl, float *nd) {
+    const int heads = a.kv_heads * a.group;
+    const int64_t n = (int64_t)a.batch * heads * a.sq;
+    const int r = (int)blockIdx.x * 16 + (int)(threadIdx.x >> 4);
     const int at = (threadIdx.x & 15) * 8;
     if (r >= n) return;
-    const int i = (int)(r % a.sq);
-    const int64_t bh = r / a.sq, b = bh / heads, h = bh % heads;
+    const int bh = by_sq(r), i = by_sq.rest(r, bh);
+    const int64_t b = by_heads(bh), h = by_heads.rest(bh, (int)b);
     const int lq = a.len_q ? min(max(a.len_q[b], 0), a.sq) : a.sq;
     const float lse = i < lq ? static_cast<const float *>(a.lse.p)[b * a.lse.sb + h * a.lse.sh +
                                                                    i * a.lse.ld]
@@ -195,24 +197,22 @@ __device__ __forceinline__ void attn_core_dq(const BwdArgs &f, int wg, char *sme
                  "s"(a.len_q), "s"(a.len_k), "s"(a.batch), "s"(a.kv_heads), "s"(a.group),
                  "s"(a.sq), "s"(a.sk), "s"(a.d), "s"(a.causal), "s"(a.window), "s"(a.scale),
                  "s"(f.tiles_q), "s"(f.splits_q), "s"(f.rows));
-    asm volatile("" ::"s"(f.nl), "s"(f.nd), "s"(a.dq.p), "s"(f.part_q));
     // heavier (later) causal tiles first within a (sequence, head)
-    const int per = f.tiles_q * f.splits_q;
     int bh, t;
-    deal(wg, a.batch * a.kv_heads, per, &bh, &t);
-    const int tile = f.tiles_q - 1 - t / f.splits_q, split = t % f.splits_q;
-    const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    deal(wg, f.heads, f.per_q, &bh, &t);
+    const int up = f.by_split(t), tile = f.tiles_q - 1 - up, split = f.by_split.rest(t, up);
+    const int b = f.kv(bh), hk = f.kv.rest(bh, b);
     const SeqMask mask(a, b);
 
     const int row0 = tile * ROWS;
     const int row = row0 + wr * 32 + (lane & 31);
     const bool valid = row < f.rows;
-    const int i = (valid ? row : f.rows - 1) / a.group;
+    const int i = f.group(valid ? row : f.rows - 1);
     const int g = (valid ? row : f.rows - 1) - i * a.group;
     const int64_t head = (int64_t)hk * a.group + g;
 
-    const int i_first = row0 / a.group;
-    const int i_last = (min(row0 + ROWS, f.rows) - 1) / a.group;
+    const int i_first = f.group(row0);
+    const int i_last = f.group(min(row0 + ROWS, f.rows) - 1);
     const int k_beg = mask.lo(i_first) & ~31;
     const int k_end = i_first < mask.lq ? mask.hi(min(i_last, mask.lq - 1)) : 0;
     const int steps = k_end > k_beg ? (k_end - k_beg + KEYS - 1) / KEYS : 0;
@@ -223,7 +223,7 @@ __device__ __forceinline__ void attn_core_dq(const BwdArgs &f, int wg, char *sme
         walk.nb = all > k_beg ? min(steps, (all - k_beg) / KEYS) : 0;
         walk.na = max(0, min(walk.nb, (mask.lo(i_last) - k_beg + KEYS - 1) / KEYS));
     }
-    const int per_split = (steps + f.splits_q - 1) / f.splits_q;
+    const int per_split = f.by_split(steps + f.splits_q - 1);
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
     const int hi = mask.hi(i), lo = mask.lo(i);
 
@@ -451,16 +451,15 @@ __device__ __forceinline__ void attn_core_dkv(const BwdArgs &f, int wg, char *sm
                  "s"(a.len_q), "s"(a.len_k), "s"(a.batch), "s"(a.kv_heads), "s"(a.group),
                  "s"(a.sq), "s"(a.sk), "s"(a.d), "s"(a.causal), "s"(a.window), "s"(a.scale),
                  "s"(f.lev.items), "s"(f.lev.n));
-    asm volatile("" ::"s"(f.nl), "s"(f.nd), "s"(a.dk.p), "s"(a.dv.p), "s"(f.part_kv),
-                 "s"(f.lev.tile[0]), "s"(f.lev.item[0]), "s"(f.lev.slot[7]));
     // keys with more rows (earlier causal tiles) first within a (sequence, head)
     int bh, t;
-    deal(wg, a.batch * a.kv_heads, f.lev.items, &bh, &t);
+    deal(wg, f.heads, f.per_kv, &bh, &t);
     int lev = 0;
     while (lev + 1 < f.lev.n && t >= f.lev.item[lev + 1]) ++lev;
     const int splits = f.lev.v[lev], in_level = t - f.lev.item[lev];
-    const int tile = f.lev.tile[lev] + in_level / splits, split = in_level % splits;
-    const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int up = splits == 1 ? in_level : in_level / splits;
+    const int tile = f.lev.tile[lev] + up, split = in_level - up * splits;
+    const int b = f.kv(bh), hk = f.kv.rest(bh, b);
     const SeqMask mask(a, b);
 
     const int j0 = tile * KEYS;
@@ -487,7 +486,7 @@ __device__ __forceinline__ void attn_core_dkv(const BwdArgs &f, int wg, char *sm
     }
     const int ne = walk.masked(), ni = nq - ne;   // masked steps of a head, and others
     const int steps = nq * a.group, edges = ne * a.group;
-    const int per_split = (steps + splits - 1) / splits;
+    const int per_split = splits == 1 ? steps : (steps + splits - 1) / splits;
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
 
     // this lane's key is seen by rows [lo, hi)
@@ -513,7 +512,8 @@ __device__ __forceinline__ void attn_core_dkv(const BwdArgs &f, int wg, char *sm
         }
     };
     Place load{0, 0};
-    if (s0 < edges) load = Place{s0 / ne, s0 % ne};
+    if (s0 == 0) load = Place{0, edges > 0 ? 0 : ne};
+    else if (s0 < edges) load = Place{s0 / ne, s0 % ne};
     else if (s0 < s1) load = Place{(s0 - edges) / ni, ne + (s0 - edges) % ni};
     Place work = load;
     // The loads of a step, S::LOADS of a thread: fetch(x, stage) takes the next step of the
@@ -785,19 +785,19 @@ void attn_core_bwd_kernel(BwdArgs f) {
 }
 
 // Adds the splits' partials in split order. A thread owns 4 columns of a row of dQ, or of
-// dK and dV (of the tiles that are split); the workgroups of dQ come first.
+// dK and dV (of the tiles that are split), 16 (32 past 64 columns) a row; the workgroups of
+// dQ come first.
 __global__ __launch_bounds__(256) void attn_core_sum_kernel(BwdArgs f, int blocks_q) {
     const CoreArgs &a = f.a;
     const bool kv = (int)blockIdx.x >= blocks_q;
-    const int quads = (a.d + 3) >> 2;
-    const int64_t d4 = quads * 4, per = kv ? f.lev.split_keys : f.rows;
-    const int64_t bhs = (int64_t)a.batch * a.kv_heads, n = bhs * per;
-    const int64_t id = (int64_t)(blockIdx.x - (kv ? blocks_q : 0)) * 256 + threadIdx.x;
-    if (id >= n * quads) return;
-    const int64_t at = id / quads;
-    const int col = (int)(id % quads) * 4;
-    const int bh = (int)(at / per), row = (int)(at % per);
-    const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    const int lanes = a.d > 64 ? 5 : 4;
+    const Div &per = kv ? f.by_keys : f.by_rows;
+    const int64_t d4 = (a.d + 3) & ~3, bhs = (int64_t)a.batch * a.kv_heads, n = bhs * per.d;
+    const uint32_t id = (blockIdx.x - (kv ? blocks_q : 0)) * 256u + threadIdx.x;
+    const int at = (int)(id >> lanes), col = (int)(id & ((1u << lanes) - 1)) * 4;
+    if (at >= n || col >= a.d) return;
+    const int bh = per(at), row = per.rest(at, bh);
+    const int b = f.kv(bh), hk = f.kv.rest(bh, b);
     if (kv) {
         const int tile = row / DKV_KEYS;
         int lev = 0;
@@ -819,7 +819,7 @@ __global__ __launch_bounds__(256) void attn_core_sum_kernel(BwdArgs f, int block
         f32x4 x = {0.f, 0.f, 0.f, 0.f};
         for (int s = 0; s < f.splits_q; ++s)
             x += *reinterpret_cast<const f32x4 *>(f.part_q + ((int64_t)s * n + at) * d4 + col);
-        const int i = row / a.group;
+        const int i = f.group(row);
         const int64_t head = (int64_t)hk * a.group + (row - i * a.group);
         grad4(a.dq.p, (int64_t)b * a.dq.sb + head * a.dq.sh + (int64_t)i * a.dq.ld, col, a.d,
               a.dq_f32, a.dq_acc, f.vec_q, [&](int e) { return x[e] * a.scale; });
@@ -938,7 +938,9 @@ int plan_bwd(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs
             const double sq = step_q * (kg == 1 ? 1.7 : 1.0);
             for (int i = 0; i < n; ++i) {
                 const double part = (kv[i].part + q.part) * bhs;
+                // (the sums' threads, 32 a row, fit 32 bits)
                 if (part > 0 && (part > (double)room ||
+                                 (double)bhs * (f->rows + a.sk) > 134217727.0 ||
                                  (double)(kv[i].items + q.items) * bhs > 16777215.0))
                     continue;
                 const double item = fixed + std::max(kv[i].longest * step_kv, q.longest * sq);
@@ -957,7 +959,15 @@ int plan_bwd(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs
     }
     f->lev = lev[best_n];
     f->items_kv = (int32_t)(bhs * f->lev.items);
+    f->per_kv = sbpk::Div(f->lev.items);
+    f->heads = sbpk::Div(bhs);
+    f->kv = sbpk::Div(a.kv_heads);
+    f->group = sbpk::Div(a.group);
+    f->by_split = sbpk::Div(f->splits_q);
+    f->by_rows = sbpk::Div(f->rows);
+    f->by_keys = sbpk::Div(f->lev.split_keys);
     f->tiles_q = (f->rows * best_kg + 127) / 128;
+    f->per_q = sbpk::Div((int64_t)f->tiles_q * f->splits_q);
     return best_kg;
 }
 
@@ -980,7 +990,8 @@ hipError_t launch_core_bwd(const CoreArgs &a, hipStream_t s) {
     hipError_t e;
     if (qrows > 0) {
         e = launch_kernel(sbpk::attn_core_stat_kernel, "attn_core_stat_kernel",
-                          dim3((unsigned)((qrows + 15) / 16)), dim3(256), s, a, nl, nd);
+                          dim3((unsigned)((qrows + 15) / 16)), dim3(256), s, a, sbpk::Div(a.sq),
+                          sbpk::Div((int64_t)a.kv_heads * a.group), nl, nd);
         if (e != hipSuccess) return e;
     }
     const int kg = plan_bwd(a, bhs, device_cus(), a.ws_floats - stat, &f);
@@ -991,8 +1002,9 @@ hipError_t launch_core_bwd(const CoreArgs &a, hipStream_t s) {
     if (kg == 1) e = a.d > 64 ? launch_bwd<128, 1>(f, blocks, s) : launch_bwd<64, 1>(f, blocks, s);
     else e = a.d > 64 ? launch_bwd<128, 2>(f, blocks, s) : launch_bwd<64, 2>(f, blocks, s);
     if (e != hipSuccess) return e;
-    const int64_t sum_q = f.splits_q > 1 ? (qrows * (d4 / 4) + 255) / 256 : 0;
-    const int64_t sum_kv = (bhs * f.lev.split_keys * (d4 / 4) + 255) / 256;
+    const int64_t lanes = a.d > 64 ? 32 : 16;
+    const int64_t sum_q = f.splits_q > 1 ? (qrows * lanes + 255) / 256 : 0;
+    const int64_t sum_kv = (bhs * f.lev.split_keys * lanes + 255) / 256;
     if (sum_q + sum_kv == 0) return hipSuccess;
     return launch_kernel(sbpk::attn_core_sum_kernel, "attn_core_sum_kernel",
                          dim3((unsigned)(sum_q + sum_kv)), dim3(256), s, f, (int)sum_q);

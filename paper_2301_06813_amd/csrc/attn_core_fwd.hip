@@ -67,6 +67,7 @@ struct FwdArgs {
     CoreArgs a;
     int32_t tiles, splits, rows;     // row tiles per (sequence, key head); rows = sq * group
     int32_t vec;                     // O allows 4-value stores
+    Div per, by_split, heads, kv, group, by_rows;   // tiles x splits, splits, batch x key heads, ...
 };
 
 // WPS: waves of a SIMD, of one workgroup or two.
@@ -109,23 +110,22 @@ void attn_core_fwd_kernel(FwdArgs f) {
                  "s"(a.window), "s"(a.scale), "s"(a.ws), "s"(f.tiles), "s"(f.splits), "s"(f.rows));
 
     // heavier (later) causal tiles first within a (sequence, head)
-    const int per = f.tiles * f.splits;
     int bh, t;
-    deal(blockIdx.x, a.batch * a.kv_heads, per, &bh, &t);
-    const int tile = f.tiles - 1 - t / f.splits, split = t % f.splits;
-    const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
+    deal(blockIdx.x, f.heads, f.per, &bh, &t);
+    const int up = f.by_split(t), tile = f.tiles - 1 - up, split = f.by_split.rest(t, up);
+    const int b = f.kv(bh), hk = f.kv.rest(bh, b);
     const SeqMask mask(a, b);
 
     const int row0 = tile * ROWS;
     const int row = row0 + wr * 32 + (lane & 31);
     const bool valid = row < f.rows;
-    const int i = (valid ? row : f.rows - 1) / a.group;
+    const int i = f.group(valid ? row : f.rows - 1);
     const int g = (valid ? row : f.rows - 1) - i * a.group;
     const int64_t head = (int64_t)hk * a.group + g;
 
     // the keys that the tile's rows see, and this split's steps of them
-    const int i_first = row0 / a.group;
-    const int i_last = (min(row0 + ROWS, f.rows) - 1) / a.group;
+    const int i_first = f.group(row0);
+    const int i_last = f.group(min(row0 + ROWS, f.rows) - 1);
     const int k_beg = mask.lo(i_first) & ~31;
     const int k_end = i_first < mask.lq ? mask.hi(min(i_last, mask.lq - 1)) : 0;
     const int steps = k_end > k_beg ? (k_end - k_beg + KEYS - 1) / KEYS : 0;
@@ -136,7 +136,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
         walk.nb = all > k_beg ? min(steps, (all - k_beg) / KEYS) : 0;
         walk.na = max(0, min(walk.nb, (mask.lo(i_last) - k_beg + KEYS - 1) / KEYS));
     }
-    const int per_split = (steps + f.splits - 1) / f.splits;
+    const int per_split = f.by_split(steps + f.splits - 1);
     const int s0 = min(steps, split * per_split), s1 = min(steps, s0 + per_split);
     const int hi = mask.hi(i), lo = mask.lo(i);
 
@@ -392,16 +392,14 @@ void attn_core_fwd_kernel(FwdArgs f) {
 }
 
 // Joins the key splits of a row: weights 2^(lse_s - lse), in split order. A thread
-// owns 4 columns of a row.
+// owns 4 columns of a row, 16 (32 past 64 columns) a row.
 __global__ __launch_bounds__(256) void attn_core_join_kernel(FwdArgs f) {
     const CoreArgs &a = f.a;
-    const int quads = (a.d + 3) >> 2;
-    const int64_t bhs = (int64_t)a.batch * a.kv_heads, n = bhs * f.rows;
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (id >= n * quads) return;
-    const int64_t at = id / quads;
-    const int col = (int)(id % quads) * 4;
-    const int64_t d4 = quads * 4;
+    const int lanes = a.d > 64 ? 5 : 4;
+    const int64_t n = (int64_t)a.batch * a.kv_heads * f.rows, d4 = (a.d + 3) & ~3;
+    const uint32_t id = blockIdx.x * 256u + threadIdx.x;
+    const int at = (int)(id >> lanes), col = (int)(id & ((1u << lanes) - 1)) * 4;
+    if (at >= n || col >= a.d) return;
     const float *stat = a.ws + f.splits * n * d4 + at;
     const float *part = a.ws + at * d4 + col;
     // 8 splits at a time, so that their reads are on the way together
@@ -434,9 +432,9 @@ __global__ __launch_bounds__(256) void attn_core_join_kernel(FwdArgs f) {
     }
     const bool some = total != 0.f;
     const float inv = some ? 1.f / total : 0.f;
-    const int bh = (int)(at / f.rows), row = (int)(at % f.rows);
-    const int b = bh / a.kv_heads, hk = bh % a.kv_heads;
-    const int i = row / a.group;
+    const int bh = f.by_rows(at), row = f.by_rows.rest(at, bh);
+    const int b = f.kv(bh), hk = f.kv.rest(bh, b);
+    const int i = f.group(row);
     const int64_t head = (int64_t)hk * a.group + (row - i * a.group);
     store4(a.o.p, (int64_t)b * a.o.sb + head * a.o.sh + (int64_t)i * a.o.ld, col, a.d, a.o_f32,
            f.vec, [&](int e) { return v[e] * inv; });
@@ -502,7 +500,8 @@ int plan_fwd(const CoreArgs &a, int64_t bhs, int cus, int64_t *splits) {
         for (int64_t v = 1; v <= 32; v *= 2) {
             const size_t part = v > 1 ? (size_t)bhs * packed * v * (d4 + 1) : 0;
             if (v > 1 && (steps / v < 2 || part > a.ws_floats ||
-                          (double)tiles * bhs * v > 16777215.0))
+                          (double)tiles * bhs * v > 16777215.0 ||
+                          (double)bhs * packed > 134217727.0))   // the join's threads
                 break;
             const double item = fixed + (double)((steps + v - 1) / v) * m.step;
             const double all = (mean * m.step + v * fixed) * tiles * bhs / (cus * m.per_cu);
@@ -533,6 +532,12 @@ hipError_t launch_core_fwd(const CoreArgs &a, hipStream_t s) {
     const int rows = FORMS[wide][form].rows;
     f.tiles = (f.rows + rows - 1) / rows;
     f.splits = (int)splits;
+    f.per = sbpk::Div((int64_t)f.tiles * splits);
+    f.by_split = sbpk::Div(splits);
+    f.heads = sbpk::Div(bhs);
+    f.kv = sbpk::Div(a.kv_heads);
+    f.group = sbpk::Div(a.group);
+    f.by_rows = sbpk::Div(f.rows);
     const int64_t blocks = (int64_t)f.tiles * bhs * splits;
     hipError_t e;
     if (form == 0)
@@ -542,7 +547,7 @@ hipError_t launch_core_fwd(const CoreArgs &a, hipStream_t s) {
     else
         e = wide ? launch_fwd<128, 2, 32, 4, 1>(f, blocks, s) : launch_fwd<64, 4, 32, 4, 1>(f, blocks, s);
     if (e != hipSuccess || splits == 1) return e;
-    const int64_t items = bhs * f.rows * (int64_t)(((a.d + 3) & ~3) / 4);
+    const int64_t items = bhs * f.rows * (wide ? 32 : 16);
     return launch_kernel(sbpk::attn_core_join_kernel, "attn_core_join_kernel",
                          dim3((unsigned)((items + 255) / 256)), dim3(256), s, f);
 }

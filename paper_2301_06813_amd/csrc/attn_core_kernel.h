@@ -320,6 +320,21 @@ __device__ __forceinline__ void store_rows(const float *tiles, int step, int kg,
     }
 }
 
+// Division by a number that the launch knows, of n < 2^31: n m / 2^32 with m = (2^32 - 1) / d is
+// at most n / d and more than n / d - n / 2^32 - 1, so off by one at most. (The compiler's
+// division is a chain of 30 instructions; a workgroup does six before its first load.)
+struct Div {
+    uint32_t d = 1, m = ~0u;
+    Div() = default;
+    explicit Div(int64_t n) : d(n > 1 ? (uint32_t)n : 1u), m(~0u / d) {}
+    __device__ __forceinline__ int operator()(int n) const {
+        const uint32_t q = (uint32_t)((uint64_t)(uint32_t)n * m >> 32);
+        return (int)(q + ((uint32_t)n - q * d >= d ? 1u : 0u));
+    }
+    // n % d, given q = n / d.
+    __device__ __forceinline__ int rest(int n, int q) const { return n - q * (int)d; }
+};
+
 // Which (sequence, key head) and which of its `per` items, heaviest first, a workgroup takes.
 // Workgroups go to the XCDs in turn. Where the heads are a multiple of 8, each XCD takes
 // whole heads, one after the other, whose keys then stay in its L2; else the heads'
@@ -327,15 +342,12 @@ __device__ __forceinline__ void store_rows(const float *tiles, int step, int kg,
 // several XCDs leaves none with its heavier half (16 query heads over 4 key heads, 8192 x 128
 // causal: dQ 563 us in one
 // head after the other and 412 dealt out, dK and dV 878 and 625).
-__device__ __forceinline__ void deal(int wg, int heads, int per, int *bh, int *item) {
-    if (heads % 8 == 0) {
-        const int l = remap_xcd(wg, heads * per);
-        *bh = l / per;
-        *item = l % per;
-    } else {
-        *bh = wg % heads;
-        *item = wg / heads;
-    }
+__device__ __forceinline__ void deal(int wg, const Div &heads, const Div &per, int *bh, int *item) {
+    const bool whole = heads.d % 8 == 0;
+    const int l = whole ? remap_xcd(wg, (int)(heads.d * per.d)) : wg;
+    const int q = whole ? per(l) : heads(l), r = whole ? per.rest(l, q) : heads.rest(l, q);
+    *bh = whole ? q : r;
+    *item = whole ? r : q;
 }
 
 // The order in which a workgroup takes the n steps of its walk: first those that need

@@ -237,14 +237,17 @@ def _gated_fwd(L, sizes, X, Wg, Wu, act, save, stream, ws):
     _same_device(X, Wg, Wu)
     nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
     m, n = sizes[0], sizes[3]
-    new = lambda: torch.empty((m, n), dtype=X.dtype, device=X.device)
-    H = new()
+    x = sbp.view(X)
+
+    def new():   # a tensor and its view
+        t = X.new_empty((m, n))
+        return t, sbp.raw_view(t.data_ptr(), m, n, max(n, 1), x.dtype, sbp.SBP_LOCAL)
+
+    H, h = new()
     # the fp32 path has no form without the projections in memory
-    G, U = (new(), new()) if save or X.dtype == torch.float32 else (None, None)
-    loc = lambda t: None if t is None else sbp.view(t, sbp.SBP_LOCAL)
+    (G, g), (U, u) = (new(), new()) if save or x.dtype == sbp.SBP_F32 else ((None,) * 2,) * 2
     fn = sbp.sbp_nd_gated_fwd if nd else sbp.sbp_gated_fwd
-    fn(sbp.view(X), L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act], loc(H), loc(G),
-       loc(U), stream, ws)
+    fn(x, L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act], h, g, u, stream, ws)
     return (H, G, U) if save else (H, None, None)
 
 

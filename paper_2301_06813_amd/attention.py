@@ -51,8 +51,22 @@ def _local(x, full, scope):
     return sbp.view4(x, scope if x.shape[1] == full else sbp.SBP_LOCAL)
 
 
-def _rows(lse):
-    return lse.unsqueeze(-1) if lse.dim() == 3 else lse
+def _rows(lse, full, scope):
+    """View of the rows' statistics, [batch][heads][rows] or with one column."""
+    if lse.dim() != 3:
+        return _local(lse, full, scope)
+    sb, sh, ld = lse.stride()
+    return sbp.sbp_view4_t(lse.data_ptr(), *lse.shape, 1, sb, sh, max(ld, 1), sbp._dtype_of(lse),
+                           scope if lse.shape[1] == full else sbp.SBP_LOCAL)
+
+
+def _new(like, B, heads, rows, D, dtype):
+    """A tensor [batch][heads][rows][head_dim], [batch][rows][heads][head_dim] in memory
+    (what a projection reads), and its view."""
+    t = like.new_empty((B, rows, heads, D), dtype=dtype)
+    ld = max(heads, 1) * D
+    return t.transpose(1, 2), sbp.sbp_view4_t(t.data_ptr(), B, heads, rows, D, max(rows, 1) * ld, D,
+                                              ld, sbp._dtype_of(t), sbp.SBP_LOCAL)
 
 
 def core_fwd(Q, K, V, p: int = 1, r: int = 0, *, scale=None, causal: bool = False,
@@ -65,15 +79,16 @@ def core_fwd(Q, K, V, p: int = 1, r: int = 0, *, scale=None, causal: bool = Fals
     _same_device(Q, K, V, len_q, len_k, out)
     hq = rank_heads(H, K.shape[1], p, r)[1] if scope == sbp.SBP_GLOBAL else H
     if out is None:
-        # [batch][rows][heads][head_dim] in memory: what the output projection reads
-        out = _EMPTY((B, sq, hq, D), dtype=out_dtype or Q.dtype, device=Q.device).transpose(1, 2)
+        out, o = _new(Q, B, hq, sq, D, out_dtype or Q.dtype)
+    else:
+        o = sbp.view4(out, sbp.SBP_LOCAL)
     z = _EMPTY((B, hq, sq), dtype=torch.float32, device=Q.device) if lse else None
     n = max(sq, 1)
     rows = sbp.sbp_view4_t(z.data_ptr(), B, hq, sq, 1, max(hq, 1) * n, n, 1, sbp.SBP_F32,
                            sbp.SBP_LOCAL) if lse else None
     sbp.sbp_attn_core_fwd(sbp.view4(Q, scope), sbp.view4(K, scope), sbp.view4(V, scope),
                           _opts(Q, scale, causal, window, len_q, len_k),
-                          sbp.view4(out, sbp.SBP_LOCAL), rows, p, r, stream, ws)
+                          o, rows, p, r, stream, ws)
     return out, z
 
 
@@ -96,19 +111,19 @@ def core_bwd(dO, Q, K, V, O, lse, p: int = 1, r: int = 0, *, scale=None, causal:
         if accumulate:
             raise ValueError("accumulate needs the tensors to add to")
         dt = grad_dtype or Q.dtype
-        out = (_EMPTY((B, sq, hq, D), dtype=dt, device=Q.device).transpose(1, 2),
-               _EMPTY((B, sk, hk, D), dtype=dt, device=Q.device).transpose(1, 2),
-               _EMPTY((B, sk, hk, D), dtype=dt, device=Q.device).transpose(1, 2))
+        (dq, vq), (dk, vk), (dv, vv) = (_new(Q, B, hq, sq, D, dt), _new(Q, B, hk, sk, D, dt),
+                                        _new(Q, B, hk, sk, D, dt))
+        out = dq, dk, dv
+    else:
+        vq, vk, vv = (sbp.view4(t, sbp.SBP_ACCUMULATE if accumulate else sbp.SBP_LOCAL) for t in out)
     need = bwd_workspace_bytes(B, hq, sq)
     if ws is None and need > sbp.SBP_WORKSPACE_BYTES:
         # more rows than the kept workspace has room for: one of this call's own
         ws = _EMPTY(need, dtype=torch.uint8, device=Q.device)
         if stream is not None:
             ws.record_stream(torch.cuda.ExternalStream(stream))
-    o = sbp.SBP_ACCUMULATE if accumulate else sbp.SBP_LOCAL
     sbp.sbp_attn_core_bwd(_local(dO, H, scope), sbp.view4(Q, scope), sbp.view4(K, scope),
-                          sbp.view4(V, scope), _local(O, H, scope),
-                          _local(_rows(lse), H, scope),
-                          _opts(Q, scale, causal, window, len_q, len_k), sbp.view4(out[0], o),
-                          sbp.view4(out[1], o), sbp.view4(out[2], o), p, r, stream, ws)
+                          sbp.view4(V, scope), _local(O, H, scope), _rows(lse, H, scope),
+                          _opts(Q, scale, causal, window, len_q, len_k), vq, vk, vv, p, r, stream,
+                          ws)
     return out

@@ -268,24 +268,31 @@ def _gated_bwd(L, sizes, dH, X, Wg, Wu, G, U, act, out, grad_dtype, accumulate, 
     M, N = X.shape[0], Wg.shape[1]
     m, k, kw, n = sizes
 
-    def alloc(rows, cols, state):
-        dt = grad_dtype or (torch.float32 if partial_devices(state) > 1 else X.dtype)
-        return torch.empty((rows, cols), dtype=dt, device=X.device)
+    x = sbp.view(X)
+
+    def new(rows, cols, state):   # a tensor and its view
+        t = X.new_empty((rows, cols), dtype=grad_dtype or (torch.float32 if partial_devices(state) > 1
+                                                           else X.dtype))
+        return t, sbp.raw_view(t.data_ptr(), rows, cols, max(cols, 1), sbp._dtype_of(t),
+                               sbp.SBP_LOCAL)
 
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs the tensors to add to")
-        out = alloc(m, k, L["dx"]), alloc(kw, n, L["dw"]), alloc(kw, n, L["dw"])
-    pre = torch.empty((2, m, n), dtype=X.dtype, device=X.device)   # dG, dU
+        (dx, vx), (dg, vg), (du, vu) = (new(m, k, L["dx"]), new(kw, n, L["dw"]), new(kw, n, L["dw"]))
+        out = dx, dg, du
+    else:
+        vx, vg, vu = (sbp.view(t, sbp.SBP_ACCUMULATE if accumulate else sbp.SBP_LOCAL) for t in out)
+    pre = X.new_empty((2, m, n))   # dG, dU
     if stream is not None:
         pre.record_stream(torch.cuda.ExternalStream(stream))
-    loc = lambda t: sbp.view(t, sbp.SBP_LOCAL)
-    grad = lambda t: sbp.view(t, sbp.SBP_ACCUMULATE if accumulate else sbp.SBP_LOCAL)
-    mine = lambda t: sbp.view(t, sbp.SBP_GLOBAL if tuple(t.shape) == (M, N) else sbp.SBP_LOCAL)
+    at = pre.data_ptr()
+    half = lambda i: sbp.raw_view(at + i * m * n * X.element_size(), m, n, max(n, 1), x.dtype,
+                                  sbp.SBP_LOCAL)
+    mine = lambda t: sbp.view(t, sbp.SBP_GLOBAL if t.shape == (M, N) else sbp.SBP_LOCAL)
     fn = sbp.sbp_nd_gated_bwd if nd else sbp.sbp_gated_bwd
-    fn(mine(dH), L["dy"], sbp.view(X), L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act],
-       mine(G), mine(U), loc(pre[0]), loc(pre[1]), grad(out[0]), grad(out[1]), grad(out[2]), stream,
-       ws)
+    fn(mine(dH), L["dy"], x, L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act], mine(G),
+       mine(U), half(0), half(1), vx, vg, vu, stream, ws)
     return out
 
 

@@ -9,7 +9,7 @@
 // the caller keeps them for the backward pass. H is made of the fp32 sums; G and U are
 // rounded to bf16 as they are stored.
 //
-// Few tiles: the reduction is split, fp32 partials of both projections go to the
+// Few tiles and a long reduction: it is split, fp32 partials of both projections go to the
 // workspace, and a second kernel adds them in split order and applies the gate.
 #include "gated.h"
 #include "gemm_bf16_dma.h"
@@ -129,10 +129,11 @@ void gated_fwd_kernel(GatedArgs g) {
             if (it + 1 < nkb) fill((it + 1) & 1);
         }
     } else {
-        // A workgroup alone on its unit spreads a step's loads over its products (8192 x 8192
-        // -> 4096: 929 -> 888 us); of two, one's loads run beside the other's products
-        // anyway (8192 x 1024 -> 512: 23.6 us at once, 25.7 spread).
-        constexpr bool SPREAD = St::LDS > 81920;
+        // A large tile alone on its unit spreads a step's loads over its products (8192 x 8192
+        // -> 4096: 929 -> 888 us); of two workgroups, one's loads run beside the other's
+        // products anyway (8192 x 1024 -> 512: 23.6 us at once, 25.7 spread), and small tiles
+        // wait for them (one row, 1024 -> 4096: 9.8 and 10.7).
+        constexpr bool SPREAD = St::LDS > 81920 && BM > 64;
         // the loads of step kb: of X, Wg or Wu (part 0 .. 2), or all (-1)
         auto issue = [&](int kb, int stage, int part) {
             char *base = smem + stage * St::BYTES;
@@ -349,9 +350,13 @@ hipError_t launch_gated_fwd(const Gated &a, hipStream_t s) {
     const int64_t kb = (a.k + 63) / 64, nt = (int64_t)g.tiles_m * g.tiles_n;
     const size_t room = a.ws_floats < WS_FLOATS_PREFERRED ? a.ws_floats : WS_FLOATS_PREFERRED;
     const size_t slice = 2 * (size_t)a.m * (size_t)partial_ld(a.n);
+    // Reductions of more than 1024 are split while workgroups are few (one row, 2048 -> 4096: 17.2 us
+    // in two launches, 19.9 whole; 64 rows, 4096 -> 512: 13.3 and 37.4); shorter ones would
+    // only gain what the second launch takes (1024 -> 4096: 11.1 us each way in a graph, 13.6
+    // and 10.9 called one by one, when both were measured).
     int64_t splits = 1;
     const int slots = tile == 0 ? cus : 2 * cus;   // workgroups at a time
-    while (nt * splits * 2 <= slots && kb / (splits * 2) >= 2 && slice * splits * 2 <= room)
+    while (kb > 16 && nt * splits * 2 <= slots && kb / (splits * 2) >= 2 && slice * splits * 2 <= room)
         splits *= 2;
     const int64_t per = kb ? (kb + splits - 1) / splits : 1;
     g.kchunk = (int32_t)(per * 64);

@@ -349,3 +349,41 @@ def test_extreme_scales(scale):
         d[0, h // 2] += torch.mm(P[0, h].t().contiguous(), dO[0, h].double())
         e[0, h // 2] += torch.mm(P[0, h].t().contiguous(), dO[0, h].double().abs())
     assert bool(((g[2].double() - d).abs() <= (2.0 ** -8 + 2.0 ** -14) * (d.abs() + e) + 2.0 ** -14).all())
+
+
+def test_offsets_past_32_bits():
+    # a cache whose second sequence, and whose last rows, lie more than 2^31 elements in
+    gap = 2 ** 31 + 64
+    if torch.cuda.mem_get_info()[0] < 24 << 30:
+        pytest.skip("needs 24 GiB of device memory")
+    S, D = 300, 64
+    # rows 2^23 + 8 elements apart (by 16-byte loads through registers), sequences `gap`
+    big = torch.empty(gap + 512 * 2 ** 14, dtype=BF, device="cuda")
+    wide = torch.empty(S * (2 ** 23 + 8), dtype=BF, device="cuda")
+    Q, dO = rn((2, 4, S, D), 81), rn((2, 4, S, D), 82)
+    K0, V0 = rn((2, 2, S, D), 83), rn((2, 2, S, D), 84)
+    K = big.as_strided((2, 2, S, D), (gap, S * D, D, 1))
+    V = big.as_strided((2, 2, S, D), (gap, S * D, D, 1), 2 * S * D)
+    K.copy_(K0)
+    V.copy_(V0)
+    say("offsets: sequences")
+    O, lse = attention.core_fwd(Q, K, V, causal=True)
+    g = attention.core_bwd(dO, Q, K, V, O, lse, causal=True)
+    O0, lse0 = attention.core_fwd(Q, K0, V0, causal=True)
+    g0 = attention.core_bwd(dO, Q, K0, V0, O0, lse0, causal=True)
+    torch.cuda.synchronize()
+    assert torch.equal(O, O0) and torch.equal(lse, lse0)
+    assert all(torch.equal(a, b) for a, b in zip(g, g0))
+    K = wide.as_strided((1, 2, S, D), (0, D, 2 ** 23 + 8, 1))
+    V = wide.as_strided((1, 2, S, D), (0, D, 2 ** 23 + 8, 1), 2 * D)
+    K.copy_(K0[:1])
+    V.copy_(V0[:1])
+    say("offsets: rows")
+    O, lse = attention.core_fwd(Q[:1], K, V, causal=True)
+    g = attention.core_bwd(dO[:1], Q[:1], K, V, O, lse, causal=True)
+    torch.cuda.synchronize()
+    wO, bO, wl = ref.forward(Q[:1], K0[:1], V0[:1], 0.125, True, 0, None, None)
+    ref.check("O", O, wO, bO)
+    for n, got, (want, bound) in zip(("dQ", "dK", "dV"), g, ref.backward(
+            dO[:1], Q[:1], K0[:1], V0[:1], O, lse, 0.125, True, 0, None, None)):
+        ref.check(n, got, want, bound)

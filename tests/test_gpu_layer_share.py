@@ -199,3 +199,44 @@ def test_layer_captured():
         say("replay", rep)
         assert torch.equal(y, y2) and torch.equal(dx, dx2)
         assert all(torch.equal(grads[n], grads2[n]) for n in WEIGHTS)
+
+
+def test_two_graphs_share_a_workspace():
+    # an attention pass and a gated pass captured into graphs of their own that share one
+    # workspace, replayed in turn on one stream: row statistics go there, and partials
+    B, S, D = 1, 1500, 64
+    rn = lambda shape, seed: inputs.randn(shape, 1.0, seed, BF, "cuda")
+    Q, K, V, dO = (rn((B, 4, S, D), 40 + i) for i in range(4))
+    X, Wg, Wu, dH = rn((40, 4096), 50), rn((4096, 96), 51), rn((4096, 96), 52), rn((40, 96), 53)
+    ws = torch.empty(sbp.SBP_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+
+    def attn():
+        O, lse = attention.core_fwd(Q, K, V, ws=ws)
+        return (O, lse, *attention.core_bwd(dO, Q, K, V, O, lse, ws=ws))
+
+    def gated():
+        H, G, U = linear.gated_fwd("COL", 1, 0, X, Wg, Wu, ws=ws)
+        return (H, G, U, *linear.gated_bwd("COL", 1, 0, dH, X, Wg, Wu, G, U, ws=ws))
+
+    sbp.sbp_profile_begin(32)
+    want = [f() for f in (attn, gated)]
+    names = " ".join(n for n, _ in sbp.sbp_profile_end(32))
+    assert all(n in names for n in ("attn_core_stat", "gated_join"))
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    graphs, got = [torch.cuda.CUDAGraph() for _ in range(2)], []
+    say("capture two")
+    for g, f in zip(graphs, (attn, gated)):
+        with torch.cuda.graph(g, stream=st):
+            got.append(f())
+    for rep in range(3):
+        for out in got:
+            for t in out:
+                t.fill_(9)
+        with torch.cuda.stream(st):
+            torch.cuda.current_stream().wait_stream(torch.cuda.default_stream())
+            for g in (graphs if rep % 2 else graphs[::-1]):
+                g.replay()
+        torch.cuda.synchronize()
+        say("replay", rep)
+        assert all(torch.equal(a, b) for w, o in zip(want, got) for a, b in zip(w, o))

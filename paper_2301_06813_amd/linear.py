@@ -18,6 +18,7 @@ import functools
 import torch
 
 from . import sbp
+from .streams import on_stream
 
 OPS = ("fwd", "bwd_data", "bwd_weight")
 
@@ -234,6 +235,8 @@ def _gated_states(sig: str, p: int, r: int, M: int, K: int, N: int):
 
 
 def _gated_fwd(L, sizes, X, Wg, Wu, act, save, stream, ws):
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, _gated_fwd, L, sizes, X, Wg, Wu, act, save, None, ws)
     _same_device(X, Wg, Wu)
     nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
     m, n = sizes[0], sizes[3]
@@ -247,7 +250,7 @@ def _gated_fwd(L, sizes, X, Wg, Wu, act, save, stream, ws):
     # the fp32 path has no form without the projections in memory
     (G, g), (U, u) = (new(), new()) if save or x.dtype == sbp.SBP_F32 else ((None,) * 2,) * 2
     fn = sbp.sbp_nd_gated_fwd if nd else sbp.sbp_gated_fwd
-    fn(x, L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act], h, g, u, stream, ws)
+    fn(x, L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act], h, g, u, None, ws)
     return (H, G, U) if save else (H, None, None)
 
 

@@ -1,0 +1,95 @@
+"""GPU tests of the torch wrappers' `stream` argument: calls on a stream that is not torch's
+current one, with work of the current stream on both sides of them that reads and writes
+blocks of the sizes that the call allocates."""
+import pytest
+import torch
+
+from paper_2301_06813_amd import inputs, linear
+
+from helpers import say
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+M, K, N = 256, 512, 1024
+
+
+def rn(shape, seed, dtype):
+    return inputs.randn(shape, 1.0, seed, dtype, "cuda")
+
+
+def gated(dtype):
+    return rn((M, K), 1, dtype), rn((K, N), 2, dtype) / 16, rn((K, N), 3, dtype) / 16
+
+
+def gated_fwd(dtype, save):
+    T = gated(dtype)
+    return (lambda **kw: linear.gated_fwd("COL", 1, 0, *T, save=save, **kw)), [(M, N)] * 3, dtype
+
+
+CALLS = {"gated forward, fp32": lambda: gated_fwd(F32, True),
+         "gated forward, fp32, H only": lambda: gated_fwd(F32, False),
+         "gated forward, bf16, H only": lambda: gated_fwd(BF, False)}
+
+
+@pytest.mark.parametrize("name", CALLS)
+def test_given_stream(name):
+    call, blocks, dtype = CALLS[name]()
+    busy = rn((4096, 4096), 9, F32)
+    alloc = lambda: [torch.empty(s, dtype=dtype, device="cuda") for s in blocks]
+    want = [t for t in call() if t is not None]
+    side = torch.cuda.Stream()
+    call(stream=side.cuda_stream)      # the stream's workspace is there
+    torch.cuda.synchronize()
+    for rep in range(3):
+        say(name, "given stream", rep)
+        # the current stream still reads blocks that it has given back when the call starts
+        old = alloc()
+        for i, t in enumerate(old):
+            t.fill_(i + 1)
+        side.wait_stream(torch.cuda.current_stream())
+        for _ in range(8):
+            busy @ busy
+        sums = [t.clone() for t in old]
+        del old, t
+        got = [t for t in call(stream=side.cuda_stream) if t is not None]
+        torch.cuda.synchronize()
+        for i, t in enumerate(sums):
+            assert bool((t == i + 1).all())
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        # the given stream is busy, and the current one fills new blocks after the call
+        with torch.cuda.stream(side):
+            for _ in range(8):
+                busy @ busy
+        got = [t for t in call(stream=side.cuda_stream) if t is not None]
+        new = alloc() + alloc()
+        for t in new:
+            t.fill_(-3)
+        torch.cuda.synchronize()
+        assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
+        assert all(bool((t == -3).all()) for t in new)
+        # dropped while the current stream still uses them
+        got = [t for t in call(stream=side.cuda_stream) if t is not None]
+        torch.cuda.current_stream().wait_stream(side)
+        for _ in range(8):
+            busy @ busy
+        kept = [t.clone() for t in got]
+        del got, t
+        call(stream=side.cuda_stream)
+        with torch.cuda.stream(side):
+            for s in blocks + blocks:
+                torch.empty(s, dtype=dtype, device="cuda").fill_(5)
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(kept, want))
+
+
+def test_the_null_stream():
+    # handle 0 is the null stream, also where another one is current
+    T = gated(F32)
+    want = linear.gated_fwd("COL", 1, 0, *T)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    say("null stream")
+    with torch.cuda.stream(side):
+        got = linear.gated_fwd("COL", 1, 0, *T, stream=0)
+    torch.cuda.default_stream().synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))

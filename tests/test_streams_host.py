@@ -1,0 +1,89 @@
+"""Which stream's memory the torch wrappers allocate when they are given a stream that is not
+torch's current one: on the CPU, with torch's streams and the library's calls replaced by
+records of what was allocated and called where. Skipped wherever a GPU is visible."""
+import contextlib
+
+import pytest
+import torch
+
+from paper_2301_06813_amd import linear, sbp
+
+pytestmark = pytest.mark.skipif(torch.cuda.is_available(), reason="replaces torch's streams")
+CALLER, GIVEN = 7, 9
+BF, F32 = torch.bfloat16, torch.float32
+
+
+class Stream:
+    def __init__(self, handle):
+        self.cuda_stream = handle
+
+
+class Record:
+    """Allocations (memory range, stream), library calls (stream, pointers), recorded uses."""
+
+    def __init__(self, monkeypatch):
+        self.stream, self.blocks, self.calls, self.uses, self.kept = CALLER, [], [], [], []
+        patch = monkeypatch.setattr
+
+        @contextlib.contextmanager
+        def inside(s):
+            was, self.stream = self.stream, s.cuda_stream
+            yield
+            self.stream = was
+
+        patch(sbp, "current_stream", lambda: self.stream)
+        patch(torch.cuda, "current_stream", lambda *a: Stream(self.stream))
+        patch(torch.cuda, "default_stream", lambda *a: Stream(0))
+        patch(torch.cuda, "ExternalStream", Stream)
+        patch(torch.cuda, "stream", inside)
+        patch(torch.cuda, "current_device", lambda: None)
+        patch(torch.Tensor, "new_empty", self.allocating(torch.Tensor.new_empty))
+        patch(torch.Tensor, "record_stream",
+              lambda t, s: self.uses.append((t.data_ptr(), s.cuda_stream)))
+        for name in ("sbp_gated_fwd",):
+            patch(sbp, name, self.library_call)
+
+    def allocating(self, make):
+        def new(*a, **kw):
+            kw.pop("device", None)
+            t = make(*a, **kw)
+            self.kept.append(t)    # no address comes twice
+            self.blocks.append((t.data_ptr(), t.numel() * t.element_size(), self.stream))
+            return t
+        return new
+
+    def library_call(self, *args):
+        stream, ws = args[-2:]
+        views = [a.data for a in args if isinstance(a, (sbp.sbp_view_t, sbp.sbp_view4_t))]
+        if isinstance(ws, torch.Tensor):
+            views.append(ws.data_ptr())
+        self.calls.append((self.stream if stream is None else stream, views))
+
+    def check(self, out, inputs, stream):
+        """Everything that the call wrote to is of `stream`'s memory, it ran there, and what
+        it returned is recorded for the caller's stream (another one than `stream`)."""
+        (ran, views), = self.calls
+        assert ran == stream
+        given = {t.data_ptr() for t in inputs}
+        written = [v for v in views if v not in given]
+        assert written
+        for v in written:
+            owner, = [s for at, n, s in self.blocks if at <= v < at + n]
+            assert owner == stream
+        for t in out:
+            assert t is None or stream == CALLER or (t.data_ptr(), CALLER) in self.uses
+        assert self.stream == CALLER
+
+
+def gated(dtype):
+    return (torch.zeros((6, 8), dtype=dtype), torch.zeros((8, 4), dtype=dtype),
+            torch.zeros((8, 4), dtype=dtype))
+
+
+@pytest.mark.parametrize("stream", [None, CALLER, GIVEN, 0])
+@pytest.mark.parametrize("save", [True, False])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_gated_forward(monkeypatch, dtype, save, stream):
+    r, T = Record(monkeypatch), gated(dtype)
+    out = linear.gated_fwd("COL", 1, 0, *T, save=save, stream=stream)
+    r.check(out, T, CALLER if stream is None else stream)

@@ -266,6 +266,9 @@ def gated_bwd_L(L: dict, dH, X, Wg, Wu, G, U, act: str = "silu", out=None, grad_
 
 
 def _gated_bwd(L, sizes, dH, X, Wg, Wu, G, U, act, out, grad_dtype, accumulate, stream, ws):
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, _gated_bwd, L, sizes, dH, X, Wg, Wu, G, U, act, out, grad_dtype,
+                         accumulate, None, ws)
     _same_device(dH, X, Wg, Wu, G, U, *(out or ()))
     nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
     M, N = X.shape[0], Wg.shape[1]
@@ -287,15 +290,13 @@ def _gated_bwd(L, sizes, dH, X, Wg, Wu, G, U, act, out, grad_dtype, accumulate, 
     else:
         vx, vg, vu = (sbp.view(t, sbp.SBP_ACCUMULATE if accumulate else sbp.SBP_LOCAL) for t in out)
     pre = X.new_empty((2, m, n))   # dG, dU
-    if stream is not None:
-        pre.record_stream(torch.cuda.ExternalStream(stream))
     at = pre.data_ptr()
     half = lambda i: sbp.raw_view(at + i * m * n * X.element_size(), m, n, max(n, 1), x.dtype,
                                   sbp.SBP_LOCAL)
     mine = lambda t: sbp.view(t, sbp.SBP_GLOBAL if t.shape == (M, N) else sbp.SBP_LOCAL)
     fn = sbp.sbp_nd_gated_bwd if nd else sbp.sbp_gated_bwd
     fn(mine(dH), L["dy"], x, L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.ACTS[act], mine(G),
-       mine(U), half(0), half(1), vx, vg, vu, stream, ws)
+       mine(U), half(0), half(1), vx, vg, vu, None, ws)
     return out
 
 

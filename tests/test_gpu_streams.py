@@ -26,9 +26,18 @@ def gated_fwd(dtype, save):
     return (lambda **kw: linear.gated_fwd("COL", 1, 0, *T, save=save, **kw)), [(M, N)] * 3, dtype
 
 
+def gated_bwd(dtype):
+    T, dH = gated(dtype), rn((M, N), 4, dtype)
+    _, G, U = linear.gated_fwd("COL", 1, 0, *T)
+    return (lambda **kw: linear.gated_bwd("COL", 1, 0, dH, *T, G, U, **kw)), \
+        [(2, M, N), (M, K), (K, N), (K, N)], dtype
+
+
 CALLS = {"gated forward, fp32": lambda: gated_fwd(F32, True),
          "gated forward, fp32, H only": lambda: gated_fwd(F32, False),
-         "gated forward, bf16, H only": lambda: gated_fwd(BF, False)}
+         "gated forward, bf16, H only": lambda: gated_fwd(BF, False),
+         "gated backward, bf16": lambda: gated_bwd(BF),
+         "gated backward, fp32": lambda: gated_bwd(F32)}
 
 
 @pytest.mark.parametrize("name", CALLS)

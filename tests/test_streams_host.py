@@ -40,7 +40,7 @@ class Record:
         patch(torch.Tensor, "new_empty", self.allocating(torch.Tensor.new_empty))
         patch(torch.Tensor, "record_stream",
               lambda t, s: self.uses.append((t.data_ptr(), s.cuda_stream)))
-        for name in ("sbp_gated_fwd",):
+        for name in ("sbp_gated_fwd", "sbp_gated_bwd"):
             patch(sbp, name, self.library_call)
 
     def allocating(self, make):
@@ -87,3 +87,16 @@ def test_gated_forward(monkeypatch, dtype, save, stream):
     r, T = Record(monkeypatch), gated(dtype)
     out = linear.gated_fwd("COL", 1, 0, *T, save=save, stream=stream)
     r.check(out, T, CALLER if stream is None else stream)
+
+
+@pytest.mark.parametrize("stream", [None, CALLER, GIVEN, 0])
+@pytest.mark.parametrize("given", [False, True], ids=["new outputs", "given outputs"])
+@pytest.mark.parametrize("dtype", [BF, F32])
+def test_gated_backward(monkeypatch, dtype, given, stream):
+    X, Wg, Wu = gated(dtype)
+    dH, G, U = (torch.zeros((6, 4), dtype=dtype) for _ in range(3))
+    out = [torch.zeros(t.shape, dtype=dtype) for t in (X, Wg, Wu)] if given else None
+    r = Record(monkeypatch)
+    got = linear.gated_bwd("COL", 1, 0, dH, X, Wg, Wu, G, U, out=out, stream=stream)
+    r.check(got, (X, Wg, Wu, dH, G, U, *(out or ())), CALLER if stream is None else stream)
+    assert not given or all(a is b for a, b in zip(got, out))

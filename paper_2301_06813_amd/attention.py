@@ -11,11 +11,13 @@ backward call's O, lse and dO may be either.
 """
 from __future__ import annotations
 
+import functools
 import math
 
 import torch
 
 from . import sbp
+from .streams import on_stream
 
 _EMPTY = torch.empty
 
@@ -75,6 +77,10 @@ def core_fwd(Q, K, V, p: int = 1, r: int = 0, *, scale=None, causal: bool = Fals
     """(O, lse): O [batch][local heads][rows][head_dim] in Q's dtype (or out_dtype, or
     the given tensor `out`) and the rows' log-sum-exp [batch][local heads][rows] in
     fp32, which the backward pass reads (None with lse=False)."""
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, functools.partial(
+            core_fwd, scale=scale, causal=causal, window=window, len_q=len_q, len_k=len_k, lse=lse,
+            out=out, out_dtype=out_dtype, scope=scope, ws=ws), Q, K, V, p, r)
     B, H, sq, D = Q.shape
     _same_device(Q, K, V, len_q, len_k, out)
     hq = rank_heads(H, K.shape[1], p, r)[1] if scope == sbp.SBP_GLOBAL else H
@@ -88,7 +94,7 @@ def core_fwd(Q, K, V, p: int = 1, r: int = 0, *, scale=None, causal: bool = Fals
                            sbp.SBP_LOCAL) if lse else None
     sbp.sbp_attn_core_fwd(sbp.view4(Q, scope), sbp.view4(K, scope), sbp.view4(V, scope),
                           _opts(Q, scale, causal, window, len_q, len_k),
-                          o, rows, p, r, stream, ws)
+                          o, rows, p, r, None, ws)
     return out, z
 
 
@@ -103,6 +109,11 @@ def core_bwd(dO, Q, K, V, O, lse, p: int = 1, r: int = 0, *, scale=None, causal:
     """(dQ, dK, dV) of rank r's heads, in the inputs' dtype (or grad_dtype), or in the
     three given tensors `out` (accumulate: added to their fp32 contents). lse is
     [batch][heads][rows] as core_fwd returns it."""
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, functools.partial(
+            core_bwd, scale=scale, causal=causal, window=window, len_q=len_q, len_k=len_k, out=out,
+            grad_dtype=grad_dtype, accumulate=accumulate, scope=scope, ws=ws), dO, Q, K, V, O, lse,
+            p, r)
     B, H, sq, D = Q.shape
     Hk, sk = K.shape[1:3]
     _same_device(dO, Q, K, V, O, lse, len_q, len_k, *(out or ()))
@@ -120,10 +131,8 @@ def core_bwd(dO, Q, K, V, O, lse, p: int = 1, r: int = 0, *, scale=None, causal:
     if ws is None and need > sbp.SBP_WORKSPACE_BYTES:
         # more rows than the kept workspace has room for: one of this call's own
         ws = _EMPTY(need, dtype=torch.uint8, device=Q.device)
-        if stream is not None:
-            ws.record_stream(torch.cuda.ExternalStream(stream))
     sbp.sbp_attn_core_bwd(_local(dO, H, scope), sbp.view4(Q, scope), sbp.view4(K, scope),
                           sbp.view4(V, scope), _local(O, H, scope), _rows(lse, H, scope),
-                          _opts(Q, scale, causal, window, len_q, len_k), vq, vk, vv, p, r, stream,
+                          _opts(Q, scale, causal, window, len_q, len_k), vq, vk, vv, p, r, None,
                           ws)
     return out

@@ -4,7 +4,7 @@ blocks of the sizes that the call allocates."""
 import pytest
 import torch
 
-from paper_2301_06813_amd import inputs, linear
+from paper_2301_06813_amd import attention, inputs, linear, sbp
 
 from helpers import say
 
@@ -33,11 +33,28 @@ def gated_bwd(dtype):
         [(2, M, N), (M, K), (K, N), (K, N)], dtype
 
 
+def heads():
+    return [rn((2, h, 300, 64), 5 + i, BF) for i, h in enumerate((8, 2, 2, 8))]
+
+
+def attn_fwd():
+    Q, K, V, _ = heads()
+    return (lambda **kw: attention.core_fwd(Q, K, V, causal=True, **kw)), [Q.shape], BF
+
+
+def attn_bwd():
+    Q, K, V, dO = heads()
+    O, lse = attention.core_fwd(Q, K, V, causal=True)
+    return (lambda **kw: attention.core_bwd(dO, Q, K, V, O, lse, causal=True, **kw)), \
+        [Q.shape, K.shape, V.shape], BF
+
+
 CALLS = {"gated forward, fp32": lambda: gated_fwd(F32, True),
          "gated forward, fp32, H only": lambda: gated_fwd(F32, False),
          "gated forward, bf16, H only": lambda: gated_fwd(BF, False),
          "gated backward, bf16": lambda: gated_bwd(BF),
-         "gated backward, fp32": lambda: gated_bwd(F32)}
+         "gated backward, fp32": lambda: gated_bwd(F32),
+         "attention forward": attn_fwd, "attention backward": attn_bwd}
 
 
 @pytest.mark.parametrize("name", CALLS)
@@ -102,3 +119,27 @@ def test_the_null_stream():
         got = linear.gated_fwd("COL", 1, 0, *T, stream=0)
     torch.cuda.default_stream().synchronize()
     assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_workspace_of_a_call(monkeypatch):
+    # more query rows than the kept workspace holds statistics of: the call brings its own
+    call, blocks, _ = attn_bwd()
+    need = attention.bwd_workspace_bytes(2, 8, 300)
+    want = call(ws=torch.empty(need, dtype=torch.uint8, device="cuda"))
+    busy = rn((4096, 4096), 9, F32)
+    side = torch.cuda.Stream()
+    monkeypatch.setattr(sbp, "SBP_WORKSPACE_BYTES", need - 32)
+    torch.cuda.synchronize()
+    for rep in range(3):
+        say("workspace of a call", rep)
+        old = torch.full((need,), 7, dtype=torch.uint8, device="cuda")
+        side.wait_stream(torch.cuda.current_stream())
+        for _ in range(8):
+            busy @ busy
+        kept = old.clone()
+        del old
+        got = call(stream=side.cuda_stream)
+        new = [torch.full((need,), 9, dtype=torch.uint8, device="cuda") for _ in range(4)]
+        torch.cuda.synchronize()
+        assert bool((kept == 7).all()) and all(bool((t == 9).all()) for t in new)
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

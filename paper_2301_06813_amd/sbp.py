@@ -353,7 +353,13 @@ def _kept_workspace(stream):
     key = (device, int(stream or 0))
     kept = _default_ws.get(key)
     if kept is None:
-        t = torch.empty(SBP_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+        make = lambda: torch.empty(SBP_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
+        if key[1] == int(current_stream() or 0):
+            t = make()
+        else:   # of `stream`'s memory: the current stream's work may still use a block of its own
+            from .streams import torch_stream
+            with torch.cuda.stream(torch_stream(key[1])):
+                t = make()
         kept = _default_ws[key] = (t, workspace(t))
     return kept
 

@@ -4,7 +4,7 @@ from __future__ import annotations
 import torch
 
 
-def _torch_stream(handle: int):
+def torch_stream(handle: int):
     return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
 
 
@@ -18,7 +18,7 @@ def on_stream(stream: int, call, *args):
     the call returns are the caller's to use once its stream waits for `stream`: they are
     recorded there, so that dropping them keeps their memory until that use is over."""
     caller = torch.cuda.current_stream()
-    with torch.cuda.stream(_torch_stream(stream)):
+    with torch.cuda.stream(torch_stream(stream)):
         out = call(*args)
     for t in out:
         if isinstance(t, torch.Tensor):

@@ -143,3 +143,36 @@ def test_workspace_of_a_call(monkeypatch):
         torch.cuda.synchronize()
         assert bool((kept == 7).all()) and all(bool((t == 9).all()) for t in new)
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_first_call_on_a_stream():
+    # the workspace that is kept for a stream is allocated by its first call: not from a
+    # block that the current stream has given back and still reads
+    T = rn((16, 8192), 1, BF), rn((8192, 64), 2, BF), rn((8192, 64), 3, BF)   # a split reduction
+    want = linear.gated_fwd("COL", 1, 0, *T)
+    busy = rn((4096, 4096), 9, F32)
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    say("first call")
+    old = torch.full((sbp.SBP_WORKSPACE_BYTES,), 7, dtype=torch.uint8, device="cuda")
+    side.wait_stream(torch.cuda.current_stream())
+    for _ in range(8):
+        busy @ busy
+    kept = old.clone()
+    del old
+    got = linear.gated_fwd("COL", 1, 0, *T, stream=side.cuda_stream)
+    L = linear.layouts("COL", 1, 0)
+    H = torch.empty((16, 64), dtype=BF, device="cuda")
+    torch.cuda.synchronize()
+    other = torch.cuda.Stream()
+    old = torch.full((sbp.SBP_WORKSPACE_BYTES,), 7, dtype=torch.uint8, device="cuda")
+    other.wait_stream(torch.cuda.current_stream())
+    for _ in range(8):
+        busy @ busy
+    kept2 = old.clone()
+    del old
+    sbp.sbp_gated_fwd(sbp.view(T[0]), L["x"], sbp.view(T[1]), sbp.view(T[2]), L["w"],
+                      sbp.SBP_ACT_SILU, sbp.view(H, sbp.SBP_LOCAL), stream=other.cuda_stream)
+    torch.cuda.synchronize()
+    assert bool((kept == 7).all()) and bool((kept2 == 7).all())
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(H, want[0])

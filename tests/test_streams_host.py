@@ -40,7 +40,10 @@ class Record:
         patch(torch.Tensor, "new_empty", self.allocating(torch.Tensor.new_empty))
         patch(torch.Tensor, "record_stream",
               lambda t, s: self.uses.append((t.data_ptr(), s.cuda_stream)))
-        patch(attention, "_EMPTY", self.allocating(torch.empty))
+        empty = self.allocating(torch.empty)
+        patch(torch, "empty", empty)
+        patch(attention, "_EMPTY", empty)
+        patch(sbp, "_default_ws", {})
         for name in ("sbp_gated_fwd", "sbp_gated_bwd", "sbp_attn_core_fwd", "sbp_attn_core_bwd"):
             patch(sbp, name, self.library_call)
 
@@ -130,3 +133,15 @@ def test_attention_backward(monkeypatch, own, stream):
     got = attention.core_bwd(dO, Q, K, V, O, lse, scale=0.5, stream=stream)
     r.check(got, (Q, K, V, dO, O, lse), CALLER if stream is None else stream)
     assert len(r.blocks) == 3 + own
+
+
+def test_kept_workspace(monkeypatch):
+    # of the stream's own memory, whichever stream is current when it is first needed
+    monkeypatch.setattr(sbp, "SBP_WORKSPACE_BYTES", 4096)
+    r = Record(monkeypatch)
+    for stream in (GIVEN, 0, CALLER):
+        ws = sbp.default_workspace(stream)
+        (at, _, owner), = [b for b in r.blocks if b[0] == ws.data]
+        assert owner == stream and r.stream == CALLER
+        assert sbp.default_workspace(stream).data == at
+    assert len(r.blocks) == 3

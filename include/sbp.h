@@ -46,8 +46,12 @@
  *     the fp32 partials of split reductions; see below. Every call can be
  *     captured into a HIP graph, including the first on a stream.
  *   - Thread safety: calls on different host threads are safe. Two calls
- *     may share a workspace only if they cannot run at the same time (e.g.
- *     they are on the same stream).
+ *     may share a workspace only if neither their launches can run at the
+ *     same time nor the calls themselves: a call may enqueue several
+ *     launches that pass data through it, so calls on one stream share one
+ *     if the host makes them one after the other (a graph that was captured
+ *     with it counts as a call wherever it is replayed), and host threads
+ *     that make calls at the same time bring workspaces of their own.
  */
 #ifndef SBP_H
 #define SBP_H

@@ -19,6 +19,7 @@ from __future__ import annotations
 
 import ctypes
 import os
+import threading
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(HERE, "libsbp.so")
@@ -339,7 +340,11 @@ def _forget_stream():
 os.register_at_fork(after_in_child=_forget_stream)
 
 
-_default_ws = {}   # (device, stream) -> (tensor, its sbp_workspace_t)
+# (device, stream, host thread) -> (tensor, its sbp_workspace_t). Stream order alone does not
+# let threads share one: a call may enqueue several launches that pass data through the
+# workspace, and ctypes lets another thread's call run between them. Kept for good, since
+# a captured graph may hold the address.
+_default_ws = {}
 
 
 def workspace(t) -> sbp_workspace_t:
@@ -350,7 +355,7 @@ def workspace(t) -> sbp_workspace_t:
 def _kept_workspace(stream):
     import torch
     device = _raw_stream[1]() if _raw_stream else torch.cuda.current_device()
-    key = (device, int(stream or 0))
+    key = (device, int(stream or 0), threading.get_ident())
     kept = _default_ws.get(key)
     if kept is None:
         make = lambda: torch.empty(SBP_WORKSPACE_BYTES, dtype=torch.uint8, device="cuda")
@@ -365,9 +370,9 @@ def _kept_workspace(stream):
 
 
 def default_workspace(stream) -> sbp_workspace_t:
-    """This module's workspace for (current device, stream): SBP_WORKSPACE_BYTES
-    allocated with torch on first use and kept (calls on one stream run in
-    order, so they can share it)."""
+    """This module's workspace for (current device, stream, calling thread):
+    SBP_WORKSPACE_BYTES allocated with torch on first use and kept (one thread's
+    calls on one stream run one after the other, so they can share it)."""
     return workspace(_kept_workspace(stream)[0])
 
 

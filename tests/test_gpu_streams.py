@@ -1,6 +1,8 @@
 """GPU tests of the torch wrappers' `stream` argument: calls on a stream that is not torch's
 current one, with work of the current stream on both sides of them that reads and writes
 blocks of the sizes that the call allocates."""
+import threading
+
 import pytest
 import torch
 
@@ -176,3 +178,45 @@ def test_first_call_on_a_stream():
     torch.cuda.synchronize()
     assert bool((kept == 7).all()) and bool((kept2 == 7).all())
     assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(H, want[0])
+
+
+def test_two_threads_on_one_stream():
+    # calls of several launches that pass data through the kept workspace, made by two host
+    # threads at once: row statistics and split partials must be the call's own
+    work = []
+    for seed in (20, 40):
+        Q, K, V, dO = (rn((1, h, s, 64), seed + i, BF) for i, (h, s) in
+                       enumerate(((8, 40), (2, 3000), (2, 3000), (8, 40))))
+        X, Wg, Wu, dH = (rn(s, seed + 5 + i, BF) for i, s in
+                         enumerate(((16, 4096), (4096, 96), (4096, 96), (16, 96))))
+
+        def calls(Q=Q, K=K, V=V, dO=dO, X=X, Wg=Wg, Wu=Wu, dH=dH):
+            O, lse = attention.core_fwd(Q, K, V)
+            H, G, U = linear.gated_fwd("COL", 1, 0, X, Wg, Wu)
+            return (O, lse, *attention.core_bwd(dO, Q, K, V, O, lse), H, G, U,
+                    *linear.gated_bwd("COL", 1, 0, dH, X, Wg, Wu, G, U))
+
+        work.append(calls)
+    sbp.sbp_profile_begin(64)
+    want = [f() for f in work]
+    names = " ".join(n for n, _ in sbp.sbp_profile_end(64))
+    assert all(n in names for n in ("core_join", "core_stat", "core_sum", "gated_join"))
+    torch.cuda.synchronize()
+    start, got = threading.Barrier(2), [[], []]
+
+    def run(i):
+        start.wait(30)
+        for _ in range(100):
+            got[i].append(work[i]())
+
+    say("two threads")
+    threads = [threading.Thread(target=run, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(100)
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert len(got[i]) == 100
+        for out in got[i]:
+            assert all(torch.equal(a, b) for a, b in zip(out, want[i]))

@@ -2,6 +2,7 @@
 torch's current one: on the CPU, with torch's streams and the library's calls replaced by
 records of what was allocated and called where. Skipped wherever a GPU is visible."""
 import contextlib
+import threading
 
 import pytest
 import torch
@@ -145,3 +146,24 @@ def test_kept_workspace(monkeypatch):
         assert owner == stream and r.stream == CALLER
         assert sbp.default_workspace(stream).data == at
     assert len(r.blocks) == 3
+
+
+def test_threads_keep_workspaces_of_their_own(monkeypatch):
+    # two threads that are there at once, on one stream: a call's launches may come between
+    # those of the other's call
+    monkeypatch.setattr(sbp, "SBP_WORKSPACE_BYTES", 4096)
+    Record(monkeypatch)
+    found, both = {}, threading.Barrier(2)
+
+    def work(i):
+        found[i] = [sbp.default_workspace(CALLER).data for _ in range(2)]
+        both.wait(30)
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(2)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+    mine = sbp.default_workspace(CALLER).data
+    assert found[0][0] == found[0][1] and found[1][0] == found[1][1]
+    assert len({found[0][0], found[1][0], mine}) == 3

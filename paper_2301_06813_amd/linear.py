@@ -159,6 +159,8 @@ def run_bwd_L(L: dict, X, W, dY, dX, dW, stream=None, accumulate_dw=False, ws=No
 
 def call_bwd(sig: str, p: int, r: int, X, W, dY, stream=None):
     """Allocate dX and dW and run both backward products; returns (dX, dW, states)."""
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, call_bwd, sig, p, r, X, W, dY)
     M, K = X.shape
     N = W.shape[1]
     dX = alloc_out("bwd_data", sig, p, r, M, K, N, X.dtype, X.device)
@@ -169,6 +171,8 @@ def call_bwd(sig: str, p: int, r: int, X, W, dY, stream=None):
 
 def call(op: str, sig: str, p: int, r: int, X, W, dY, stream=None):
     """Allocate the output and run; returns (out, state)."""
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, call, op, sig, p, r, X, W, dY)
     ref = X if X is not None else dY
     M = (X if X is not None else dY).shape[0]
     K = X.shape[1] if X is not None else W.shape[0]
@@ -181,6 +185,8 @@ def call(op: str, sig: str, p: int, r: int, X, W, dY, stream=None):
 def call_nd(op: str, factors, mesh, coord, X, W, dY, stream=None):
     """nd form of call: the device at mesh coordinate coord under the per-axis
     factors; returns (out, nd state)."""
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, call_nd, op, factors, mesh, coord, X, W, dY)
     L = nd_layouts(factors, mesh, coord)
     ref = X if X is not None else dY
     M = ref.shape[0]
@@ -193,6 +199,8 @@ def call_nd(op: str, factors, mesh, coord, X, W, dY, stream=None):
 
 def call_bwd_nd(factors, mesh, coord, X, W, dY, stream=None):
     """nd form of call_bwd; returns (dX, dW, states)."""
+    if stream is not None and stream != sbp.current_stream():
+        return on_stream(stream, call_bwd_nd, factors, mesh, coord, X, W, dY)
     L = nd_layouts(factors, mesh, coord)
     M, K = X.shape
     N = W.shape[1]

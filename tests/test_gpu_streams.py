@@ -51,12 +51,24 @@ def attn_bwd():
         [Q.shape, K.shape, V.shape], BF
 
 
+def linear_fwd():
+    X, W, _ = gated(BF)
+    return (lambda **kw: linear.call("fwd", "COL", 1, 0, X, W, None, **kw)[:1]), [(M, N)], BF
+
+
+def linear_bwd():
+    (X, W, _), dY = gated(F32), rn((M, N), 4, F32)
+    return (lambda **kw: linear.call_bwd_nd(("COL", "DP"), (1, 1), (0, 0), X, W, dY, **kw)[:2]), \
+        [(M, K), (K, N)], F32
+
+
 CALLS = {"gated forward, fp32": lambda: gated_fwd(F32, True),
          "gated forward, fp32, H only": lambda: gated_fwd(F32, False),
          "gated forward, bf16, H only": lambda: gated_fwd(BF, False),
          "gated backward, bf16": lambda: gated_bwd(BF),
          "gated backward, fp32": lambda: gated_bwd(F32),
-         "attention forward": attn_fwd, "attention backward": attn_bwd}
+         "attention forward": attn_fwd, "attention backward": attn_bwd,
+         "linear forward": linear_fwd, "linear backward on a mesh, fp32": linear_bwd}
 
 
 @pytest.mark.parametrize("name", CALLS)

@@ -45,7 +45,8 @@ class Record:
         patch(torch, "empty", empty)
         patch(attention, "_EMPTY", empty)
         patch(sbp, "_default_ws", {})
-        for name in ("sbp_gated_fwd", "sbp_gated_bwd", "sbp_attn_core_fwd", "sbp_attn_core_bwd"):
+        for name in ("sbp_gated_fwd", "sbp_gated_bwd", "sbp_attn_core_fwd", "sbp_attn_core_bwd",
+                     "sbp_linear_fwd", "sbp_linear_bwd", "sbp_nd_linear_fwd", "sbp_nd_linear_bwd"):
             patch(sbp, name, self.library_call)
 
     def allocating(self, make):
@@ -167,3 +168,16 @@ def test_threads_keep_workspaces_of_their_own(monkeypatch):
     mine = sbp.default_workspace(CALLER).data
     assert found[0][0] == found[0][1] and found[1][0] == found[1][1]
     assert len({found[0][0], found[1][0], mine}) == 3
+
+
+@pytest.mark.parametrize("stream", [None, CALLER, GIVEN, 0])
+@pytest.mark.parametrize("nd", [False, True], ids=["1-D", "mesh"])
+def test_linear(monkeypatch, nd, stream):
+    X, W, dY = torch.zeros((6, 8)), torch.zeros((8, 4)), torch.zeros((6, 4))
+    at = (("COL", "DP"), (1, 1), (0, 0)) if nd else ("COL", 1, 0)
+    fwd, bwd = (linear.call_nd, linear.call_bwd_nd) if nd else (linear.call, linear.call_bwd)
+    for make in (lambda: fwd("fwd", *at, X, W, None, stream=stream)[:1],
+                 lambda: bwd(*at, X, W, dY, stream=stream)[:2]):
+        with monkeypatch.context() as m:
+            r = Record(m)
+            r.check(make(), (X, W, dY), CALLER if stream is None else stream)

@@ -393,7 +393,10 @@ __device__ __forceinline__ void attn_core_dq(const BwdArgs &f, int wg, char *sme
                         : whole ? (int64_t)b * a.dq.sb + head * a.dq.sh + (int64_t)i * a.dq.ld
                                 : (((int64_t)split * a.batch * a.kv_heads + bh) * f.rows + row) * d4;
     float *const put = reinterpret_cast<float *>(smem);
-    stage_rows<DP>(put + wave * PUT_FLOATS<DP>, o, whole ? a.scale : 1.f, lane);
+    // rows past the sequence's length or without keys: zero, though values that are not finite
+    // may have reached their sums as 0 x infinity
+    const bool some = live && lo < hi;
+    stage_rows<DP>(put + wave * PUT_FLOATS<DP>, o, !some ? 0.f : whole ? a.scale : 1.f, lane);
     __syncthreads();
     store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
 }

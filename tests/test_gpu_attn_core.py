@@ -387,3 +387,30 @@ def test_offsets_past_32_bits():
     for n, got, (want, bound) in zip(("dQ", "dK", "dV"), g, ref.backward(
             dO[:1], Q[:1], K0[:1], V0[:1], O, lse, 0.125, True, 0, None, None)):
         ref.check(n, got, want, bound)
+
+
+@pytest.mark.parametrize("bad", [float("inf"), float("nan")], ids=["inf", "nan"])
+@pytest.mark.parametrize("dims", [(2, 4, 2, 70, 90, 64), (2, 2, 1, 130, 200, 128), (1, 2, 2, 40, 4000, 64),
+                                  (2, 4, 2, 70, 90, 44)], ids=["64", "128", "split", "unaligned"])
+def test_rows_without_keys_beside_values_that_are_not_finite(dims, bad):
+    # rows past their sequence's length, and rows that the mask leaves nothing, have zero
+    # results whatever the keys and values inside the lengths hold; accumulated gradients stay
+    B, H, Hk, sq, sk, D = dims
+    Q, K, V, dO = tensors(*dims, 140)
+    K[:, :, 2], V[:, :, 5] = bad, bad
+    for nq, nk, causal, dead in ((sq - 9, sk - 30, False, slice(sq - 9, sq)),
+                                 (sq - 9, sk, True, slice(sq - 9, sq)),
+                                 (sq, sq - 20, True, slice(0, 20))):
+        kw = dict(causal=causal, len_q=lens([nq] * B), len_k=lens([nk] * B))
+        say("not finite", dims, bad, nq, nk, causal)
+        O, lse = attention.core_fwd(Q, K, V, **kw)
+        assert bool((O[:, :, dead] == 0).all()) and bool((lse[:, :, dead] == -math.inf).all())
+        O0, lse0 = attention.core_fwd(Q, torch.zeros_like(K), torch.zeros_like(V), **kw)
+        dQ, dK, dV = attention.core_bwd(dO, Q, K, V, O0, lse0, **kw)
+        assert bool((dQ[:, :, dead] == 0).all())
+        assert bool((dK[:, :, nk:] == 0).all()) and bool((dV[:, :, nk:] == 0).all())
+        old = [rn(t.shape, 150 + i, F32) for i, t in enumerate((Q, K, V))]
+        out = [t.clone() for t in old]
+        attention.core_bwd(dO, Q, K, V, O0, lse0, out=out, accumulate=True, **kw)
+        assert torch.equal(out[0][:, :, dead], old[0][:, :, dead])
+        assert all(torch.equal(a[:, :, nk:], b[:, :, nk:]) for a, b in zip(out[1:], old[1:]))

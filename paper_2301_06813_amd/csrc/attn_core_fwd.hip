@@ -10,7 +10,10 @@
 // broadcast, and P^T goes from the exponentials into the second product without
 // leaving its registers.
 //
-//   * exp(scale (s - m)) is one multiply-add and one base-2 exponential a score.
+//   * exp(scale (s - m)) is one multiply-add and one base-2 exponential a score. That
+//     multiply-add takes off m's product rounded, which is as good as the difference while
+//     the product is small; where it is not (FAR) the difference is formed first, so that
+//     the largest score has the weight 1 however large it is.
 //     The maximum is moved only when a row's grows by more than 8 in the exponent:
 //     until then sums and outputs grow by up to 2^8, far inside fp32, and rescaling
 //     is skipped by the whole wave.
@@ -62,6 +65,10 @@ __device__ __forceinline__ void store4(void *base, int64_t at, int col, int d, b
             if (col + e < d) p[e] = f32_to_bf16_bits(value(e));
     }
 }
+
+// Exponents of base 2 beyond which a wave forms differences of scores first: the rounding of
+// m c is at most 2^-15 below it.
+constexpr float FAR = 1024.f;
 
 struct FwdArgs {
     CoreArgs a;
@@ -203,6 +210,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
     const float c = a.scale * LOG2E;
     const float grow = 8.f / c;
     float m = -INFINITY, l = 0.f;
+    float mc = 0.f, limit = -INFINITY;   // what exponents add to s c; where the maximum moves
     f32x16 o[DB];
 #pragma unroll
     for (int x = 0; x < DB; ++x) o[x] = splat16(0.f);
@@ -236,20 +244,30 @@ void attn_core_fwd_kernel(FwdArgs f) {
         const int key = k0 + 8 * (r >> 2) + 4 * half + (r & 3);
         s[r] = key >= lo && key < hi ? s[r] : -INFINITY;
     };
-    // Moves the maximum to `top`, a lane's own scores' maximum, where it grew by enough.
-    auto rise = [&](float top) __attribute__((always_inline)) {
+    // Moves the maximum to `top`, the maximum of a lane's own scores s, where it grew by enough.
+    // Where a row's is FAR, s become differences from it, and every block comes here.
+    auto rise = [&](f32x16 &s, float top) __attribute__((always_inline)) {
         float t0, t1;
         halves(top, &t0, &t1);
         top = fmaxf(t0, t1);
-        if (__any(top > m + grow)) {
+        if (__any(top > limit)) {
             const float mn = fmaxf(m, top);
             const float x = mn == -INFINITY ? 1.f : exp2_((m - mn) * c);
             m = mn;
+            limit = m + grow;
+            mc = m == -INFINITY ? 0.f : -m * c;
             l *= x;
 #pragma unroll
             for (int db = 0; db < DB; ++db)
 #pragma unroll
                 for (int r = 0; r < 16; ++r) o[db][r] *= x;
+            if (__any(fabsf(mc) > FAR)) {
+                const float base = m == -INFINITY ? 0.f : m;
+#pragma unroll
+                for (int r = 0; r < 16; ++r) s[r] -= base;
+                mc = 0.f;
+                limit = -INFINITY;
+            }
         }
     };
     // Waits for the step after x, and prepares the load of a later one.
@@ -283,7 +301,6 @@ void attn_core_fwd_kernel(FwdArgs f) {
             const int now = TURN ? kb & 1 : 0;
             f32x16 &s = sp[now], &s_n = sp[ONE - now];
             bf16x8 tv[2][DB], p[2];
-            const float mc = m == -INFINITY ? 0.f : -m * c;
             __builtin_amdgcn_sched_barrier(0);
             __builtin_amdgcn_s_setprio(1);
             scores(s_n, nx, last ? 0 : (kb + 1) * 32, [&](int part) __attribute__((always_inline)) {
@@ -322,7 +339,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
                     }
                     __builtin_amdgcn_sched_barrier(0);
                 }
-            if (!last || x + 1 < s1) rise(top);
+            if (!last || x + 1 < s1) rise(s_n, top);
             if constexpr (!TURN) sp[0] = sp[1];
         }
         rd.move(by);
@@ -339,7 +356,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
             hide(sp[0], kw, r);
             top = fmaxf(top, sp[0][r]);
         }
-        rise(top);
+        rise(sp[0], top);
     }
     int x = s0;
     for (; x < min(s1, walk.masked()); ++x) take(x, std::true_type{});
@@ -369,7 +386,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
     }
     // a row that sees no key: O = 0, lse = -infinity
     const bool some = live && l != 0.f;
-    const float lse2 = some ? m * c + __builtin_amdgcn_logf(l) : -INFINITY;
+    const float log_l = __builtin_amdgcn_logf(l);
     const bool whole = f.splits == 1;
     const int64_t d4 = (a.d + 3) & ~3;
     const int64_t at = (((int64_t)split * a.batch * a.kv_heads) + bh) * f.rows + row;
@@ -382,10 +399,12 @@ void attn_core_fwd_kernel(FwdArgs f) {
     stage_rows<DP>(put + wave * PUT_FLOATS<DP>, o, some ? mul / l : 0.f, lane);
     if (valid && half == 0 && kg == 0) {
         if (!whole)
-            a.ws[(int64_t)f.splits * a.batch * a.kv_heads * f.rows * d4 + at] = lse2;
+            a.ws[(int64_t)f.splits * a.batch * a.kv_heads * f.rows * d4 + at] =
+                some ? m * c + log_l : -INFINITY;
         else if (a.lse.p)
             static_cast<float *>(a.lse.p)[(int64_t)b * a.lse.sb + head * a.lse.sh +
-                                          (int64_t)i * a.lse.ld] = lse2 * LN2;
+                                          (int64_t)i * a.lse.ld] =
+                some ? __builtin_fmaf(m, a.scale, log_l * LN2) : -INFINITY;
     }
     __syncthreads();
     store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);

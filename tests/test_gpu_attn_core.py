@@ -414,3 +414,48 @@ def test_rows_without_keys_beside_values_that_are_not_finite(dims, bad):
         attention.core_bwd(dO, Q, K, V, O0, lse0, out=out, accumulate=True, **kw)
         assert torch.equal(out[0][:, :, dead], old[0][:, :, dead])
         assert all(torch.equal(a[:, :, nk:], b[:, :, nk:]) for a, b in zip(out[1:], old[1:]))
+
+
+def peaked(dims, peak, ties, seed, pad=0):
+    """Scores that are exact: `peak` for the keys of `ties`, 0 for the others (scale 1)."""
+    B, H, Hk, sq, sk, D = dims
+    Q, K = (torch.zeros((B, h, s, D + pad), dtype=BF, device="cuda")[..., :D] for h, s in ((H, sq), (Hk, sk)))
+    Q[..., 0] = 1.0
+    K[:, :, ties, 0] = peak
+    return Q, K, rn((B, Hk, sk, D + pad), seed)[..., :D], rn((B, H, sq, D), seed + 1)
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 10, 2.0 ** 20, 2.0 ** 30, 1e9, 2.0 ** 40, 2.0 ** 100])
+@pytest.mark.parametrize("dims,pad", [((1, 4, 2, 70, 90, 64), 0), ((2, 2, 2, 300, 500, 128), 0),
+                                      ((1, 2, 2, 70, 90, 40), 3)], ids=["64", "128", "unaligned"])
+def test_maxima_of_any_size(dims, pad, scale):
+    # the largest score far beyond 2^24: its weight is still one against itself. Three keys
+    # share it, each with a third
+    ties = [17, 40, 61]
+    for peak in (3.0, 5.6875, -5.6875):
+        Q, K, V, _ = peaked(dims, peak, ties, 160, pad)
+        if peak < 0:          # every key but those three
+            ties = [j for j in range(dims[4]) if j not in ties]
+        say("maxima", dims, peak, scale)
+        O, lse = attention.core_fwd(Q, K, V, scale=scale, out_dtype=F32)
+        v = V.double().repeat_interleave(dims[1] // dims[2], 1)[:, :, ties]
+        want = v.mean(2, keepdim=True)
+        # weights of equal size, exact as operands: sums and a division in fp32
+        assert bool(((O.double() - want).abs() <= ref.F * v.abs().mean(2, keepdim=True)).all())
+        # one rounding of a sum of the largest score and a logarithm
+        top = max(peak, 0.0) * scale
+        far = (lse.double() - (top + math.log(len(ties)))).abs()
+        assert float(far.max()) <= 2.0 ** -23 * top + 2.0 ** -20, float(far.max())
+
+
+def test_large_queries_and_keys():
+    # the same from large Q and K at an ordinary scale: scores of 3 2^34 D
+    Q, K, V, _ = peaked((1, 4, 2, 70, 90, 64), 1.0, [17, 40, 61], 165)
+    Q[:] = 2.0 ** 17
+    K[:] = torch.where(K[..., :1] > 0, 3.0 * 2 ** 17, 2.0 ** 17)
+    say("large Q and K")
+    O, lse = attention.core_fwd(Q, K, V, scale=0.125, out_dtype=F32)
+    v = V.double().repeat_interleave(2, 1)[:, :, [17, 40, 61]]
+    assert bool(((O.double() - v.mean(2, keepdim=True)).abs() <= ref.F * v.abs().mean(2, keepdim=True)).all())
+    top = 3.0 * 2 ** 34 * 64 * 0.125
+    assert float((lse.double() - top).abs().max()) <= 2.0 ** -23 * top

@@ -77,6 +77,14 @@ struct FwdArgs {
     Div per, by_split, heads, kv, group, by_rows;   // tiles x splits, splits, batch x key heads, ...
 };
 
+// The split parts' statistics, behind their partial outputs: a row's maximum and its sum of
+// exponents, apart, since a large maximum has no bits left for the logarithm of the sum.
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ f32x2 *stats_of(const FwdArgs &f, int64_t d4) {
+    return reinterpret_cast<f32x2 *>(f.a.ws +
+                                     (int64_t)f.splits * f.a.batch * f.a.kv_heads * f.rows * d4);
+}
+
 // WPS: waves of a SIMD, of one workgroup or two.
 template <int DP, int KG, int KT, int NW_, int WPS_, bool DMA>
 struct FwdShape {
@@ -399,8 +407,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
     stage_rows<DP>(put + wave * PUT_FLOATS<DP>, o, some ? mul / l : 0.f, lane);
     if (valid && half == 0 && kg == 0) {
         if (!whole)
-            a.ws[(int64_t)f.splits * a.batch * a.kv_heads * f.rows * d4 + at] =
-                some ? m * c + log_l : -INFINITY;
+            stats_of(f, d4)[at] = some ? f32x2{m, l} : f32x2{-INFINITY, 0.f};
         else if (a.lse.p)
             static_cast<float *>(a.lse.p)[(int64_t)b * a.lse.sb + head * a.lse.sh +
                                           (int64_t)i * a.lse.ld] =
@@ -410,7 +417,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
     store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
 }
 
-// Joins the key splits of a row: weights 2^(lse_s - lse), in split order. A thread
+// Joins the key splits of a row, in split order: weights l_s 2^((m_s - m) c). A thread
 // owns 4 columns of a row, 16 (32 past 64 columns) a row.
 __global__ __launch_bounds__(256) void attn_core_join_kernel(FwdArgs f) {
     const CoreArgs &a = f.a;
@@ -419,33 +426,34 @@ __global__ __launch_bounds__(256) void attn_core_join_kernel(FwdArgs f) {
     const uint32_t id = blockIdx.x * 256u + threadIdx.x;
     const int at = (int)(id >> lanes), col = (int)(id & ((1u << lanes) - 1)) * 4;
     if (at >= n || col >= a.d) return;
-    const float *stat = a.ws + f.splits * n * d4 + at;
+    const f32x2 *stat = stats_of(f, d4) + at;
     const float *part = a.ws + at * d4 + col;
+    const float c = a.scale * LOG2E;
     // 8 splits at a time, so that their reads are on the way together
     float top = -INFINITY, total = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     for (int s = 0; s < f.splits; s += 8) {
-        float w[8];
+        f32x2 w[8];
         f32x4 x[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
             const bool in = s + j < f.splits;
-            w[j] = in ? stat[(s + j) * n] : -INFINITY;
+            w[j] = in ? stat[(s + j) * n] : f32x2{-INFINITY, 0.f};
             x[j] = in ? *reinterpret_cast<const f32x4 *>(part + (s + j) * n * d4)
                       : f32x4{0.f, 0.f, 0.f, 0.f};
         }
         float high = top;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) high = fmaxf(high, w[j]);
+        for (int j = 0; j < 8; ++j) high = fmaxf(high, w[j][0]);
         const float base = high == -INFINITY ? 0.f : high;
-        const float old = exp2_(top - base);
+        const float old = exp2_((top - base) * c);
         total *= old;
         v *= old;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-            w[j] = exp2_(w[j] - base);
-            total += w[j];
-            v += x[j] * w[j];
+            const float e = w[j][1] * exp2_((w[j][0] - base) * c);
+            total += e;
+            v += x[j] * e;
         }
         top = high;
     }
@@ -460,7 +468,7 @@ __global__ __launch_bounds__(256) void attn_core_join_kernel(FwdArgs f) {
     if (a.lse.p && col == 0)
         static_cast<float *>(a.lse.p)[(int64_t)b * a.lse.sb + head * a.lse.sh +
                                       (int64_t)i * a.lse.ld] =
-            some ? (top + __builtin_amdgcn_logf(total)) * LN2 : -INFINITY;
+            some ? __builtin_fmaf(top, a.scale, __builtin_amdgcn_logf(total) * LN2) : -INFINITY;
 }
 
 }  // namespace sbpk
@@ -517,7 +525,7 @@ int plan_fwd(const CoreArgs &a, int64_t bhs, int cus, int64_t *splits) {
                                 ? steps * (1.0 - 0.5 * std::min<double>(1.0, (double)a.sq / a.sk))
                                 : (double)steps;
         for (int64_t v = 1; v <= 32; v *= 2) {
-            const size_t part = v > 1 ? (size_t)bhs * packed * v * (d4 + 1) : 0;
+            const size_t part = v > 1 ? (size_t)bhs * packed * v * (d4 + 2) : 0;
             if (v > 1 && (steps / v < 2 || part > a.ws_floats ||
                           (double)tiles * bhs * v > 16777215.0 ||
                           (double)bhs * packed > 134217727.0))   // the join's threads

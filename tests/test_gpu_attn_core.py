@@ -459,3 +459,23 @@ def test_large_queries_and_keys():
     assert bool(((O.double() - v.mean(2, keepdim=True)).abs() <= ref.F * v.abs().mean(2, keepdim=True)).all())
     top = 3.0 * 2 ** 34 * 64 * 0.125
     assert float((lse.double() - top).abs().max()) <= 2.0 ** -23 * top
+
+
+@pytest.mark.parametrize("scale", [1.0, 2.0 ** 20, 2.0 ** 30, 1e9, 2.0 ** 100])
+@pytest.mark.parametrize("dims", [(1, 8, 2, 3, 3000, 64), (1, 2, 2, 1, 4096, 128), (1, 1, 1, 40, 3000, 44)],
+                         ids=["64", "128", "unaligned"])
+def test_maxima_of_any_size_over_splits(dims, scale):
+    # the largest score once in the first split of the keys, three times in the last one: each
+    # of the four has a quarter, however small log 3 is beside it
+    ties = [40, dims[4] - 60, dims[4] - 31, dims[4] - 9]
+    for peak in (100.0, 181.0):
+        Q, K, V, _ = peaked(dims, peak, ties, 170)
+        say("maxima over splits", dims, peak, scale)
+        sbp.sbp_profile_begin(8)
+        O, lse = attention.core_fwd(Q, K, V, scale=scale, out_dtype=F32)
+        assert any("join" in n for n, _ in sbp.sbp_profile_end(8))
+        v = V.double().repeat_interleave(dims[1] // dims[2], 1)[:, :, ties]
+        want = v.mean(2, keepdim=True)
+        assert bool(((O.double() - want).abs() <= ref.F * v.abs().mean(2, keepdim=True)).all())
+        far = (lse.double() - (peak * scale + math.log(4))).abs()
+        assert float(far.max()) <= 2.0 ** -23 * peak * scale + 2.0 ** -20, float(far.max())

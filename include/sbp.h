@@ -486,6 +486,10 @@ typedef struct {
  * gradient (not to O or lse: SBP_ERR_SHAPE). Scores, row statistics and sums are fp32;
  * P and dS are rounded to bf16 as operands of the matrix products, so fp32 outputs
  * carry that rounding too.
+ * The forward call takes finite scores of any size. The backward call recomputes P
+ * from lse, whose 24 bits leave it off by a factor of up to exp(2^-22 |lse|): 2^-10 of it
+ * where the scores, scaled, reach 2^12, a sixteenth at 2^18, and no use from 2^22 on (past
+ * 2^28 P may overflow).
  *
  * Head split: key heads split over p devices by the balanced rule, query heads with
  * them (rank r has G per key head of its share). Q, K and V share one scope; dO, O

@@ -92,7 +92,7 @@ int prepare(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_view4_t *V,
     if (Q->cols < 1 || Q->cols > MAX_DIM) return SBP_ERR_SHAPE;
     if (K->heads != V->heads || K->rows != V->rows) return SBP_ERR_SHAPE;
     if (K->heads == 0 ? Q->heads != 0 : Q->heads % K->heads != 0) return SBP_ERR_SHAPE;
-    // (beyond these scales lse / scale or a score's exponent leaves fp32)
+    // (beyond these scales lse / scale, or the scale in base 2 times small scores, leaves fp32)
     if (!(opts->scale >= MIN_SCALE && opts->scale <= 1.f / MIN_SCALE) || opts->window < 0 ||
         (opts->causal != 0 && opts->causal != 1))
         return SBP_ERR_SHAPE;

@@ -479,3 +479,38 @@ def test_maxima_of_any_size_over_splits(dims, scale):
         assert bool(((O.double() - want).abs() <= ref.F * v.abs().mean(2, keepdim=True)).all())
         far = (lse.double() - (peak * scale + math.log(4))).abs()
         assert float(far.max()) <= 2.0 ** -23 * peak * scale + 2.0 ** -20, float(far.max())
+
+
+@pytest.mark.parametrize("scale", [2.0 ** 6, 1e3, 2.0 ** 10, 2.0 ** 14])
+@pytest.mark.parametrize("dims", [(1, 4, 2, 70, 90, 64), (2, 2, 2, 300, 500, 128)], ids=["64", "128"])
+def test_gradients_at_large_scores(dims, scale):
+    # P from an fp32 lse is off by a factor of up to exp(2^-22 |lse|) = 1 + R; what follows from
+    # it as in ref.backward's bounds
+    B, H, Hk, sq, sk, D = dims
+    ties = [17, 40, 61]
+    for peak in (3.0, 5.6875):
+        Q, K, V, dO = peaked(dims, peak, ties, 180)
+        say("gradients at large scores", dims, peak, scale)
+        O, lse = attention.core_fwd(Q, K, V, scale=scale)
+        g = attention.core_bwd(dO, Q, K, V, O, lse, scale=scale, grad_dtype=F32)
+        R = math.expm1(2.0 ** -22 * float(lse.max()))
+        P = torch.zeros((sq, sk), dtype=torch.float64, device="cuda")
+        P[:, ties] = 1 / 3
+        want = [torch.zeros(t.shape, dtype=torch.float64, device="cuda") for t in (Q, K, V)]
+        room = [torch.zeros_like(t) for t in want]
+        mm = lambda a, b: torch.mm(a.contiguous(), b.contiguous())
+        for b in range(B):
+            for h in range(H):
+                c = h * Hk // H
+                q, k, v, do, o = (t.double() for t in (Q[b, h], K[b, c], V[b, c], dO[b, h], O[b, h]))
+                D_ = (do * o).sum(1, keepdim=True)
+                dS = P * (mm(do, v.t()) - D_)
+                e = ref.U * dS.abs() + (R + ref.F) * P * (mm(do.abs(), v.abs().t()) +
+                                                          (do * o).abs().sum(1, keepdim=True))
+                for i, x in enumerate((scale * mm(dS, k), scale * mm(dS.t(), q), mm(P.t(), do))):
+                    want[i][b, (h, c, c)[i]] += x
+                for i, x in enumerate((scale * mm(e, k.abs()), scale * mm(e.t(), q.abs()),
+                                       (R + ref.U + ref.F) * mm(P.t(), do.abs()))):
+                    room[i][b, (h, c, c)[i]] += x
+        for n, got, w, r in zip(("dQ", "dK", "dV"), g, want, room):
+            ref.check(n, got, w, r)

@@ -511,7 +511,8 @@ typedef struct {
  * Errors: those of the calls above; SBP_ERR_SHAPE also for D outside [1, 128], H not a
  * multiple of Hk, more than 2^29 rows of a sequence, or more of them in all than a
  * launch covers (B H_r Sq > 2^28 - 16, or 2^24 tiles of 32 keys or of 32 rows of a
- * group). Outputs may interleave in one buffer
+ * group; in the backward call 2^24 tiles of 64 keys and of 64 rows of a group, taken
+ * together). Outputs may interleave in one buffer
  * (dQ, dK and dV as parts of a fused gradient) when their strides agree and their
  * columns do not meet. */
 int sbp_attn_core_fwd(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_view4_t *V,

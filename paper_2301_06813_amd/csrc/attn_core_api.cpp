@@ -238,6 +238,10 @@ int sbp_attn_core_bwd(const sbp_view4_t *dO, const sbp_view4_t *Q, const sbp_vie
     int rc = prepare(Q, K, V, opts, p, r, &c);
     if (rc) return rc;
     sbpi::CoreArgs &a = c.a;
+    // one launch holds the workgroups of dK and dV and those of dQ, 256 threads for 64 keys or
+    // 64 packed rows and more
+    const int64_t tiles = (a.sk + int64_t(63)) / 64 + ((int64_t)a.sq * a.group + 63) / 64;
+    if ((double)a.batch * a.kv_heads * (double)tiles > 16777215.0) return SBP_ERR_SHAPE;
     if ((rc = query_operand(dO, c, Q, Q->cols, &a.dout))) return rc;
     if ((rc = query_operand(O, c, Q, Q->cols, &a.o))) return rc;
     if ((rc = query_operand(lse, c, Q, 1, &a.lse))) return rc;

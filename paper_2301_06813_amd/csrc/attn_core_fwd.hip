@@ -491,16 +491,16 @@ hipError_t launch_fwd(const sbpk::FwdArgs &f, int64_t blocks, hipStream_t s) {
                          dim3((unsigned)blocks), dim3(64 * NW), s, f);
 }
 
-// The kernel's forms: rows of a tile, keys of a step, workgroups of a unit, us of a step. The
+// The kernel's forms: rows of a tile, keys of a step, waves, workgroups of a unit, us of a step. The
 // second and third give up speed a row for smaller tiles: 16 heads over 4 of 8192 x 128,
 // causal, take 277, 343 and 472 us; 16 heads of 1024 x 64, causal, 19.3, 14.6 and 17.0; 64
 // key heads with 4 rows each, 4096 x 64, whose keys are split, 17.3, 13.8 and 13.8.
 struct Form {
-    int rows, keys, per_cu;
+    int rows, keys, waves, per_cu;
     double step;
 };
-constexpr Form FORMS[2][3] = {{{128, 64, 2, 0.9}, {64, 64, 2, 0.55}, {32, 128, 1, 0.6}},
-                              {{256, 64, 1, 1.4}, {128, 64, 1, 1.0}, {64, 64, 1, 0.75}}};
+constexpr Form FORMS[2][3] = {{{128, 64, 4, 2, 0.9}, {64, 64, 4, 2, 0.55}, {32, 128, 4, 1, 0.6}},
+                              {{256, 64, 8, 1, 1.4}, {128, 64, 8, 1, 1.0}, {64, 64, 4, 1, 0.75}}};
 
 // The form (returned) and key splits that the following time expects least of: an item takes
 // so much a step, and `fixed` besides; the busiest unit has an even share of all items and
@@ -526,8 +526,9 @@ int plan_fwd(const CoreArgs &a, int64_t bhs, int cus, int64_t *splits) {
                                 : (double)steps;
         for (int64_t v = 1; v <= 32; v *= 2) {
             const size_t part = v > 1 ? (size_t)bhs * packed * v * (d4 + 2) : 0;
+            // a launch's threads fit 32 bits (the last form's always do, with whole walks)
+            if ((double)tiles * bhs * v * (64 * m.waves) > 4294967295.0) break;
             if (v > 1 && (steps / v < 2 || part > a.ws_floats ||
-                          (double)tiles * bhs * v > 16777215.0 ||
                           (double)bhs * packed > 134217727.0))   // the join's threads
                 break;
             const double item = fixed + (double)((steps + v - 1) / v) * m.step;

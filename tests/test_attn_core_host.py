@@ -185,3 +185,28 @@ def test_lengths_are_int32():
         sbp.attn_opts(1.0, len_q=torch.zeros(3, dtype=torch.int64))
     with pytest.raises(ValueError):
         sbp.attn_opts(1.0, len_k=torch.zeros(6, dtype=torch.int32)[::2])
+
+
+TB = 1 << 20   # MiB
+
+
+@pytest.mark.parametrize("heads,rows,keys,fits", [
+    ((1 << 23) - 1, 8, 8, True), (1 << 23, 8, 8, False), ((1 << 23) - 1, 32, 32, True),
+    (1 << 23, 1, 32, False), (1 << 23, 8, 0, True), ((1 << 24) - 1, 0, 32, True)])
+def test_backward_workgroups(heads, rows, keys, fits):
+    # dK's and dV's workgroups and dQ's are of one launch; what fits is then refused for its
+    # workspace, which lies on Q. The forward call takes all of these
+    q, k, v, do, o, lse, dq, dk, dv = (
+        v4(i * TB, heads, 1, r, c, t, s, sh=max(r, 1) * c) for i, (r, c, t, s) in enumerate(
+            [(rows, 32, BF, GL), (keys, 32, BF, GL), (keys, 32, BF, GL), (rows, 32, BF, LO),
+             (rows, 32, BF, LO), (rows, 1, F32, LO), (rows, 32, BF, LO), (keys, 32, BF, LO),
+             (keys, 32, BF, LO)], 1))
+    on = q if rows else k
+    call = dict(do=do, q=q, k=k, v=v, o=o, lse=lse, opts=opts(), dq=dq, dk=dk, dv=dv, p=1, r=0,
+                ws=sbp.sbp_workspace_t(on.data, MB))
+    with pytest.raises(sbp.SbpError) as ei:
+        bwd(call)
+    assert ei.value.code == (sbp.SBP_ERR_ALIAS if fits else sbp.SBP_ERR_SHAPE)
+    with pytest.raises(sbp.SbpError) as ei:
+        fwd(call)
+    assert ei.value.code == sbp.SBP_ERR_ALIAS

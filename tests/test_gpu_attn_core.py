@@ -514,3 +514,17 @@ def test_gradients_at_large_scores(dims, scale):
                     room[i][b, (h, c, c)[i]] += x
         for n, got, w, r in zip(("dQ", "dK", "dV"), g, want, room):
             ref.check(n, got, w, r)
+
+
+def test_most_heads():
+    # 2^23 key heads of one row without keys: as many workgroups of 256 threads, and no form of
+    # 512 threads, fit one launch
+    n, D = 1 << 23, 72
+    if torch.cuda.mem_get_info()[0] < 8 << 30:
+        pytest.skip("needs 8 GiB of device memory")
+    Q = torch.ones((n, 1, 1, D), dtype=BF, device="cuda")
+    K = torch.empty((n, 1, 0, D), dtype=BF, device="cuda")
+    say("most heads")
+    O, lse = attention.core_fwd(Q, K, K)
+    torch.cuda.synchronize()
+    assert int(torch.count_nonzero(O)) == 0 and bool((lse == -math.inf).all())

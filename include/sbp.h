@@ -375,8 +375,8 @@ typedef enum { SBP_ACT_SILU = 0, SBP_ACT_GELU = 1, SBP_ACT_RELU = 2 } sbp_act_t;
  * rounded once, from the sum of both products.
  *
  * No output may overlap an input or another output. ws as for sbp_linear_fwd. Errors:
- * those of the linear calls; SBP_ERR_SHAPE also for an unknown act and for outputs of 2^22
- * tiles of 64 x 64 or more. */
+ * those of the linear calls; SBP_ERR_SHAPE also for an unknown act, for outputs of 2^22
+ * tiles of 64 x 64 or more, and for dX, dWg and dWu of 2^23 such tiles together. */
 int sbp_gated_fwd(const sbp_view_t *X, const sbp_layout_t *lx, const sbp_view_t *Wg,
                   const sbp_view_t *Wu, const sbp_layout_t *lw, int32_t act,
                   sbp_view_t *H, sbp_layout_t *lh_out, sbp_view_t *G, sbp_view_t *U,

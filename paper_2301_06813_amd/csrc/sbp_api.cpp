@@ -611,11 +611,11 @@ int gradient(const sbp_view_t *v, int64_t rows, int64_t cols, int32_t in_dtype, 
     return SBP_OK;
 }
 
-// A launch's workgroups (64 x 64 tiles of 512 threads at most) fit its 32-bit thread
-// count.
-bool tiles_fit(int64_t m, int64_t n) {
-    return (double)((m + 63) / 64) * (double)((n + 63) / 64) < 4194304.0;
-}
+// Tiles of 64 x 64, the smallest that a workgroup of 512 threads at most takes: fewer than 2^23
+// in one launch, whose threads then fit 32 bits. (The element-wise kernels take a thread for
+// 4 elements of a row, of 2^22 tiles at most.)
+double tiles64(int64_t m, int64_t n) { return (double)((m + 63) / 64) * (double)((n + 63) / 64); }
+constexpr double MOST_TILES = 4194304.0;
 
 // X, Wg and Wu of rank r, and the states st of H, dH, dX and the weights' gradients. H must
 // be whole on every device that holds it: act of a partial sum is no partial sum.
@@ -634,9 +634,7 @@ int gate_operands(const sbp_view_t *X, const L *lx, const sbp_view_t *Wg, const 
     if (x->global && wg->global && x->gcols != wg->grows) return SBP_ERR_SHAPE;
     if (x->global && wu->global && x->gcols != wu->grows) return SBP_ERR_SHAPE;
     if (x->cols != wg->rows || wu->rows != wg->rows || wu->cols != wg->cols) return SBP_ERR_SHAPE;
-    if (!tiles_fit(x->rows, wg->cols) || !tiles_fit(x->rows, x->cols) ||
-        !tiles_fit(x->cols, wg->cols))
-        return SBP_ERR_SHAPE;
+    if (tiles64(x->rows, wg->cols) >= MOST_TILES) return SBP_ERR_SHAPE;
     return SBP_OK;
 }
 
@@ -721,6 +719,9 @@ int gated_bwd(const sbp_view_t *dH, const L *ldh, const sbp_view_t *X, const L *
     L st[4];
     int rc = gate_operands(X, lx, Wg, Wu, lw, act, &x, &wg, &wu, st);
     if (rc) return rc;
+    // dX, dWg and dWu are of one launch
+    const double td = tiles64(x.rows, x.cols), tw = tiles64(x.cols, wg.cols);
+    if (td >= MOST_TILES || tw >= MOST_TILES || td + 2 * tw >= 2 * MOST_TILES) return SBP_ERR_SHAPE;
     if ((rc = check_pair(ldh, lw))) return rc;
     if (!one_signature(lx, lw, ldh)) return SBP_ERR_SIGNATURE;
     if ((rc = gate_input(dH, ldh, x, wg, x.rows, wg.cols, &dh))) return rc;

@@ -149,3 +149,32 @@ def test_partial_devices():
     n = linear.nd_layouts(("DP", "COL"), (2, 3), (0, 0))
     assert linear.partial_devices(n["dx"]) == 3 and linear.partial_devices(n["dw"]) == 2
     assert linear.partial_devices(n["y"]) == 1
+
+
+TB = 1 << 20   # MiB
+
+
+def large(m, k, n, backward):
+    """One device's call of these sizes; its workspace lies on X, which is found last."""
+    l = linear.layouts("COL", 1, 0)
+    x, h = v(TB, m, k), [v((i + 4) * TB, m, n) for i in range(6)]
+    c = dict(x=x, lx=l["x"], wg=v(2 * TB, k, n), wu=v(3 * TB, k, n), lw=l["w"],
+             act=sbp.SBP_ACT_SILU, h=h[0], g=h[1], u=h[2], dh=h[3], ldh=l["dy"], dg=h[4], du=h[5],
+             dx=v(10 * TB, m, k), dwg=v(11 * TB, k, n), dwu=v(12 * TB, k, n),
+             ws=sbp.sbp_workspace_t(x.data, MB))
+    with pytest.raises(sbp.SbpError) as ei:
+        (bwd if backward else fwd)(c)
+    return ei.value.code
+
+
+def test_tiles_of_a_launch():
+    # the backward call's three products are of one launch: fewer than 2^23 tiles together,
+    # where each output has fewer than 2^22
+    assert large(64, 64 * 2047, 64 * 2048, True) == sbp.SBP_ERR_ALIAS
+    assert large(64 * 3, 64 * 2047, 64 * 2048, True) == sbp.SBP_ERR_SHAPE
+    assert large(64 * 2048, 64 * 2048, 64, True) == sbp.SBP_ERR_SHAPE
+    # the forward call has one output, whatever X's and the weights' sizes
+    assert large(64 * 2048, 64 * 2048, 64, False) == sbp.SBP_ERR_ALIAS
+    assert large(64, 64 * 2048, 64 * 2048, False) == sbp.SBP_ERR_ALIAS
+    assert large(64 * 2048, 64, 64 * 2047, False) == sbp.SBP_ERR_ALIAS
+    assert large(64 * 2048, 64, 64 * 2048, False) == sbp.SBP_ERR_SHAPE

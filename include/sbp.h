@@ -372,7 +372,11 @@ typedef enum { SBP_ACT_SILU = 0, SBP_ACT_GELU = 1, SBP_ACT_RELU = 2 } sbp_act_t;
  * products, whose fp32 results carry that rounding too). dX, dWg, dWu: fp32, or for bf16
  * inputs bf16 where they are no partial sum of several devices (a sum over one device
  * is the tensor); SBP_ACCUMULATE adds to fp32 contents. dWg and dWu have one dtype. dX is
- * rounded once, from the sum of both products.
+ * rounded once, from the sum of both products (twice, once per product, where an fp32
+ * operand's leading dimension is 2^21 or more). bf16 calls are fastest with K, N, every
+ * operand's start (16 bytes) and leading dimension multiples of 8, one leading dimension of
+ * Wg and Wu, and one of dG and dU; with others the operands pass through registers (8192 x
+ * 8192 with 8192 x 4096 weights: 1.86 ms, and 2.44 where Wu's rows are longer than Wg's).
  *
  * No output may overlap an input or another output. ws as for sbp_linear_fwd. Errors:
  * those of the linear calls; SBP_ERR_SHAPE also for an unknown act, for outputs of 2^22

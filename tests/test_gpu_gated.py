@@ -293,3 +293,117 @@ def test_weights_with_strides_of_their_own(shape, dtype):
     for ws in (None, sbp.NO_WORKSPACE):
         say("own strides", shape, dtype, ws is None)
         both(X, Wg, Wu, dH, ws=ws, G=G, U=U)
+
+
+WIDE = (1 << 21) + 4     # elements from row to row, past what the pipelined kernels' offsets reach
+
+
+@pytest.mark.parametrize("which", ["X", "weights", "all"])
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_rows_far_apart(dtype, which):
+    # operands with leading dimensions past 2^21: bf16 through registers; fp32 gradients as two
+    # pairs of products, the second of which adds its dX to the first's
+    M, K, N = 70, 72, 96
+    T = make(M, K, N, 140, dtype)
+    wide = torch.empty(80 * WIDE, dtype=dtype, device="cuda")
+
+    def far(t, i):          # the same matrix with its rows WIDE apart
+        v = wide.as_strided(t.shape, (WIDE, 1), 128 * i)
+        v.copy_(t)
+        return v
+
+    X, Wg, Wu, dH = (far(t, i) if which == "all" or (which == "X") == (i == 0) and i < 3 else t
+                     for i, t in enumerate(T))
+    say("rows far apart", dtype, which)
+    sbp.sbp_profile_begin(32)
+    (H, G, U), grads = both(X, Wg, Wu, dH)
+    names = " ".join(n for n, _ in sbp.sbp_profile_end(32))
+    if dtype == F32:
+        assert "gemm_f32_gated_bwd" not in names
+    if which == "all":
+        G, U = far(G, 4), far(U, 5)
+        both(X, Wg, Wu, dH, G=G, U=U)
+    wants = ref.backward(dH, X, Wg, Wu, G, U, "silu")
+    old = [rn(t.shape, 1.0, 150 + i, F32) for i, t in enumerate(grads)]
+    for ws in (None, sbp.NO_WORKSPACE):
+        say("accumulating", ws is None)
+        out = [t.clone() for t in old]
+        linear.gated_bwd("COL", 1, 0, dH, X, Wg, Wu, G, U, out=out, accumulate=True, ws=ws)
+        torch.cuda.synchronize()
+        for (n, (want, bound)), got, was in zip(wants.items(), out, old):
+            # adding to the contents rounds twice more (fp32 dX: once per product)
+            extra = 3 * ref.E * (was.double().abs() + want.abs() + bound)
+            ref.check(n, got, want + was.double(), bound + extra)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_offsets_past_32_bits(dtype):
+    # an operand whose rows lie on both sides of 2^31 elements, and outputs that do
+    if torch.cuda.mem_get_info()[0] < 48 << 30:
+        pytest.skip("needs 48 GiB of device memory")
+    M, K, N = 70, 72, 96
+    X, Wg, Wu, dH = make(M, K, N, 160, dtype)
+    ld = (1 << 31) // 40 + 8          # row 40 starts past 2^31
+    say("offsets", dtype)
+    wide = torch.empty(72 * ld, dtype=dtype, device="cuda")
+    far = lambda buf, t: buf.as_strided(t.shape, (ld, 1))
+    want_f = ref.forward(X, Wg, Wu, "silu")
+    H, G, U = linear.gated_fwd("COL", 1, 0, X, Wg, Wu)
+    want_b = ref.backward(dH, X, Wg, Wu, G, U, "silu")
+    for i in range(3):
+        T = [X, Wg, Wu]
+        T[i] = far(wide, T[i])
+        T[i].copy_((X, Wg, Wu)[i])
+        say("offsets of operand", i)
+        for (n, (want, bound)), got in zip(want_f.items(), linear.gated_fwd("COL", 1, 0, *T)):
+            ref.check(n, got, want, bound)
+        for (n, (want, bound)), got in zip(want_b.items(),
+                                           linear.gated_bwd("COL", 1, 0, dH, *T, G, U)):
+            ref.check(n, got, want, bound)
+    for i in range(3):
+        out = [torch.empty_like(t) for t in (X, Wg, Wu)]
+        out[i] = far(wide, out[i])
+        say("offsets of gradient", i)
+        linear.gated_bwd("COL", 1, 0, dH, X, Wg, Wu, G, U, out=out)
+        for (n, (want, bound)), got in zip(want_b.items(), out):
+            ref.check(n, got, want, bound)
+    v, L, g, u = far(wide, H), linear.layouts("COL", 1, 0), torch.empty_like(G), torch.empty_like(U)
+    say("offsets of H")
+    sbp.sbp_gated_fwd(sbp.view(X), L["x"], sbp.view(Wg), sbp.view(Wu), L["w"], sbp.SBP_ACT_SILU,
+                      *(sbp.view(t, sbp.SBP_LOCAL) for t in (v, g, u)))
+    torch.cuda.synchronize()
+    ref.check("H", v, *want_f["H"])
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype", [BF, F32], ids=["bf16", "f32"])
+def test_extreme_preactivations_every_gradient(act, dtype):
+    # gates far out on both sides: all three gradients and H against the gate's limits, act(x) = x
+    # or 0 and its slope 1 or 0 (at |x| of 200 and more SiLU and GELU are within 2^-100 of them)
+    M, K, N = 16, 8, 24
+    X, Wg, Wu, dH = make(M, K, N, 170, dtype)
+    far = torch.tensor([-1e18, -3e4, -200.0, 200.0, 3e4, 1e18], device="cuda")
+    G = far.repeat(4)[None].expand(M, N).contiguous().to(dtype)
+    U = rn((M, N), 1.0, 171, dtype)
+    say("extremes", act, dtype)
+    out = linear.gated_bwd("COL", 1, 0, dH, X, Wg, Wu, G, U, act, grad_dtype=F32)
+    on = (G > 0).double()
+    a, u = G.double() * on, ref.U_BF if dtype == BF else ref.U_F32
+    dG, dU = dH.double() * U.double() * on, dH.double() * a
+    Xt, W = X.double().t(), (Wg.double().t(), Wu.double().t())
+    want = (ref.mm(dG, W[0]) + ref.mm(dU, W[1]), ref.mm(Xt, dG), ref.mm(Xt, dU))
+    e = [u * t.abs() + ref.A * s.abs() for t, s in ((dG, dH.double() * U.double()), (dU, dU))]
+    sizes = (ref.mm(dG.abs(), W[0].abs()) + ref.mm(dU.abs(), W[1].abs()), ref.mm(Xt.abs(), dG.abs()),
+             ref.mm(Xt.abs(), dU.abs()))
+    off = (ref.mm(e[0], W[0].abs()) + ref.mm(e[1], W[1].abs()), ref.mm(Xt.abs(), e[0]),
+           ref.mm(Xt.abs(), e[1]))
+    terms = (2 * N, M, M)
+    for n, got, w, b, s, t in zip(("dX", "dWg", "dWu"), out, want, off, sizes, terms):
+        ref.check(n, got, w, b + (t + 8) * ref.E * (1 + u) * s + 2.0 ** -99)
+    # H from such sums: one reduction index, whose products are exact
+    X1, W1 = torch.ones((M, 1), dtype=dtype, device="cuda"), G[:1]
+    Wu1 = rn((1, N), 1.0, 172, dtype)
+    H, g, _ = linear.gated_fwd("COL", 1, 0, X1, W1, Wu1, act)
+    assert torch.equal(g, G)
+    h = a * Wu1.double()
+    ref.check("H", H, h, ref.A * h.abs() + 2.0 ** -99)

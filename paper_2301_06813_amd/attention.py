@@ -58,7 +58,9 @@ def _rows(lse, full, scope):
     if lse.dim() != 3:
         return _local(lse, full, scope)
     sb, sh, ld = lse.stride()
-    return sbp.sbp_view4_t(lse.data_ptr(), *lse.shape, 1, sb, sh, max(ld, 1), sbp._dtype_of(lse),
+    if lse.shape[2] <= 1:   # as in sbp.view
+        ld = max(ld, 1)
+    return sbp.sbp_view4_t(lse.data_ptr(), *lse.shape, 1, sb, sh, ld, sbp._dtype_of(lse),
                            scope if lse.shape[1] == full else sbp.SBP_LOCAL)
 
 

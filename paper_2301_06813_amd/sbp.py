@@ -289,7 +289,9 @@ def view(t, scope=SBP_GLOBAL) -> sbp_view_t:
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("views need unit column stride")
-    return sbp_view_t(t.data_ptr(), rows, cols, max(ld, cols, 1), _dtype_of(t), scope)
+    if rows <= 1 or cols == 0:   # a stride that no element has; else the library refuses ld < cols
+        ld = max(ld, cols, 1)
+    return sbp_view_t(t.data_ptr(), rows, cols, ld, _dtype_of(t), scope)
 
 
 def view4(t, scope=SBP_GLOBAL) -> sbp_view4_t:
@@ -303,8 +305,9 @@ def view4(t, scope=SBP_GLOBAL) -> sbp_view4_t:
     sb, sh, ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("views need unit column stride")
-    return sbp_view4_t(t.data_ptr(), batch, heads, rows, cols, sb, sh, max(ld, cols, 1),
-                       _dtype_of(t), scope)
+    if rows <= 1 or cols == 0:   # as in view
+        ld = max(ld, cols, 1)
+    return sbp_view4_t(t.data_ptr(), batch, heads, rows, cols, sb, sh, ld, _dtype_of(t), scope)
 
 
 def raw_view(ptr, rows, cols, ld, dtype, scope=SBP_GLOBAL) -> sbp_view_t:

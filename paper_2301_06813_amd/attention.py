@@ -17,7 +17,7 @@ import math
 import torch
 
 from . import sbp
-from .streams import on_stream
+from .streams import on_stream, same_device
 
 _EMPTY = torch.empty
 
@@ -28,15 +28,6 @@ def rank_heads(heads: int, kv_heads: int, p: int, r: int):
     hk = kv_heads // p + (r < kv_heads % p)
     k0 = r * (kv_heads // p) + min(r, kv_heads % p)
     return k0 * group, hk * group, k0, hk
-
-
-def _same_device(*tensors):
-    """The library's calls run on the current device, whose tensors these must be."""
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != device:
-            raise ValueError("tensors are on %s, the current device is cuda:%d"
-                             % (t.device, device))
 
 
 def _opts(Q, scale, causal, window, len_q, len_k):
@@ -84,7 +75,7 @@ def core_fwd(Q, K, V, p: int = 1, r: int = 0, *, scale=None, causal: bool = Fals
             core_fwd, scale=scale, causal=causal, window=window, len_q=len_q, len_k=len_k, lse=lse,
             out=out, out_dtype=out_dtype, scope=scope, ws=ws), Q, K, V, p, r)
     B, H, sq, D = Q.shape
-    _same_device(Q, K, V, len_q, len_k, out)
+    same_device(Q, K, V, len_q, len_k, out, ws)
     hq = rank_heads(H, K.shape[1], p, r)[1] if scope == sbp.SBP_GLOBAL else H
     if out is None:
         out, o = _new(Q, B, hq, sq, D, out_dtype or Q.dtype)
@@ -118,7 +109,7 @@ def core_bwd(dO, Q, K, V, O, lse, p: int = 1, r: int = 0, *, scale=None, causal:
             p, r)
     B, H, sq, D = Q.shape
     Hk, sk = K.shape[1:3]
-    _same_device(dO, Q, K, V, O, lse, len_q, len_k, *(out or ()))
+    same_device(dO, Q, K, V, O, lse, len_q, len_k, ws, *(out or ()))
     hq, hk = (H, Hk) if scope != sbp.SBP_GLOBAL else rank_heads(H, Hk, p, r)[1::2]
     if out is None:
         if accumulate:

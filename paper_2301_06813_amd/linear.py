@@ -18,7 +18,7 @@ import functools
 import torch
 
 from . import sbp
-from .streams import on_stream
+from .streams import on_stream, same_device
 
 OPS = ("fwd", "bwd_data", "bwd_weight")
 
@@ -211,15 +211,6 @@ def call_bwd_nd(factors, mesh, coord, X, W, dY, stream=None):
 
 
 # ------------------------------------------------ gated feed-forward block
-def _same_device(*tensors):
-    """The library's calls run on the current device, whose tensors these must be."""
-    device = torch.cuda.current_device()
-    for t in tensors:
-        if t is not None and t.device.index != device:
-            raise ValueError("tensors are on %s, the current device is cuda:%d"
-                             % (t.device, device))
-
-
 def gated_fwd_L(L: dict, X, Wg, Wu, act: str = "silu", save: bool = True, stream=None, ws=None):
     """(H, G, U) of the device's shares of global X, Wg and Wu under the states in L
     (``layouts`` or ``nd_layouts``): H = act(X Wg) * (X Wu), and the projections that the
@@ -245,7 +236,7 @@ def _gated_states(sig: str, p: int, r: int, M: int, K: int, N: int):
 def _gated_fwd(L, sizes, X, Wg, Wu, act, save, stream, ws):
     if stream is not None and stream != sbp.current_stream():
         return on_stream(stream, _gated_fwd, L, sizes, X, Wg, Wu, act, save, None, ws)
-    _same_device(X, Wg, Wu)
+    same_device(X, Wg, Wu, ws)
     nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
     m, n = sizes[0], sizes[3]
     x = sbp.view(X)
@@ -277,7 +268,7 @@ def _gated_bwd(L, sizes, dH, X, Wg, Wu, G, U, act, out, grad_dtype, accumulate, 
     if stream is not None and stream != sbp.current_stream():
         return on_stream(stream, _gated_bwd, L, sizes, dH, X, Wg, Wu, G, U, act, out, grad_dtype,
                          accumulate, None, ws)
-    _same_device(dH, X, Wg, Wu, G, U, *(out or ()))
+    same_device(dH, X, Wg, Wu, G, U, ws, *(out or ()))
     nd = isinstance(L["x"], sbp.sbp_nd_layout_t)
     M, N = X.shape[0], Wg.shape[1]
     m, k, kw, n = sizes

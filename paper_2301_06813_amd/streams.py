@@ -1,4 +1,5 @@
-"""Torch's memory for calls on a stream that is not torch's current one."""
+"""Torch's memory for calls on a stream that is not torch's current one, and the device of a
+call's tensors."""
 from __future__ import annotations
 
 import torch
@@ -24,3 +25,13 @@ def on_stream(stream: int, call, *args):
         if isinstance(t, torch.Tensor):
             t.record_stream(caller)
     return out
+
+
+def same_device(*tensors):
+    """The library's calls run on the current device, whose tensors these must be (None and
+    workspaces that are no tensors aside)."""
+    device = torch.cuda.current_device()
+    for t in tensors:
+        if isinstance(t, torch.Tensor) and t.device.index != device:
+            raise ValueError("tensors are on %s, the current device is cuda:%d"
+                             % (t.device, device))

@@ -181,3 +181,30 @@ def test_linear(monkeypatch, nd, stream):
         with monkeypatch.context() as m:
             r = Record(m)
             r.check(make(), (X, W, dY), CALLER if stream is None else stream)
+
+
+class Elsewhere(torch.Tensor):
+    """A tensor of another device."""
+    device = property(lambda self: torch.device("cuda:1"))
+
+
+@pytest.mark.parametrize("call", ["gated_fwd", "gated_bwd", "core_fwd", "core_bwd"])
+def test_workspace_on_another_device(monkeypatch, call):
+    X, Wg, Wu = gated(BF)
+    dH = torch.zeros((6, 4), dtype=BF)
+    Q, K, V, dO = heads(4, 2, 2, 4)
+    ws = torch.zeros(4096, dtype=torch.uint8)
+    r = Record(monkeypatch)
+    make = {"gated_fwd": lambda w: linear.gated_fwd("COL", 1, 0, X, Wg, Wu, ws=w),
+            "gated_bwd": lambda w: linear.gated_bwd("COL", 1, 0, dH, X, Wg, Wu, dH, dH, ws=w),
+            "core_fwd": lambda w: attention.core_fwd(Q, K, V, ws=w),
+            "core_bwd": lambda w: attention.core_bwd(dO, Q, K, V, dO, torch.zeros((2, 4, 6)), ws=w)}[call]
+    for good in (None, ws, sbp.NO_WORKSPACE):
+        make(good)
+    assert len(r.calls) == 3
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(torch.Tensor, "device", property(lambda self: torch.device("cuda:0")))
+    make(ws)
+    with pytest.raises(ValueError, match="cuda:1"):
+        make(ws.as_subclass(Elsewhere))
+    assert len(r.calls) == 4

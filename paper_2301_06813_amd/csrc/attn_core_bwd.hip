@@ -920,10 +920,10 @@ Way split_q(const CoreArgs &a, int64_t rows, int64_t v) {
 // Wave groups of dQ (returned) and the splits: those that the following time expects least
 // of. An item takes so much a step, and `fixed` besides; the busiest unit has an even share
 // of all items and a fifth of the longest; partials are written and read once, by one more
-// launch. (16 heads over 4 of 8192 x 128, causal: 1055 us whole, 1022 with dK's and dV's longest
-// walk in two parts, 1045 in three, 1084 whole with dQ in two groups; 16 heads of 1024 x 64,
-// causal: 26 whole with dQ in two groups, 30 in one, 34 with the longest walk in two parts; 4
-// heads of 1024 rows and 4096 keys of 64: 30 split, 46 whole.)
+// launch. (In a graph, 16 heads over 4 of 8192 x 128, causal: 1023 us whole, with dK's and dV's
+// longest walk in two parts and in three, 1075 whole with dQ in two groups; 16 heads of 1024
+// x 64, causal: 25 whole with dQ in two groups, 30 in one, 34 with the longest walk in two
+// parts; 4 heads of 1024 rows and 4096 keys of 64: 30 split, 46 whole.)
 int plan_bwd(const CoreArgs &a, int64_t bhs, int cus, size_t room, sbpk::BwdArgs *f) {
     const bool wide = a.d > 64;
     const double slots = cus * (wide ? 1.0 : 2.0), fixed = 4.0;

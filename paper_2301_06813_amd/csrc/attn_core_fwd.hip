@@ -21,8 +21,8 @@
 //     like the framework's other bf16 operands); the row sum adds the fp32 values.
 //   * The next block's scores are computed beside this block's exponentials, and its
 //     maximum beside this block's product with V (written one after the other,
-//     16 heads over 4 of 8192 x 128, causal, took 314 us; so 260, 1.06 PFLOP/s, the
-//     matrix cores busy half of the time at two waves per SIMD).
+//     16 heads over 4 of 8192 x 128, causal, took 314 us; so 256, 1.07 PFLOP/s, at two
+//     waves per SIMD).
 //   * With KG wave groups, group k takes the k-th part of every step's keys; their
 //     (m, l, O) are joined through LDS at the end. Few rows and many keys are also
 //     split over workgroups, whose normalised partial outputs and row statistics
@@ -493,8 +493,10 @@ hipError_t launch_fwd(const sbpk::FwdArgs &f, int64_t blocks, hipStream_t s) {
 
 // The kernel's forms: rows of a tile, keys of a step, waves, workgroups of a unit, us of a step. The
 // second and third give up speed a row for smaller tiles: 16 heads over 4 of 8192 x 128,
-// causal, take 277, 343 and 472 us; 16 heads of 1024 x 64, causal, 19.3, 14.6 and 17.0; 64
-// key heads with 4 rows each, 4096 x 64, whose keys are split, 17.3, 13.8 and 13.8.
+// causal, take 256, 292 and 405 us (in a graph, like all of these); 16 heads of 1024 x 64,
+// causal, 19.1, 14.3 and 16.9; one token of 16 sequences, 4 key heads with 4 rows each, 4096 x
+// 64, whose keys are split, 20.4, 18.4 and 19.3 (20.0, 17.5 and 16.5 where the sequences
+// have from 4096 keys down to 1200, which the host does not know).
 struct Form {
     int rows, keys, waves, per_cu;
     double step;

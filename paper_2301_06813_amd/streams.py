@@ -32,6 +32,6 @@ def same_device(*tensors):
     workspaces that are no tensors aside)."""
     device = torch.cuda.current_device()
     for t in tensors:
-        if isinstance(t, torch.Tensor) and t.device.index != device:
+        if t is not None and isinstance(t, torch.Tensor) and t.device.index != device:
             raise ValueError("tensors are on %s, the current device is cuda:%d"
                              % (t.device, device))

@@ -502,9 +502,9 @@ typedef struct {
  *
  * Rows that see no key get O = 0, lse = -infinity and dQ = 0, whatever the other rows
  * hold (accumulated gradients stay as they are); so do rows past len_q and, in dK and dV,
- * keys past len_k, whose inputs are never read. Between the other rows, within the lengths,
- * a non-finite K, V, Q or dO row may reach every row of its head and sequence, also those
- * that do not see it or that it does not see. lse may be NULL in the forward call.
+ * keys past len_k, whose inputs are never read. Else a non-finite K, V, Q or dO row within
+ * the lengths may reach every row of its head and sequence, also those that do not see it
+ * or that it does not see. lse may be NULL in the forward call.
  *
  * ws: the forward call uses a workspace, if it has one, to split the keys of few rows
  * over workgroups. The backward call needs 8 bytes per query row of the rank

@@ -529,6 +529,130 @@ int sbp_attn_core_bwd(const sbp_view4_t *dO, const sbp_view4_t *Q,
                       sbp_view4_t *dQ, sbp_view4_t *dK, sbp_view4_t *dV, int32_t p,
                       int32_t r, const sbp_workspace_t *ws, hipStream_t stream);
 
+/* --------------------------------------------------- rotary positions --- */
+
+/* Which columns of a head's first `dim` make a pair: HALVES (i, i + dim / 2), PAIRS
+ * (2 i, 2 i + 1), for i in [0, dim / 2). */
+typedef enum { SBP_ROPE_HALVES = 0, SBP_ROPE_PAIRS = 1 } sbp_rope_order_t;
+
+/* Frequency of pair i, radians a position: f_i = base^(-2 i / dim), and for contexts that are
+ * `factor` times as long as the `context` a model was trained on
+ *   LINEAR    f_i / factor
+ *   BASE      base factor^(dim / (dim - 2)) in place of base (dim 2: base itself)
+ *   BY_TURNS  f_i w + f_i / factor (1 - w), w = (n_i - low) / (high - low) limited to [0, 1],
+ *             where n_i = context f_i / 2 pi are pair i's turns over the context
+ *   BY_PAIRS  f_i (1 - w) + f_i / factor w, w = (i - a) / max(b - a, 0.001) limited to [0, 1],
+ *             a = max(0, floor(at(high))), b = min(dim - 1, ceil(at(low))), where at(n) =
+ *             dim ln(context / (2 pi n)) / (2 ln base) is the pair with n turns */
+typedef enum { SBP_ROPE_PLAIN = 0, SBP_ROPE_LINEAR = 1, SBP_ROPE_BASE = 2,
+               SBP_ROPE_BY_TURNS = 3, SBP_ROPE_BY_PAIRS = 4 } sbp_rope_scaling_t;
+
+/* The dim / 2 frequencies as turns a position, in units of 2^-64 turn, to HOST memory; the
+ * caller copies them to the device once. The angle of a position is a product modulo 2^64, so
+ * far positions lose nothing: at t it is off by t 2^-62 turns at most (the frequencies are
+ * computed in the host's long double). Pure host function. Errors: SBP_ERR_NULL, SBP_ERR_SHAPE
+ * (dim odd or outside [2, 128], base <= 1 or not finite, an unknown scaling; for a scaling
+ * factor <= 0; BY_TURNS and BY_PAIRS context <= 0, low <= 0 or high <= low; or a number that is
+ * not finite). */
+int sbp_rope_turns(int32_t dim, double base, int32_t scaling, double factor, double low,
+                   double high, double context, uint64_t *turns);
+
+/* A rotation: the table of sbp_rope_turns in device memory, and its dim. `mul` multiplies the
+ * rotated columns (1: a pure rotation). */
+typedef struct {
+    const uint64_t *turns;
+    int32_t dim;      /* even, 2 .. the head dimension; columns past it are copied */
+    int32_t order;    /* sbp_rope_order_t */
+    float mul;        /* finite */
+} sbp_rope_t;
+
+/* The rows' positions, any int32, read when the call runs. per_row: row i of sequence b is at
+ * pos[b ld + i]; else at pos[b ld] + i. A NULL sbp_places_t: at i. */
+typedef struct {
+    const int32_t *pos;
+    int64_t ld;
+    int32_t per_row;
+} sbp_places_t;
+
+/* Rotation of rank r's heads of Q and K by the positions of their rows, in one launch (K and Ko
+ * may be NULL). At position t, with c = mul cos(t f_i) and s = mul sin(t f_i), pair i becomes
+ *   sbp_rope_fwd   y1 = x1 c - x2 s,  y2 = x2 c + x1 s
+ *   sbp_rope_bwd   dx1 = dy1 c + dy2 s,  dx2 = dy2 c - dy1 s
+ * Q: [B][H][S][D], K: [B][Hk][S][D], one scope; heads split as for softmax attention (without
+ * K: the heads of Q by the balanced rule). 1 <= D <= 128. Outputs hold rank r's heads.
+ * Inputs bf16 or fp32 (one dtype); outputs of one dtype, the inputs', or fp32 for bf16 inputs
+ * (SBP_ERR_DTYPE; SBP_ACCUMULATE: SBP_ERR_SHAPE). Angles, cosines and products are fp32 or
+ * better, each output is rounded once. An output may be the rank's part of its own input
+ * (the same address, strides and dtype: in place); else no output may overlap an input or the
+ * other output, but for outputs that interleave as those of sbp_attn_core_bwd may.
+ * Errors: those of the attention calls; SBP_ERR_SHAPE also for more than 2^29 rows of a
+ * sequence, or 2^31 pairs of a row and a part of 16 columns over the rank's heads. */
+int sbp_rope_fwd(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_rope_t *rope,
+                 const sbp_places_t *at, sbp_view4_t *Qo, sbp_view4_t *Ko, int32_t p, int32_t r,
+                 hipStream_t stream);
+int sbp_rope_bwd(const sbp_view4_t *dQo, const sbp_view4_t *dKo, const sbp_rope_t *rope,
+                 const sbp_places_t *at, sbp_view4_t *dQ, sbp_view4_t *dK, int32_t p, int32_t r,
+                 hipStream_t stream);
+
+/* --------------------------------------- paged cache of keys and values --- */
+
+/* A cache is two views [pages][heads][tokens of a page][D], one of keys and one of values, of
+ * any strides (a page's tokens or its heads outside). Token t of sequence b is row t % P
+ * of page table[b table_ld + t / P], P tokens a page. All arrays are device memory, read when a
+ * call runs. The new tokens' rows (of Q, K, V and O) are
+ *   padded   row_q NULL: views of `seqs` batches, sequence b the first len_q[b] rows of batch b
+ *            (limited to [0, rows]; len_q NULL: all)
+ *   packed   views of one batch, sequence b rows row_q[b] .. row_q[b + 1] - 1 (limited to the
+ *            view, and to none where they descend). len_q must be NULL. Rows of no sequence
+ *            are never read or written.
+ * len_k[b]: tokens that sequence b has in the cache once its n new ones are there, so that new
+ * token i is at place len_k[b] - n + i. */
+typedef struct {
+    const int32_t *table;
+    int64_t table_ld;     /* >= width */
+    int32_t seqs, width;  /* sequences; entries of a table row: width P tokens at most */
+    const int32_t *len_k; /* [seqs] */
+    const int32_t *len_q; /* [seqs], or NULL */
+    const int32_t *row_q; /* [seqs + 1], or NULL */
+} sbp_pages_t;
+
+/* Stores the new tokens' keys and values in the cache. With `rope` the keys are rotated on
+ * the way by their places, and with Q and Qo (both or neither NULL) Q's rows by theirs, all in
+ * one launch. Without `rope` Q must be NULL.
+ * K, V: [B][Hk][S][D] and Q: [B][H][S][D], of one scope, bf16; Kc, Vc: the cache, bf16, of one
+ * scope, which may be another (LOCAL: rank r's heads). Qo: rank r's heads, bf16 or fp32; it
+ * may be the rank's part of Q itself. Heads split as for softmax attention.
+ * Tokens at places outside [0, width P), or on a page outside [0, pages), are not stored; nothing
+ * else of the cache is written. Two tokens of one call must not share a row of the cache (it
+ * would hold parts of either). Qo's rows past len_q stay as they are.
+ * Errors: those of the attention calls; SBP_ERR_SHAPE also for P < 1, width P > 2^29, more than
+ * 2^20 sequences, 2^31 pairs as for sbp_rope_fwd, or rows that do not fit `seqs`; SBP_ERR_ALIAS
+ * also for a cache that overlaps another operand or whose own elements overlap. */
+int sbp_paged_append(const sbp_view4_t *K, const sbp_view4_t *V, const sbp_pages_t *pages,
+                     const sbp_rope_t *rope, sbp_view4_t *Kc, sbp_view4_t *Vc,
+                     const sbp_view4_t *Q, sbp_view4_t *Qo, int32_t p, int32_t r,
+                     hipStream_t stream);
+
+/* Softmax attention of the new tokens over the cache (sbp_attn_core_fwd's formulas): query i
+ * of the n new ones of a sequence sees key j when
+ *     j < len_k  (limited to [0, width P]),
+ *     causal:      j <= i + len_k - n
+ *     window > 0:  j >  i + len_k - n - window
+ * and j's page is in [0, pages): keys on other pages are not seen. Entries of the table whose
+ * keys no query of the sequence sees are not read.
+ * Q: [B][H][S][D] bf16; Kc, Vc: [pages][Hk][P][D] bf16, of Q's scope; H a multiple of Hk,
+ * 1 <= D <= 128; O and lse (fp32, may be NULL) as in sbp_attn_core_fwd, rounding and
+ * scores' size too. Rows that see no key, and padded rows past len_q, get O = 0, lse = -infinity.
+ * A non-finite K, V or Q row that some query of its sequence sees may reach every row of its
+ * head and sequence; cache rows that no query of the sequence sees are not read.
+ * ws: splits the work into equal parts, if there is one; results are the same up to fp32
+ * summation order, and identical for identical lengths and workspace sizes.
+ * Errors: those of sbp_attn_core_fwd and sbp_paged_append. */
+int sbp_paged_attn(const sbp_view4_t *Q, const sbp_view4_t *Kc, const sbp_view4_t *Vc,
+                   const sbp_pages_t *pages, float scale, int32_t causal, int32_t window,
+                   sbp_view4_t *O, sbp_view4_t *lse, int32_t p, int32_t r,
+                   const sbp_workspace_t *ws, hipStream_t stream);
+
 /* ------------------------------------- cost model and strategy search --- */
 
 /* Collectives of the alpha-beta model (Sec. 3.1, Table 2). */

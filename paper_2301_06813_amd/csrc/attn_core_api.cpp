@@ -14,46 +14,6 @@ namespace {
 
 using namespace sbpa;
 
-constexpr int64_t MAX_ROWS = int64_t(1) << 29;   // i + len_k - len_q + window fits 32 bits
-constexpr int64_t MAX_DIM = 128;
-constexpr float MIN_SCALE = 0x1p-100f;
-
-// check_view4, and element offsets that stay inside 62 bits.
-int check_bounded(const sbp_view4_t *v) {
-    int rc = check_view4(v);
-    if (rc) return rc;
-    const double last = (double)v->batch * (double)v->stride_b +
-                        (double)v->heads * (double)v->stride_h + (double)v->rows * (double)v->ld +
-                        (double)v->cols;
-    return last > 1e18 ? SBP_ERR_SHAPE : SBP_OK;
-}
-
-// Two outputs of the same element size whose rows interleave in one buffer -- the
-// Q, K and V parts of a fused gradient -- and so share spans but no element: equal
-// row and batch strides, every head of a row inside [0, ld), and the two footprints
-// disjoint within a row.
-bool interleaved(const sbp_view4_t *x, const sbp_view4_t *y) {
-    if (x->dtype != y->dtype || x->ld != y->ld || x->rows != y->rows) return false;
-    if (x->batch > 1 && (x->stride_b != y->stride_b || x->stride_b < x->rows * x->ld)) return false;
-    const int64_t fx = (x->heads - 1) * x->stride_h + x->cols;
-    const int64_t fy = (y->heads - 1) * y->stride_h + y->cols;
-    const sbp_view4_t *a = x, *b = y;
-    int64_t fa = fx, fb = fy;
-    if (reinterpret_cast<uintptr_t>(b->data) < reinterpret_cast<uintptr_t>(a->data)) {
-        std::swap(a, b);
-        std::swap(fa, fb);
-    }
-    const uintptr_t gap =
-        reinterpret_cast<uintptr_t>(b->data) - reinterpret_cast<uintptr_t>(a->data);
-    if (gap % elsz(a->dtype)) return false;
-    const int64_t at = (int64_t)(gap / elsz(a->dtype));
-    return fa <= at && at + fb <= a->ld;
-}
-
-bool outputs_clash(const sbp_view4_t *x, const sbp_view4_t *y) {
-    return overlap(span4(x->data, x, x->heads), span4(y->data, y, y->heads)) && !interleaved(x, y);
-}
-
 // The call's operands on rank r: Q's heads are split in groups, one group per key
 // head of the rank's share.
 struct Call {
@@ -62,17 +22,6 @@ struct Call {
     int64_t q0 = 0;                // rank's first query head
     int64_t H = 0;                 // query heads of the GLOBAL views, or hq
 };
-
-sbpi::CoreView kernel_view(const sbp_view4_t *v, int64_t first_head) {
-    sbpi::CoreView o;
-    o.p = v->data;
-    if (o.p && v->heads > 0)
-        o.p = static_cast<char *>(v->data) + first_head * v->stride_h * elsz(v->dtype);
-    o.sb = v->stride_b;
-    o.sh = v->stride_h;
-    o.ld = v->ld;
-    return o;
-}
 
 // Checks Q, K, V, the options and the rank; fills the shapes and views of them.
 int prepare(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_view4_t *V,
@@ -149,47 +98,9 @@ int query_operand(const sbp_view4_t *v, const Call &c, const sbp_view4_t *Q, int
     return SBP_OK;
 }
 
-// An output of `heads` local heads.
-int output(const sbp_view4_t *v, int64_t batch, int64_t heads, int64_t rows, int64_t cols,
-           sbpi::CoreView *out) {
-    int rc = check_bounded(v);
-    if (rc) return rc;
-    if (v->batch != batch || v->heads != heads || v->rows != rows || v->cols != cols)
-        return SBP_ERR_SHAPE;
-    if (v->scope == SBP_ACCUMULATE && v->dtype != SBP_F32) return SBP_ERR_DTYPE;
-    if (!injective(v)) return SBP_ERR_SHAPE;
-    *out = kernel_view(v, 0);
-    return SBP_OK;
-}
-
 std::pair<uintptr_t, uintptr_t> span_of(const sbpi::CoreView &v, const sbp_view4_t *s,
                                         int64_t heads) {
     return span4(v.p, s, heads);
-}
-
-// 16-byte rows, and tile offsets that fit a 31-bit buffer offset (256 rows at most).
-bool rows16(const sbpi::CoreView &v, int64_t d) {
-    return reinterpret_cast<uintptr_t>(v.p) % 16 == 0 && v.ld % 8 == 0 && v.sb % 8 == 0 &&
-           v.sh % 8 == 0 && d % 8 == 0 && v.ld < (int64_t(1) << 21);
-}
-
-std::pair<uintptr_t, uintptr_t> lens_span(const int32_t *p, int64_t batch) {
-    const uintptr_t b = reinterpret_cast<uintptr_t>(p);
-    return p ? std::make_pair(b, b + (uintptr_t)(4 * batch)) : std::make_pair(uintptr_t(0), uintptr_t(0));
-}
-
-int check_ws(const sbp_workspace_t *ws, sbpi::CoreArgs *a,
-             std::pair<uintptr_t, uintptr_t> *span) {
-    *span = {0, 0};
-    if (!ws || ws->bytes == 0) return SBP_OK;
-    if (ws->bytes < 0) return SBP_ERR_SHAPE;
-    if (!ws->data) return SBP_ERR_NULL;
-    const uintptr_t b = reinterpret_cast<uintptr_t>(ws->data);
-    if (b & 15) return SBP_ERR_ALIGN;
-    a->ws = static_cast<float *>(ws->data);
-    a->ws_floats = (size_t)ws->bytes / sizeof(float);
-    *span = {b, b + (uintptr_t)ws->bytes};
-    return SBP_OK;
 }
 
 int finish(hipError_t e) { return e == hipSuccess ? SBP_OK : hip_error(e); }
@@ -214,7 +125,7 @@ int sbp_attn_core_fwd(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_view
         if (lse->dtype != SBP_F32) return SBP_ERR_DTYPE;
     }
     std::pair<uintptr_t, uintptr_t> wspan;
-    if ((rc = check_ws(ws, &a, &wspan))) return rc;
+    if ((rc = check_ws(ws, &a.ws, &a.ws_floats, &wspan))) return rc;
     const std::pair<uintptr_t, uintptr_t> ins[5] = {
         span_of(a.q, Q, c.hq), span_of(a.k, K, c.hk), span_of(a.v, V, c.hk),
         lens_span(a.len_q, Q->batch), lens_span(a.len_k, Q->batch)};
@@ -257,7 +168,7 @@ int sbp_attn_core_bwd(const sbp_view4_t *dO, const sbp_view4_t *Q, const sbp_vie
     a.dk_acc = dK->scope == SBP_ACCUMULATE;
     a.dv_acc = dV->scope == SBP_ACCUMULATE;
     std::pair<uintptr_t, uintptr_t> wspan;
-    if ((rc = check_ws(ws, &a, &wspan))) return rc;
+    if ((rc = check_ws(ws, &a.ws, &a.ws_floats, &wspan))) return rc;
     const std::pair<uintptr_t, uintptr_t> ins[8] = {
         span_of(a.q, Q, c.hq),        span_of(a.k, K, c.hk),
         span_of(a.v, V, c.hk),        span_of(a.dout, dO, c.hq),

@@ -50,12 +50,18 @@ EXPORTS = ("sbp_shard_index", "sbp_signature", "sbp_linear_fwd", "sbp_linear_bwd
            "sbp_attn_context_bwd", "sbp_set_override_orients", "sbp_collective_cost",
            "sbp_boxing_cost", "sbp_chain_cost", "sbp_search_strategy", "sbp_linear_bwd_noalloc",
            "sbp_attn_core_fwd", "sbp_attn_core_bwd", "sbp_gated_fwd", "sbp_gated_bwd",
-           "sbp_nd_gated_fwd", "sbp_nd_gated_bwd")
+           "sbp_nd_gated_fwd", "sbp_nd_gated_bwd", "sbp_rope_turns", "sbp_rope_fwd", "sbp_rope_bwd",
+           "sbp_paged_append", "sbp_paged_attn")
 
 SBP_COLL_ALLREDUCE, SBP_COLL_ALLGATHER, SBP_COLL_REDUCESCATTER, SBP_COLL_ALLTOALL = 0, 1, 2, 3
 SBP_SIG_DP, SBP_SIG_COL, SBP_SIG_KS, SBP_SIG_PB, SBP_SIG_BP, SBP_SIG_BB = 0, 1, 2, 3, 4, 5
 SBP_ACT_SILU, SBP_ACT_GELU, SBP_ACT_RELU = 0, 1, 2
 ACTS = {"silu": SBP_ACT_SILU, "gelu": SBP_ACT_GELU, "relu": SBP_ACT_RELU}
+SBP_ROPE_HALVES, SBP_ROPE_PAIRS = 0, 1
+SBP_ROPE_PLAIN, SBP_ROPE_LINEAR, SBP_ROPE_BASE, SBP_ROPE_BY_TURNS, SBP_ROPE_BY_PAIRS = 0, 1, 2, 3, 4
+ROPE_ORDERS = {"halves": SBP_ROPE_HALVES, "pairs": SBP_ROPE_PAIRS}
+ROPE_SCALINGS = {None: SBP_ROPE_PLAIN, "linear": SBP_ROPE_LINEAR, "base": SBP_ROPE_BASE,
+                 "turns": SBP_ROPE_BY_TURNS, "pairs": SBP_ROPE_BY_PAIRS}
 SIG_IDS = {"DP": 0, "COL": 1, "KS": 2, "PB": 3, "BP": 4, "BB": 5}
 
 SBP_MAX_MESH_DIMS = 4
@@ -114,6 +120,21 @@ class sbp_attn_opts_t(ctypes.Structure):
     _fields_ = [("scale", ctypes.c_float), ("causal", ctypes.c_int32),
                 ("window", ctypes.c_int32), ("len_q", ctypes.c_void_p),
                 ("len_k", ctypes.c_void_p)]
+
+
+class sbp_rope_t(ctypes.Structure):
+    _fields_ = [("turns", ctypes.c_void_p), ("dim", ctypes.c_int32), ("order", ctypes.c_int32),
+                ("mul", ctypes.c_float)]
+
+
+class sbp_places_t(ctypes.Structure):
+    _fields_ = [("pos", ctypes.c_void_p), ("ld", ctypes.c_int64), ("per_row", ctypes.c_int32)]
+
+
+class sbp_pages_t(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_ld", ctypes.c_int64),
+                ("seqs", ctypes.c_int32), ("width", ctypes.c_int32), ("len_k", ctypes.c_void_p),
+                ("len_q", ctypes.c_void_p), ("row_q", ctypes.c_void_p)]
 
 
 class sbp_chain_t(ctypes.Structure):
@@ -245,6 +266,18 @@ def lib():
                                         ctypes.c_void_p]
         L.sbp_attn_core_bwd.argtypes = [V4, V4, V4, V4, V4, V4, OPT, V4, V4, V4, ctypes.c_int32,
                                         ctypes.c_int32, WS, ctypes.c_void_p]
+        ROPE, PLACES, PAGES = P(sbp_rope_t), P(sbp_places_t), P(sbp_pages_t)
+        L.sbp_rope_turns.argtypes = [ctypes.c_int32, ctypes.c_double, ctypes.c_int32,
+                                     ctypes.c_double, ctypes.c_double, ctypes.c_double,
+                                     ctypes.c_double, P(ctypes.c_uint64)]
+        for fn in ("sbp_rope_fwd", "sbp_rope_bwd"):
+            getattr(L, fn).argtypes = [V4, V4, ROPE, PLACES, V4, V4, ctypes.c_int32, ctypes.c_int32,
+                                       ctypes.c_void_p]
+        L.sbp_paged_append.argtypes = [V4, V4, PAGES, ROPE, V4, V4, V4, V4, ctypes.c_int32,
+                                       ctypes.c_int32, ctypes.c_void_p]
+        L.sbp_paged_attn.argtypes = [V4, V4, V4, PAGES, ctypes.c_float, ctypes.c_int32,
+                                     ctypes.c_int32, V4, V4, ctypes.c_int32, ctypes.c_int32, WS,
+                                     ctypes.c_void_p]
         D = ctypes.c_double
         L.sbp_collective_cost.argtypes = [ctypes.c_int32, ctypes.c_int32, D, D, D, P(D)]
         L.sbp_boxing_cost.argtypes = [P(sbp_layout_t), P(sbp_layout_t), D, D, D, P(D),
@@ -641,6 +674,57 @@ def sbp_attn_core_bwd(dO, Q, K, V, O, lse, opts: sbp_attn_opts_t, dQ, dK, dV, p:
     rc = (_lib or lib()).sbp_attn_core_bwd(ref(dO), ref(Q), ref(K), ref(V), ref(O), ref(lse),
                                            ref(opts), ref(dQ), ref(dK), ref(dV), p, r,
                                            ref(_ws(ws, s)), ctypes.c_void_p(s))
+    if rc:
+        _check(rc)
+
+
+# ----------------------------------------------------- rotary positions
+def sbp_rope_turns(dim: int, base: float = 10000.0, scaling: int = SBP_ROPE_PLAIN,
+                   factor: float = 1.0, low: float = 1.0, high: float = 32.0,
+                   context: float = 1.0) -> list[int]:
+    """The dim / 2 frequencies, in 2^-64 turns a position."""
+    turns = (ctypes.c_uint64 * max(dim // 2, 1))()
+    _check(lib().sbp_rope_turns(dim, base, scaling, factor, low, high, context, turns))
+    return list(turns)
+
+
+def _ref(x):
+    return None if x is None else ctypes.byref(x)
+
+
+def sbp_rope_fwd(Q, K, rope: sbp_rope_t, at, Qo, Ko, p: int, r: int, stream=None):
+    """Qo and Ko: Q and K (or None) rotated by the positions of their rows (at: an
+    sbp_places_t, or None)."""
+    rc = (_lib or lib()).sbp_rope_fwd(_ref(Q), _ref(K), _ref(rope), _ref(at), _ref(Qo), _ref(Ko), p,
+                                      r, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def sbp_rope_bwd(dQo, dKo, rope: sbp_rope_t, at, dQ, dK, p: int, r: int, stream=None):
+    """dQ and dK from the gradients of sbp_rope_fwd's outputs."""
+    rc = (_lib or lib()).sbp_rope_bwd(_ref(dQo), _ref(dKo), _ref(rope), _ref(at), _ref(dQ),
+                                      _ref(dK), p, r, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+# ------------------------------------------------------------ paged cache
+def sbp_paged_append(K, V, pages: sbp_pages_t, rope, Kc, Vc, Q, Qo, p: int, r: int, stream=None):
+    """New tokens' K and V into the cache Kc, Vc; K and Q (into Qo) rotated with a rope."""
+    rc = (_lib or lib()).sbp_paged_append(_ref(K), _ref(V), _ref(pages), _ref(rope), _ref(Kc),
+                                          _ref(Vc), _ref(Q), _ref(Qo), p, r, _stream(stream))
+    if rc:
+        _check(rc)
+
+
+def sbp_paged_attn(Q, Kc, Vc, pages: sbp_pages_t, scale: float, causal: int, window: int, O, lse,
+                   p: int, r: int, stream=None, ws=None):
+    """O and lse (a view, or None) of rank r's heads over the cache."""
+    s = current_stream() if stream is None else stream
+    rc = (_lib or lib()).sbp_paged_attn(_ref(Q), _ref(Kc), _ref(Vc), _ref(pages), scale, causal,
+                                        window, _ref(O), _ref(lse), p, r, _ref(_ws(ws, s)),
+                                        ctypes.c_void_p(s))
     if rc:
         _check(rc)
 

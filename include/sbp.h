@@ -586,7 +586,7 @@ typedef struct {
  * (the same address, strides and dtype: in place); else no output may overlap an input or the
  * other output, but for outputs that interleave as those of sbp_attn_core_bwd may.
  * Errors: those of the attention calls; SBP_ERR_SHAPE also for more than 2^29 rows of a
- * sequence, or 2^31 pairs of a row and a part of 16 columns over the rank's heads. */
+ * sequence, or 2^31 / ((D + 31) / 16) rows over the rank's heads. */
 int sbp_rope_fwd(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_rope_t *rope,
                  const sbp_places_t *at, sbp_view4_t *Qo, sbp_view4_t *Ko, int32_t p, int32_t r,
                  hipStream_t stream);
@@ -602,9 +602,10 @@ int sbp_rope_bwd(const sbp_view4_t *dQo, const sbp_view4_t *dKo, const sbp_rope_
  * call runs. The new tokens' rows (of Q, K, V and O) are
  *   padded   row_q NULL: views of `seqs` batches, sequence b the first len_q[b] rows of batch b
  *            (limited to [0, rows]; len_q NULL: all)
- *   packed   views of one batch, sequence b rows row_q[b] .. row_q[b + 1] - 1 (limited to the
- *            view, and to none where they descend). len_q must be NULL. Rows of no sequence
- *            are never read or written.
+ *   packed   views of one batch, sequence b rows row_q[b] .. row_q[b + 1] - 1, limited to the
+ *            view. row_q must not descend (else whose row is whose is not defined, but nothing
+ *            outside the views is touched). len_q must be NULL. Rows of no sequence are never
+ *            read or written.
  * len_k[b]: tokens that sequence b has in the cache once its n new ones are there, so that new
  * token i is at place len_k[b] - n + i. */
 typedef struct {
@@ -626,7 +627,7 @@ typedef struct {
  * else of the cache is written. Two tokens of one call must not share a row of the cache (it
  * would hold parts of either). Qo's rows past len_q stay as they are.
  * Errors: those of the attention calls; SBP_ERR_SHAPE also for P < 1, width P > 2^29, more than
- * 2^20 sequences, 2^31 pairs as for sbp_rope_fwd, or rows that do not fit `seqs`; SBP_ERR_ALIAS
+ * 2^20 sequences, more rows over the heads of Q, K and V than sbp_rope_fwd takes, or rows that do not fit `seqs`; SBP_ERR_ALIAS
  * also for a cache that overlaps another operand or whose own elements overlap. */
 int sbp_paged_append(const sbp_view4_t *K, const sbp_view4_t *V, const sbp_pages_t *pages,
                      const sbp_rope_t *rope, sbp_view4_t *Kc, sbp_view4_t *Vc,

@@ -1,7 +1,11 @@
 // paged_append.hip -- new tokens' keys and values to their places in a paged cache, with the
 // rotation of K and Q on the way.
 //
-// A thread owns a pair of columns of a new token, over all heads of Q, K and V.
+// A thread owns 16 columns of a new token and takes them in HEADS of the heads of Q, K and V, one
+// after the other (rope.hip): the token's place gives both its row of the cache and its
+// angles. In a packed batch a wave finds its first row's sequence by a search of 64 places at a
+// time. The bound is memory, for few tokens the chain of loads from a row to its page.
+#include "attn_core_kernel.h"
 #include "paged_kernel.h"
 #include "profile.h"
 #include "rope_kernel.h"
@@ -10,50 +14,73 @@ namespace sbpk {
 
 using sbpi::AppendArgs;
 
-template <typename TQ>
-__global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
+struct AppendLaunch {
+    AppendArgs a;
+    int32_t threads;                 // rows x head groups x units
+    Div units, groups, rows, page;   // of a head, of a row, of a batch, tokens of a page
+};
+
+template <typename TQ, int HEADS>
+__global__ __launch_bounds__(256) void paged_append_kernel(AppendLaunch f) {
+    const AppendArgs &a = f.a;
     const Rotation &r = a.rot;
-    const int half = r.dim / 2, units = half + (a.d - r.dim);
-    const SeqRows s = rows_of(a.at, blockIdx.y);
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int u = (int)(id % units);
-    const int64_t i = id / units;
-    if (i >= s.n) return;
-    const int64_t t = (int64_t)s.len - s.n + i;
-    int one = r.dim + (u - half), two = one;
-    float c = 1.f, sn = 0.f;
-    if (u < half) {
-        columns(r, u, &one, &two);
-        angle(r.turns[u], t, r.mul, &c, &sn);
+    const uint32_t id = blockIdx.x * 256u + threadIdx.x;
+    if (blockIdx.x * 256u + (threadIdx.x & ~63u) >= (uint32_t)f.threads) return;   // whole waves
+    const int rest = f.units(id), ui = f.units.rest(id, rest);
+    const int row = f.groups(rest), hg = f.groups.rest(rest, row);
+    int b = f.rows(row), i = f.rows.rest(row, b);
+    const int batch = b;
+    int n = a.at.rows, first = 0;
+    bool live = id < (uint32_t)f.threads;
+    if (a.at.row_q) {
+        // the last sequence that begins at or before the row
+        b = sequence_of(a.at, __builtin_amdgcn_readfirstlane(row));
+        while (live && b < a.at.seqs && a.at.row_q[b + 1] <= row) ++b;
+        live = live && b >= 0 && b < a.at.seqs;
+        if (!live) b = 0;
+        first = max(a.at.row_q[b], 0);
+        n = min(a.at.row_q[b + 1], a.at.rows) - first;
+    } else if (a.at.len_q) {
+        n = min(max(a.at.len_q[b], 0), a.at.rows);
     }
-    auto turn = [&](const uint16_t *in, auto *out) {
-        const float v = load1(in + one), w = load1(in + two);
-        if (u < half) {
-            store1(out + one, v * c - w * sn);
-            store1(out + two, w * c + v * sn);
-        } else {
-            store1(out + one, v);
+    const int new_i = i - first;
+    if (!live || new_i < 0 || new_i >= n) return;
+    const int64_t t = (int64_t)a.at.len_k[b] - n + new_i;
+    const int heads = a.q_heads + 2 * a.kv_heads, step = (int)f.groups.d;
+    const Unit u = unit_of(r, a.d, ui);
+    // head h of Q's, then K's, then V's
+    Pair<uint16_t> x[HEADS];
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = hg + k * step;
+        const int hk = h - a.q_heads, hv = hk - a.kv_heads;
+        const CoreView &v = hk < 0 ? a.q : hv < 0 ? a.k : a.v;
+        const int m = hk < 0 ? h : hv < 0 ? hk : hv;
+        if (h < heads) x[k].load(static_cast<const uint16_t *>(v.p) + batch * v.sb + m * v.sh + i * v.ld, u);
+    }
+    int page = -1, slot = 0;
+    if (t >= 0 && t < (int64_t)a.at.width * a.at.page) {
+        const int at = f.page((int)t);
+        slot = f.page.rest((int)t, at);
+        page = a.at.table[b * a.at.table_ld + at];
+    }
+    Angles g;
+    if (u.turn) g.find(r, ui, t, false);
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = hg + k * step;
+        const int hk = h - a.q_heads, hv = hk - a.kv_heads;
+        if (h >= heads) continue;
+        if (hk < 0) {
+            put(x[k], g, u, r.pairs,
+                static_cast<TQ *>(a.qo.p) + batch * a.qo.sb + h * a.qo.sh + i * a.qo.ld);
+        } else if (page >= 0 && page < a.at.pages) {
+            const CoreView &v = hv < 0 ? a.kc : a.vc;
+            Unit w = u;
+            w.turn = u.turn && hv < 0;
+            put(x[k], g, w, r.pairs, static_cast<uint16_t *>(v.p) + page * v.sb +
+                                         (hv < 0 ? hk : hv) * v.sh + slot * v.ld);
         }
-    };
-    auto row = [&](const CoreView &v, int h) {
-        return static_cast<uint16_t *>(v.p) + s.batch * v.sb + h * v.sh + (s.first + i) * v.ld;
-    };
-    if (a.q.p)
-        for (int h = 0; h < a.q_heads; ++h)
-            turn(row(a.q, h), static_cast<TQ *>(a.qo.p) + s.batch * a.qo.sb + h * a.qo.sh +
-                                  (s.first + i) * a.qo.ld);
-    if (t < 0 || t >= (int64_t)a.at.width * a.at.page) return;
-    const int page = a.at.table[blockIdx.y * a.at.table_ld + t / a.at.page];
-    if (page < 0 || page >= a.at.pages) return;
-    auto slot = [&](const CoreView &v, int h) {
-        return static_cast<uint16_t *>(v.p) + page * v.sb + h * v.sh + (t % a.at.page) * v.ld;
-    };
-    for (int h = 0; h < a.kv_heads; ++h) {
-        turn(row(a.k, h), slot(a.kc, h));
-        const uint16_t *in = row(a.v, h);
-        uint16_t *out = slot(a.vc, h);
-        out[one] = in[one];
-        out[two] = in[two];
     }
 }
 
@@ -61,12 +88,30 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendArgs a) {
 
 namespace sbpi {
 
+namespace {
+
+template <typename TQ>
+hipError_t launch(const AppendArgs &a, hipStream_t s) {
+    sbpk::AppendLaunch f;
+    f.a = a;
+    const int64_t rows = (int64_t)a.batch * a.at.rows;
+    const int heads = a.q_heads + 2 * a.kv_heads, units = sbpk::units_of(a.rot, a.d);
+    const bool many = rows * heads * units > (int64_t)device_cus() * 2048;
+    const int groups = many ? (heads + 3) / 4 : heads;
+    f.threads = (int32_t)(rows * groups * units);
+    f.units = sbpk::Div(units);
+    f.groups = sbpk::Div(groups);
+    f.rows = sbpk::Div(a.at.rows);
+    f.page = sbpk::Div(a.at.page);
+    const dim3 grid((unsigned)((f.threads + 255ll) / 256)), block(256);
+    return many ? launch_kernel(sbpk::paged_append_kernel<TQ, 4>, "paged_append_kernel<4>", grid, block, s, f)
+                : launch_kernel(sbpk::paged_append_kernel<TQ, 1>, "paged_append_kernel<1>", grid, block, s, f);
+}
+
+}  // namespace
+
 hipError_t launch_append(const AppendArgs &a, int qo_f32, hipStream_t s) {
-    const int64_t n = (int64_t)a.at.rows * (a.rot.dim / 2 + a.d - a.rot.dim);
-    const dim3 grid((unsigned)((n + 255) / 256), (unsigned)a.at.seqs), block(256);
-    if (qo_f32)
-        return launch_kernel(sbpk::paged_append_kernel<float>, "paged_append_kernel", grid, block, s, a);
-    return launch_kernel(sbpk::paged_append_kernel<uint16_t>, "paged_append_kernel", grid, block, s, a);
+    return qo_f32 ? launch<float>(a, s) : launch<uint16_t>(a, s);
 }
 
 }  // namespace sbpi

@@ -13,6 +13,11 @@ namespace sbpk {
 
 using sbpi::PagedArgs;
 
+__device__ __forceinline__ float load1(const uint16_t *p) {
+    return __builtin_bit_cast(float, (uint32_t)*p << 16);
+}
+__device__ __forceinline__ void store1(uint16_t *p, float v) { *p = f32_to_bf16_bits(v); }
+
 __global__ __launch_bounds__(256) void paged_attn_kernel(PagedArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t id = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);

@@ -29,4 +29,21 @@ __device__ __forceinline__ SeqRows rows_of(const Pages &p, int b) {
     return s;
 }
 
+// The last sequence whose first row is at or before `row` (uniform over the wave; -1: none, seqs:
+// row lies behind all), of first rows that do not descend. Every step looks at 64 places
+// of what is left; a whole wave calls it.
+__device__ __forceinline__ int sequence_of(const Pages &p, int row) {
+    const int lane = threadIdx.x & 63;
+    int lo = -1, n = p.seqs + 1;      // the answer is lo or one of the next n
+    while (n > 0) {
+        const int step = (n + 63) / 64, at = lo + (lane + 1) * step;
+        const bool in = at <= lo + n && p.row_q[at] <= row;
+        const int below = __builtin_popcountll(__ballot(in));
+        const int end = lo + n;
+        lo += below * step;
+        n = min(step - 1, end - lo);
+    }
+    return lo;
+}
+
 }  // namespace sbpk

@@ -1,57 +1,84 @@
 // rope.hip -- rotary positions of Q and K, forward and backward.
 //
-// A thread owns a pair of columns of a row, over all heads of Q and K: its angle is computed
-// once.
+// A thread owns 16 columns (8 pairs) of a row and turns them in HEADS heads of Q and K, one
+// after the other: the angles are computed once for these, while the heads' values are on
+// the way. The bound is memory: each element is read once and written once.
+#include "attn_core_kernel.h"
 #include "profile.h"
 #include "rope_kernel.h"
 
 namespace sbpk {
 
-template <typename TI, typename TO>
-__global__ __launch_bounds__(256) void rope_kernel(RopeArgs a) {
+struct RopeLaunch {
+    RopeArgs a;
+    int32_t threads;                 // rows x head groups x units
+    Div units, groups, rows;         // of a head, of a row, of a sequence
+};
+
+template <typename TI, typename TO, int HEADS>
+__global__ __launch_bounds__(256) void rope_kernel(RopeLaunch f) {
+    const RopeArgs &a = f.a;
     const Rotation &r = a.rot;
-    const int half = r.dim / 2, units = half + (a.d - r.dim);
-    const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    const int u = (int)(id % units);
-    const int64_t row = id / units;
-    if (row >= (int64_t)a.batch * a.rows) return;
-    const int b = (int)(row / a.rows), i = (int)(row % a.rows);
-    int one = r.dim + (u - half), two = one;
-    float c = 1.f, s = 0.f;
-    if (u < half) {
-        columns(r, u, &one, &two);
+    const uint32_t id = blockIdx.x * 256u + threadIdx.x;
+    if (id >= (uint32_t)f.threads) return;
+    const int rest = f.units(id), ui = f.units.rest(id, rest);
+    const int row = f.groups(rest), hg = f.groups.rest(rest, row);
+    const int b = f.rows(row), i = f.rows.rest(row, b);
+    const Unit u = unit_of(r, a.d, ui);
+    const int heads = a.heads[0] + a.heads[1], step = (int)f.groups.d;
+    auto at = [&](const CoreView (&v)[2], int h) {    // element offset of head h's row
+        return h < a.heads[0] ? b * v[0].sb + i * v[0].ld + h * v[0].sh
+                              : b * v[1].sb + i * v[1].ld + (h - a.heads[0]) * v[1].sh;
+    };
+    auto base = [&](const CoreView (&v)[2], int h) { return h < a.heads[0] ? v[0].p : v[1].p; };
+    Pair<TI> x[HEADS];
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = hg + k * step;
+        if (h < heads) x[k].load(static_cast<const TI *>(base(a.in, h)) + at(a.in, h), u);
+    }
+    Angles g;
+    if (u.turn) {
         int64_t t = i;
         if (a.pos) t = a.pos_per_row ? a.pos[b * a.pos_ld + i] : (int64_t)a.pos[b * a.pos_ld] + i;
-        angle(r.turns[u], t, r.mul, &c, &s);
-        if (a.back) s = -s;
+        g.find(r, ui, t, a.back);
     }
-    for (int x = 0; x < 2; ++x)
-        for (int h = 0; h < a.heads[x]; ++h) {
-            const TI *in = static_cast<const TI *>(a.in[x].p) + b * a.in[x].sb + h * a.in[x].sh +
-                           i * a.in[x].ld;
-            TO *out = static_cast<TO *>(a.out[x].p) + b * a.out[x].sb + h * a.out[x].sh +
-                      i * a.out[x].ld;
-            const float v = load1(in + one), w = load1(in + two);
-            if (u < half) {
-                store1(out + one, v * c - w * s);
-                store1(out + two, w * c + v * s);
-            } else {
-                store1(out + one, v);
-            }
-        }
+#pragma unroll
+    for (int k = 0; k < HEADS; ++k) {
+        const int h = hg + k * step;
+        if (h < heads) put(x[k], g, u, r.pairs, static_cast<TO *>(base(a.out, h)) + at(a.out, h));
+    }
 }
 
 }  // namespace sbpk
 
 namespace sbpi {
 
+namespace {
+
+template <typename TI, typename TO>
+hipError_t launch(const RopeArgs &a, hipStream_t s) {
+    sbpk::RopeLaunch f;
+    f.a = a;
+    const int64_t rows = (int64_t)a.batch * a.rows;
+    const int heads = a.heads[0] + a.heads[1], units = sbpk::units_of(a.rot, a.d);
+    const bool many = rows * heads * units > (int64_t)device_cus() * 2048;
+    const int groups = many ? (heads + 3) / 4 : heads;
+    f.threads = (int32_t)(rows * groups * units);
+    f.units = sbpk::Div(units);
+    f.groups = sbpk::Div(groups);
+    f.rows = sbpk::Div(a.rows);
+    const dim3 grid((unsigned)((f.threads + 255ll) / 256)), block(256);
+    return many ? launch_kernel(sbpk::rope_kernel<TI, TO, 4>, "rope_kernel<4>", grid, block, s, f)
+                : launch_kernel(sbpk::rope_kernel<TI, TO, 1>, "rope_kernel<1>", grid, block, s, f);
+}
+
+}  // namespace
+
 hipError_t launch_rope(const RopeArgs &a, int in_f32, int out_f32, hipStream_t s) {
-    const int64_t n = (int64_t)a.batch * a.rows * (a.rot.dim / 2 + a.d - a.rot.dim);
-    const dim3 grid((unsigned)((n + 255) / 256)), block(256);
-    if (in_f32) return launch_kernel(sbpk::rope_kernel<float, float>, "rope_kernel", grid, block, s, a);
-    if (out_f32)
-        return launch_kernel(sbpk::rope_kernel<uint16_t, float>, "rope_kernel", grid, block, s, a);
-    return launch_kernel(sbpk::rope_kernel<uint16_t, uint16_t>, "rope_kernel", grid, block, s, a);
+    if (in_f32) return launch<float, float>(a, s);
+    if (out_f32) return launch<uint16_t, float>(a, s);
+    return launch<uint16_t, uint16_t>(a, s);
 }
 
 }  // namespace sbpi

@@ -31,44 +31,11 @@
 
 #include <algorithm>
 
-#include "attn_core_kernel.h"
+#include "attn_core_walk.h"
 #include "gemm.h"
 #include "profile.h"
 
 namespace sbpk {
-
-// O rows of 4 consecutive values starting at column `col` (col < d).
-template <class F>
-__device__ __forceinline__ void store4(void *base, int64_t at, int col, int d, bool f32, bool vec,
-                                       F value) {
-    if (f32) {
-        float *p = static_cast<float *>(base) + at + col;
-        if (vec && col + 4 <= d) {
-            f32x4 v = {value(0), value(1), value(2), value(3)};
-            *reinterpret_cast<f32x4 *>(p) = v;
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < d) p[e] = value(e);
-    } else {
-        uint16_t *p = static_cast<uint16_t *>(base) + at + col;
-        if (vec && col + 4 <= d) {
-            u32x2 w;
-            w[0] = (uint32_t)f32_to_bf16_bits(value(0)) | (uint32_t)f32_to_bf16_bits(value(1)) << 16;
-            w[1] = (uint32_t)f32_to_bf16_bits(value(2)) | (uint32_t)f32_to_bf16_bits(value(3)) << 16;
-            *reinterpret_cast<u32x2 *>(p) = w;
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (col + e < d) p[e] = f32_to_bf16_bits(value(e));
-    }
-}
-
-// Exponents of base 2 beyond which a wave forms differences of scores first: the rounding of
-// m c is at most 2^-15 below it.
-constexpr float FAR = 1024.f;
 
 struct FwdArgs {
     CoreArgs a;
@@ -85,30 +52,13 @@ __device__ __forceinline__ f32x2 *stats_of(const FwdArgs &f, int64_t d4) {
                                      (int64_t)f.splits * f.a.batch * f.a.kv_heads * f.rows * d4);
 }
 
-// WPS: waves of a SIMD, of one workgroup or two.
-template <int DP, int KG, int KT, int NW_, int WPS_, bool DMA>
-struct FwdShape {
-    static constexpr int NW = NW_, WPS = WPS_;
-    static constexpr int ROWS = 32 * NW / KG, KEYS = KG * KT;
-    using Tile = RowTile<DP, KEYS, NW>;
-    static constexpr int STAGE = 2 * Tile::BYTES;    // K, then V
-    static constexpr int LOADS = 2 * Tile::NV;
-    static constexpr int ROOM = 163840 / (4 * WPS / NW);
-    static constexpr int FIT = ROOM / STAGE;
-    static constexpr int NS = !DMA ? 3 : FIT > 4 ? 4 : FIT;
-    static constexpr int PUT = NW * PUT_FLOATS<DP> * 4;
-    static constexpr int STATS = NW * 64 * 2 * 4;
-    static constexpr int LDS = NS * STAGE > PUT + STATS ? NS * STAGE : PUT + STATS;
-    static_assert(FIT >= NS && NS >= 3 && LDS <= ROOM, "three stages");
-};
-
 template <int DP, int KG, int KT, int NW, int WPS, bool DMA>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(WPS, WPS)))
 void attn_core_fwd_kernel(FwdArgs f) {
     using S = FwdShape<DP, KG, KT, NW, WPS, DMA>;
     using Tile = typename S::Tile;
     constexpr int ROWS = S::ROWS, NS = S::NS, KEYS = S::KEYS;
-    constexpr int NB = KT / 32, KS = DP / 16, DB = DP / 32;
+    constexpr int KS = DP / 16;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
     const uint32_t lds0 = lds_at(smem);
     const CoreArgs &a = f.a;
@@ -205,166 +155,39 @@ void attn_core_fwd_kernel(FwdArgs f) {
         if (s0 + 1 < s1) fetch(s0 + 1, 1);
     }
 
+    FwdRows<S> w(lds0 + kg * KT / Tile::RPS * Tile::SEG, lane, a.scale, lo, hi);
     // rows past a sequence's queries read nothing
     const bool live = valid && i < mask.lq;
     const uint16_t *Q = static_cast<const uint16_t *>(a.q.p) + (int64_t)b * a.q.sb +
                         head * a.q.sh + (int64_t)i * a.q.ld;
-    bf16x8 qf[KS];
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
-        qf[ks] = row_frag<DMA>(Q, ks * 16 + 8 * half, live ? a.d : 0);
-    settle(qf);
+        w.qf[ks] = row_frag<DMA>(Q, ks * 16 + 8 * half, live ? a.d : 0);
+    settle(w.qf);
 
-    const float c = a.scale * LOG2E;
-    const float grow = 8.f / c;
-    float m = -INFINITY, l = 0.f;
-    float mc = 0.f, limit = -INFINITY;   // what exponents add to s c; where the maximum moves
-    f32x16 o[DB];
-#pragma unroll
-    for (int x = 0; x < DB; ++x) o[x] = splat16(0.f);
-
-    // Two phases a block of 32 keys: the next block's scores beside this one's exponentials;
-    // then this block's product with V beside the next one's maximum. The first phase has
-    // priority over the other wave's second, which waits for less (16 heads over 4 of
-    // 8192 x 128, causal: 273 us without, 260).
-    typename Tile::Reader rd(lds0 + kg * KT / Tile::RPS * Tile::SEG, lane);
-    f32x16 sp[2];                   // scores of this block and the next, in turn
-    int stage = 0;                  // of the step at work
-    auto scores = [&](f32x16 &s, const typename Tile::Reader &r, int r0, auto beside)
-                      __attribute__((always_inline)) {
-        // operands are read AHEAD products early
-        constexpr int AHEAD = KS < 4 ? KS : 4;
-        bf16x8 k[KS];
-        s = splat16(0.f);
-#pragma unroll
-        for (int ks = 0; ks < AHEAD; ++ks) k[ks] = r.frag(r0, ks, 0);
-        beside(0);
-        __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-        for (int ks = 0; ks < KS; ++ks) {
-            if (ks + AHEAD < KS) k[ks + AHEAD] = r.frag(r0, ks + AHEAD, 0);
-            s = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k[ks], qf[ks], s, 0, 0, 0);
-            beside(ks + 1);
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    };
-    auto hide = [&](f32x16 &s, int k0, int r) {   // what this row does not see
-        const int key = k0 + 8 * (r >> 2) + 4 * half + (r & 3);
-        s[r] = key >= lo && key < hi ? s[r] : -INFINITY;
-    };
-    // Moves the maximum to `top`, the maximum of a lane's own scores s, where it grew by enough.
-    // Where a row's is FAR, s become differences from it, and every block comes here.
-    auto rise = [&](f32x16 &s, float top) __attribute__((always_inline)) {
-        float t0, t1;
-        halves(top, &t0, &t1);
-        top = fmaxf(t0, t1);
-        if (__any(top > limit)) {
-            const float mn = fmaxf(m, top);
-            const float x = mn == -INFINITY ? 1.f : exp2_((m - mn) * c);
-            m = mn;
-            limit = m + grow;
-            mc = m == -INFINITY ? 0.f : -m * c;
-            l *= x;
-#pragma unroll
-            for (int db = 0; db < DB; ++db)
-#pragma unroll
-                for (int r = 0; r < 16; ++r) o[db][r] *= x;
-            if (__any(fabsf(mc) > FAR)) {
-                const float base = m == -INFINITY ? 0.f : m;
-#pragma unroll
-                for (int r = 0; r < 16; ++r) s[r] -= base;
-                mc = 0.f;
-                limit = -INFINITY;
-            }
-        }
-    };
     // Waits for the step after x, and prepares the load of a later one.
     auto advance = [&](int x) __attribute__((always_inline)) {
         if constexpr (DMA) {
             wait_vm<(NS - 3) * S::LOADS>();
             __syncthreads();
-            fetch(x + NS - 1, stage == 0 ? NS - 1 : stage - 1);
+            fetch(x + NS - 1, w.stage == 0 ? NS - 1 : w.stage - 1);
         } else {
-            if (x + 1 < s1) arrive(stage == NS - 1 ? 0 : stage + 1);
+            if (x + 1 < s1) arrive(w.stage == NS - 1 ? 0 : w.stage + 1);
             __syncthreads();
             if (x + 2 < s1) fetch(x + 2, 0);
         }
     };
-    // EDGE: some row of the tile does not see every key of the step
+    auto seen = [&](int k0) { return w.seen(k0); };
+    auto first_key = [&](int x) { return k_beg + walk.step(x) * KEYS + kg * KT; };
     auto take = [&](int x, auto edge) __attribute__((always_inline)) {
-        constexpr bool EDGE = decltype(edge)::value;
-        const int kw = k_beg + walk.step(x) * KEYS + kg * KT;
-        const int kn = k_beg + walk.step(x + 1) * KEYS + kg * KT;
-        const bool wrap = stage == NS - 1;
-        const int by = wrap ? -(NS - 1) * S::STAGE : S::STAGE;
-#pragma unroll
-        for (int kb = 0; kb < NB; ++kb) {
-            const bool last = kb == NB - 1;
-            if (last) advance(x);
-            typename Tile::Reader nx = rd;       // where the next block lies
-            if (last) nx.move(by);
-            // with an even number of blocks a step the two take turns in place
-            constexpr bool TURN = NB % 2 == 0;
-            constexpr int ONE = 1;
-            const int now = TURN ? kb & 1 : 0;
-            f32x16 &s = sp[now], &s_n = sp[ONE - now];
-            bf16x8 tv[2][DB], p[2];
-            __builtin_amdgcn_sched_barrier(0);
-            __builtin_amdgcn_s_setprio(1);
-            scores(s_n, nx, last ? 0 : (kb + 1) * 32, [&](int part) __attribute__((always_inline)) {
-#pragma unroll
-                for (int r = 0; r < 16; ++r) {
-                    if (!in_part(r, part, KS + 1)) continue;
-                    s[r] = exp2_(__builtin_fmaf(s[r], c, mc));
-                    l += s[r];
-                    if (r % 8 == 7) p[r / 8] = pack8(s, r - 7);
-                }
-                // the first 16 keys' columns
-                if (part > KS - DB)
-                    tv[0][part - 1 - (KS - DB)] = rd.frag_t(part - 1 - (KS - DB), kb * 32, Tile::BYTES);
-            });
-            __builtin_amdgcn_s_setprio(0);
-            // the loads of a step, spread over its blocks: the last one's first
-            constexpr int PER = (S::LOADS + NB - 1) / NB;
-            const int first = last ? 0 : (kb + 1) * PER;
-            float top = -INFINITY;
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int db = 0; db < DB; ++db) {
-                    o[db] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(tv[h][db], p[h], o[db], 0, 0, 0);
-                    if (h == 0) tv[1][db] = rd.frag_t(db, kb * 32 + 16, Tile::BYTES);
-                    const int k = h * DB + db;
-#pragma unroll
-                    for (int q = PER * k / (2 * DB); q < PER * (k + 1) / (2 * DB); ++q)
-                        if (first + q < S::LOADS) fetch_part(first + q);
-                    // the next scores are there one product later
-#pragma unroll
-                    for (int r = 0; r < 16; ++r) {
-                        if (k == 0 || !in_part(r, k - 1, 2 * DB - 1)) continue;
-                        if constexpr (EDGE) hide(s_n, last ? kn : kw + (kb + 1) * 32, r);
-                        top = fmaxf(top, s_n[r]);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
-                }
-            if (!last || x + 1 < s1) rise(s_n, top);
-            if constexpr (!TURN) sp[0] = sp[1];
-        }
-        rd.move(by);
-        stage = wrap ? 0 : stage + 1;
+        w.template take<decltype(edge)::value>(first_key(x), first_key(x + 1), x + 1 < s1, seen,
+                                               [&]() __attribute__((always_inline)) { advance(x); },
+                                               fetch_part);
     };
     if (s0 < s1) {
         if constexpr (DMA) wait_vm<(NS - 2) * S::LOADS>();
         __syncthreads();
-        scores(sp[0], rd, 0, [](int) {});
-        const int kw = k_beg + walk.step(s0) * KEYS + kg * KT;
-        float top = -INFINITY;
-#pragma unroll
-        for (int r = 0; r < 16; ++r) {
-            hide(sp[0], kw, r);
-            top = fmaxf(top, sp[0][r]);
-        }
-        rise(sp[0], top);
+        w.begin(first_key(s0), seen);
     }
     int x = s0;
     for (; x < min(s1, walk.masked()); ++x) take(x, std::true_type{});
@@ -372,26 +195,8 @@ void attn_core_fwd_kernel(FwdArgs f) {
     wait_vm<0>();      // no load is on its way to LDS any more
     __syncthreads();
 
-    float l0, l1;
-    halves(l, &l0, &l1);
-    l = l0 + l1;
-    float mul = 1.f;         // 2^((m - the groups' maximum) c)
-    if constexpr (KG > 1) {
-        float *const stats = reinterpret_cast<float *>(smem + S::PUT) + lane;
-        stats[wave * 128] = m;
-        stats[wave * 128 + 64] = l;
-        __syncthreads();
-        const float *const p = stats + wr * KG * 128;
-        float mn = p[0];
-#pragma unroll
-        for (int k = 1; k < KG; ++k) mn = fmaxf(mn, p[k * 128]);
-        const float ms = mn == -INFINITY ? 0.f : mn;
-        l = 0.f;
-#pragma unroll
-        for (int k = 0; k < KG; ++k) l += p[k * 128 + 64] * exp2_((p[k * 128] - ms) * c);
-        mul = exp2_((m - ms) * c);
-        m = mn;
-    }
+    const float mul = w.join_groups(reinterpret_cast<float *>(smem + S::PUT) + lane, wave, wr);
+    const float m = w.m, l = w.l;
     // a row that sees no key: O = 0, lse = -infinity
     const bool some = live && l != 0.f;
     const float log_l = __builtin_amdgcn_logf(l);
@@ -404,7 +209,7 @@ void attn_core_fwd_kernel(FwdArgs f) {
                         : whole ? (int64_t)b * a.o.sb + head * a.o.sh + (int64_t)i * a.o.ld
                                 : at * d4;
     float *const put = reinterpret_cast<float *>(smem);
-    stage_rows<DP>(put + wave * PUT_FLOATS<DP>, o, some ? mul / l : 0.f, lane);
+    stage_rows<DP>(put + wave * PUT_FLOATS<DP>, w.o, some ? mul / l : 0.f, lane);
     if (valid && half == 0 && kg == 0) {
         if (!whole)
             stats_of(f, d4)[at] = some ? f32x2{m, l} : f32x2{-INFINITY, 0.f};

@@ -31,15 +31,16 @@ namespace sbpk {
 using sbpi::PagedArgs;
 
 constexpr int PAGES_AT_ONCE = 1024;
-constexpr int FIXED = 4;             // an item's fixed part, in steps
 constexpr int SHORTEST = 2;          // steps that a cut leaves on either side
-constexpr int SHARE = 8;             // units (steps and fixed parts) of a workgroup at least
 
 // What workgroup w leaves for the join where its share begins inside an item that workgroup
 // w - 1 began: the item's parts are in slot 1 of w - 1 and in slots 0 of w .. last. Else last < 0.
 struct Cut {
-    int32_t last, seq, head, tile;
+    int32_t last, head, row;         // first packed row of the tile
+    int32_t batch, first, rows;      // of its sequence
+    int32_t spare[2];
 };
+constexpr int CUT_FLOATS = sizeof(Cut) / 4;
 
 struct PagedLaunch {
     PagedArgs a;
@@ -47,8 +48,21 @@ struct PagedLaunch {
     int32_t split;                   // items may be cut
     int32_t vec;                     // O allows 4-value stores
     int32_t groups;                  // workgroups
-    Div page, group;
+    int32_t fixed, scale;            // an item's fixed part in steps; a unit has 2^scale steps
+    Div page, group, by_groups;
 };
+
+// The line of items. Its units are steps (`fixed` more an item), or, where the items are few and
+// short, equal parts of them: an item of n steps has 1 + (n - 1) per, and a workgroup's share is one
+// part, since a second one would cost it as much again.
+struct Line {
+    int32_t share;                   // units of a workgroup
+    float per;                       // 0: units are steps
+};
+
+// A value that all lanes have, in a scalar register: the compiler keeps what it loads in vector
+// registers, and all that follows from it.
+__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
 
 // The workspace: cuts, statistics (a row's maximum and sum), partial outputs.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
@@ -57,17 +71,10 @@ __host__ __device__ inline int64_t slot_floats(int64_t rows, int d) {
 }
 __device__ __forceinline__ Cut *cuts_of(const PagedLaunch &f) { return reinterpret_cast<Cut *>(f.a.ws); }
 __device__ __forceinline__ f32x2 *stats_of(const PagedLaunch &f) {
-    return reinterpret_cast<f32x2 *>(f.a.ws + 4 * (int64_t)f.groups);
+    return reinterpret_cast<f32x2 *>(f.a.ws + CUT_FLOATS * (int64_t)f.groups);
 }
 __device__ __forceinline__ float *parts_of(const PagedLaunch &f) {
-    return f.a.ws + 4 * (int64_t)f.groups + 4 * (int64_t)f.groups * f.slot_rows;
-}
-
-// A value that all lanes have, in a scalar register: the compiler keeps what it loads or gets from
-// LDS in vector registers, and all that follows from it.
-__device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirstlane(x); }
-__device__ __forceinline__ int64_t uniform(int64_t x) {
-    return (int64_t)((uint64_t)(uint32_t)uniform((int)(x >> 32)) << 32 | (uint32_t)uniform((int)x));
+    return f.a.ws + (CUT_FLOATS + 4 * f.slot_rows) * (int64_t)f.groups;
 }
 
 // A sequence: its rows (packed ones of the group: `rows`, of which those of n queries are in use),
@@ -75,16 +82,15 @@ __device__ __forceinline__ int64_t uniform(int64_t x) {
 struct Seq {
     SeqRows at;
     int rows, lk, off;
-    __device__ __forceinline__ Seq(const PagedArgs &a, int b) : Seq(a, rows_of(a.at, b)) {}
-    // The sequence that a whole workgroup works on.
-    __device__ __forceinline__ static Seq shared(const PagedArgs &a, int b) {
-        const SeqRows r = rows_of(a.at, b);
-        return Seq(a, SeqRows{a.at.row_q ? 0 : b, uniform(r.first), uniform(r.n), uniform(r.len)});
-    }
     __device__ __forceinline__ Seq(const PagedArgs &a, const SeqRows &r) : at(r) {
         rows = (a.at.row_q ? at.n : a.at.rows) * a.group;
         lk = min(max(at.len, 0), a.at.width * a.at.page);
         off = lk - at.n;
+    }
+    // The sequence that a whole workgroup works on.
+    __device__ __forceinline__ static Seq shared(const PagedArgs &a, int b) {
+        const SeqRows r = rows_of(a.at, b);
+        return Seq(a, SeqRows{a.at.row_q ? 0 : b, uniform(r.first), uniform(r.n), uniform(r.len)});
     }
     __device__ __forceinline__ int hi(const PagedArgs &a, int i) const {
         return a.causal ? max(0, min(lk, i + 1 + off)) : lk;
@@ -106,51 +112,49 @@ struct TileKeys {
         lo = s.lo(f.a, first);
         beg = lo & ~31;
         end = first <= last ? s.hi(f.a, last) : 0;
-        steps = end > lo ? (end - beg + KEYS - 1) / KEYS : 0;
+        steps = end > lo ? (int)((uint32_t)(end - beg + KEYS - 1) / KEYS) : 0;
     }
     // An item without steps counts as one: its rows are cleared.
     __device__ __forceinline__ int length() const { return max(steps, 1); }
-    __device__ __forceinline__ int cost() const { return FIXED + length(); }
+    __device__ __forceinline__ int cost(const PagedLaunch &f, const Line &line) const {
+        if (line.per != 0.f) return 1 + (int)((float)(length() - 1) * line.per);
+        return f.fixed + ((length() + (1 << f.scale) - 1) >> f.scale);
+    }
     // Where a cut u units into the item falls: it ends one part and begins the other.
-    __device__ __forceinline__ int cut(int64_t u, bool split) const {
+    __device__ __forceinline__ int cut(const PagedLaunch &f, const Line &line, int u) const {
+        const int c = cost(f, line), n = length();
         if (u <= 0) return 0;
-        if (u >= cost()) return length();
-        const int s = (int)u - FIXED;
-        if (!split) return 2 * s < length() ? 0 : length();
-        return s < SHORTEST ? 0 : length() - s < SHORTEST ? length() : s;
+        if (u >= c) return n;
+        if (line.per != 0.f) return (int)((float)u * ((float)n / (float)c));    // c <= n: grows with u
+        const int s = (u - f.fixed) << f.scale;
+        if (!f.split) return 2 * s < n ? 0 : n;
+        return s < SHORTEST ? 0 : n - s < SHORTEST ? n : s;
     }
 };
 
-__device__ __forceinline__ int64_t wave_up(int64_t x, int by) {
-    const uint32_t lo = __shfl_up((uint32_t)x, by), hi = __shfl_up((uint32_t)((uint64_t)x >> 32), by);
-    return (int64_t)((uint64_t)hi << 32 | lo);
+// Sum of x over this lane and those before it.
+__device__ __forceinline__ int upto_lane(int x) {
+    x += __builtin_amdgcn_update_dpp(0, x, 0x111, 0xf, 0xf, false);    // 1, 2, 4, 8 lanes up
+    x += __builtin_amdgcn_update_dpp(0, x, 0x112, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x114, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x118, 0xf, 0xf, false);
+    x += __builtin_amdgcn_update_dpp(0, x, 0x142, 0xa, 0xf, false);    // lanes 15 and 47, then 31
+    x += __builtin_amdgcn_update_dpp(0, x, 0x143, 0xc, 0xf, false);
+    return x;
 }
 
-// Sum of x over this and earlier threads of the workgroup; *total: over all. `room` holds NW.
-template <int NW>
-__device__ __forceinline__ int64_t scan(int64_t x, int64_t *room, int64_t *total) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int by = 1; by < 64; by *= 2) {
-        const int64_t y = wave_up(x, by);
-        if (lane >= by) x += y;
-    }
-    __syncthreads();
-    if (lane == 63) room[wave] = x;
-    __syncthreads();
-    int64_t sum = 0;
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-        if (w < wave) x += room[w];
-        sum += room[w];
-    }
-    *total = sum;
-    return x;
+// The kernel's arguments, to be read again: what the compiler reads before a loop of items it keeps
+// through all of them, spilled from scalar to vector registers.
+__device__ __forceinline__ const PagedLaunch &again() {
+    uint64_t p = (uint64_t)__builtin_amdgcn_kernarg_segment_ptr();
+    asm volatile("" : "+s"(p));
+    return *(const PagedLaunch *)(const __attribute__((address_space(4))) PagedLaunch *)p;
 }
 
 template <int DP, int KG, int KT, int NW, int WPS, bool DMA>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(WPS, WPS)))
-void paged_attn_kernel(PagedLaunch f) {
+void paged_attn_kernel(PagedLaunch f0) {
+    const PagedLaunch &f = f0;
     using S = FwdShape<DP, KG, KT, NW, WPS, DMA>;
     using Tile = typename S::Tile;
     constexpr int ROWS = S::ROWS, NS = S::NS, KEYS = S::KEYS, KS = DP / 16, NV = Tile::NV;
@@ -167,83 +171,99 @@ void paged_attn_kernel(PagedLaunch f) {
     const int64_t d4 = (a.d + 3) & ~3;
     const int wg = remap_xcd(blockIdx.x, f.groups);    // neighbours on the line share an L2
 
-    // This workgroup's part of the line, `left` units from unit u of tile `tile` of head hk of
-    // sequence b on.
-    int64_t cut0, u, left, total = 0;
-    int b, hk, wgs;
+    // This workgroup's part of the line: `left` units from unit u of tile `tile` of head hk of
+    // sequence b on. Every wave adds up the sequences by itself, a lane each. (Units fit 31 bits:
+    // the launch chooses their scale.)
+    int left, u, b = 0, hk, tile = 0;
+    Line line{0, 0.f};
+    Seq seq(a, SeqRows{0, 0, 0, 0});
     {
-        int64_t *const room = reinterpret_cast<int64_t *>(smem);
-        int64_t one = 0, upto = 0, sum = 0;    // a sequence's units a head; sums over the threads'
-        auto sums = [&](int base) {
+        SeqRows r{0, 0, 0, 0};
+        int one, upto, sum, at = 0;      // units of a head of the lane's sequence; sums
+        // 64 sequences at a time: first all, for the total; then, where the line changes to parts,
+        // the (64 at most) again; else on until the share's begin. (One loop, so that its code,
+        // run cold, is fetched once.)
+        enum { TOTAL, PARTS, FIND } pass = TOTAL;
+        for (int total = 0;;) {
+            int tiles = 0;
             one = 0;
-            if (base + tid < a.at.seqs) {
-                const Seq s(a, base + tid);
-                for (int t = 0; t * ROWS < s.rows; ++t) one += Keys(f, s, t).cost();
+            if (b + lane < a.at.seqs) {
+                r = rows_of(a.at, b + lane);
+                const Seq s(a, r);
+                for (; tiles * ROWS < s.rows; ++tiles) one += Keys(f, s, tiles).cost(f, line);
             }
-            upto = scan<NW>(one * a.kv_heads, room, &sum);
-        };
-        for (int base = 0; base < a.at.seqs; base += 64 * NW) {
-            sums(base);
+            upto = upto_lane(one * a.kv_heads);
+            sum = __builtin_amdgcn_readlane(upto, 63);
+            if (pass == FIND) {
+                if (at < sum || b + 64 >= a.at.seqs) break;
+                at -= sum;
+                b += 64;
+                continue;
+            }
             total += sum;
+            if (b + 64 < a.at.seqs) {
+                b += 64;
+                continue;
+            }
+            line.share = f.by_groups(total) + 1;
+            if (pass == TOTAL && b == 0 && f.split && f.scale == 0 && line.share < 32) {
+                const int items = __builtin_amdgcn_readlane(upto_lane(tiles), 63) * a.kv_heads;
+                if (4 * items <= f.groups) {
+                    // 1 + (n - 1) per parts an item: no more than workgroups, of 3 steps and more
+                    line.per = min((float)(f.groups - 1 - items) / (float)(total - f.fixed * items),
+                                   1.f / 3);
+                    pass = PARTS;
+                    total = 0;
+                    continue;
+                }
+            }
+            at = line.share * wg;
+            left = min(line.share, total - at);
+            if (left <= 0) {
+                if (f.split && tid == 0) cuts_of(f)[wg].last = -1;
+                return;
+            }
+            if (b == 0) break;
+            b = 0;
+            pass = FIND;
         }
-        total = uniform(total);
-        wgs = (int)min((int64_t)f.groups, max(total / SHARE, (int64_t)1));
-        if (total == 0 || wg >= wgs) {
-            if (f.split && tid == 0) cuts_of(f)[wg] = Cut{-1, 0, 0, 0};
-            return;
-        }
-        cut0 = total * wg / wgs;
-        left = total * (wg + 1) / wgs - cut0;
-        int64_t before = 0;
-        int base = 0;
-        for (;; base += 64 * NW) {
-            if (a.at.seqs > 64 * NW) sums(base);
-            if (cut0 < before + sum || base + 64 * NW >= a.at.seqs) break;
-            before += sum;
-        }
-        const int64_t in = cut0 - (before + upto - one * a.kv_heads);
-        if (in >= 0 && in < one * a.kv_heads) {
-            const int64_t head = (in | one) >> 32 ? in / one : (int64_t)((uint32_t)in / (uint32_t)one);
-            room[NW] = base + tid;
-            room[NW + 1] = head;
-            room[NW + 2] = in - head * one;
-        }
-        __syncthreads();
-        b = uniform((int)room[NW]);
-        hk = uniform((int)room[NW + 1]);
-        u = uniform(room[NW + 2]);
-        __syncthreads();
+        const int in = at - (upto - one * a.kv_heads);
+        const uint64_t here = __ballot(in >= 0 && in < one * a.kv_heads);
+        if (!here) return;     // (lengths that changed under way)
+        const int l = __builtin_ctzll(here);
+        b += l;
+        one = __builtin_amdgcn_readlane(one, l);
+        u = __builtin_amdgcn_readlane(in, l);
+        hk = (int)((uint32_t)u / (uint32_t)one);
+        u -= hk * one;
+        seq = Seq(a, SeqRows{a.at.row_q ? 0 : b, __builtin_amdgcn_readlane(r.first, l),
+                             __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)});
     }
-    int tile = 0;
-    Seq seq = Seq::shared(a, b);
-    while (u >= Keys(f, seq, tile).cost()) u -= Keys(f, seq, tile++).cost();
+    for (int c; u >= (c = Keys(f, seq, tile).cost(f, line)); ++tile) u -= c;
     if (f.split) {
         const Keys k(f, seq, tile);
-        Cut cut{-1, b, hk, tile};
-        const int at = k.cut(u, true);
-        if (wg > 0 && at > 0 && at < k.length() && k.cut(total * (wg - 1) / wgs - cut0 + u, true) == 0) {
+        Cut cut{-1, hk, tile * ROWS, seq.at.batch, seq.at.first, seq.rows, {0, 0}};
+        const int at = k.cut(f, line, u);
+        if (at > 0 && at < k.length() && k.cut(f, line, u - line.share) == 0) {
             // the workgroup of the item's last unit, unless its share's begin is moved to the end
-            const int64_t begin = cut0 - u, end = begin + k.cost();
-            int64_t w = min((int64_t)wgs - 1, (end - 1) * wgs / total);
-            while (w + 1 < wgs && total * (w + 1) / wgs < end) ++w;
-            while (total * w / wgs >= end) --w;
-            if (k.cut(total * w / wgs - begin, true) == k.length()) --w;
-            cut.last = (int)w;
+            int w = (int)((uint32_t)(k.cost(f, line) - u - 1) / (uint32_t)line.share);
+            if (w > 0 && k.cut(f, line, u + w * line.share) == k.length()) --w;
+            cut.last = wg + w;
         }
         if (tid == 0) cuts_of(f)[wg] = cut;
     }
 
-    const uint16_t *const K0 = static_cast<const uint16_t *>(a.kc.p);
-    const uint16_t *const V0 = static_cast<const uint16_t *>(a.vc.p);
     // a lane's place in a load's rows (DMA)
     const int row_of = lane / Tile::CPR, chunk = (lane % Tile::CPR) ^ Tile::swz(row_of);
     const int place_k = chunk * 8 < a.d ? (row_of * (int)a.kc.ld + chunk * 8) * 2 : OOB;
     const int place_v = chunk * 8 < a.d ? (row_of * (int)a.vc.ld + chunk * 8) * 2 : OOB;
 
     while (left > 0) {
+        const PagedLaunch &f = again();
+        const PagedArgs &a = f.a;
         const Keys k(f, seq, tile);
-        const int64_t until = min((int64_t)k.cost(), u + left);
-        const int s0 = k.cut(u, f.split), s1 = k.cut(until, f.split);
+        const int until = min(k.cost(f, line), u + left);
+        const int s0 = k.cut(f, line, u), s1 = k.cut(f, line, until);
         if (s0 < s1) {
             const bool whole = s0 == 0 && s1 == k.length();
             const int end1 = min(s1, k.steps);
@@ -262,13 +282,12 @@ void paged_attn_kernel(PagedLaunch f) {
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks)
                 w.qf[ks] = row_frag<DMA>(Q, ks * 16 + 8 * half, live ? a.d : 0);
-            settle(w.qf);
-            const bool idle = !__any(live);               // a wave without rows only loads
             // steps whose keys every row of the tile sees
             const int all = min(seq.hi(a, k.first), seq.lk);
             const int nb = min(k.steps, max(0, all - k.beg) / KEYS);
             const int na = min(nb, max(0, seq.lo(a, k.last) - k.beg + KEYS - 1) / KEYS);
-            const uint16_t *const K = K0 + hk * a.kc.sh, *const V = V0 + hk * a.vc.sh;
+            const uint16_t *const K = static_cast<const uint16_t *>(a.kc.p) + hk * a.kc.sh;
+            const uint16_t *const V = static_cast<const uint16_t *>(a.vc.p) + hk * a.vc.sh;
 
             // as many steps at a time as their pages' numbers have room
             const int some = max(1, (int)min((int64_t)(PAGES_AT_ONCE - 2) * a.at.page / KEYS, (int64_t)1 << 24));
@@ -289,6 +308,7 @@ void paged_attn_kernel(PagedLaunch f) {
                     }
                     numbers[x] = e;
                 }
+                if (sa == s0) settle(w.qf);
                 if (lane == 0) missing[wave] = 0;
                 if (__any(bad) && lane == 0) missing[wave] = 1;
                 wait_vm<0>();        // stores of an earlier item too: the loads below are counted
@@ -302,37 +322,44 @@ void paged_attn_kernel(PagedLaunch f) {
                 w.rd = reader;
                 w.stage = 0;
 
-                // Loads of the step that is x-th in the walk: on DMA, the page of each load's rows
-                // is read from LDS one step ahead.
+                // Loads of the step that is x-th in the walk. On DMA, the page of each load's rows is
+                // read from LDS a step ahead, and a load's descriptor is made where it is issued,
+                // beside a product: all of a step's at once after the barrier they were waited for.
                 auto key0 = [&](int x) { return k_beg + walk.step(x) * KEYS; };
-                int32_t next[NV];
-                i32x4 to_k[NV], to_v[NV];
-                int skip[NV];                // rows of a load in front of what is seen
+                int32_t next[NV];            // page of load j's rows, and their place on it
+                int slot[NV], rows_left[NV], skip = 0;
                 uint32_t to = 0;
                 typename Tile::Regs rk, rv;
                 auto look = [&](int x) __attribute__((always_inline)) {
+                    const int key = key0(x) + wave * Tile::RPS;
+                    skip = k.lo - key;
 #pragma unroll
                     for (int j = 0; j < NV; ++j) {
-                        const int p = f.page(key0(x) + (j * NW + wave) * Tile::RPS) - page0;
-                        next[j] = numbers[min(max(p, 0), PAGES_AT_ONCE - 1)];
+                        const int at = key + j * (NW * Tile::RPS), p = f.page(at);
+                        next[j] = numbers[min(p - page0, PAGES_AT_ONCE - 1)];
+                        slot[j] = at - p * a.at.page;
+                        rows_left[j] = x < n ? k.end - at : 0;
+                    }
+                };
+                auto part = [&](int q) __attribute__((always_inline)) {
+                    if constexpr (DMA) {
+                        const int j = q < NV ? q : q - NV;
+                        const CoreView &c = q < NV ? a.kc : a.vc;
+                        const int e = uniform(next[j]), ld2 = (int)c.ld * 2;
+                        // strides are 16-byte units below 2^32, rows of a page span less than 2^31 bytes
+                        const uint64_t at = (uint64_t)(uint32_t)e * (uint32_t)(c.sb >> 3) << 4;
+                        i32x4 r = make_rsrc(reinterpret_cast<const char *>(q < NV ? K : V) + at +
+                                            (uint32_t)(slot[j] * ld2));
+                        r[2] = uniform(e < 0 ? 0 : min(Tile::RPS, max(0, rows_left[j])) * ld2);
+                        const int out = row_of < skip - j * (NW * Tile::RPS) ? OOB : 0;
+                        dma16_at(r, to + (j * NW + wave) * Tile::SEG + (q < NV ? 0 : Tile::BYTES),
+                                 (q < NV ? place_k : place_v) | out);
                     }
                 };
                 auto fetch = [&](int x, int stage) __attribute__((always_inline)) {
                     if constexpr (DMA) {
-#pragma unroll
-                        for (int j = 0; j < NV; ++j) {
-                            const int key = key0(x) + (j * NW + wave) * Tile::RPS;
-                            const int p = __builtin_amdgcn_readfirstlane(next[j]);
-                            const int at = key - f.page(key) * a.at.page;
-                            const int m = x < n && p >= 0 ? min(Tile::RPS, max(0, k.end - key)) : 0;
-                            to_k[j] = make_rsrc(K + p * a.kc.sb + at * a.kc.ld);
-                            to_v[j] = make_rsrc(V + p * a.vc.sb + at * a.vc.ld);
-                            to_k[j][2] = __builtin_amdgcn_readfirstlane(m * (int)a.kc.ld * 2);
-                            to_v[j][2] = __builtin_amdgcn_readfirstlane(m * (int)a.vc.ld * 2);
-                            skip[j] = k.lo - key;
-                        }
+                        look(x);
                         to = lds0 + stage * S::STAGE;
-                        look(x + 1);
                     } else {
                         auto load = [&](typename Tile::Regs &v, const uint16_t *base, const CoreView &c) {
 #pragma unroll
@@ -349,15 +376,6 @@ void paged_attn_kernel(PagedLaunch f) {
                         };
                         load(rk, K, a.kc);
                         load(rv, V, a.vc);
-                    }
-                };
-                auto part = [&](int q) __attribute__((always_inline)) {
-                    if constexpr (DMA) {
-                        const int j = q < NV ? q : q - NV;
-                        const uint32_t lds = to + (j * NW + wave) * Tile::SEG;
-                        const int out = row_of < skip[j] ? OOB : 0;
-                        if (q < NV) dma16_at(to_k[j], lds, place_k | out);
-                        else dma16_at(to_v[j], lds + Tile::BYTES, place_v | out);
                     }
                 };
                 auto arrive = [&](int stage) {
@@ -380,15 +398,16 @@ void paged_attn_kernel(PagedLaunch f) {
                     }
                 };
                 if constexpr (DMA) {
-                    look(0);
-#pragma unroll
-                    for (int x = 0; x < NS - 1; ++x) {
+#pragma unroll 1
+                    for (int x = 0; x < NS - 1; ++x) {       // (short code: it is run cold)
                         fetch(x, x);
 #pragma unroll
                         for (int p = 0; p < S::LOADS; ++p) part(p);
                     }
-                    fetch(n, NS - 1);        // nothing, for the parts before the first advance
-                    look(NS - 1);
+                    // nothing, for the parts before the first advance
+#pragma unroll
+                    for (int j = 0; j < NV; ++j) rows_left[j] = 0;
+                    to = lds0 + (NS - 1) * S::STAGE;
                     wait_vm<(NS - 2) * S::LOADS>();
                 } else {
                     fetch(0, 0);
@@ -411,24 +430,17 @@ void paged_attn_kernel(PagedLaunch f) {
                         mine(x), mine(x + 1), x + 1 < n, seen,
                         [&]() __attribute__((always_inline)) { advance(x); }, part);
                 };
-                if (idle) {
-                    for (int x = 0; x < n; ++x) {
-                        advance(x);
-#pragma unroll
-                        for (int p = 0; p < S::LOADS; ++p) part(p);
-                        w.stage = after();
-                    }
-                } else {
-                    w.begin(mine(0), seen);
-                    int x = 0;
-                    for (; x < min(n, walk.masked()); ++x) take(x, std::true_type{});
-                    for (; x < n; ++x) take(x, std::false_type{});
-                }
+                w.begin(mine(0), seen);
+                int x = 0;
+                for (; x < min(n, walk.masked()); ++x) take(x, std::true_type{});
+                for (; x < n; ++x) take(x, std::false_type{});
                 wait_vm<0>();      // no load is on its way to LDS any more
                 __syncthreads();
                 sa = sb;
             }
 
+            const PagedLaunch &f = again();
+            const PagedArgs &a = f.a;
             const float mul = w.join_groups(reinterpret_cast<float *>(smem + S::PUT) + lane, wave, wr);
             const float m = w.m, l = w.l;
             // a row that sees no key: O = 0, lse = -infinity
@@ -473,7 +485,7 @@ void paged_attn_kernel(PagedLaunch f) {
 // (x, y) takes row block y of the item that workgroup x + 1 continues. A row's LANES threads own 4
 // columns each, SHARES threads a column's parts in turn.
 template <int LANES, int SHARES>
-__global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f, int rows_of_tile) {
+__global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f) {
     constexpr int AT_ONCE = 256 / (LANES * SHARES);
     __shared__ float room[256][6];
     const PagedArgs &a = f.a;
@@ -482,12 +494,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f, int rows
     if (cut.last < 0) return;
     const int tid = threadIdx.x, lane = tid % LANES, share = tid / LANES % SHARES;
     const int in = blockIdx.y * AT_ONCE + tid / (LANES * SHARES);
-    const Seq seq(a, cut.seq);
-    const int row = cut.tile * rows_of_tile + in, col = lane * 4;
-    const bool valid = in < f.slot_rows && row < seq.rows && col < a.d;
+    const int row = cut.row + in, col = lane * 4;
+    const bool valid = in < f.slot_rows && row < cut.rows && col < a.d;
     const int64_t d4 = (a.d + 3) & ~3;
     const float c = a.scale * LOG2E;
-    const int n = cut.last - w + 2;
+    const int n = min(cut.last, f.groups - 1) - w + 2;
     float top = -INFINITY, sum = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (valid)
@@ -544,11 +555,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f, int rows
     const bool some = sum != 0.f;
     const float inv = some ? 1.f / sum : 0.f;
     const int i = f.group(row);
-    const int64_t head = (int64_t)cut.head * a.group + (row - i * a.group), at = seq.at.first + i;
-    store4(a.o.p, seq.at.batch * a.o.sb + head * a.o.sh + at * a.o.ld, col, a.d, a.o_f32, f.vec,
+    const int64_t head = (int64_t)cut.head * a.group + (row - i * a.group), at = cut.first + i;
+    store4(a.o.p, cut.batch * a.o.sb + head * a.o.sh + at * a.o.ld, col, a.d, a.o_f32, f.vec,
            [&](int e) { return v[e] * inv; });
     if (a.lse.p && col == 0)
-        static_cast<float *>(a.lse.p)[seq.at.batch * a.lse.sb + head * a.lse.sh + at * a.lse.ld] =
+        static_cast<float *>(a.lse.p)[cut.batch * a.lse.sb + head * a.lse.sh + at * a.lse.ld] =
             some ? __builtin_fmaf(top, a.scale, __builtin_amdgcn_logf(sum) * LN2) : -INFINITY;
 }
 
@@ -570,13 +581,18 @@ hipError_t launch(const sbpk::PagedLaunch &f, bool dma, hipStream_t s) {
     return launch_kernel(sbpk::paged_attn_kernel<DP, KG, KT, NW, WPS, false>, name, grid, block, s, f);
 }
 
-// The kernel's forms: rows of a tile, keys of a step, workgroups of a unit, us of a step.
+// The kernel's forms: rows of a tile, keys of a step, workgroups of a unit, us of a step, an item's
+// fixed part in steps. The second gives up speed a row for smaller tiles: a chunk of 2048 of 16
+// heads over 4, 32768 keys, takes 588 and 790 us at 128 columns, 504 and 708 at 64; one token of 32
+// sequences of 64 heads over 8, 4096 x 128, 165 and 117.
 struct Form {
-    int rows, keys, per_cu;
+    int rows, per_cu;
     double step;
+    int fixed;
 };
-constexpr Form FORMS[2][3] = {{{128, 64, 2, 0.9}, {64, 64, 2, 0.55}, {32, 128, 1, 0.6}},
-                              {{256, 64, 1, 1.4}, {128, 64, 1, 1.0}, {64, 64, 1, 0.75}}};
+constexpr int KEYS = 64;
+constexpr Form FORMS[2][2] = {{{128, 2, 2.03, 5}, {64, 2, 1.43, 6}},
+                              {{256, 1, 2.33, 5}, {128, 1, 1.59, 6}}};
 
 }  // namespace
 
@@ -593,37 +609,45 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     const int64_t rows = (int64_t)a.at.rows * a.group;
     int form = 0;
     double best = 1e300;
-    for (int k = 0; k < 3; ++k) {
+    for (int k = 0; k < 2; ++k) {
         const Form &m = FORMS[wide][k];
         const double tiles = a.at.row_q ? (double)(rows / m.rows) + a.at.seqs
                                         : (double)((rows + m.rows - 1) / m.rows) * a.at.seqs;
-        const double t = tiles * m.step / (m.keys * m.per_cu);
+        const double t = tiles * m.step / m.per_cu;
         if (t < best) best = t, form = k;
     }
     const Form &m = FORMS[wide][form];
     f.slot_rows = (int32_t)std::min<int64_t>(m.rows, rows);
     const int64_t most = (int64_t)device_cus() * m.per_cu;
-    const int64_t each = 4 + 2 * sbpk::slot_floats(f.slot_rows, a.d);
+    const int64_t each = sbpk::CUT_FLOATS + 2 * sbpk::slot_floats(f.slot_rows, a.d);
     // with a workspace for half of the workgroups items may be cut
     const int64_t room = (int64_t)(a.ws_floats / (size_t)each);
     f.split = room >= most / 2;
     f.groups = (int32_t)(f.split ? std::min(room, most) : most);
-    // rows of one load lie on one page
+    f.by_groups = sbpk::Div(f.groups);
+    // units of all items, at most: below 2^31
+    const double most_tiles = a.at.row_q ? (double)(rows / m.rows) + a.at.seqs
+                                         : (double)((rows + m.rows - 1) / m.rows) * a.at.seqs;
+    const double steps = (double)a.at.width * a.at.page / KEYS + 2;
+    f.fixed = m.fixed;
+    f.scale = 0;
+    while (most_tiles * a.kv_heads * (steps / (double)(1 << f.scale) + 1 + f.fixed) > 1e9) ++f.scale;
+    // rows of one load lie on one page, whose offsets fit the loads' arithmetic
     const int per_load = wide ? 4 : 8;
-    const bool dma = a.aligned && a.at.page % per_load == 0;
+    const bool dma = a.aligned && a.at.page % per_load == 0 &&
+                     std::max(a.kc.sb, a.vc.sb) < int64_t(1) << 35 &&
+                     (double)a.at.page * std::max(a.kc.ld, a.vc.ld) < 1073741824.0;
     hipError_t e;
     if (form == 0)
         e = wide ? launch<128, 1, 64, 8, 2>(f, dma, s) : launch<64, 1, 64, 4, 2>(f, dma, s);
-    else if (form == 1)
-        e = wide ? launch<128, 2, 32, 8, 2>(f, dma, s) : launch<64, 2, 32, 4, 2>(f, dma, s);
     else
-        e = wide ? launch<128, 2, 32, 4, 1>(f, dma, s) : launch<64, 4, 32, 4, 1>(f, dma, s);
+        e = wide ? launch<128, 2, 32, 8, 2>(f, dma, s) : launch<64, 2, 32, 4, 2>(f, dma, s);
     if (e != hipSuccess || !f.split || f.groups < 2) return e;
     auto join = [&](auto kernel, int at_once) {
         const dim3 grid((unsigned)(f.groups - 1), (unsigned)((f.slot_rows + at_once - 1) / at_once));
-        return launch_kernel(kernel, "paged_join_kernel", grid, dim3(256), s, f, m.rows);
+        return launch_kernel(kernel, "paged_join_kernel", grid, dim3(256), s, f);
     };
-    if (form == 2)    // few rows, perhaps of many parts
+    if (f.slot_rows <= 32)    // perhaps of many parts
         return wide ? join(sbpk::paged_join_kernel<32, 4>, 2) : join(sbpk::paged_join_kernel<16, 4>, 4);
     return wide ? join(sbpk::paged_join_kernel<32, 1>, 8) : join(sbpk::paged_join_kernel<16, 1>, 16);
 }

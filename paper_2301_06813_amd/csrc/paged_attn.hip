@@ -66,9 +66,6 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 
 // The workspace: cuts, statistics (a row's maximum and sum), partial outputs.
 typedef float f32x2 __attribute__((ext_vector_type(2)));
-__host__ __device__ inline int64_t slot_floats(int64_t rows, int d) {
-    return rows * (2 + ((d + 3) & ~3));
-}
 __device__ __forceinline__ Cut *cuts_of(const PagedLaunch &f) { return reinterpret_cast<Cut *>(f.a.ws); }
 __device__ __forceinline__ f32x2 *stats_of(const PagedLaunch &f) {
     return reinterpret_cast<f32x2 *>(f.a.ws + CUT_FLOATS * (int64_t)f.groups);
@@ -143,6 +140,13 @@ __device__ __forceinline__ int upto_lane(int x) {
     return x;
 }
 
+// Where a partial output of one wave group lies in its slot: the registers' order, quads of columns
+// 8 t + 4 (lane / 32) .. + 3 of row 32 wr + lane % 32 side by side for a wave's lanes.
+template <int DP>
+__device__ __forceinline__ int part_place(int wr, int t, int lane) {
+    return ((wr * (DP / 8) + t) * 64 + lane) * 4;
+}
+
 // The kernel's arguments, to be read again: what the compiler reads before a loop of items it keeps
 // through all of them, spilled from scalar to vector registers.
 __device__ __forceinline__ const PagedLaunch &again() {
@@ -169,6 +173,10 @@ void paged_attn_kernel(PagedLaunch f0) {
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int kg = wave % KG, wr = wave / KG;
     const int64_t d4 = (a.d + 3) & ~3;
+    // the arguments' lines, read at once: each first read of one is a trip to memory
+    asm volatile("" ::"s"(a.at.table), "s"(a.at.len_k), "s"(a.at.rows), "s"(a.q.sh), "s"(a.kc.p),
+                 "s"(a.vc.p), "s"(a.o.p), "s"(a.lse.p), "s"(a.kv_heads), "s"(a.d), "s"(a.ws),
+                 "s"(f.slot_rows), "s"(f.fixed), "s"(f.by_groups.m));
     const int wg = remap_xcd(blockIdx.x, f.groups);    // neighbours on the line share an L2
 
     // This workgroup's part of the line: `left` units from unit u of tile `tile` of head hk of
@@ -178,7 +186,12 @@ void paged_attn_kernel(PagedLaunch f0) {
     Line line{0, 0.f};
     Seq seq(a, SeqRows{0, 0, 0, 0});
     {
+        constexpr int FEW = 2;
         SeqRows r{0, 0, 0, 0};
+        auto one_of = [&](const SeqRows &r, int base, int l) {    // lane l's sequence
+            return Seq(a, SeqRows{a.at.row_q ? 0 : base + l, __builtin_amdgcn_readlane(r.first, l),
+                                  __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)});
+        };
         int one, upto, sum, at = 0;      // units of a head of the lane's sequence; sums
         // 64 sequences at a time: first all, for the total; then, where the line changes to parts,
         // the (64 at most) again; else on until the share's begin. (One loop, so that its code,
@@ -190,7 +203,17 @@ void paged_attn_kernel(PagedLaunch f0) {
             if (b + lane < a.at.seqs) {
                 r = rows_of(a.at, b + lane);
                 const Seq s(a, r);
-                for (; tiles * ROWS < s.rows; ++tiles) one += Keys(f, s, tiles).cost(f, line);
+                tiles = (s.rows + ROWS - 1) / ROWS;
+                for (int t = 0; t < min(tiles, FEW); ++t) one += Keys(f, s, t).cost(f, line);
+            }
+            // the further tiles of longer ones: the wave, one sequence after the other
+            for (uint64_t more = __ballot(tiles > FEW); more; more &= more - 1) {
+                const int l = __builtin_ctzll(more);
+                const Seq s = one_of(r, b, l);
+                int c = 0;
+                for (int t = FEW + lane; t * ROWS < s.rows; t += 64) c += Keys(f, s, t).cost(f, line);
+                c = __builtin_amdgcn_readlane(upto_lane(c), 63);
+                if (lane == l) one += c;
             }
             upto = upto_lane(one * a.kv_heads);
             sum = __builtin_amdgcn_readlane(upto, 63);
@@ -231,39 +254,52 @@ void paged_attn_kernel(PagedLaunch f0) {
         const uint64_t here = __ballot(in >= 0 && in < one * a.kv_heads);
         if (!here) return;     // (lengths that changed under way)
         const int l = __builtin_ctzll(here);
+        seq = one_of(r, b, l);
         b += l;
         one = __builtin_amdgcn_readlane(one, l);
         u = __builtin_amdgcn_readlane(in, l);
         hk = (int)((uint32_t)u / (uint32_t)one);
         u -= hk * one;
-        seq = Seq(a, SeqRows{a.at.row_q ? 0 : b, __builtin_amdgcn_readlane(r.first, l),
-                             __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)});
-    }
-    for (int c; u >= (c = Keys(f, seq, tile).cost(f, line)); ++tile) u -= c;
-    if (f.split) {
-        const Keys k(f, seq, tile);
-        Cut cut{-1, hk, tile * ROWS, seq.at.batch, seq.at.first, seq.rows, {0, 0}};
-        const int at = k.cut(f, line, u);
-        if (at > 0 && at < k.length() && k.cut(f, line, u - line.share) == 0) {
-            // the workgroup of the item's last unit, unless its share's begin is moved to the end
-            int w = (int)((uint32_t)(k.cost(f, line) - u - 1) / (uint32_t)line.share);
-            if (w > 0 && k.cut(f, line, u + w * line.share) == k.length()) --w;
-            cut.last = wg + w;
+        // the tile, among 64 at a time
+        while (seq.rows > ROWS) {
+            const int t = tile + lane;
+            const int c = t * ROWS < seq.rows ? Keys(f, seq, t).cost(f, line) : 0, up = upto_lane(c);
+            const uint64_t in_tile = __ballot(u < up);
+            if (in_tile) {
+                const int l = __builtin_ctzll(in_tile);
+                u -= __builtin_amdgcn_readlane(up - c, l);
+                tile += l;
+                break;
+            }
+            u -= __builtin_amdgcn_readlane(up, 63);
+            if ((tile += 64) * ROWS >= seq.rows) return;      // (as above)
         }
-        if (tid == 0) cuts_of(f)[wg] = cut;
     }
-
     // a lane's place in a load's rows (DMA)
     const int row_of = lane / Tile::CPR, chunk = (lane % Tile::CPR) ^ Tile::swz(row_of);
     const int place_k = chunk * 8 < a.d ? (row_of * (int)a.kc.ld + chunk * 8) * 2 : OOB;
     const int place_v = chunk * 8 < a.d ? (row_of * (int)a.vc.ld + chunk * 8) * 2 : OOB;
 
-    while (left > 0) {
+    for (bool noted = !f.split; left > 0;) {
         const PagedLaunch &f = again();
         const PagedArgs &a = f.a;
         const Keys k(f, seq, tile);
         const int until = min(k.cost(f, line), u + left);
         const int s0 = k.cut(f, line, u), s1 = k.cut(f, line, until);
+        // The share's begin, for the join: noted while the first loads are on their way (and stored
+        // before those to LDS, which are counted).
+        auto note = [&]() {
+            noted = true;
+            if (tid) return;
+            Cut cut{-1, hk, tile * ROWS, seq.at.batch, seq.at.first, seq.rows, {0, 0}};
+            if (s0 > 0 && s0 < k.length() && k.cut(f, line, u - line.share) == 0) {
+                // the workgroup of the item's last unit, unless its share's begin is moved to the end
+                int w = (int)((uint32_t)(k.cost(f, line) - u - 1) / (uint32_t)line.share);
+                if (w > 0 && k.cut(f, line, u + w * line.share) == k.length()) --w;
+                cut.last = wg + w;
+            }
+            cuts_of(f)[wg] = cut;
+        };
         if (s0 < s1) {
             const bool whole = s0 == 0 && s1 == k.length();
             const int end1 = min(s1, k.steps);
@@ -297,14 +333,16 @@ void paged_attn_kernel(PagedLaunch f0) {
                 const int page0 = f.page(k_beg);
                 const int count = f.page(min(k_beg + n * KEYS, k.end) - 1) - page0 + 1;
                 bool bad = false;
-                for (int x = tid; x < count; x += 64 * NW) {
-                    int e = -1;
-                    if ((page0 + x + 1) * a.at.page > k.lo) {
-                        e = a.at.table[b * a.at.table_ld + page0 + x];
-                        if (e < 0 || e >= a.at.pages) {
-                            e = -1;
-                            bad = true;
-                        }
+                auto number = [&](int x) {       // of the x-th page; pages before the first row seen aside
+                    const bool in = x < count && (page0 + x + 1) * a.at.page > k.lo;
+                    return in ? a.at.table[b * a.at.table_ld + page0 + x] : 0;
+                };
+                int e = number(tid);
+                if (!noted) note();
+                for (int x = tid; x < count; x += 64 * NW, e = number(x)) {
+                    if (e < 0 || e >= a.at.pages) {
+                        e = -1;
+                        bad = true;
                     }
                     numbers[x] = e;
                 }
@@ -445,26 +483,47 @@ void paged_attn_kernel(PagedLaunch f0) {
             const float m = w.m, l = w.l;
             // a row that sees no key: O = 0, lse = -infinity
             const bool some_key = live && l != 0.f;
-            const int64_t slot = (2 * (int64_t)wg + (s0 > 0 ? 0 : 1)) * f.slot_rows + (row - row0);
-            const RowsOut out{whole ? a.o.p : parts_of(f), whole ? a.d : (int)d4, !whole || a.o_f32,
-                              false, !whole || f.vec};
-            const int64_t off = !valid ? -1
-                                : whole ? seq.at.batch * a.o.sb + head * a.o.sh + at_row * a.o.ld
-                                        : slot * d4;
-            float *const put = reinterpret_cast<float *>(smem);
-            stage_rows<DP>(put + wave * PUT_FLOATS<DP>, w.o, some_key ? mul / l : 0.f, lane);
-            if (valid && half == 0 && kg == 0) {
-                if (!whole)
-                    stats_of(f)[slot] = some_key ? f32x2{m, l} : f32x2{-INFINITY, 0.f};
-                else if (a.lse.p)
-                    static_cast<float *>(a.lse.p)[seq.at.batch * a.lse.sb + head * a.lse.sh +
-                                                  at_row * a.lse.ld] =
-                        some_key ? __builtin_fmaf(m, a.scale, __builtin_amdgcn_logf(l) * LN2) : -INFINITY;
+            const int64_t slot = (2 * (int64_t)wg + (s0 > 0 ? 0 : 1)) * f.slot_rows;
+            if (KG == 1 && !whole) {
+                // as the registers hold it: 16 bytes a lane, 1 KB a store
+                if (wr * 32 < f.slot_rows) {
+                    const float by = some_key ? 1.f / l : 0.f;
+                    float *const at = parts_of(f) + slot * DP + part_place<DP>(wr, 0, lane);
+#pragma unroll
+                    for (int t = 0; t < DP / 8; ++t) {
+                        f32x4 v;
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            v[e] = by != 0.f ? w.o[t / 4][t % 4 * 4 + e] * by : 0.f;
+                        if (8 * t + 4 * half < a.d) *reinterpret_cast<f32x4 *>(at + t * 256) = v;
+                    }
+                    if (half == 0)
+                        stats_of(f)[slot + wr * 32 + lane] = some_key ? f32x2{m, l}
+                                                                      : f32x2{-INFINITY, 0.f};
+                }
+            } else {
+                const RowsOut out{whole ? a.o.p : parts_of(f), whole ? a.d : (int)d4,
+                                  !whole || a.o_f32, false, !whole || f.vec};
+                const int64_t off = !valid ? -1
+                                    : whole ? seq.at.batch * a.o.sb + head * a.o.sh + at_row * a.o.ld
+                                            : (slot + row - row0) * d4;
+                float *const put = reinterpret_cast<float *>(smem);
+                stage_rows<DP>(put + wave * PUT_FLOATS<DP>, w.o, some_key ? mul / l : 0.f, lane);
+                if (valid && half == 0 && kg == 0) {
+                    if (!whole)
+                        stats_of(f)[slot + row - row0] = some_key ? f32x2{m, l} : f32x2{-INFINITY, 0.f};
+                    else if (a.lse.p)
+                        static_cast<float *>(a.lse.p)[seq.at.batch * a.lse.sb + head * a.lse.sh +
+                                                      at_row * a.lse.ld] =
+                            some_key ? __builtin_fmaf(m, a.scale, __builtin_amdgcn_logf(l) * LN2)
+                                     : -INFINITY;
+                }
+                __syncthreads();
+                store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
+                __syncthreads();       // before the next item's loads
             }
-            __syncthreads();
-            store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
-            __syncthreads();       // before the next item's loads
         }
+        if (!noted) note();
         left -= until - u;
         u = 0;
         if (left <= 0) break;
@@ -482,19 +541,29 @@ void paged_attn_kernel(PagedLaunch f0) {
 }
 
 // Joins the parts of the items that were cut, in their order: weights l_s 2^((m_s - m) c). Workgroup
-// (x, y) takes row block y of the item that workgroup x + 1 continues. A row's LANES threads own 4
+// (x, y) takes a piece of the item that workgroup x + 1 continues. DP > 0: the parts lie in the
+// registers' order, a wave takes the quads t of 32 rows; else in rows, a row's LANES threads own 4
 // columns each, SHARES threads a column's parts in turn.
-template <int LANES, int SHARES>
+template <int DP, int LANES, int SHARES>
 __global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f) {
-    constexpr int AT_ONCE = 256 / (LANES * SHARES);
-    __shared__ float room[256][6];
+    __shared__ float room[SHARES > 1 ? 256 : 1][6];
     const PagedArgs &a = f.a;
     const int w = blockIdx.x + 1;
     const Cut cut = cuts_of(f)[w];
     if (cut.last < 0) return;
-    const int tid = threadIdx.x, lane = tid % LANES, share = tid / LANES % SHARES;
-    const int in = blockIdx.y * AT_ONCE + tid / (LANES * SHARES);
-    const int row = cut.row + in, col = lane * 4;
+    const int tid = threadIdx.x;
+    int in, col, place = 0, share = 0;
+    if constexpr (DP > 0) {
+        const int unit = blockIdx.y * 4 + (tid >> 6), wr = unit / (DP / 8), t = unit % (DP / 8);
+        in = wr * 32 + (tid & 31);
+        col = 8 * t + (tid >> 5 & 1) * 4;
+        place = part_place<DP>(wr, t, tid & 63);
+    } else {
+        in = blockIdx.y * (256 / (LANES * SHARES)) + tid / (LANES * SHARES);
+        col = tid % LANES * 4;
+        share = tid / LANES % SHARES;
+    }
+    const int row = cut.row + in;
     const bool valid = in < f.slot_rows && row < cut.rows && col < a.d;
     const int64_t d4 = (a.d + 3) & ~3;
     const float c = a.scale * LOG2E;
@@ -508,10 +577,11 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int k = s + j * SHARES;
-                const int64_t slot = (2 * (int64_t)(w - 1 + k) + (k ? 0 : 1)) * f.slot_rows + in;
-                z[j] = k < n ? stats_of(f)[slot] : f32x2{-INFINITY, 0.f};
-                x[j] = k < n ? *reinterpret_cast<const f32x4 *>(parts_of(f) + slot * d4 + col)
-                             : f32x4{0.f, 0.f, 0.f, 0.f};
+                const int64_t slot = (2 * (int64_t)(w - 1 + k) + (k ? 0 : 1)) * f.slot_rows;
+                const float *const part = parts_of(f) + (DP > 0 ? slot * DP + place
+                                                                : (slot + in) * d4 + col);
+                z[j] = k < n ? stats_of(f)[slot + in] : f32x2{-INFINITY, 0.f};
+                x[j] = k < n ? *reinterpret_cast<const f32x4 *>(part) : f32x4{0.f, 0.f, 0.f, 0.f};
             }
             float high = top;
 #pragma unroll
@@ -617,9 +687,12 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
         if (t < best) best = t, form = k;
     }
     const Form &m = FORMS[wide][form];
-    f.slot_rows = (int32_t)std::min<int64_t>(m.rows, rows);
+    // a slot holds the rows that a tile can have: whole waves' in the first form, whose partial
+    // outputs lie as the registers hold them
+    const int padded = wide ? 128 : 64;
+    f.slot_rows = (int32_t)std::min<int64_t>(m.rows, form == 0 ? (rows + 31) / 32 * 32 : rows);
     const int64_t most = (int64_t)device_cus() * m.per_cu;
-    const int64_t each = sbpk::CUT_FLOATS + 2 * sbpk::slot_floats(f.slot_rows, a.d);
+    const int64_t each = sbpk::CUT_FLOATS + 2 * (int64_t)f.slot_rows * (2 + (form == 0 ? padded : (a.d + 3) & ~3));
     // with a workspace for half of the workgroups items may be cut
     const int64_t room = (int64_t)(a.ws_floats / (size_t)each);
     f.split = room >= most / 2;
@@ -643,13 +716,21 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     else
         e = wide ? launch<128, 2, 32, 8, 2>(f, dma, s) : launch<64, 2, 32, 4, 2>(f, dma, s);
     if (e != hipSuccess || !f.split || f.groups < 2) return e;
-    auto join = [&](auto kernel, int at_once) {
-        const dim3 grid((unsigned)(f.groups - 1), (unsigned)((f.slot_rows + at_once - 1) / at_once));
-        return launch_kernel(kernel, "paged_join_kernel", grid, dim3(256), s, f);
+    auto join = [&](auto kernel, int pieces) {
+        return launch_kernel(kernel, "paged_join_kernel", dim3((unsigned)(f.groups - 1), (unsigned)pieces),
+                             dim3(256), s, f);
     };
+    if (form == 0) {    // 4 quads of 32 rows a workgroup
+        const int pieces = f.slot_rows / 32 * padded / 32;
+        return wide ? join(sbpk::paged_join_kernel<128, 1, 1>, pieces)
+                    : join(sbpk::paged_join_kernel<64, 1, 1>, pieces);
+    }
+    auto rows_of = [&](int at_once) { return (f.slot_rows + at_once - 1) / at_once; };
     if (f.slot_rows <= 32)    // perhaps of many parts
-        return wide ? join(sbpk::paged_join_kernel<32, 4>, 2) : join(sbpk::paged_join_kernel<16, 4>, 4);
-    return wide ? join(sbpk::paged_join_kernel<32, 1>, 8) : join(sbpk::paged_join_kernel<16, 1>, 16);
+        return wide ? join(sbpk::paged_join_kernel<0, 32, 4>, rows_of(2))
+                    : join(sbpk::paged_join_kernel<0, 16, 4>, rows_of(4));
+    return wide ? join(sbpk::paged_join_kernel<0, 32, 1>, rows_of(8))
+                : join(sbpk::paged_join_kernel<0, 16, 1>, rows_of(16));
 }
 
 }  // namespace sbpi

@@ -95,7 +95,7 @@ def _turn(call, rope, Q, K, p, r, pos, out, out_dtype, scope, stream):
         else:
             ko = sbp.sbp_view4_t(at + hq * D * t.element_size(), B, hk, S, D, sb, D, ld, dt,
                                  sbp.SBP_LOCAL)
-            out = t[:, :hq], t[:, hq:]
+            out = t.split_with_sizes((hq, hk), 1)
     else:
         qo, ko = (None if t is None else sbp.view4(t, sbp.SBP_LOCAL) for t in out)
     call(q, k, rope.view, places(pos, B, S), qo, ko, p, r, None)

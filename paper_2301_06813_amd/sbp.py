@@ -366,6 +366,14 @@ def current_stream():
     return s
 
 
+def current_device() -> int:
+    """Torch's current device (asked for directly as in current_stream, once that was called)."""
+    if _raw_stream:
+        return _raw_stream[1]()
+    import torch
+    return torch.cuda.current_device()
+
+
 def _forget_stream():
     global _raw_stream
     _raw_stream = None
@@ -390,7 +398,7 @@ def workspace(t) -> sbp_workspace_t:
 
 def _kept_workspace(stream):
     import torch
-    device = _raw_stream[1]() if _raw_stream else torch.cuda.current_device()
+    device = current_device()
     key = (device, int(stream or 0), threading.get_ident())
     kept = _default_ws.get(key)
     if kept is None:
@@ -688,23 +696,19 @@ def sbp_rope_turns(dim: int, base: float = 10000.0, scaling: int = SBP_ROPE_PLAI
     return list(turns)
 
 
-def _ref(x):
-    return None if x is None else ctypes.byref(x)
-
-
 def sbp_rope_fwd(Q, K, rope: sbp_rope_t, at, Qo, Ko, p: int, r: int, stream=None):
     """Qo and Ko: Q and K (or None) rotated by the positions of their rows (at: an
     sbp_places_t, or None)."""
-    rc = (_lib or lib()).sbp_rope_fwd(_ref(Q), _ref(K), _ref(rope), _ref(at), _ref(Qo), _ref(Ko), p,
-                                      r, _stream(stream))
+    rc = (_lib or lib()).sbp_rope_fwd(Q, K, rope, at, Qo, Ko, p, r,
+                                      current_stream() if stream is None else stream)
     if rc:
         _check(rc)
 
 
 def sbp_rope_bwd(dQo, dKo, rope: sbp_rope_t, at, dQ, dK, p: int, r: int, stream=None):
     """dQ and dK from the gradients of sbp_rope_fwd's outputs."""
-    rc = (_lib or lib()).sbp_rope_bwd(_ref(dQo), _ref(dKo), _ref(rope), _ref(at), _ref(dQ),
-                                      _ref(dK), p, r, _stream(stream))
+    rc = (_lib or lib()).sbp_rope_bwd(dQo, dKo, rope, at, dQ, dK, p, r,
+                                      current_stream() if stream is None else stream)
     if rc:
         _check(rc)
 
@@ -712,8 +716,8 @@ def sbp_rope_bwd(dQo, dKo, rope: sbp_rope_t, at, dQ, dK, p: int, r: int, stream=
 # ------------------------------------------------------------ paged cache
 def sbp_paged_append(K, V, pages: sbp_pages_t, rope, Kc, Vc, Q, Qo, p: int, r: int, stream=None):
     """New tokens' K and V into the cache Kc, Vc; K and Q (into Qo) rotated with a rope."""
-    rc = (_lib or lib()).sbp_paged_append(_ref(K), _ref(V), _ref(pages), _ref(rope), _ref(Kc),
-                                          _ref(Vc), _ref(Q), _ref(Qo), p, r, _stream(stream))
+    rc = (_lib or lib()).sbp_paged_append(K, V, pages, rope, Kc, Vc, Q, Qo, p, r,
+                                          current_stream() if stream is None else stream)
     if rc:
         _check(rc)
 
@@ -722,9 +726,8 @@ def sbp_paged_attn(Q, Kc, Vc, pages: sbp_pages_t, scale: float, causal: int, win
                    p: int, r: int, stream=None, ws=None):
     """O and lse (a view, or None) of rank r's heads over the cache."""
     s = current_stream() if stream is None else stream
-    rc = (_lib or lib()).sbp_paged_attn(_ref(Q), _ref(Kc), _ref(Vc), _ref(pages), scale, causal,
-                                        window, _ref(O), _ref(lse), p, r, _ref(_ws(ws, s)),
-                                        ctypes.c_void_p(s))
+    rc = (_lib or lib()).sbp_paged_attn(Q, Kc, Vc, pages, scale, causal, window, O, lse, p, r,
+                                        _ws(ws, s), s)
     if rc:
         _check(rc)
 

@@ -4,6 +4,10 @@ from __future__ import annotations
 
 import torch
 
+from . import sbp
+
+_TENSOR = torch.Tensor
+
 
 def torch_stream(handle: int):
     return torch.cuda.ExternalStream(handle) if handle else torch.cuda.default_stream()
@@ -30,8 +34,8 @@ def on_stream(stream: int, call, *args):
 def same_device(*tensors):
     """The library's calls run on the current device, whose tensors these must be (None and
     workspaces that are no tensors aside)."""
-    device = torch.cuda.current_device()
+    device = sbp.current_device()
     for t in tensors:
-        if t is not None and isinstance(t, torch.Tensor) and t.device.index != device:
+        if t is not None and isinstance(t, _TENSOR) and t.device.index != device:
             raise ValueError("tensors are on %s, the current device is cuda:%d"
                              % (t.device, device))

@@ -586,7 +586,7 @@ typedef struct {
  * (the same address, strides and dtype: in place); else no output may overlap an input or the
  * other output, but for outputs that interleave as those of sbp_attn_core_bwd may.
  * Errors: those of the attention calls; SBP_ERR_SHAPE also for more than 2^29 rows of a
- * sequence, or 2^31 / ((D + 31) / 16) rows over the rank's heads. */
+ * sequence, or 2^31 / ((D + 23) / 8) rows over the rank's heads. */
 int sbp_rope_fwd(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_rope_t *rope,
                  const sbp_places_t *at, sbp_view4_t *Qo, sbp_view4_t *Ko, int32_t p, int32_t r,
                  hipStream_t stream);

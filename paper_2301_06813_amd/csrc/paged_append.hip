@@ -4,7 +4,9 @@
 // A thread owns 16 columns of a new token and takes them in HEADS of the heads of Q, K and V, one
 // after the other (rope.hip): the token's place gives both its row of the cache and its
 // angles. In a packed batch a wave finds its first row's sequence by a search of 64 places at a
-// time. The bound is memory, for few tokens the chain of loads from a row to its page.
+// time. The bound is memory, for few tokens the chain of loads from a row to its page. (7172 new
+// tokens of 64 + 8 + 8 heads of 128: 87 us with one head a thread, 64 with two, 65 with three, 67
+// with four, 72 with eight.)
 #include "attn_core_kernel.h"
 #include "paged_kernel.h"
 #include "profile.h"
@@ -13,6 +15,8 @@
 namespace sbpk {
 
 using sbpi::AppendArgs;
+
+constexpr int R = 8;                 // pairs of a unit
 
 struct AppendLaunch {
     AppendArgs a;
@@ -47,9 +51,9 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendLaunch f) {
     if (!live || new_i < 0 || new_i >= n) return;
     const int64_t t = (int64_t)a.at.len_k[b] - n + new_i;
     const int heads = a.q_heads + 2 * a.kv_heads, step = (int)f.groups.d;
-    const Unit u = unit_of(r, a.d, ui);
+    const Unit u = unit_of<R>(r, a.d, ui);
     // head h of Q's, then K's, then V's
-    Pair<uint16_t> x[HEADS];
+    Pair<uint16_t, R> x[HEADS];
 #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
         const int h = hg + k * step;
@@ -64,7 +68,7 @@ __global__ __launch_bounds__(256) void paged_append_kernel(AppendLaunch f) {
         slot = f.page.rest((int)t, at);
         page = a.at.table[b * a.at.table_ld + at];
     }
-    Angles g;
+    Angles<R> g;
     if (u.turn) g.find(r, ui, t, false);
 #pragma unroll
     for (int k = 0; k < HEADS; ++k) {
@@ -95,16 +99,16 @@ hipError_t launch(const AppendArgs &a, hipStream_t s) {
     sbpk::AppendLaunch f;
     f.a = a;
     const int64_t rows = (int64_t)a.batch * a.at.rows;
-    const int heads = a.q_heads + 2 * a.kv_heads, units = sbpk::units_of(a.rot, a.d);
+    const int heads = a.q_heads + 2 * a.kv_heads, units = sbpk::units_of<sbpk::R>(a.rot, a.d);
     const bool many = rows * heads * units > (int64_t)device_cus() * 2048;
-    const int groups = many ? (heads + 3) / 4 : heads;
+    const int groups = many ? (heads + 1) / 2 : heads;
     f.threads = (int32_t)(rows * groups * units);
     f.units = sbpk::Div(units);
     f.groups = sbpk::Div(groups);
     f.rows = sbpk::Div(a.at.rows);
     f.page = sbpk::Div(a.at.page);
     const dim3 grid((unsigned)((f.threads + 255ll) / 256)), block(256);
-    return many ? launch_kernel(sbpk::paged_append_kernel<TQ, 4>, "paged_append_kernel<4>", grid, block, s, f)
+    return many ? launch_kernel(sbpk::paged_append_kernel<TQ, 2>, "paged_append_kernel<2>", grid, block, s, f)
                 : launch_kernel(sbpk::paged_append_kernel<TQ, 1>, "paged_append_kernel<1>", grid, block, s, f);
 }
 

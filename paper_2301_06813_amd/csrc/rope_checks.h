@@ -26,10 +26,10 @@ inline std::pair<uintptr_t, uintptr_t> turns_span(const sbpi::Rotation &r) {
     return {b, b + (uintptr_t)(r.dim / 2 * 8)};
 }
 
-// Rows times heads times units of 16 columns (rotated and copied columns apart, so one more
-// than the head dimension has) stay below 2^31.
+// Rows times heads times units of 8 columns and more (rotated and copied columns apart, so two
+// more at most than the head dimension has) stay below 2^31.
 inline bool rotation_fits(double rows, double heads, int64_t d) {
-    return rows * heads * (double)((d + 31) / 16) < 2147483648.0;
+    return rows * heads * (double)((d + 23) / 8) < 2147483648.0;
 }
 
 }  // namespace sbpa

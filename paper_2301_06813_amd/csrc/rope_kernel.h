@@ -43,106 +43,96 @@ __device__ __forceinline__ void angle(uint64_t turns, int64_t t, float mul, floa
     *s *= mul;
 }
 
-// A head's columns are taken in units of 16: first the rotated ones, 8 pairs a unit, then the
-// others. A unit is two runs of up to 8 columns.
+// A head's columns are taken in units of 2 R: first the rotated ones, R pairs a unit, then the
+// others. A unit is two runs of up to R columns.
 struct Unit {
     int one, two;     // first columns of the runs
     int n, m;         // columns of the runs
     bool turn;        // the columns make pairs, else they are copied
 };
 
+template <int R>
 __host__ __device__ inline int units_of(const Rotation &r, int d) {
-    return (r.dim / 2 + 7) / 8 + (d - r.dim + 15) / 16;
+    return (r.dim / 2 + R - 1) / R + (d - r.dim + 2 * R - 1) / (2 * R);
 }
 
+template <int R>
 __device__ __forceinline__ Unit unit_of(const Rotation &r, int d, int u) {
-    const int half = r.dim / 2, turned = (half + 7) / 8;
+    const int half = r.dim / 2, turned = (half + R - 1) / R;
     Unit x;
     x.turn = u < turned;
     if (x.turn) {
-        const int k = min(8, half - 8 * u);      // pairs
-        x.one = r.pairs ? 16 * u : 8 * u;
-        x.two = r.pairs ? 16 * u + 8 : half + 8 * u;
-        x.n = r.pairs ? min(8, 2 * k) : k;
-        x.m = r.pairs ? max(0, 2 * k - 8) : k;
+        const int k = min(R, half - R * u);      // pairs
+        x.one = r.pairs ? 2 * R * u : R * u;
+        x.two = r.pairs ? x.one + R : half + R * u;
+        x.n = r.pairs ? min(R, 2 * k) : k;
+        x.m = r.pairs ? max(0, 2 * k - R) : k;
     } else {
-        x.one = r.dim + 16 * (u - turned);
-        x.two = x.one + 8;
-        x.n = min(8, d - x.one);
-        x.m = min(8, max(0, d - x.two));
+        x.one = r.dim + 2 * R * (u - turned);
+        x.two = x.one + R;
+        x.n = min(R, d - x.one);
+        x.m = min(R, max(0, d - x.two));
     }
     return x;
 }
 
-// 8 values in the memory's type, which may be any element's address: whole runs move in 16-byte
-// accesses (which need no alignment), others value by value.
-template <typename T>
-struct Run;
+// R values in the memory's type at any element's address (global accesses need no alignment): a
+// whole run in one access, or two for 32 bytes; a shorter one in 8, 4 and 2 bytes.
+template <typename T, int R>
+struct Run {
+    static constexpr int WORDS = R * (int)sizeof(T) / 4;
+    typedef uint32_t V __attribute__((ext_vector_type(WORDS)));
+    typedef V V_any __attribute__((aligned(2)));
+    typedef uint64_t D_any __attribute__((aligned(2)));
+    typedef uint32_t W_any __attribute__((aligned(2)));
+    V v;
 
-template <>
-struct Run<uint16_t> {
-    u32x4 v;
-    __device__ __forceinline__ void load(const uint16_t *p, int n) {
-        if (n == 8) {
-            v = *reinterpret_cast<const u32x4_any *>(p);
+    __device__ __forceinline__ void load(const T *from, int n) {
+        if (n == R) {
+            v = *reinterpret_cast<const V_any *>(from);
             return;
         }
-        v = u32x4{0u, 0u, 0u, 0u};
+        const char *p = reinterpret_cast<const char *>(from);
+        const int bytes = n * (int)sizeof(T);
+        uint64_t first = 0, rest = 0;
+        if (bytes & 8) first = *reinterpret_cast<const D_any *>(p), p += 8;
+        if (bytes & 4) rest = *reinterpret_cast<const W_any *>(p), p += 4;
+        if (bytes & 2) rest |= (uint64_t)*reinterpret_cast<const uint16_t *>(p) << (bytes & 4 ? 32 : 0);
+        const uint64_t lo = bytes & 8 ? first : rest, hi = bytes & 8 ? rest : 0;
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) v[e / 2] |= (uint32_t)p[e] << (16 * (e & 1));
+        for (int w = 0; w < WORDS; ++w) v[w] = (uint32_t)((w < 2 ? lo : hi) >> (32 * (w & 1)));
     }
-    __device__ __forceinline__ void store(uint16_t *p, int n) const {
-        if (n == 8) {
-            *reinterpret_cast<u32x4_any *>(p) = v;
+    __device__ __forceinline__ void store(T *to, int n) const {
+        if (n == R) {
+            *reinterpret_cast<V_any *>(to) = v;
             return;
         }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = (uint16_t)(v[e / 2] >> (16 * (e & 1)));
+        char *p = reinterpret_cast<char *>(to);
+        const int bytes = n * (int)sizeof(T);
+        const uint64_t lo = v[0] | (uint64_t)v[1] << 32;
+        const uint64_t hi = WORDS > 2 ? v[WORDS - 2] | (uint64_t)v[WORDS - 1] << 32 : 0;
+        uint64_t rest = bytes & 8 ? hi : lo;
+        if (bytes & 8) *reinterpret_cast<D_any *>(p) = lo, p += 8;
+        if (bytes & 4) *reinterpret_cast<W_any *>(p) = (uint32_t)rest, p += 4, rest >>= 32;
+        if (bytes & 2) *reinterpret_cast<uint16_t *>(p) = (uint16_t)rest;
     }
     __device__ __forceinline__ float get(int e) const {
-        return __builtin_bit_cast(float, e & 1 ? v[e / 2] & 0xffff0000u : v[e / 2] << 16);
+        // (a copy: the cast of a vector's element itself takes the first one)
+        const uint32_t w = v[e * (int)sizeof(T) / 4];
+        return __builtin_bit_cast(float, sizeof(T) == 4 ? w : e & 1 ? w & 0xffff0000u : w << 16);
     }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
+    __device__ __forceinline__ void set(const float (&x)[R]) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2)
-            v[e / 2] = (uint32_t)f32_to_bf16_bits(x[e]) | (uint32_t)f32_to_bf16_bits(x[e + 1]) << 16;
+        for (int w = 0; w < WORDS; ++w) {
+            if constexpr (sizeof(T) == 4) v[w] = __builtin_bit_cast(uint32_t, x[w]);
+            else v[w] = (uint32_t)f32_to_bf16_bits(x[2 * w]) | (uint32_t)f32_to_bf16_bits(x[2 * w + 1]) << 16;
+        }
     }
 };
 
-template <>
-struct Run<float> {
-    f32x4 v[2];
-    __device__ __forceinline__ void load(const float *p, int n) {
-        if (n == 8) {
-            v[0] = *reinterpret_cast<const f32x4_any *>(p);
-            v[1] = *reinterpret_cast<const f32x4_any *>(p + 4);
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e / 4][e % 4] = e < n ? p[e] : 0.f;
-    }
-    __device__ __forceinline__ void store(float *p, int n) const {
-        if (n == 8) {
-            *reinterpret_cast<f32x4_any *>(p) = v[0];
-            *reinterpret_cast<f32x4_any *>(p + 4) = v[1];
-            return;
-        }
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-            if (e < n) p[e] = v[e / 4][e % 4];
-    }
-    __device__ __forceinline__ float get(int e) const { return v[e / 4][e % 4]; }
-    __device__ __forceinline__ void set(const float (&x)[8]) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e / 4][e % 4] = x[e];
-    }
-};
-
-template <typename T>
+template <typename T, int R>
 struct Pair {
-    Run<T> one, two;
+    Run<T, R> one, two;
     __device__ __forceinline__ void load(const T *row, const Unit &u) {
         one.load(row + u.one, u.n);
         two.load(row + u.two, u.m);
@@ -150,46 +140,49 @@ struct Pair {
 };
 
 // The angles of unit u's pairs at position t.
+template <int R>
 struct Angles {
-    float c[8], s[8];
+    float c[R], s[R];
     __device__ __forceinline__ void find(const Rotation &r, int u, int64_t t, bool back) {
         const int last = r.dim / 2 - 1;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            angle(r.turns[min(8 * u + e, last)], t, r.mul, &c[e], &s[e]);
+        for (int e = 0; e < R; ++e) {
+            angle(r.turns[min(R * u + e, last)], t, r.mul, &c[e], &s[e]);
             if (back) s[e] = -s[e];
         }
     }
 };
 
 // Stores a unit, turned by its angles or as it is, to `row`. In the order of pairs a run
-// holds 4 pairs whose columns are neighbours; else the runs hold 8 pairs' first and second.
-template <typename TI, typename TO>
-__device__ __forceinline__ void put(const Pair<TI> &x, const Angles &a, const Unit &u, bool pairs, TO *row) {
-    float one[8], two[8];
+// holds R / 2 pairs whose columns are neighbours; else the runs hold R pairs' first and second.
+template <typename TI, typename TO, int R>
+__device__ __forceinline__ void put(const Pair<TI, R> &x, const Angles<R> &a, const Unit &u, bool pairs,
+                                    TO *row) {
+    float one[R], two[R];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
+    for (int e = 0; e < R; ++e) {
         one[e] = x.one.get(e);
         two[e] = x.two.get(e);
     }
     if (u.turn && !pairs) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
+        for (int e = 0; e < R; ++e) {
             const float v = one[e], w = two[e];
             one[e] = v * a.c[e] - w * a.s[e];
             two[e] = w * a.c[e] + v * a.s[e];
         }
     } else if (u.turn) {
 #pragma unroll
-        for (int e = 0; e < 8; e += 2) {
+        for (int e = 0; e < R; e += 2) {
+            const int k = e / 2, l = (e + R) / 2;
             const float v = one[e], w = one[e + 1], y = two[e], z = two[e + 1];
-            one[e] = v * a.c[e / 2] - w * a.s[e / 2];
-            one[e + 1] = w * a.c[e / 2] + v * a.s[e / 2];
-            two[e] = y * a.c[e / 2 + 4] - z * a.s[e / 2 + 4];
-            two[e + 1] = z * a.c[e / 2 + 4] + y * a.s[e / 2 + 4];
+            one[e] = v * a.c[k] - w * a.s[k];
+            one[e + 1] = w * a.c[k] + v * a.s[k];
+            two[e] = y * a.c[l] - z * a.s[l];
+            two[e + 1] = z * a.c[l] + y * a.s[l];
         }
     }
-    Run<TO> r;
+    Run<TO, R> r;
     r.set(one);
     r.store(row + u.one, u.n);
     r.set(two);

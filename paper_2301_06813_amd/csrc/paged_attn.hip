@@ -470,6 +470,15 @@ void paged_attn_kernel(PagedLaunch f0) {
                 };
                 w.begin(mine(0), seen);
                 int x = 0;
+                // a wave without rows only loads (ahead of the loops, which it then passes by: as a
+                // branch of theirs, or in place of them, it costs 50 registers and more)
+                if (!__any(live))
+                    for (; x < n; ++x) {
+                        advance(x);
+#pragma unroll
+                        for (int p = 0; p < S::LOADS; ++p) part(p);
+                        w.stage = after();
+                    }
                 for (; x < min(n, walk.masked()); ++x) take(x, std::true_type{});
                 for (; x < n; ++x) take(x, std::false_type{});
                 wait_vm<0>();      // no load is on its way to LDS any more

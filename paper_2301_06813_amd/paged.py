@@ -64,7 +64,7 @@ class Cache:
         if Q is not None:
             B, H, S, D = Q.shape
             if out is None:
-                hq = H if scope != sbp.SBP_GLOBAL else rank_heads(H, K.shape[1], p, r)[1]
+                hq = H if p == 1 or scope != sbp.SBP_GLOBAL else rank_heads(H, K.shape[1], p, r)[1]
                 out, qo = _new(Q, B, hq, S, D, out_dtype or Q.dtype)
             else:
                 qo = sbp.view4(out, sbp.SBP_LOCAL)
@@ -89,7 +89,7 @@ class Cache:
                 lse=lse, out=out, out_dtype=out_dtype, ws=ws), Q, table, len_k, p, r)
         B, H, S, D = Q.shape
         same_device(Q, table, len_k, len_q, row_q, out, ws, self.k, self.v)
-        hq = H if self.scope != sbp.SBP_GLOBAL else rank_heads(H, self.k.shape[1], p, r)[1]
+        hq = H if p == 1 or self.scope != sbp.SBP_GLOBAL else rank_heads(H, self.k.shape[1], p, r)[1]
         if out is None:
             out, o = _new(Q, B, hq, S, D, out_dtype or Q.dtype)
         else:

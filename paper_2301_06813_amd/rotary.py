@@ -79,23 +79,24 @@ def _turn(call, rope, Q, K, p, r, pos, out, out_dtype, scope, stream):
     B, H, S, D = Q.shape
     same_device(Q, K, pos, rope.turns, *(out or ()))
     Hk = H if K is None else K.shape[1]
-    hq, hk = (H, Hk) if scope != sbp.SBP_GLOBAL else rank_heads(H, Hk, p, r)[1::2]
+    hq, hk = (H, Hk) if p == 1 or scope != sbp.SBP_GLOBAL else rank_heads(H, Hk, p, r)[1::2]
     q = sbp.view4(Q, scope)
     k = None if K is None else sbp.view4(K, scope)
     if out is None:
         # one block for both, [batch][rows][heads][dim] with K's heads behind Q's
         n = hq if K is None else hq + hk
-        t = Q.new_empty((B, S, n, D), dtype=out_dtype or Q.dtype)
+        t = Q.new_empty((B, S, n, D), dtype=out_dtype) if out_dtype else Q.new_empty((B, S, n, D))
         ld = max(n, 1) * D
         dt, at, sb = sbp._dtype_of(t), t.data_ptr(), max(S, 1) * ld
+        strides = sb, D, ld, 1
         qo = sbp.sbp_view4_t(at, B, hq, S, D, sb, D, ld, dt, sbp.SBP_LOCAL)
-        t = t.transpose(1, 2)
         if K is None:
-            ko, out = None, (t, None)
+            ko, out = None, (t.as_strided((B, hq, S, D), strides), None)
         else:
             ko = sbp.sbp_view4_t(at + hq * D * t.element_size(), B, hk, S, D, sb, D, ld, dt,
                                  sbp.SBP_LOCAL)
-            out = t.split_with_sizes((hq, hk), 1)
+            out = (t.as_strided((B, hq, S, D), strides),
+                   t.as_strided((B, hk, S, D), strides, hq * D))
     else:
         qo, ko = (None if t is None else sbp.view4(t, sbp.SBP_LOCAL) for t in out)
     call(q, k, rope.view, places(pos, B, S), qo, ko, p, r, None)

@@ -660,18 +660,19 @@ hipError_t launch(const sbpk::PagedLaunch &f, bool dma, hipStream_t s) {
     return launch_kernel(sbpk::paged_attn_kernel<DP, KG, KT, NW, WPS, false>, name, grid, block, s, f);
 }
 
-// The kernel's forms: rows of a tile, keys of a step, workgroups of a unit, us of a step, an item's
-// fixed part in steps. The second gives up speed a row for smaller tiles: a chunk of 2048 of 16
-// heads over 4, 32768 keys, takes 588 and 790 us at 128 columns, 504 and 708 at 64; one token of 32
-// sequences of 64 heads over 8, 4096 x 128, 165 and 117.
+// The kernel's forms: rows of a tile, workgroups of a unit, us of a step of KEYS. The second gives
+// up speed a row for smaller tiles: a chunk of 2048 of 16 heads over 4, 32768 keys, takes 523 and
+// 666 us at 128 columns, 430 and 568 at 64; chunks of 8 of 8 sequences, 64 heads over 8, 8192 x
+// 128, 57 and 50; one token of 16 sequences, 16 heads over 4, up to 4096 x 64, 18 and 17.6.
 struct Form {
     int rows, per_cu;
     double step;
-    int fixed;
 };
 constexpr int KEYS = 64;
-constexpr Form FORMS[2][2] = {{{128, 2, 2.03, 5}, {64, 2, 1.43, 6}},
-                              {{256, 1, 2.33, 5}, {128, 1, 1.59, 6}}};
+constexpr Form FORMS[2][2] = {{{128, 2, 1.73}, {64, 2, 1.15}}, {{256, 1, 2.08}, {128, 1, 1.34}}};
+// An item's fixed part in steps: 2 and 5 differ by 12 % where items are short (prompts among
+// tokens, 16 steps each: 42 us for 48), by 2 % elsewhere, to either side.
+constexpr int FIXED = 3;
 
 }  // namespace
 
@@ -711,9 +712,9 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     const double most_tiles = a.at.row_q ? (double)(rows / m.rows) + a.at.seqs
                                          : (double)((rows + m.rows - 1) / m.rows) * a.at.seqs;
     const double steps = (double)a.at.width * a.at.page / KEYS + 2;
-    f.fixed = m.fixed;
+    f.fixed = FIXED;
     f.scale = 0;
-    while (most_tiles * a.kv_heads * (steps / (double)(1 << f.scale) + 1 + f.fixed) > 1e9) ++f.scale;
+    while (most_tiles * a.kv_heads * (steps / (double)(1 << f.scale) + 1 + FIXED) > 1e9) ++f.scale;
     // rows of one load lie on one page, whose offsets fit the loads' arithmetic
     const int per_load = wide ? 4 : 8;
     const bool dma = a.aligned && a.at.page % per_load == 0 &&

@@ -1,7 +1,7 @@
 // paged_append.hip -- new tokens' keys and values to their places in a paged cache, with the
 // rotation of K and Q on the way.
 //
-// A thread owns 16 columns of a new token and takes them in HEADS of the heads of Q, K and V, one
+// A thread owns R pairs of columns of a new token and takes them in HEADS of the heads of Q, K and V, one
 // after the other (rope.hip): the token's place gives both its row of the cache and its
 // angles. In a packed batch a wave finds its first row's sequence by a search of 64 places at a
 // time. The bound is memory, for few tokens the chain of loads from a row to its page. (7172 new
@@ -16,7 +16,9 @@ namespace sbpk {
 
 using sbpi::AppendArgs;
 
-constexpr int R = 8;                 // pairs of a unit
+// Pairs of a unit: 16 bytes of Qo's type.
+template <typename TQ>
+constexpr int PAIRS_OF = 16 / (int)sizeof(TQ);
 
 struct AppendLaunch {
     AppendArgs a;
@@ -26,29 +28,31 @@ struct AppendLaunch {
 
 template <typename TQ, int HEADS>
 __global__ __launch_bounds__(256) void paged_append_kernel(AppendLaunch f) {
+    constexpr int R = PAIRS_OF<TQ>;
     const AppendArgs &a = f.a;
     const Rotation &r = a.rot;
     const uint32_t id = blockIdx.x * 256u + threadIdx.x;
     if (blockIdx.x * 256u + (threadIdx.x & ~63u) >= (uint32_t)f.threads) return;   // whole waves
     const int rest = f.units(id), ui = f.units.rest(id, rest);
     const int row = f.groups(rest), hg = f.groups.rest(rest, row);
-    int b = f.rows(row), i = f.rows.rest(row, b);
-    const int batch = b;
-    int n = a.at.rows, first = 0;
-    bool live = id < (uint32_t)f.threads;
+    const bool live = id < (uint32_t)f.threads;
+    int b = 0, batch = 0, i = row, n = a.at.rows, first = 0;
     if (a.at.row_q) {
         // the last sequence that begins at or before the row
         b = sequence_of(a.at, __builtin_amdgcn_readfirstlane(row));
-        while (live && b < a.at.seqs && a.at.row_q[b + 1] <= row) ++b;
-        live = live && b >= 0 && b < a.at.seqs;
-        if (!live) b = 0;
+        if (!live) return;
+        while (b < a.at.seqs && a.at.row_q[b + 1] <= row) ++b;
+        if (b < 0 || b >= a.at.seqs) return;
         first = max(a.at.row_q[b], 0);
         n = min(a.at.row_q[b + 1], a.at.rows) - first;
-    } else if (a.at.len_q) {
-        n = min(max(a.at.len_q[b], 0), a.at.rows);
+    } else {
+        if (!live) return;
+        b = batch = f.rows(row);
+        i = f.rows.rest(row, b);
+        if (a.at.len_q) n = min(max(a.at.len_q[b], 0), a.at.rows);
     }
     const int new_i = i - first;
-    if (!live || new_i < 0 || new_i >= n) return;
+    if (new_i < 0 || new_i >= n) return;
     const int64_t t = (int64_t)a.at.len_k[b] - n + new_i;
     const int heads = a.q_heads + 2 * a.kv_heads, step = (int)f.groups.d;
     const Unit u = unit_of<R>(r, a.d, ui);
@@ -99,7 +103,7 @@ hipError_t launch(const AppendArgs &a, hipStream_t s) {
     sbpk::AppendLaunch f;
     f.a = a;
     const int64_t rows = (int64_t)a.batch * a.at.rows;
-    const int heads = a.q_heads + 2 * a.kv_heads, units = sbpk::units_of<sbpk::R>(a.rot, a.d);
+    const int heads = a.q_heads + 2 * a.kv_heads, units = sbpk::units_of<sbpk::PAIRS_OF<TQ>>(a.rot, a.d);
     const bool many = rows * heads * units > (int64_t)device_cus() * 2048;
     const int groups = many ? (heads + 1) / 2 : heads;
     f.threads = (int32_t)(rows * groups * units);

@@ -178,6 +178,7 @@ void paged_attn_kernel(PagedLaunch f0) {
                  "s"(a.vc.p), "s"(a.o.p), "s"(a.lse.p), "s"(a.kv_heads), "s"(a.d), "s"(a.ws),
                  "s"(f.slot_rows), "s"(f.fixed), "s"(f.by_groups.m));
     const int wg = remap_xcd(blockIdx.x, f.groups);    // neighbours on the line share an L2
+    if (f.split && tid == 0) cuts_of(f)[wg].last = -1;
 
     // This workgroup's part of the line: `left` units from unit u of tile `tile` of head hk of
     // sequence b on. Every wave adds up the sequences by itself, a lane each. (Units fit 31 bits:
@@ -242,10 +243,7 @@ void paged_attn_kernel(PagedLaunch f0) {
             }
             at = line.share * wg;
             left = min(line.share, total - at);
-            if (left <= 0) {
-                if (f.split && tid == 0) cuts_of(f)[wg].last = -1;
-                return;
-            }
+            if (left <= 0) return;
             if (b == 0) break;
             b = 0;
             pass = FIND;
@@ -290,15 +288,13 @@ void paged_attn_kernel(PagedLaunch f0) {
         // before those to LDS, which are counted).
         auto note = [&]() {
             noted = true;
-            if (tid) return;
-            Cut cut{-1, hk, tile * ROWS, seq.at.batch, seq.at.first, seq.rows, {0, 0}};
             if (s0 > 0 && s0 < k.length() && k.cut(f, line, u - line.share) == 0) {
                 // the workgroup of the item's last unit, unless its share's begin is moved to the end
                 int w = (int)((uint32_t)(k.cost(f, line) - u - 1) / (uint32_t)line.share);
                 if (w > 0 && k.cut(f, line, u + w * line.share) == k.length()) --w;
-                cut.last = wg + w;
+                if (tid == 0)
+                    cuts_of(f)[wg] = Cut{wg + w, hk, tile * ROWS, seq.at.batch, seq.at.first, seq.rows, {0, 0}};
             }
-            cuts_of(f)[wg] = cut;
         };
         if (s0 < s1) {
             const bool whole = s0 == 0 && s1 == k.length();

@@ -65,8 +65,8 @@ int rope(const sbp_view4_t *Q, const sbp_view4_t *K, const sbp_rope_t *rope_, co
     a.back = back;
     std::pair<uintptr_t, uintptr_t> arrays[2] = {turns_span(a.rot), {0, 0}};
     if (at) {
-        if ((at->per_row != 0 && at->per_row != 1) || at->ld < 0 || at->ld > (int64_t(1) << 40) ||
-            (at->per_row && Q->batch > 1 && at->ld < Q->rows))
+        if ((at->per_row != 0 && at->per_row != 1) || at->ld < 0 ||
+            (double)Q->batch * (double)at->ld > 1e18)
             return SBP_ERR_SHAPE;
         const bool some = Q->batch > 0 && Q->rows > 0;
         if (some && !at->pos) return SBP_ERR_NULL;

@@ -8,6 +8,8 @@
 // polynomials take.
 #pragma once
 
+#include <type_traits>
+
 #include "gemm_bf16_dma.h"
 #include "rope.h"
 
@@ -76,11 +78,12 @@ __device__ __forceinline__ Unit unit_of(const Rotation &r, int d, int u) {
     return x;
 }
 
-// R values in the memory's type at any element's address (global accesses need no alignment): a
-// whole run in one access, or two for 32 bytes; a shorter one in 8, 4 and 2 bytes.
+// R values in the memory's type, 16 bytes at most, at any element's address (global accesses need
+// no alignment): a whole run in one access, a shorter one in 8, 4 and 2 bytes.
 template <typename T, int R>
 struct Run {
     static constexpr int WORDS = R * (int)sizeof(T) / 4;
+    static_assert(WORDS == 2 || WORDS == 4, "8 or 16 bytes");
     typedef uint32_t V __attribute__((ext_vector_type(WORDS)));
     typedef V V_any __attribute__((aligned(2)));
     typedef uint64_t D_any __attribute__((aligned(2)));
@@ -158,6 +161,12 @@ struct Angles {
 template <typename TI, typename TO, int R>
 __device__ __forceinline__ void put(const Pair<TI, R> &x, const Angles<R> &a, const Unit &u, bool pairs,
                                     TO *row) {
+    if constexpr (std::is_same<TI, TO>::value)
+        if (!u.turn) {                // bit for bit
+            x.one.store(row + u.one, u.n);
+            x.two.store(row + u.two, u.m);
+            return;
+        }
     float one[R], two[R];
 #pragma unroll
     for (int e = 0; e < R; ++e) {

@@ -53,8 +53,7 @@ def places(pos, batch: int, rows: int):
         return sbp.sbp_places_t(pos.data_ptr(), pos.stride(0), 0)
     if pos.shape != (batch, rows) or (rows > 1 and pos.stride(1) != 1):
         raise ValueError("one position per sequence, or per row with unit stride")
-    ld = pos.stride(0)
-    return sbp.sbp_places_t(pos.data_ptr(), max(ld, rows) if batch <= 1 else ld, 1)
+    return sbp.sbp_places_t(pos.data_ptr(), pos.stride(0), 1)
 
 
 def fwd(rope: Rope, Q, K=None, p: int = 1, r: int = 0, *, pos=None, out=None, out_dtype=None,

@@ -438,3 +438,119 @@ def test_refused_from_torch():
     with pytest.raises(sbp.SbpError) as e:
         b.cache.attend(b.Q, table, lens, len_q=i32([1, 1]), row_q=i32([0, 1, 2]))
     assert e.value.code == sbp.SBP_ERR_SHAPE
+
+
+# ------------------------------------------------------- many shapes, edges
+def draw(seed):
+    """A batch of sizes that meet the tiles', pages' and parts' edges in ever other ways."""
+    import random
+    r = random.Random(seed)
+    Hk = r.choice((1, 2, 3, 8))
+    group = r.choice((1, 2, 4, 5, 8, 16))
+    D = r.choice((8, 16, 40, 64, 64, 96, 128, 128, r.randrange(1, 129)))
+    P = r.choice((4, 8, 16, 16, 32, 100, 257, r.randrange(1, 64)))
+    n = r.choice((1, 2, 5, 33, 130))
+    most = {1: 700, 2: 400, 5: 150, 33: 30, 130: 5}[n]
+    new = [r.choice((0, 1, 1, 1, r.randrange(1, most + 1))) for _ in range(n)]
+    lens = [r.choice((x, x + r.randrange(0, 40), x + r.randrange(0, 3000 // n + 200))) for x in new]
+    return dict(new=new, lens=lens, heads=(Hk * group, Hk), D=D, P=P,
+                layout=r.choice(("token", "head", "both", "odd")), packed=r.random() < 0.6,
+                pad=r.randrange(0, 3), gap=r.randrange(0, 2), seed=seed), dict(
+                    causal=r.random() < 0.8, window=r.choice((0, 0, 0, 1, 50, 700)),
+                    out_dtype=r.choice((BF, F32)))
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_attention_of_drawn_shapes(seed):
+    shape, kw = draw(1000 + seed)
+    if max(shape["new"]) == 0:
+        shape["new"][0] = 1
+        shape["lens"][0] += 1
+    check_attn(Batch(**shape), **kw)
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_append_of_drawn_shapes(seed):
+    shape, _ = draw(2000 + seed)
+    if max(shape["new"]) == 0:
+        shape["new"][0] = 1
+        shape["lens"][0] += 1
+    b = Batch(**shape)
+    rot, order = b.D // 2 * 2, ("halves", "pairs")[seed % 2]
+    kc, kb, vc, q, qb = plain_append(b, rot, order)
+    kw = dict(Q=b.Q, rope=rotary.Rope(rot, order=order), out_dtype=(BF, F32)[seed // 2 % 2]) if rot else {}
+    out = b.cache.append(b.K, b.V, *b.args(), **kw, **b.rows())
+    torch.cuda.synchronize()
+    rope_ref.check("keys", b.kc, kc, kb)
+    assert torch.equal(b.kc.cpu().double()[kb == 0], kc[kb == 0])
+    assert torch.equal(b.vc.cpu().double(), vc)
+    for x, first, n in b.seqs if rot else ():
+        s = slice(first, first + n)
+        rope_ref.check("Q", out[x, :, s], q[x, :, s], qb[x, :, s])
+
+
+def test_copied_columns_and_values_keep_their_bits():
+    """Not-a-numbers of any payload, infinities, subnormal numbers, -0."""
+    b = Batch([70, 3], [90, 3], (2, 2), 48, 16, packed=True)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    bits = torch.randint(-(1 << 15), 1 << 15, b.V.shape, generator=g, device="cuda", dtype=torch.int16)
+    bits[..., ::3] |= 0x7f80                       # every exponent bit
+    b.V.copy_(bits.view(BF))
+    b.K[..., 16:] = bits.view(BF)[..., 16:]
+    b.cache.append(b.K, b.V, *b.args(), rope=rotary.Rope(16), **b.rows())
+    raw = lambda t: t.contiguous().view(torch.int16)
+    for x, i, page, slot, t in pref.places(b.seqs, b.len, b.table, b.kc.shape[0], b.P):
+        assert torch.equal(raw(b.vc[page, :, slot]), raw(b.V[x, :, i]))
+        assert torch.equal(raw(b.kc[page, :, slot, 16:]), raw(b.K[x, :, i, 16:]))
+
+
+@pytest.mark.parametrize("new", [1, 3])
+def test_room_for_more_steps_than_31_bits_count(new):
+    """A table whose rows have room for 2^29 tokens: the units of the items, at most, pass 2^31
+    and are taken coarser; results as with a table of their size."""
+    B, H, Hk, D, P = 64, 16, 16, 64, 512
+    lens = [1 + 53 * i for i in range(B)]
+    b = Batch([new] * B, [max(new, n) for n in lens], (H, Hk), D, P, "head")
+    wide = torch.full((B, 1 << 20), -1, dtype=torch.int32, device="cuda")
+    table = i32(b.table)
+    wide[:, :table.shape[1]] = table
+    s = 1 / 8
+    want, bound, wl, _ = pref.attend(b.Q, b.kc, b.vc, b.table, b.len, b.seqs, s, True, 0)
+    for ws in (None, sbp.NO_WORKSPACE):
+        O, lse = b.cache.attend(b.Q, wide, i32(b.len), scale=s, ws=ws)
+        pref.check("O", O, want, bound)
+        assert float((lse.double() - wl).abs().max()) <= 2.0 ** -14
+
+
+@pytest.mark.parametrize("packed", [False, True])
+def test_many_sequences(packed):
+    """More sequences than the lanes of a wave count at once, among them many without tokens."""
+    n = 700
+    new = [(0, 1, 1, 2, 5)[i * i % 5] for i in range(n)]
+    lens = [x + (i * 37) % 90 for i, x in enumerate(new)]
+    b = Batch(new, lens, (4, 2), 64, 16, packed=packed)
+    check_attn(b)
+    kc, kb, vc, q, qb = plain_append(b, 64, "halves")
+    b.cache.append(b.K, b.V, *b.args(), rope=rotary.Rope(64), **b.rows())
+    rope_ref.check("keys", b.kc, kc, kb)
+    assert torch.equal(b.vc.cpu().double(), vc)
+
+
+def test_no_pages_no_lse_strided_output():
+    b = Batch([2, 3], [20, 30], (4, 2), 64, 16)
+    out = torch.full((2, 4, 3, 70), 7.0, dtype=F32, device="cuda")
+    want, _ = b.cache.attend(b.Q, *b.args(), **b.rows(), out_dtype=F32)
+    O, lse = b.cache.attend(b.Q, *b.args(), **b.rows(), out=out[..., 3:67], lse=False)
+    assert lse is None and torch.equal(O, want)
+    assert float((out[..., :3] - 7).abs().max()) == 0 and float((out[..., 67:] - 7).abs().max()) == 0
+    none = paged.Cache(b.kc[:0], b.vc[:0])
+    O, lse = none.attend(b.Q, *b.args(), **b.rows())
+    assert float(O.abs().max()) == 0 and (lse == -math.inf).all()
+    none.append(b.K, b.V, *b.args(), **b.rows())
+
+
+def test_one_long_sequence_in_many_parts():
+    """A single item of one key head, cut into as many parts as there are workgroups."""
+    for new in (1, 2):
+        check_attn(Batch([new], [40000], (8, 1), 64, 16, "head"))
+        check_attn(Batch([new], [40000], (8, 1), 128, 64, "head"))

@@ -213,3 +213,25 @@ def test_refused_from_torch():
     with pytest.raises(sbp.SbpError) as e:
         rotary.fwd(rotary.Rope(18), Q, K)
     assert e.value.code == sbp.SBP_ERR_SHAPE
+
+
+def test_positions_with_any_strides():
+    """Positions shared by all sequences (a stride of 0), and a column of a wider tensor."""
+    Q, K = fused(3, 20, 4, 2, 64, 23)
+    rope = rotary.Rope(64)
+    row = torch.randint(0, 9000, (20,), dtype=torch.int32, device="cuda")
+    want = rotary.fwd(rope, Q, K, pos=row.expand(3, 20).contiguous())
+    got = rotary.fwd(rope, Q, K, pos=row.expand(3, 20))
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    wide = torch.randint(0, 9000, (3, 7), dtype=torch.int32, device="cuda")
+    want = rotary.fwd(rope, Q, K, pos=wide[:, 4].contiguous())
+    got = rotary.fwd(rope, Q, K, pos=wide[:, 4])
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_copied_columns_keep_their_bits():
+    g = torch.Generator(device="cuda").manual_seed(25)
+    x = torch.randint(-(1 << 15), 1 << 15, (2, 3, 5, 40), generator=g, device="cuda", dtype=torch.int16)
+    x[..., ::3] |= 0x7f80
+    y, _ = rotary.fwd(rotary.Rope(12), x.view(BF))
+    assert torch.equal(y[..., 12:].contiguous().view(torch.int16), x[..., 12:])

@@ -112,7 +112,7 @@ CASES = [
     ("output rows", dict(ko=v4(80, 2, 2, 60, 32, scope=LO)), S),
     ("output rows overlap", dict(qo=v4(64, 2, 4, 64, 32, scope=LO, ld=32, sh=32)), S),
     ("places: flag", dict(at=sbp.sbp_places_t(201 * MB, 64, 2)), S),
-    ("places: rows overlap", dict(at=sbp.sbp_places_t(201 * MB, 63, 1)), S),
+    ("places beyond 62 bits", dict(at=sbp.sbp_places_t(201 * MB, 1 << 60, 1)), S),
     ("places: negative ld", dict(at=sbp.sbp_places_t(201 * MB, -1, 0)), S),
     ("places: null", dict(at=sbp.sbp_places_t(None, 64, 1)), N),
     ("places: misaligned", dict(at=sbp.sbp_places_t(201 * MB + 2, 64, 1)), sbp.SBP_ERR_ALIGN),

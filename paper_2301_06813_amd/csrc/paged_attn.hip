@@ -34,11 +34,11 @@ constexpr int PAGES_AT_ONCE = 1024;
 constexpr int SHORTEST = 2;          // steps that a cut leaves on either side
 
 // What workgroup w leaves for the join where its share begins inside an item that workgroup
-// w - 1 began: the item's parts are in slot 1 of w - 1 and in slots 0 of w .. last. Else last < 0.
+// w - 1 began: the item's parts are those of w - 1 .. last (slot_of). Else last < 0.
 struct Cut {
     int32_t last, head, row;         // first packed row of the tile
     int32_t batch, first, rows;      // of its sequence
-    int32_t spare[2];
+    int32_t parts, spare;            // whether the line's units are parts
 };
 constexpr int CUT_FLOATS = sizeof(Cut) / 4;
 
@@ -47,14 +47,18 @@ struct PagedLaunch {
     int32_t slot_rows;               // rows of a partial output
     int32_t split;                   // items may be cut
     int32_t vec;                     // O allows 4-value stores
-    int32_t groups;                  // workgroups
+    int32_t groups, slots;           // workgroups, partial outputs that the workspace holds
     int32_t fixed, scale;            // an item's fixed part in steps; a unit has 2^scale steps
-    Div page, group, by_groups;
+    Div page, group, by_half;        // by_half: workgroups with two partial outputs each
 };
 
-// The line of items. Its units are steps (`fixed` more an item), or, where the items are few and
-// short, equal parts of them: an item of n steps has 1 + (n - 1) per, and a workgroup's share is one
-// part, since a second one would cost it as much again.
+// The line of items. Its units are steps (`fixed` more an item), or equal parts of items, a part a
+// workgroup: an item of n steps has 1 + floor((n - 1) per). Parts are taken where they are no more
+// than the workgroups though hardly longer than shares of steps: no workgroup then has a second
+// item to begin, and an item's parts begin and end where its neighbours' do, so that keys that one
+// workgroup reads are in the L2 for others (a chunk of 2048 of 16 heads over 4, 65536 keys: 1039 us
+// in shares of steps, 1009 in two parts an item; one token of 16 sequences of 32 heads over 2, 8192
+// x 64: 27.3 and 24.4 with the join).
 struct Line {
     int32_t share;                   // units of a workgroup
     float per;                       // 0: units are steps
@@ -71,7 +75,12 @@ __device__ __forceinline__ f32x2 *stats_of(const PagedLaunch &f) {
     return reinterpret_cast<f32x2 *>(f.a.ws + CUT_FLOATS * (int64_t)f.groups);
 }
 __device__ __forceinline__ float *parts_of(const PagedLaunch &f) {
-    return f.a.ws + (CUT_FLOATS + 4 * f.slot_rows) * (int64_t)f.groups;
+    return f.a.ws + CUT_FLOATS * (int64_t)f.groups + 2 * (int64_t)f.slots * f.slot_rows;
+}
+// The partial output of a workgroup that has one, or, in shares of steps, two: of an item that it
+// began, and of one that it did not.
+__device__ __forceinline__ int64_t slot_of(int wg, bool began, bool parts) {
+    return parts ? wg : 2 * (int64_t)wg + (began ? 1 : 0);
 }
 
 // A sequence: its rows (packed ones of the group: `rows`, of which those of n queries are in use),
@@ -176,7 +185,7 @@ void paged_attn_kernel(PagedLaunch f0) {
     // the arguments' lines, read at once: each first read of one is a trip to memory
     asm volatile("" ::"s"(a.at.table), "s"(a.at.len_k), "s"(a.at.rows), "s"(a.q.sh), "s"(a.kc.p),
                  "s"(a.vc.p), "s"(a.o.p), "s"(a.lse.p), "s"(a.kv_heads), "s"(a.d), "s"(a.ws),
-                 "s"(f.slot_rows), "s"(f.fixed), "s"(f.by_groups.m));
+                 "s"(f.slot_rows), "s"(f.fixed), "s"(f.by_half.m));
     const int wg = remap_xcd(blockIdx.x, f.groups);    // neighbours on the line share an L2
     if (f.split && tid == 0) cuts_of(f)[wg].last = -1;
 
@@ -194,10 +203,11 @@ void paged_attn_kernel(PagedLaunch f0) {
                                   __builtin_amdgcn_readlane(r.n, l), __builtin_amdgcn_readlane(r.len, l)});
         };
         int one, upto, sum, at = 0;      // units of a head of the lane's sequence; sums
-        // 64 sequences at a time: first all, for the total; then, where the line changes to parts,
-        // the (64 at most) again; else on until the share's begin. (One loop, so that its code,
+        // 64 sequences at a time: first all, for the total; then, where parts are tried, the (64 at
+        // most) again; else on until the share's begin. (One loop, so that its code,
         // run cold, is fetched once.)
         enum { TOTAL, PARTS, FIND } pass = TOTAL;
+        int steps_one = 0, steps_upto = 0, steps_total = 0, steps_share = 0;
         for (int total = 0;;) {
             int tiles = 0;
             one = 0;
@@ -229,17 +239,27 @@ void paged_attn_kernel(PagedLaunch f0) {
                 b += 64;
                 continue;
             }
-            line.share = f.by_groups(total) + 1;
-            if (pass == TOTAL && b == 0 && f.split && f.scale == 0 && line.share < 32) {
+            if (pass == TOTAL) {
+                line.share = f.by_half(max(total - 1, 0)) + 1;
                 const int items = __builtin_amdgcn_readlane(upto_lane(tiles), 63) * a.kv_heads;
-                if (4 * items <= f.groups) {
-                    // 1 + (n - 1) per parts an item: no more than workgroups, of 3 steps and more
-                    line.per = min((float)(f.groups - 1 - items) / (float)(total - f.fixed * items),
-                                   1.f / 3);
+                if (b == 0 && f.split && f.scale == 0 && items < f.groups) {
+                    // parts of 25/24 of an even share, 2 steps at least
+                    line.per = min((float)f.groups * 24 / ((float)(total - f.fixed * items) * 25), 1.f / 2);
+                    steps_one = one;
+                    steps_upto = upto;
+                    steps_total = total;
+                    steps_share = line.share;
                     pass = PARTS;
                     total = 0;
                     continue;
                 }
+            } else if (total > f.groups) {     // too many parts: back to steps
+                one = steps_one;
+                upto = steps_upto;
+                total = steps_total;
+                line = Line{steps_share, 0.f};
+            } else {
+                line.share = 1;
             }
             at = line.share * wg;
             left = min(line.share, total - at);
@@ -293,7 +313,8 @@ void paged_attn_kernel(PagedLaunch f0) {
                 int w = (int)((uint32_t)(k.cost(f, line) - u - 1) / (uint32_t)line.share);
                 if (w > 0 && k.cut(f, line, u + w * line.share) == k.length()) --w;
                 if (tid == 0)
-                    cuts_of(f)[wg] = Cut{wg + w, hk, tile * ROWS, seq.at.batch, seq.at.first, seq.rows, {0, 0}};
+                    cuts_of(f)[wg] = Cut{wg + w,       hk,       tile * ROWS,     seq.at.batch, seq.at.first,
+                                         seq.rows, line.per != 0.f, 0};
             }
         };
         if (s0 < s1) {
@@ -488,7 +509,7 @@ void paged_attn_kernel(PagedLaunch f0) {
             const float m = w.m, l = w.l;
             // a row that sees no key: O = 0, lse = -infinity
             const bool some_key = live && l != 0.f;
-            const int64_t slot = (2 * (int64_t)wg + (s0 > 0 ? 0 : 1)) * f.slot_rows;
+            const int64_t slot = slot_of(wg, s0 == 0, line.per != 0.f) * f.slot_rows;
             if (KG == 1 && !whole) {
                 // as the registers hold it: 16 bytes a lane, 1 KB a store
                 if (wr * 32 < f.slot_rows) {
@@ -582,7 +603,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const int k = s + j * SHARES;
-                const int64_t slot = (2 * (int64_t)(w - 1 + k) + (k ? 0 : 1)) * f.slot_rows;
+                const int64_t slot = slot_of(w - 1 + k, k == 0, cut.parts) * f.slot_rows;
                 const float *const part = parts_of(f) + (DP > 0 ? slot * DP + place
                                                                 : (slot + in) * d4 + col);
                 z[j] = k < n ? stats_of(f)[slot + in] : f32x2{-INFINITY, 0.f};
@@ -697,13 +718,15 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     // outputs lie as the registers hold them
     const int padded = wide ? 128 : 64;
     f.slot_rows = (int32_t)std::min<int64_t>(m.rows, form == 0 ? (rows + 31) / 32 * 32 : rows);
+    // with a slot for each workgroup items may be cut; in shares of steps, where a workgroup has two,
+    // fewer workgroups have one if the slots are less
     const int64_t most = (int64_t)device_cus() * m.per_cu;
-    const int64_t each = sbpk::CUT_FLOATS + 2 * (int64_t)f.slot_rows * (2 + (form == 0 ? padded : (a.d + 3) & ~3));
-    // with a workspace for half of the workgroups items may be cut
-    const int64_t room = (int64_t)(a.ws_floats / (size_t)each);
-    f.split = room >= most / 2;
-    f.groups = (int32_t)(f.split ? std::min(room, most) : most);
-    f.by_groups = sbpk::Div(f.groups);
+    const int64_t slot = (int64_t)f.slot_rows * (2 + (form == 0 ? padded : (a.d + 3) & ~3));
+    const int64_t slots = ((int64_t)a.ws_floats - sbpk::CUT_FLOATS * most) / slot;
+    f.split = slots >= most;
+    f.groups = (int32_t)most;
+    f.slots = (int32_t)std::min(slots, 2 * most);
+    f.by_half = sbpk::Div(f.split ? f.slots / 2 : f.groups);
     // units of all items, at most: below 2^31
     const double most_tiles = a.at.row_q ? (double)(rows / m.rows) + a.at.seqs
                                          : (double)((rows + m.rows - 1) / m.rows) * a.at.seqs;

@@ -242,7 +242,9 @@ void paged_attn_kernel(PagedLaunch f0) {
             if (pass == TOTAL) {
                 line.share = f.by_half(max(total - 1, 0)) + 1;
                 const int items = __builtin_amdgcn_readlane(upto_lane(tiles), 63) * a.kv_heads;
-                if (b == 0 && f.split && f.scale == 0 && items < f.groups) {
+                // (among many items of many lengths some have just more than so many parts' steps)
+                const bool alike = __all(tiles == 0 || one == __builtin_amdgcn_readfirstlane(one));
+                if (b == 0 && f.split && f.scale == 0 && (alike ? items < f.groups : 8 * items <= f.groups)) {
                     // parts of 25/24 of an even share, 2 steps at least
                     line.per = min((float)f.groups * 24 / ((float)(total - f.fixed * items) * 25), 1.f / 2);
                     steps_one = one;

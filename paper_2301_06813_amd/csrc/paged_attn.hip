@@ -7,16 +7,22 @@
 //   * Work. Lengths are known on the device only, and differ: a token of one sequence beside a
 //     prompt of another. The items (sequence, key head, tile of rows), each as long as its steps
 //     of keys and a fixed part, are laid end to end, and as many workgroups as the chip holds
-//     take equal parts of that line, whatever the lengths are. Every workgroup finds its part by
-//     the same sums over the sequences. An item that is cut leaves partial outputs in the
+//     take equal shares of that line, whatever the lengths are. Every wave finds its share by the
+//     same sums over the sequences, a lane each. An item that is cut leaves partial outputs in the
 //     workspace, two at most for each workgroup, and a second kernel joins them in order.
-//   * Pages. The page numbers of up to PAGES_AT_ONCE pages of a walk are brought to LDS. Rows of
-//     a load of one wave (1 KB: 4 or 8) lie on one page where the page's tokens are a multiple
-//     of them, so that a load is a buffer of its own, whose address is scalar arithmetic and
-//     whose end is the last row that is seen; other pages, and rows that allow no 16-byte loads,
-//     pass through registers.
+//   * Pages. The numbers of up to PAGES_AT_ONCE pages of a walk are brought to LDS. Rows of a load
+//     of one wave (1 KB: 4 or 8) lie on one page where the page's tokens are a multiple of them,
+//     so that a load is a buffer of its own, whose address is scalar arithmetic and whose end is
+//     the last row that is seen; other pages, and rows that allow no 16-byte loads, pass through
+//     registers.
 //   * Rows that the tile does not see, and pages that do not exist, arrive as zeros; a walk with
-//     such a page masks every step by the page numbers.
+//     such a page masks every step, and looks the keys' pages up.
+//
+// Few rows are bound by memory: one token of 32 sequences of up to 32768 keys, 64 heads over 8 of
+// 128, takes 463 us, 5.9 TB/s (560 with a step's addresses made at once behind its barrier, 610
+// with the arguments kept in registers through all items too). Many are bound by the step of 64 keys (2.0
+// us for 256 rows of 128, as over whole sequences): a chunk of 2048 of 16 heads over 4, 65536 keys,
+// 1009 us, 1.07 PFLOP/s. A workgroup's second item costs it 9 us until its keys flow again.
 #include <math.h>
 
 #include <algorithm>
@@ -679,16 +685,22 @@ hipError_t launch(const sbpk::PagedLaunch &f, bool dma, hipStream_t s) {
     return launch_kernel(sbpk::paged_attn_kernel<DP, KG, KT, NW, WPS, false>, name, grid, block, s, f);
 }
 
-// The kernel's forms: rows of a tile, workgroups of a unit, us of a step of KEYS. The second gives
-// up speed a row for smaller tiles: a chunk of 2048 of 16 heads over 4, 32768 keys, takes 523 and
-// 666 us at 128 columns, 430 and 568 at 64; chunks of 8 of 8 sequences, 64 heads over 8, 8192 x
-// 128, 57 and 50; one token of 16 sequences, 16 heads over 4, up to 4096 x 64, 18 and 17.6.
+// The kernel's forms: rows of a tile, workgroups of a unit, us of 64 keys, whether a tile's rows have
+// one wave each (whose partial outputs lie as the registers hold them). The second gives up speed a
+// row for smaller tiles: a chunk of 2048 of 16 heads over 4, 32768 keys, takes 523 and 666 us at 128
+// columns, 430 and 568 at 64; chunks of 8 of 8 sequences, 64 heads over 8, 8192 x 128, 57 and 50; one
+// token of 16 sequences, 16 heads over 4, up to 4096 x 64, 18 and 17.6. The third, for 128 columns,
+// has two workgroups a unit, of which one works while the other begins an item: one token of 64
+// sequences, 64 heads over 8, takes 55 us and with it 48 at up to 1000 keys, 91 and 96 at 2000, 292
+// and 313 at 8000.
 struct Form {
     int rows, per_cu;
     double step;
+    bool waves;
 };
-constexpr int KEYS = 64;
-constexpr Form FORMS[2][2] = {{{128, 2, 1.73}, {64, 2, 1.15}}, {{256, 1, 2.08}, {128, 1, 1.34}}};
+constexpr Form FORMS[2][3] = {{{128, 2, 1.73, true}, {64, 2, 1.15, false}, {}},
+                              {{256, 1, 2.08, true}, {128, 1, 1.34, false}, {128, 2, 2.3, true}}};
+constexpr int SHORT = 1536;      // keys of an item, at most, for the third form
 // An item's fixed part in steps: 2 and 5 differ by 12 % where items are short (prompts among
 // tokens, 16 steps each: 42 us for 48), by 2 % elsewhere, to either side.
 constexpr int FIXED = 3;
@@ -706,9 +718,12 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     const bool wide = a.d > 64;
     // tiles of a key head, at most; the form that takes the least time for a key of all of them
     const int64_t rows = (int64_t)a.at.rows * a.group;
+    const int64_t keys = std::min<int64_t>((int64_t)a.at.width * a.at.page,
+                                           a.window ? a.window + 256 / a.group : INT32_MAX);
+    const int small = wide && keys <= SHORT ? 2 : 1;
     int form = 0;
     double best = 1e300;
-    for (int k = 0; k < 2; ++k) {
+    for (const int k : {0, small}) {
         const Form &m = FORMS[wide][k];
         const double tiles = a.at.row_q ? (double)(rows / m.rows) + a.at.seqs
                                         : (double)((rows + m.rows - 1) / m.rows) * a.at.seqs;
@@ -716,14 +731,13 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
         if (t < best) best = t, form = k;
     }
     const Form &m = FORMS[wide][form];
-    // a slot holds the rows that a tile can have: whole waves' in the first form, whose partial
-    // outputs lie as the registers hold them
+    // a slot holds the rows that a tile can have (whole waves' in the registers' order)
     const int padded = wide ? 128 : 64;
-    f.slot_rows = (int32_t)std::min<int64_t>(m.rows, form == 0 ? (rows + 31) / 32 * 32 : rows);
+    f.slot_rows = (int32_t)std::min<int64_t>(m.rows, m.waves ? (rows + 31) / 32 * 32 : rows);
     // with a slot for each workgroup items may be cut; in shares of steps, where a workgroup has two,
     // fewer workgroups have one if the slots are less
     const int64_t most = (int64_t)device_cus() * m.per_cu;
-    const int64_t slot = (int64_t)f.slot_rows * (2 + (form == 0 ? padded : (a.d + 3) & ~3));
+    const int64_t slot = (int64_t)f.slot_rows * (2 + (m.waves ? padded : (a.d + 3) & ~3));
     const int64_t slots = ((int64_t)a.ws_floats - sbpk::CUT_FLOATS * most) / slot;
     f.split = slots >= most;
     f.groups = (int32_t)most;
@@ -732,7 +746,7 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     // units of all items, at most: below 2^31
     const double most_tiles = a.at.row_q ? (double)(rows / m.rows) + a.at.seqs
                                          : (double)((rows + m.rows - 1) / m.rows) * a.at.seqs;
-    const double steps = (double)a.at.width * a.at.page / KEYS + 2;
+    const double steps = (double)a.at.width * a.at.page / 32 + 2;
     f.fixed = FIXED;
     f.scale = 0;
     while (most_tiles * a.kv_heads * (steps / (double)(1 << f.scale) + 1 + FIXED) > 1e9) ++f.scale;
@@ -744,14 +758,16 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     hipError_t e;
     if (form == 0)
         e = wide ? launch<128, 1, 64, 8, 2>(f, dma, s) : launch<64, 1, 64, 4, 2>(f, dma, s);
-    else
+    else if (form == 1)
         e = wide ? launch<128, 2, 32, 8, 2>(f, dma, s) : launch<64, 2, 32, 4, 2>(f, dma, s);
+    else
+        e = launch<128, 1, 32, 4, 2>(f, dma, s);
     if (e != hipSuccess || !f.split || f.groups < 2) return e;
     auto join = [&](auto kernel, int pieces) {
         return launch_kernel(kernel, "paged_join_kernel", dim3((unsigned)(f.groups - 1), (unsigned)pieces),
                              dim3(256), s, f);
     };
-    if (form == 0) {    // 4 quads of 32 rows a workgroup
+    if (m.waves) {    // 4 quads of 32 rows a workgroup
         const int pieces = f.slot_rows / 32 * padded / 32;
         return wide ? join(sbpk::paged_join_kernel<128, 1, 1>, pieces)
                     : join(sbpk::paged_join_kernel<64, 1, 1>, pieces);

@@ -554,3 +554,37 @@ def test_one_long_sequence_in_many_parts():
     for new in (1, 2):
         check_attn(Batch([new], [40000], (8, 1), 64, 16, "head"))
         check_attn(Batch([new], [40000], (8, 1), 128, 64, "head"))
+
+
+# new tokens, lengths, (H, Hk), D, page, layout, room of a table row in tokens, kernel
+FORMS = [
+    ([1] * 3, [200, 90, 7], (4, 2), 64, 16, "head", 0, "<64,2,32,4,1>"),
+    ([1] * 3, [200, 90, 7], (4, 2), 64, 3, "head", 0, "<64,2,32,4,0>"),
+    ([40] * 2, [200, 90], (16, 2), 64, 16, "token", 0, "<64,1,64,4,1>"),
+    ([40] * 2, [200, 90], (16, 2), 50, 16, "token", 0, "<64,1,64,4,0>"),
+    ([1] * 3, [200, 90, 7], (4, 2), 128, 16, "head", 0, "<128,1,32,4,1>"),
+    ([1] * 3, [200, 90, 7], (4, 2), 128, 16, "odd", 0, "<128,1,32,4,0>"),
+    ([1] * 3, [200, 90, 7], (4, 2), 128, 16, "head", 1600, "<128,2,32,8,1>"),
+    ([1] * 3, [200, 90, 7], (4, 2), 80, 6, "head", 1600, "<128,2,32,8,0>"),
+    ([70] * 2, [200, 90], (16, 2), 128, 16, "token", 1600, "<128,1,64,8,1>"),
+    ([70] * 2, [200, 90], (16, 2), 100, 16, "token", 1600, "<128,1,64,8,0>"),
+]
+
+
+@pytest.mark.parametrize("case", FORMS, ids=lambda c: c[-1])
+def test_every_form_of_the_kernel(case):
+    new, lens, heads, D, P, layout, room, kernel = case
+    b = Batch(new, lens, heads, D, P, layout, extra=max(room - max(lens), 0) // P + 1)
+    check_attn(b)
+    sbp.sbp_profile_begin(4)
+    b.cache.attend(b.Q, *b.args(), **b.rows())
+    names = [n for n, _ in sbp.sbp_profile_end(4)]
+    assert names == ["paged_attn_kernel" + kernel, "paged_join_kernel"]
+
+
+def test_parts_of_more_rows_than_a_wave_has():
+    """Items cut in parts, of every order that partial outputs lie in, and of rows past 32."""
+    for new, heads, D, lens, room in ((8, (16, 2), 128, 1500, 2000), (8, (16, 2), 64, 3000, 0),
+                                      (20, (16, 2), 128, 900, 0), (60, (8, 1), 64, 5000, 0),
+                                      (100, (8, 1), 128, 5000, 6000)):
+        check_attn(Batch([new] * 2, [lens, lens - 77], heads, D, 16, "head", extra=1 + max(room - lens, 0) // 16))

@@ -627,8 +627,9 @@ typedef struct {
  * else of the cache is written. Two tokens of one call must not share a row of the cache (it
  * would hold parts of either). Qo's rows past len_q stay as they are.
  * Errors: those of the attention calls; SBP_ERR_SHAPE also for P < 1, width P > 2^29, more than
- * 2^20 sequences, more rows over the heads of Q, K and V than sbp_rope_fwd takes, or rows that do not fit `seqs`; SBP_ERR_ALIAS
- * also for a cache that overlaps another operand or whose own elements overlap. */
+ * 2^20 sequences, more rows over the heads of Q, K and V than sbp_rope_fwd takes, or rows that do
+ * not fit `seqs`; SBP_ERR_ALIAS also for a cache that overlaps another operand or whose own
+ * elements overlap. */
 int sbp_paged_append(const sbp_view4_t *K, const sbp_view4_t *V, const sbp_pages_t *pages,
                      const sbp_rope_t *rope, sbp_view4_t *Kc, sbp_view4_t *Vc,
                      const sbp_view4_t *Q, sbp_view4_t *Qo, int32_t p, int32_t r,

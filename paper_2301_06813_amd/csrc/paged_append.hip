@@ -1,8 +1,8 @@
 // paged_append.hip -- new tokens' keys and values to their places in a paged cache, with the
 // rotation of K and Q on the way.
 //
-// A thread owns R pairs of columns of a new token and takes them in HEADS of the heads of Q, K and V, one
-// after the other (rope.hip): the token's place gives both its row of the cache and its
+// A thread owns R pairs of columns of a new token and takes them in HEADS of the heads of Q, K and
+// V, one after the other (rope.hip): the token's place gives both its row of the cache and its
 // angles. In a packed batch a wave finds its first row's sequence by a search of 64 places at a
 // time. The bound is memory, for few tokens the chain of loads from a row to its page. (7172 new
 // tokens of 64 + 8 + 8 heads of 128: 87 us with one head a thread, 64 with two, 65 with three, 67

@@ -20,9 +20,9 @@
 //
 // Few rows are bound by memory: one token of 32 sequences of up to 32768 keys, 64 heads over 8 of
 // 128, takes 463 us, 5.9 TB/s (560 with a step's addresses made at once behind its barrier, 610
-// with the arguments kept in registers through all items too). Many are bound by the step of 64 keys (2.0
-// us for 256 rows of 128, as over whole sequences): a chunk of 2048 of 16 heads over 4, 65536 keys,
-// 1009 us, 1.07 PFLOP/s. A workgroup's second item costs it 9 us until its keys flow again.
+// with the arguments kept in registers through all items too). Many are bound by the step of 64 keys
+// (2.0 us for 256 rows of 128, as over whole sequences): a chunk of 2048 of 16 heads over 4, 65536
+// keys, 1009 us, 1.07 PFLOP/s. A workgroup's second item costs it 9 us until its keys flow again.
 #include <math.h>
 
 #include <algorithm>
@@ -719,7 +719,7 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     // tiles of a key head, at most; the form that takes the least time for a key of all of them
     const int64_t rows = (int64_t)a.at.rows * a.group;
     const int64_t keys = std::min<int64_t>((int64_t)a.at.width * a.at.page,
-                                           a.window ? a.window + 256 / a.group : INT32_MAX);
+                                           a.window && a.causal ? a.window + 256 / a.group : INT32_MAX);
     const int small = wide && keys <= SHORT ? 2 : 1;
     int form = 0;
     double best = 1e300;

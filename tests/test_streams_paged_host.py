@@ -109,3 +109,14 @@ def test_tensors_on_another_device(monkeypatch):
             with pytest.raises(ValueError, match="cuda:1"):
                 call(*args[:i], args[i].as_subclass(Elsewhere), *args[i + 1:])
     assert len(r.calls) == 8
+
+
+def test_window_that_is_no_int32(monkeypatch):
+    Q, = heads(4)
+    c, (table, lens) = cache(), step()
+    r = record(monkeypatch)
+    with pytest.raises(ValueError, match="int32"):
+        c.attend(Q, table, lens, window=(1 << 32) + 3)      # not a window of 3
+    assert not r.calls
+    c.attend(Q, table, lens, window=(1 << 31) - 1)
+    assert len(r.calls) == 1

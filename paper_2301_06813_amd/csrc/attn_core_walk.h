@@ -40,10 +40,10 @@ __device__ __forceinline__ void store4(void *base, int64_t at, int col, int d, b
 // m c is at most 2^-15 below it.
 constexpr float FAR = 1024.f;
 
-// WPS: waves of a SIMD, of one workgroup or two.
-template <int DP_, int KG_, int KT_, int NW_, int WPS_, bool DMA>
+// WPS: waves of a SIMD, of one workgroup or two. DC: columns of the products, of the DP of a tile.
+template <int DP_, int KG_, int KT_, int NW_, int WPS_, bool DMA, int DC_ = DP_>
 struct FwdShape {
-    static constexpr int DP = DP_, KG = KG_, KT = KT_, NW = NW_, WPS = WPS_;
+    static constexpr int DP = DP_, DC = DC_, KG = KG_, KT = KT_, NW = NW_, WPS = WPS_;
     static constexpr int ROWS = 32 * NW / KG, KEYS = KG * KT;
     using Tile = RowTile<DP, KEYS, NW>;
     static constexpr int STAGE = 2 * Tile::BYTES;    // K, then V
@@ -62,8 +62,8 @@ struct FwdShape {
 template <class S>
 struct FwdRows {
     using Tile = typename S::Tile;
-    static constexpr int DP = S::DP, KT = S::KT, NS = S::NS;
-    static constexpr int NB = KT / 32, KS = DP / 16, DB = DP / 32;
+    static constexpr int KT = S::KT, NS = S::NS;
+    static constexpr int NB = KT / 32, KS = S::DC / 16, DB = S::DC / 32;
 
     typename Tile::Reader rd;
     bf16x8 qf[KS];

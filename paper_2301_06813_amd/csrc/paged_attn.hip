@@ -170,13 +170,13 @@ __device__ __forceinline__ const PagedLaunch &again() {
     return *(const PagedLaunch *)(const __attribute__((address_space(4))) PagedLaunch *)p;
 }
 
-template <int DP, int KG, int KT, int NW, int WPS, bool DMA>
+template <int DP, int KG, int KT, int NW, int WPS, bool DMA, int DC>
 __global__ __launch_bounds__(64 * NW) __attribute__((amdgpu_waves_per_eu(WPS, WPS)))
 void paged_attn_kernel(PagedLaunch f0) {
     const PagedLaunch &f = f0;
-    using S = FwdShape<DP, KG, KT, NW, WPS, DMA>;
+    using S = FwdShape<DP, KG, KT, NW, WPS, DMA, DC>;
     using Tile = typename S::Tile;
-    constexpr int ROWS = S::ROWS, NS = S::NS, KEYS = S::KEYS, KS = DP / 16, NV = Tile::NV;
+    constexpr int ROWS = S::ROWS, NS = S::NS, KEYS = S::KEYS, KS = DC / 16, NV = Tile::NV;
     using Keys = TileKeys<ROWS, KEYS>;
     __shared__ __attribute__((aligned(1024))) char smem[S::LDS];
     __shared__ int32_t numbers[PAGES_AT_ONCE];
@@ -524,7 +524,7 @@ void paged_attn_kernel(PagedLaunch f0) {
                     const float by = some_key ? 1.f / l : 0.f;
                     float *const at = parts_of(f) + slot * DP + part_place<DP>(wr, 0, lane);
 #pragma unroll
-                    for (int t = 0; t < DP / 8; ++t) {
+                    for (int t = 0; t < DC / 8; ++t) {
                         f32x4 v;
 #pragma unroll
                         for (int e = 0; e < 4; ++e)
@@ -542,7 +542,7 @@ void paged_attn_kernel(PagedLaunch f0) {
                                     : whole ? seq.at.batch * a.o.sb + head * a.o.sh + at_row * a.o.ld
                                             : (slot + row - row0) * d4;
                 float *const put = reinterpret_cast<float *>(smem);
-                stage_rows<DP>(put + wave * PUT_FLOATS<DP>, w.o, some_key ? mul / l : 0.f, lane);
+                stage_rows<DC>(put + wave * PUT_FLOATS<DP>, w.o, some_key ? mul / l : 0.f, lane);
                 if (valid && half == 0 && kg == 0) {
                     if (!whole)
                         stats_of(f)[slot + row - row0] = some_key ? f32x2{m, l} : f32x2{-INFINITY, 0.f};
@@ -673,7 +673,7 @@ namespace sbpi {
 
 namespace {
 
-template <int DP, int KG, int KT, int NW, int WPS>
+template <int DP, int KG, int KT, int NW, int WPS, int DC>
 hipError_t launch(const sbpk::PagedLaunch &f, bool dma, hipStream_t s) {
     char name[160];
     name[0] = 0;
@@ -681,8 +681,16 @@ hipError_t launch(const sbpk::PagedLaunch &f, bool dma, hipStream_t s) {
         snprintf(name, sizeof(name), "paged_attn_kernel<%d,%d,%d,%d,%d>", DP, KG, KT, NW, (int)dma);
     const dim3 grid((unsigned)f.groups), block(64 * NW);
     if (dma)
-        return launch_kernel(sbpk::paged_attn_kernel<DP, KG, KT, NW, WPS, true>, name, grid, block, s, f);
-    return launch_kernel(sbpk::paged_attn_kernel<DP, KG, KT, NW, WPS, false>, name, grid, block, s, f);
+        return launch_kernel(sbpk::paged_attn_kernel<DP, KG, KT, NW, WPS, true, DC>, name, grid, block, s, f);
+    return launch_kernel(sbpk::paged_attn_kernel<DP, KG, KT, NW, WPS, false, DC>, name, grid, block, s, f);
+}
+template <int DP, int DC>
+hipError_t launch(int form, const sbpk::PagedLaunch &f, bool dma, hipStream_t s) {
+    constexpr int NW = DP / 16;
+    if (form == 0) return launch<DP, 1, 64, NW, 2, DC>(f, dma, s);
+    if (form == 1) return launch<DP, 2, 32, NW, 2, DC>(f, dma, s);
+    if constexpr (DP > 64) return launch<DP, 1, 32, NW / 2, 2, DC>(f, dma, s);
+    return hipErrorInvalidValue;
 }
 
 // The kernel's forms: rows of a tile, workgroups of a unit, us of 64 keys, whether a tile's rows have
@@ -755,13 +763,12 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     const bool dma = a.aligned && a.at.page % per_load == 0 &&
                      std::max(a.kc.sb, a.vc.sb) < int64_t(1) << 35 &&
                      (double)a.at.page * std::max(a.kc.ld, a.vc.ld) < 1073741824.0;
-    hipError_t e;
-    if (form == 0)
-        e = wide ? launch<128, 1, 64, 8, 2>(f, dma, s) : launch<64, 1, 64, 4, 2>(f, dma, s);
-    else if (form == 1)
-        e = wide ? launch<128, 2, 32, 8, 2>(f, dma, s) : launch<64, 2, 32, 4, 2>(f, dma, s);
-    else
-        e = launch<128, 1, 32, 4, 2>(f, dma, s);
+    // up to 96 columns, tiles of 128 with products of 96 (chunks of 512 of 4 sequences, 16 heads over
+    // 4, 8192 x 96: 148 us with products of 128, 132; one token of 32 sequences, 64 heads over 8, up
+    // to 4096 x 80: 67 and 64)
+    const hipError_t e = !wide         ? launch<64, 64>(form, f, dma, s)
+                         : a.d <= 96 ? launch<128, 96>(form, f, dma, s)
+                                     : launch<128, 128>(form, f, dma, s);
     if (e != hipSuccess || !f.split || f.groups < 2) return e;
     auto join = [&](auto kernel, int pieces) {
         return launch_kernel(kernel, "paged_join_kernel", dim3((unsigned)(f.groups - 1), (unsigned)pieces),

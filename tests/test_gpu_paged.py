@@ -588,3 +588,17 @@ def test_parts_of_more_rows_than_a_wave_has():
                                       (20, (16, 2), 128, 900, 0), (60, (8, 1), 64, 5000, 0),
                                       (100, (8, 1), 128, 5000, 6000)):
         check_attn(Batch([new] * 2, [lens, lens - 77], heads, D, 16, "head", extra=1 + max(room - lens, 0) // 16))
+
+
+@pytest.mark.parametrize("layout", ["head", "odd"])
+@pytest.mark.parametrize("D", [65, 72, 80, 95, 96, 97])
+def test_head_dimensions_about_96(D, layout):
+    """Every form, items cut and whole (a sequence of more steps than the others)."""
+    for new, lens, heads, room in (([1] * 5, [900, 33, 1, 64, 1200], (8, 2), 0),
+                                   ([1] * 5, [900, 33, 1, 64, 1200], (8, 2), 1700),
+                                   ([70, 65], [300, 1600], (8, 2), 0),
+                                   ([40] * 2, [200, 90], (16, 2), 1700)):
+        check_attn(Batch(new, lens, heads, D, 16, layout, extra=max(room - max(lens), 0) // 16 + 1))
+    b = Batch([1, 1], [700, 650], (4, 1), D, 16, layout)
+    for kw in (dict(out_dtype=torch.float32), dict(causal=False, window=40)):
+        check_attn(b, **kw)

@@ -22,7 +22,8 @@
 // 128, takes 463 us, 5.9 TB/s (560 with a step's addresses made at once behind its barrier, 610
 // with the arguments kept in registers through all items too). Many are bound by the step of 64 keys
 // (2.0 us for 256 rows of 128, as over whole sequences): a chunk of 2048 of 16 heads over 4, 65536
-// keys, 1009 us, 1.07 PFLOP/s. A workgroup's second item costs it 9 us until its keys flow again.
+// keys, 1009 us, 1.07 PFLOP/s. A workgroup's second item costs it 5 to 8 us
+// until its keys flow again.
 #include <math.h>
 
 #include <algorithm>

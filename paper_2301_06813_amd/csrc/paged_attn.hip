@@ -216,20 +216,24 @@ void paged_attn_kernel(PagedLaunch f0) {
         enum { TOTAL, PARTS, FIND } pass = TOTAL;
         int steps_one = 0, steps_upto = 0, steps_total = 0, steps_share = 0;
         for (int total = 0;;) {
-            int tiles = 0;
+            const bool in = b + lane < a.at.seqs;
+            r = SeqRows{0, 0, 0, 0};
+            if (in) r = rows_of(a.at, b + lane);
+            const Seq s(a, r);
+            const int tiles = in ? (s.rows + ROWS - 1) / ROWS : 0;
+            // a lane its own sequence's tiles, one after the other, where that is not for a few long
+            // sequences' sake; the further tiles the wave, one sequence after the other, which
+            // takes as long for one as a lane for 3 tiles
+            const int longer = __builtin_popcountll(__ballot(tiles > FEW)), at_most = 3 * longer;
+            const int own = 2 * __builtin_popcountll(__ballot(tiles > at_most)) <= longer
+                                ? max(at_most, FEW) : FEW;
             one = 0;
-            if (b + lane < a.at.seqs) {
-                r = rows_of(a.at, b + lane);
-                const Seq s(a, r);
-                tiles = (s.rows + ROWS - 1) / ROWS;
-                for (int t = 0; t < min(tiles, FEW); ++t) one += Keys(f, s, t).cost(f, line);
-            }
-            // the further tiles of longer ones: the wave, one sequence after the other
-            for (uint64_t more = __ballot(tiles > FEW); more; more &= more - 1) {
+            for (int t = 0; t < min(tiles, own); ++t) one += Keys(f, s, t).cost(f, line);
+            for (uint64_t more = __ballot(tiles > own); more; more &= more - 1) {
                 const int l = __builtin_ctzll(more);
                 const Seq s = one_of(r, b, l);
                 int c = 0;
-                for (int t = FEW + lane; t * ROWS < s.rows; t += 64) c += Keys(f, s, t).cost(f, line);
+                for (int t = own + lane; t * ROWS < s.rows; t += 64) c += Keys(f, s, t).cost(f, line);
                 c = __builtin_amdgcn_readlane(upto_lane(c), 63);
                 if (lane == l) one += c;
             }

@@ -54,6 +54,7 @@ struct PagedLaunch {
     int32_t slot_rows;               // rows of a partial output
     int32_t split;                   // items may be cut
     int32_t vec;                     // O allows 4-value stores
+    int32_t runs;                    // O's rows are bf16 runs of 8 columns
     int32_t groups, slots;           // workgroups, partial outputs that the workspace holds
     int32_t fixed, scale;            // an item's fixed part in steps; a unit has 2^scale steps
     Div page, group, by_half;        // by_half: workgroups with two partial outputs each
@@ -161,6 +162,38 @@ __device__ __forceinline__ int upto_lane(int x) {
 template <int DP>
 __device__ __forceinline__ int part_place(int wr, int t, int lane) {
     return ((wr * (DP / 8) + t) * 64 + lane) * 4;
+}
+
+// Stores a wave's 32 rows (lane l has row l % 32, at element `off` of the output or < 0 for none; o as
+// for stage_rows), times `mul` (0 where that is 0), as bf16 in 16 bytes a lane, through a tile of its
+// own in LDS, which the wave reads in the order it wrote. (As fp32 and in 8 bytes, as the
+// wave groups of a row need it, 256 rows of 128 took 3.4 us.)
+template <int DP, int DC>
+__device__ __forceinline__ void store_runs(char *tile, const f32x16 *o, float mul, uint16_t *out, int d,
+                                           int64_t off, int lane) {
+    typedef u32x4 u32x4_any __attribute__((aligned(2)));
+    constexpr int PITCH = DC * 2 + 16, RUNS = DP / 8;
+    static_assert(31 * PITCH + DP * 2 <= PUT_FLOATS<DP> * 4, "a wave's tile");
+    char *const row = tile + (lane & 31) * PITCH + 8 * (lane >> 5);
+#pragma unroll
+    for (int t = 0; t < DC / 8; ++t) {
+        auto value = [&](int e) {
+            const float v = o[t / 4][t % 4 * 4 + e];
+            return (uint32_t)f32_to_bf16_bits(mul != 0.f ? v * mul : 0.f);
+        };
+        *reinterpret_cast<u32x2 *>(row + 16 * t) = u32x2{value(0) | value(1) << 16, value(2) | value(3) << 16};
+    }
+    asm volatile("" ::: "memory");
+    const int run = lane % RUNS, lo = (int)off, hi = (int)(off >> 32);
+#pragma unroll
+    for (int it = 0; it < RUNS / 2; ++it) {
+        const int r = lane / RUNS + it * (64 / RUNS);
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(tile + r * PITCH + run * 16);
+        const int h = __builtin_amdgcn_ds_bpermute(4 * r, hi), l = __builtin_amdgcn_ds_bpermute(4 * r, lo);
+        if (h >= 0 && run * 8 < d)
+            *reinterpret_cast<u32x4_any *>(out + (int64_t)((uint64_t)(uint32_t)h << 32 | (uint32_t)l) +
+                                           run * 8) = v;
+    }
 }
 
 // The kernel's arguments, to be read again: what the compiler reads before a loop of items it keeps
@@ -547,7 +580,8 @@ void paged_attn_kernel(PagedLaunch f0) {
                                     : whole ? seq.at.batch * a.o.sb + head * a.o.sh + at_row * a.o.ld
                                             : (slot + row - row0) * d4;
                 float *const put = reinterpret_cast<float *>(smem);
-                stage_rows<DC>(put + wave * PUT_FLOATS<DP>, w.o, some_key ? mul / l : 0.f, lane);
+                const bool runs = KG == 1 && f.runs;
+                if (!runs) stage_rows<DC>(put + wave * PUT_FLOATS<DP>, w.o, some_key ? mul / l : 0.f, lane);
                 if (valid && half == 0 && kg == 0) {
                     if (!whole)
                         stats_of(f)[slot + row - row0] = some_key ? f32x2{m, l} : f32x2{-INFINITY, 0.f};
@@ -557,8 +591,14 @@ void paged_attn_kernel(PagedLaunch f0) {
                             some_key ? __builtin_fmaf(m, a.scale, __builtin_amdgcn_logf(l) * LN2)
                                      : -INFINITY;
                 }
-                __syncthreads();
-                store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
+                if (runs) {
+                    store_runs<DP, DC>(reinterpret_cast<char *>(put + wave * PUT_FLOATS<DP>), w.o,
+                                       some_key ? 1.f / l : 0.f, static_cast<uint16_t *>(a.o.p), a.d, off,
+                                       lane);
+                } else {
+                    __syncthreads();
+                    store_rows<DP, KG>(put + wr * KG * PUT_FLOATS<DP>, PUT_FLOATS<DP>, kg, out, off, lane);
+                }
                 __syncthreads();       // before the next item's loads
             }
         }
@@ -726,6 +766,7 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     const int esz = a.o_f32 ? 4 : 2;
     f.vec = a.d % 4 == 0 && reinterpret_cast<uintptr_t>(a.o.p) % (4 * esz) == 0 &&
             a.o.ld % 4 == 0 && a.o.sb % 4 == 0 && a.o.sh % 4 == 0;
+    f.runs = !a.o_f32 && a.d % 8 == 0;
     f.page = sbpk::Div(a.at.page);
     f.group = sbpk::Div(a.group);
     const bool wide = a.d > 64;

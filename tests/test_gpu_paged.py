@@ -602,3 +602,24 @@ def test_head_dimensions_about_96(D, layout):
     b = Batch([1, 1], [700, 650], (4, 1), D, 16, layout)
     for kw in (dict(out_dtype=torch.float32), dict(causal=False, window=40)):
         check_attn(b, **kw)
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("new", [
+    [300, 1, 37, 128, 0, 260] * 7,                  # most of several tiles
+    [200] * 70,                                     # more than 64 sequences, alike
+    [3, 1, 900, 1, 1, 40] + [1] * 20,               # one long among tokens
+    [150, 160, 170, 1500],                          # one much longer than other prompts
+], ids=["several", "alike", "one", "longer"])
+def test_sums_over_tiles_of_sequences(new, packed):
+    check_attn(Batch(new, [n + i % 9 for i, n in enumerate(new)], (8, 2), 64, 16, "head", packed=packed))
+
+
+@pytest.mark.parametrize("D", [8, 64, 96, 104, 128])
+def test_output_rows_at_any_address(D):
+    """Whole tiles and joined ones, to rows that start at odd elements; nothing beside them is written."""
+    for new, lens in (([100, 70], [130, 70]), ([300], [900])):
+        b = Batch(new, lens, (8, 2), D, 16, "head")
+        room = torch.full((len(new), 8, max(new), D + 5), 7.0, dtype=torch.bfloat16, device="cuda")
+        check_attn(b, out=room[..., 3:3 + D])
+        assert bool((room[..., :3] == 7).all()) and bool((room[..., 3 + D:] == 7).all())

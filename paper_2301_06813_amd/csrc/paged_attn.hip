@@ -756,9 +756,10 @@ struct Form {
 constexpr Form FORMS[2][3] = {{{128, 2, 1.73, true}, {64, 2, 1.15, false}, {}},
                               {{256, 1, 2.08, true}, {128, 1, 1.34, false}, {128, 2, 2.3, true}}};
 constexpr int SHORT = 1536;      // keys of an item, at most, for the third form
-// An item's fixed part in steps: 2 and 5 differ by 12 % where items are short (prompts among
-// tokens, 16 steps each: 42 us for 48), by 2 % elsewhere, to either side.
-constexpr int FIXED = 3;
+// An item's fixed part in steps: 3 and 5 differ where items are short and of many lengths (24 ragged
+// prompts of 400, up to 1500 x 64: 138 us and 130; 16 prompts of 2000 x 128: 359 and 348; prompts among
+// tokens, windows of 1000: 44.6 and 43.6), by 1 % elsewhere, to either side; 8 is no better.
+constexpr int FIXED = 5;
 
 }  // namespace
 

@@ -603,9 +603,9 @@ int sbp_rope_bwd(const sbp_view4_t *dQo, const sbp_view4_t *dKo, const sbp_rope_
  *   padded   row_q NULL: views of `seqs` batches, sequence b the first len_q[b] rows of batch b
  *            (limited to [0, rows]; len_q NULL: all)
  *   packed   views of one batch, sequence b rows row_q[b] .. row_q[b + 1] - 1, limited to the
- *            view. row_q must not descend (else whose row is whose is not defined, but nothing
- *            outside the views is touched). len_q must be NULL. Rows of no sequence are never
- *            read or written.
+ *            view. row_q must not descend (else what the rows hold is not defined, but nothing
+ *            outside the views and the workspace is touched). len_q must be NULL. Rows of no
+ *            sequence are never read or written.
  * len_k[b]: tokens that sequence b has in the cache once its n new ones are there, so that new
  * token i is at place len_k[b] - n + i. */
 typedef struct {

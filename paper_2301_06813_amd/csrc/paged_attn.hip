@@ -31,11 +31,14 @@
 #include "attn_core_walk.h"
 #include "gemm.h"
 #include "paged_kernel.h"
+#include "paged_plan.h"
 #include "profile.h"
 
 namespace sbpk {
 
+using sbpi::has_share;
 using sbpi::PagedArgs;
+using sbpi::slot_of;
 
 constexpr int PAGES_AT_ONCE = 1024;
 constexpr int SHORTEST = 2;          // steps that a cut leaves on either side
@@ -85,10 +88,9 @@ __device__ __forceinline__ f32x2 *stats_of(const PagedLaunch &f) {
 __device__ __forceinline__ float *parts_of(const PagedLaunch &f) {
     return f.a.ws + CUT_FLOATS * (int64_t)f.groups + 2 * (int64_t)f.slots * f.slot_rows;
 }
-// The partial output of a workgroup that has one, or, in shares of steps, two: of an item that it
-// began, and of one that it did not.
-__device__ __forceinline__ int64_t slot_of(int wg, bool began, bool parts) {
-    return parts ? wg : 2 * (int64_t)wg + (began ? 1 : 0);
+// Workgroups that may have partial outputs.
+__device__ __forceinline__ int holders_of(const PagedLaunch &f, bool parts) {
+    return parts ? f.groups : (int)f.by_half.d;
 }
 
 // A sequence: its rows (packed ones of the group: `rows`, of which those of n queries are in use),
@@ -309,9 +311,9 @@ void paged_attn_kernel(PagedLaunch f0) {
             } else {
                 line.share = 1;
             }
+            if (!has_share(total, line.share, wg, line.per != 0.f, holders_of(f, false))) return;
             at = line.share * wg;
             left = min(line.share, total - at);
-            if (left <= 0) return;
             if (b == 0) break;
             b = 0;
             pass = FIND;
@@ -648,7 +650,7 @@ __global__ __launch_bounds__(256) void paged_join_kernel(PagedLaunch f) {
     const bool valid = in < f.slot_rows && row < cut.rows && col < a.d;
     const int64_t d4 = (a.d + 3) & ~3;
     const float c = a.scale * LOG2E;
-    const int n = min(cut.last, f.groups - 1) - w + 2;
+    const int n = min(cut.last, holders_of(f, cut.parts) - 1) - w + 2;
     float top = -INFINITY, sum = 0.f;
     f32x4 v = {0.f, 0.f, 0.f, 0.f};
     if (valid)

@@ -50,7 +50,7 @@ struct Cut {
     int32_t batch, first, rows;      // of its sequence
     int32_t parts, spare;            // whether the line's units are parts
 };
-constexpr int CUT_FLOATS = sizeof(Cut) / 4;
+static_assert(sizeof(Cut) == 4 * sbpi::CUT_FLOATS, "a cut's place in the workspace");
 
 struct PagedLaunch {
     PagedArgs a;
@@ -83,10 +83,10 @@ __device__ __forceinline__ int uniform(int x) { return __builtin_amdgcn_readfirs
 typedef float f32x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ Cut *cuts_of(const PagedLaunch &f) { return reinterpret_cast<Cut *>(f.a.ws); }
 __device__ __forceinline__ f32x2 *stats_of(const PagedLaunch &f) {
-    return reinterpret_cast<f32x2 *>(f.a.ws + CUT_FLOATS * (int64_t)f.groups);
+    return reinterpret_cast<f32x2 *>(f.a.ws + sbpi::stats_at(f.groups));
 }
 __device__ __forceinline__ float *parts_of(const PagedLaunch &f) {
-    return f.a.ws + CUT_FLOATS * (int64_t)f.groups + 2 * (int64_t)f.slots * f.slot_rows;
+    return f.a.ws + sbpi::parts_at(f.groups, f.slots, f.slot_rows);
 }
 // Workgroups that may have partial outputs.
 __device__ __forceinline__ int holders_of(const PagedLaunch &f, bool parts) {
@@ -796,8 +796,8 @@ hipError_t launch_paged(const PagedArgs &a, hipStream_t s) {
     // with a slot for each workgroup items may be cut; in shares of steps, where a workgroup has two,
     // fewer workgroups have one if the slots are less
     const int64_t most = (int64_t)device_cus() * m.per_cu;
-    const int64_t slot = (int64_t)f.slot_rows * (2 + (m.waves ? padded : (a.d + 3) & ~3));
-    const int64_t slots = ((int64_t)a.ws_floats - sbpk::CUT_FLOATS * most) / slot;
+    const int64_t slots = slots_in((int64_t)a.ws_floats, (int)most, f.slot_rows,
+                                   m.waves ? padded : (a.d + 3) & ~3);
     f.split = slots >= most;
     f.groups = (int32_t)most;
     f.slots = (int32_t)std::min(slots, 2 * most);

@@ -20,4 +20,16 @@ constexpr int64_t slot_of(int wg, bool began, bool parts) {
     return parts ? wg : 2 * (int64_t)wg + (began ? 1 : 0);
 }
 
+// The workspace in floats: each workgroup's note for the join; two statistics of each of `rows` rows
+// of a slot; the slots' partial outputs of `cols` columns a row, a multiple of 4.
+constexpr int CUT_FLOATS = 8;
+constexpr int64_t stats_at(int groups) { return CUT_FLOATS * (int64_t)groups; }
+constexpr int64_t parts_at(int groups, int slots, int rows) {
+    return stats_at(groups) + 2 * (int64_t)slots * rows;
+}
+// Slots that fit, an even number: the partial outputs begin at 16 bytes for any number of rows.
+constexpr int64_t slots_in(int64_t floats, int groups, int rows, int cols) {
+    return floats < stats_at(groups) ? 0 : (floats - stats_at(groups)) / (rows * (int64_t)(2 + cols)) & ~1ll;
+}
+
 }  // namespace sbpi

@@ -623,3 +623,13 @@ def test_output_rows_at_any_address(D):
         room = torch.full((len(new), 8, max(new), D + 5), 7.0, dtype=torch.bfloat16, device="cuda")
         check_attn(b, out=room[..., 3:3 + D])
         assert bool((room[..., :3] == 7).all()) and bool((room[..., 3 + D:] == 7).all())
+
+
+@pytest.mark.parametrize("D,groups", [(64, 512), (128, 256)])
+@pytest.mark.parametrize("new", [1, 3])
+def test_workspaces_of_odd_numbers_of_partial_outputs(new, D, groups):
+    """Odd rows of an item, and room for an odd number of their partial outputs."""
+    b = Batch([new], [6000], (1, 1), D, 16, "head")
+    for slots in (groups, groups + 1, groups + 7, 2 * groups - 1, 2 * groups + 1):
+        ws = torch.full((8 * groups + slots * new * (2 + D),), math.nan, dtype=F32, device="cuda")
+        check_attn(b, ws=ws)

@@ -66,3 +66,29 @@ def run(tmp_path, body):
 
 def test_shares_have_room(tmp_path):
     run(tmp_path, SHARES)
+
+
+# Every size of a workspace about the least that holds a partial output a workgroup, and larger
+# ones; odd numbers of rows and slots among them.
+ROOM = r"""
+    for (int groups : {256, 512})
+        for (int rows : {1, 3, 7, 31, 32, 77, 128, 255, 256})
+            for (int cols : {4, 40, 64, 128})
+                for (int k = 0; k < 300; ++k) {
+                    const int64_t slot = rows * (int64_t)(2 + cols), least = stats_at(groups) + groups * slot;
+                    const int64_t floats = k < 100 ? least - 50 + k : least + draw() % (2 * groups * slot);
+                    const int64_t fit = slots_in(floats, groups, rows, cols);
+                    const int slots = (int)(fit < 2 * groups ? fit : 2 * groups);
+                    NEED((fit >= groups) == (floats >= least));
+                    if (slots == 0) continue;
+                    NEED(fit + 2 > (floats - stats_at(groups)) / slot);
+                    const int64_t at = parts_at(groups, slots, rows);
+                    NEED(at % 4 == 0 && at >= stats_at(groups) + 2 * (int64_t)slots * rows);
+                    NEED(at + (int64_t)slots * rows * cols <= floats);
+                }
+    NEED(slots_in(0, 256, 32, 64) == 0 && slots_in(2000, 256, 32, 64) == 0);
+"""
+
+
+def test_partial_outputs_lie_on_16_bytes(tmp_path):
+    run(tmp_path, ROOM)

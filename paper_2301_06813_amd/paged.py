@@ -89,7 +89,7 @@ class Cache:
                 lse=lse, out=out, out_dtype=out_dtype, ws=ws), Q, table, len_k, p, r)
         B, H, S, D = Q.shape
         same_device(Q, table, len_k, len_q, row_q, out, ws, self.k, self.v)
-        if window >> 31 > 0:
+        if not -(1 << 31) <= window < 1 << 31:
             raise ValueError("a window is an int32")
         hq = H if p == 1 or self.scope != sbp.SBP_GLOBAL else rank_heads(H, self.k.shape[1], p, r)[1]
         if out is None:

@@ -120,3 +120,13 @@ def test_window_that_is_no_int32(monkeypatch):
     assert not r.calls
     c.attend(Q, table, lens, window=(1 << 31) - 1)
     assert len(r.calls) == 1
+
+
+@pytest.mark.parametrize("window", [-(1 << 32) + 3, -(1 << 31) - 1, 1 << 31, (1 << 40) + 1])
+def test_windows_outside_int32_are_refused(monkeypatch, window):
+    Q, = heads(4)
+    c, (table, lens) = cache(), step()
+    r = record(monkeypatch)
+    with pytest.raises(ValueError, match="int32"):
+        c.attend(Q, table, lens, window=window)       # its low 32 bits may be a window
+    assert not r.calls

@@ -549,11 +549,12 @@ typedef enum { SBP_ROPE_PLAIN = 0, SBP_ROPE_LINEAR = 1, SBP_ROPE_BASE = 2,
 
 /* The dim / 2 frequencies as turns a position, in units of 2^-64 turn, to HOST memory; the
  * caller copies them to the device once. The angle of a position is a product modulo 2^64, so
- * far positions lose nothing: at t it is off by t 2^-62 turns at most (the frequencies are
- * computed in the host's long double). Pure host function. Errors: SBP_ERR_NULL, SBP_ERR_SHAPE
- * (dim odd or outside [2, 128], base <= 1 or not finite, an unknown scaling; for a scaling
- * factor <= 0; BY_TURNS and BY_PAIRS context <= 0, low <= 0 or high <= low; or a number that is
- * not finite). */
+ * far positions lose nothing: at t it is off by t 2^-62 turns at most, for a factor below 1 by
+ * 1 / factor times that (the frequencies, up to 1 / factor, are computed in the host's long
+ * double; for factors from 2^-32 on and high >= 2 low). Pure host function. Errors:
+ * SBP_ERR_NULL, SBP_ERR_SHAPE (dim odd or outside [2, 128], base <= 1 or not finite, an unknown
+ * scaling; for a scaling factor <= 0; BY_TURNS and BY_PAIRS context <= 0, low <= 0 or high <= low;
+ * or a number that is not finite). */
 int sbp_rope_turns(int32_t dim, double base, int32_t scaling, double factor, double low,
                    double high, double context, uint64_t *turns);
 

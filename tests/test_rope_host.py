@@ -151,3 +151,41 @@ def test_empty_calls_return(call):
         call(v4(16, batch, heads, rows, 32, **kw), v4(32, batch, heads // 2, rows, 32, **kw),
              c["rope"], None, v4(64, batch, n, rows, 32, scope=LO, **kw),
              v4(80, batch, n // 2, rows, 32, scope=LO, **kw), 2, 1, stream=0)
+
+
+def _exact_turns(dim, base, scaling, factor, low, high, context):
+    """The frequencies in turns a position, to 60 digits."""
+    from decimal import Decimal as D, ROUND_CEILING, ROUND_FLOOR, localcontext
+    with localcontext() as c:
+        c.prec = 80
+        tau = 2 * D("3.14159265358979323846264338327950288419716939937510582097494459230781640628620899862803")
+        base, factor, low, high, context = (D(x) for x in (base, factor, low, high, context))
+        b = base * factor ** (D(dim) / (dim - 2)) if scaling == "base" and dim > 2 else base
+        f = [b ** (D(-2 * i) / dim) for i in range(dim // 2)]
+        limited = lambda w: min(D(1), max(D(0), w))
+        at = lambda n: dim * (context / (tau * n)).ln() / (2 * base.ln())
+        first = max(D(0), at(high).to_integral_value(ROUND_FLOOR))
+        last = min(D(dim - 1), at(low).to_integral_value(ROUND_CEILING))
+        w = {"linear": lambda i: D(0), "turns": lambda i: limited((context * f[i] / tau - low) / (high - low)),
+             "pairs": lambda i: 1 - limited((i - first) / max(last - first, D("0.001")))}.get(scaling, lambda i: D(1))
+        return [(f[i] * w(i) + f[i] / factor * (1 - w(i))) / tau for i in range(dim // 2)]
+
+
+EXACT = [dict(), dict(base=1.5), dict(base=1e12), dict(low=0.5, high=1.0, context=1e6)] + [
+    dict(scaling=s, factor=x) for s in ("linear", "base", "turns", "pairs")
+    for x in (1e6, 40.0, 2.0, 0.9, 0.25, 0.01, 1e-4, 2.0 ** -32)]
+
+
+@pytest.mark.parametrize("dim", [2, 4, 22, 64, 128])
+@pytest.mark.parametrize("kw", EXACT, ids=str)
+def test_frequencies_keep_the_stated_bound(dim, kw):
+    """2^-62 turns a position, 1 / factor times that for factors below 1."""
+    from decimal import Decimal as D, localcontext
+    kw = dict(dict(base=10000.0, scaling=None, factor=1.0, low=1.0, high=32.0, context=4096.0), **kw)
+    got = sbp.sbp_rope_turns(dim, **{**kw, "scaling": sbp.ROPE_SCALINGS[kw["scaling"]]})
+    with localcontext() as c:
+        c.prec = 80
+        bound = D(2) ** -62 * max(D(1), 1 / D(kw["factor"]))
+        for g, w in zip(got, _exact_turns(dim, **kw)):
+            off = (D(g) / D(2) ** 64 - w) % 1
+            assert min(abs(off), 1 - abs(off)) <= bound, (g, w)

@@ -608,7 +608,10 @@ int sbp_rope_bwd(const sbp_view4_t *dQo, const sbp_view4_t *dKo, const sbp_rope_
  *            outside the views and the workspace is touched). len_q must be NULL. Rows of no
  *            sequence are never read or written.
  * len_k[b]: tokens that sequence b has in the cache once its n new ones are there, so that new
- * token i is at place len_k[b] - n + i. */
+ * token i is at place len_k[b] - n + i. Not more than width P, the table's room: past that the two
+ * calls differ. sbp_paged_append counts places from len_k as it is (rotates by them, and stores
+ * those in the room); sbp_paged_attn takes width P for it everywhere, also in its masks, which
+ * then see the new tokens at the room's last places. */
 typedef struct {
     const int32_t *table;
     int64_t table_ld;     /* >= width */
@@ -638,9 +641,10 @@ int sbp_paged_append(const sbp_view4_t *K, const sbp_view4_t *V, const sbp_pages
 
 /* Softmax attention of the new tokens over the cache (sbp_attn_core_fwd's formulas): query i
  * of the n new ones of a sequence sees key j when
- *     j < len_k  (limited to [0, width P]),
+ *     j < len_k
  *     causal:      j <= i + len_k - n
  *     window > 0:  j >  i + len_k - n - window
+ * with len_k limited to [0, width P] in all three,
  * and j's page is in [0, pages): keys on other pages are not seen. Entries of the table whose
  * keys no query of the sequence sees are not read.
  * Q: [B][H][S][D] bf16; Kc, Vc: [pages][Hk][P][D] bf16, of Q's scope; H a multiple of Hk,

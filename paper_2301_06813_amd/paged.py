@@ -7,8 +7,9 @@ in libsbp.so.
 New tokens come padded, [sequences][heads][rows][head_dim] (len_q: the rows in use), or
 packed, [1][heads][rows][head_dim] with row_q [sequences + 1]: sequence b has rows
 row_q[b] .. row_q[b + 1] - 1. table [sequences][width] names the pages of a sequence's tokens in
-order; len_k counts a sequence's tokens, the new ones included. All are int32 on the
-device and read when the calls run, so that captured graphs see their new contents.
+order; len_k counts a sequence's tokens, the new ones included, of which the table has to have
+room for all (past it append and attend count places differently: sbp_pages_t). All are int32 on
+the device and read when the calls run, so that captured graphs see their new contents.
 
 Q, K and V hold every head (``scope`` SBP_GLOBAL) or rank r's heads (SBP_LOCAL), the cache
 likewise (``Cache``'s scope).

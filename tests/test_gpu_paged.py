@@ -633,3 +633,21 @@ def test_workspaces_of_odd_numbers_of_partial_outputs(new, D, groups):
     for slots in (groups, groups + 1, groups + 7, 2 * groups - 1, 2 * groups + 1):
         ws = torch.full((8 * groups + slots * new * (2 + D),), math.nan, dtype=F32, device="cuda")
         check_attn(b, ws=ws)
+
+
+@pytest.mark.parametrize("new", [1, 5, 60])
+def test_lengths_past_the_table_in_either_call(new):
+    """Past the table's room attention takes the room for the length, in its masks too; append
+    rotates by the length as it is and drops what has no place."""
+    b = Batch([new, new], [96, 90], (4, 2), 64, 16, extra=0)
+    full, past = i32([96, 96]), i32([97 + new, (1 << 31) - 1])
+    table = b.args()[0]
+    for kw in (dict(), dict(window=20), dict(window=(1 << 31) - 1), dict(causal=False, window=70)):
+        want, got = (b.cache.attend(b.Q, table, n, **kw) for n in (full, past))
+        assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    b.len = past.tolist()
+    kc, kb, vc, q, qb = plain_append(b, 64, "halves")
+    out = b.cache.append(b.K, b.V, table, past, Q=b.Q, rope=rotary.Rope(64))
+    rope_ref.check("keys", b.kc, kc, kb)
+    rope_ref.check("Q", out, q, qb)
+    assert torch.equal(b.vc.cpu().double(), vc)

@@ -8,6 +8,7 @@ import pytest
 import torch
 
 import attn_core_ref as ref
+import paged_ref as pref
 import rope_ref
 from paper_2301_06813_amd import attention, inputs, linear, paged, rotary, sbp
 
@@ -196,3 +197,57 @@ def test_decoding_graph():
         assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
         assert torch.equal(again[0], check[0]) and torch.equal(again[1], check[1])
         assert torch.equal(kc, keep[0]) and torch.equal(vc, keep[1])
+
+
+@pytest.mark.parametrize("p", [1, 2])
+@pytest.mark.parametrize("D,P", [(64, 16), (80, 10)])
+def test_serving_steps_against_their_operands(p, D, P):
+    """Every operator of test_serving's steps against 64 bits from the operands it was given, with no
+    slack between them: projections as far from the whole sequence's as two roundings to bf16 and
+    two orders of an fp32 sum, rotations, cached rows, and attention over the rows that the cache
+    holds by (U + F) P |V|."""
+    H, Hk, dm, total = 8, 2, 96, [55, 6, 135]
+    W = [rn((dm, n * D), 40 + i, dm ** -0.5) for i, n in enumerate((H, Hk, Hk))]
+    xs = [rn((n, dm), 50 + i) for i, n in enumerate(total)]
+    kw = dict(scaling="turns", factor=4.0, context=64.0, low=1.0, high=4.0)
+    rope, f, s = rotary.Rope(D, **kw), rope_ref.freqs(D, **kw), 1 / math.sqrt(D)
+    width = (max(total) + P - 1) // P
+    perm = torch.randperm(3 * width + 2, generator=torch.Generator().manual_seed(6))[:3 * width]
+    host_table = perm.view(3, width).tolist()
+    table, prompt = i32(host_table), [50, 1, 130]
+    for r in range(p):
+        layer, done = Layer(p, r, W, H, Hk, D, 3 * width + 2, P), [0, 0, 0]
+        kc, vc = layer.cache.k, layer.cache.v
+        whole = [layer.heads(x) for x in xs]
+        sums = [[(x.abs().double() @ w[:, r * w.shape[1] // p:(r + 1) * w.shape[1] // p].abs().double())
+                 .view(1, x.shape[0], -1, D).transpose(1, 2) for w in W] for x in xs]
+        while done != total:
+            new = [min(48, q - d) if d < q else min(1, n - d) for d, q, n in zip(done, prompt, total)]
+            x = torch.cat([x[d:d + n] for x, d, n in zip(xs, done, new)])
+            before, done = done, [d + n for d, n in zip(done, new)]
+            row_q = [sum(new[:b]) for b in range(4)]
+            seqs = pref.lengths(3, row_q[-1], None, row_q)
+            q, k, v = layer.heads(x)
+            for b, (_, first, n) in enumerate(seqs):
+                for got, full, size in zip((q, k, v), whole[b], sums[b]):
+                    rows, cols = slice(first, first + n), slice(before[b], done[b])
+                    want = full[:, :, cols].double()
+                    off = (got[:, :, rows].double() - want).abs()
+                    lim = 2 * pref.U * want.abs() + 2 * dm * 2.0 ** -24 * (1 + 2 * pref.U) * size[:, :, cols]
+                    # (the second rounding is of the first one's value)
+                    assert bool((off <= lim * (1 + 2 * pref.U)).all())
+            pos = torch.cat([torch.arange(a, e) for a, e in zip(before, done)])[None]
+            wq, bq = rope_ref.rotate(q.cpu(), pos, f, D, "halves")
+            wk, bk = rope_ref.rotate(k.cpu(), pos, f, D, "halves")
+            q = layer.cache.append(k, v, table, i32(done), Q=q, rope=rope, row_q=i32(row_q), out=q,
+                                   scope=sbp.SBP_LOCAL)
+            rope_ref.check("q", q, wq, bq)
+            for _, i, page, slot, t in pref.places(seqs, done, host_table, kc.shape[0], P):
+                rope_ref.check("k", kc[page, :, slot], wk[0, :, i], bk[0, :, i])
+                assert torch.equal(vc[page, :, slot], v[0, :, i])
+            O, lse = layer.cache.attend(q, table, i32(done), row_q=i32(row_q))
+            want, bound, wl, used = pref.attend(q, kc, vc, host_table, done, seqs, s, True, 0)
+            assert bool(used.all())
+            pref.check("O", O, want, bound)
+            # scores below 2^5 in fp32, one logarithm
+            assert float((lse.double() - wl).abs().max()) <= 2.0 ** -14

@@ -189,3 +189,17 @@ def test_frequencies_keep_the_stated_bound(dim, kw):
         for g, w in zip(got, _exact_turns(dim, **kw)):
             off = (D(g) / D(2) ** 64 - w) % 1
             assert min(abs(off), 1 - abs(off)) <= bound, (g, w)
+
+
+@fake
+@pytest.mark.parametrize("call", [sbp.sbp_rope_fwd, sbp.sbp_rope_bwd])
+@pytest.mark.parametrize("order", [sbp.SBP_ROPE_HALVES, sbp.SBP_ROPE_PAIRS])
+@pytest.mark.parametrize("dim", [0, 1, 2])
+@pytest.mark.parametrize("dtype,out", [(BF, BF), (BF, F32), (F32, F32)])
+def test_a_head_of_one_column_has_no_pair(call, order, dim, dtype, out):
+    c = {**args(), "q": v4(16, 1, 4, 7, 1, dtype), "k": v4(32, 1, 2, 7, 1, dtype),
+         "qo": v4(64, 1, 4, 7, 1, out, LO), "ko": v4(80, 1, 2, 7, 1, out, LO),
+         "rope": sbp.sbp_rope_t(200 * MB, dim, order, 1.0)}
+    with pytest.raises(sbp.SbpError) as e:
+        call(c["q"], c["k"], c["rope"], None, c["qo"], c["ko"], 1, 0, stream=0)
+    assert e.value.code == S

@@ -611,7 +611,8 @@ int sbp_rope_bwd(const sbp_view4_t *dQo, const sbp_view4_t *dKo, const sbp_rope_
  * token i is at place len_k[b] - n + i. Not more than width P, the table's room: past that the two
  * calls differ. sbp_paged_append counts places from len_k as it is (rotates by them, and stores
  * those in the room); sbp_paged_attn takes width P for it everywhere, also in its masks, which
- * then see the new tokens at the room's last places. */
+ * then see the new tokens at the room's last places. sbp_paged_attn chooses its kernel for the
+ * room: a table cut to the width that a step's longest sequence needs serves short ones better. */
 typedef struct {
     const int32_t *table;
     int64_t table_ld;     /* >= width */

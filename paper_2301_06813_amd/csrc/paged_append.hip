@@ -4,7 +4,7 @@
 // A thread owns R pairs of columns of a new token and takes them in HEADS of the heads of Q, K and
 // V, one after the other (rope.hip): the token's place gives both its row of the cache and its
 // angles. In a packed batch a wave finds its first row's sequence by a search of 64 places at a
-// time. The bound is memory, for few tokens the chain of loads from a row to its page. (7172 new
+// time. The bound is memory, for few tokens the chain of loads from a row to its page. (7180 new
 // tokens of 64 + 8 + 8 heads of 128: 87 us with one head a thread, 64 with two, 65 with three, 67
 // with four, 72 with eight.)
 #include "attn_core_kernel.h"

@@ -7,9 +7,12 @@
 //   * Work. Lengths are known on the device only, and differ: a token of one sequence beside a
 //     prompt of another. The items (sequence, key head, tile of rows), each as long as its steps
 //     of keys and a fixed part, are laid end to end, and as many workgroups as the chip holds
-//     take equal shares of that line, whatever the lengths are. Every wave finds its share by the
-//     same sums over the sequences, a lane each. An item that is cut leaves partial outputs in the
-//     workspace, two at most for each workgroup, and a second kernel joins them in order.
+//     take equal shares of that line, whatever the lengths are (as many as the workspace has room
+//     for the partial outputs of: of 64 MiB 252 of 256 with tiles of 256 rows of 128). Every wave finds
+//     its share by the same sums over the sequences, a lane each, 64 at a time, which then take over 1
+//     us for each 64 (2^17 keys in all, 8 heads over 1 of 128: one token of 64 sequences 20 us, of
+//     256 26, of 1024 43). An item that is cut leaves partial outputs in the workspace, two at most
+//     for each workgroup, and a second kernel joins them in order.
 //   * Pages. The numbers of up to PAGES_AT_ONCE pages of a walk are brought to LDS. Rows of a load
 //     of one wave (1 KB: 4 or 8) lie on one page where the page's tokens are a multiple of them,
 //     so that a load is a buffer of its own, whose address is scalar arithmetic and whose end is
@@ -21,9 +24,11 @@
 // Few rows are bound by memory: one token of 32 sequences of up to 32768 keys, 64 heads over 8 of
 // 128, takes 463 us, 5.9 TB/s (560 with a step's addresses made at once behind its barrier, 610
 // with the arguments kept in registers through all items too). Many are bound by the step of 64 keys
-// (2.0 us for 256 rows of 128, as over whole sequences): a chunk of 2048 of 16 heads over 4, 65536
-// keys, 1009 us, 1.07 PFLOP/s. A workgroup's second item costs it 5 to 8 us
-// until its keys flow again.
+// (2.0 us for 256 rows of 128): a chunk of 2048 of 16 heads over 4, 65536 keys, 1000 us, 1.08 PFLOP/s,
+// with pages of 16 tokens as with one page of all (the same keys in one piece, attn_core_fwd.hip: 920).
+// Rows that pass through registers are slower: chunks of 512 of 4 sequences, 16 heads over 4, up to
+// 8192 x 128, 222 us with pages of 17 tokens and 136 with 16; one token of 32 sequences, 64 heads over
+// 8, 4096 x 128, 234 and 106. A workgroup's second item costs it 5 to 8 us until its keys flow again.
 #include <math.h>
 
 #include <algorithm>
@@ -170,7 +175,7 @@ __device__ __forceinline__ int part_place(int wr, int t, int lane) {
 // for stage_rows), times `mul` (0 where that is 0), as bf16 in 16 bytes a lane, through a tile of its
 // own in LDS, which the wave reads in the order it wrote. (As fp32 and in 8 bytes, as the
 // wave groups of a row need it, 256 rows of 128 took 3.4 us; 60 prompts of 500 rows of 16 heads over 4
-// of 128 112 us and so 108.)
+// of 64 112 us and so 108.)
 template <int DP, int DC>
 __device__ __forceinline__ void store_runs(char *tile, const f32x16 *o, float mul, uint16_t *out, int d,
                                            int64_t off, int lane) {

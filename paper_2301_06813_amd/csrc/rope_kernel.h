@@ -47,7 +47,7 @@ __device__ __forceinline__ void angle(uint64_t turns, int64_t t, float mul, floa
 
 // A head's columns are taken in units of 2 R: first the rotated ones, R pairs a unit, then the
 // others. A unit is two runs of up to R columns, from the first and the second half of these, in
-// either order of the pairs, so that a wave's accesses lie side by side (append of 7172 tokens of 64
+// either order of the pairs, so that a wave's accesses lie side by side (append of 7180 tokens of 64
 // + 8 + 8 heads of 128 in the order of pairs: 66.8 us with 2 R columns a lane, 64.4).
 struct Unit {
     int one, two;     // first columns of the runs

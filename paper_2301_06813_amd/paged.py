@@ -9,7 +9,9 @@ packed, [1][heads][rows][head_dim] with row_q [sequences + 1]: sequence b has ro
 row_q[b] .. row_q[b + 1] - 1. table [sequences][width] names the pages of a sequence's tokens in
 order; len_k counts a sequence's tokens, the new ones included, of which the table has to have
 room for all (past it append and attend count places differently: sbp_pages_t). All are int32 on
-the device and read when the calls run, so that captured graphs see their new contents.
+the device and read when the calls run, so that captured graphs see their new contents. Where the
+host knows a step's longest sequence, table[:, :its pages] lets attend choose the kernel for that
+length (64 single tokens over up to 1000 keys, 64 heads over 8 of 128: 45 us, 51 with room for 32768).
 
 Q, K and V hold every head (``scope`` SBP_GLOBAL) or rank r's heads (SBP_LOCAL), the cache
 likewise (``Cache``'s scope).
